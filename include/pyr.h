@@ -384,6 +384,130 @@ pyr_status_t pyr_glue_rope(void* x, const int32_t* pos, int64_t tokens, int32_t 
 pyr_status_t pyr_glue_swiglu(const void* gate, const void* up, void* out, int64_t n, int32_t dtype, void* stream);
 pyr_status_t pyr_glue_argmax(const void* x, int32_t* out, int64_t rows, int32_t n, int32_t dtype, void* stream);
 
+/*
+ * A paged cache held in 4 bits. (No counterpart in the paper, whose cache is one block per layer: this is how a
+ * serving engine keeps what the selection leaves.) A POOL of pages, and LISTS of pages that hold rows in order: one list
+ * is one layer's cache of one sequence, with a length of its own. Lists share pages: forking one counts its pages once
+ * more instead of copying them. All state lies in one device buffer of the caller's, lengths and page tables included,
+ * so every call below works from device memory alone and can be captured into a CUDA graph and replayed.
+ *
+ * Format. A page is [n_kv_heads][page_rows / 16] tiles of 16 rows. A tile is, in this order: the K codes (16 rows of
+ * head_dim / 2 bytes), the V codes, and for K and then V one 32-bit word per row and group of `group` dimensions (row
+ * major): bf16 scale in the low half, bf16 zero in the high half. tile bytes = 16 * (head_dim + 8 * head_dim / group).
+ * Codes lie in the order in which the attention's matrix fragments take them: with u = group / 32 and g the group,
+ * word j * (head_dim / 32) + g * u + t (j < 4, t < u) of a K row holds the eight dimensions from
+ * g * group + 8 * (j * u + t) on, low nibble first; 16-bit half i * (head_dim / 32) + g * u + t (i < 8) of a V row holds
+ * the four dimensions from g * group + 4 * (i * u + t) on.
+ * Values, every step in IEEE single precision with rounding to nearest even: zero = min(x) rounded down to bf16, scale =
+ * (max(x) - zero) / 15 rounded up to bf16 (0 below 2^-100), code = rint((x - zero) * (1 / scale)), and a code stands for
+ * scale * code + zero, which is at most scale / 2 (and a rounding) from x. A group for which max(x) - zero is not finite
+ * (an Inf, a NaN, a range beyond single precision) is stored as NaN, so that it shows in what reads it.
+ *
+ * Calls on one handle must be ordered: on one stream, or by events. Two calls, or two replayed graphs, of one handle
+ * that can overlap on the GPU race on its tables and on its workspace. Device errors (a list id, count, kept index or
+ * page out of range, no free page, the same list twice where it would be written twice) cannot be returned by an
+ * asynchronous call: the list concerned (or, in pyr_pages_reserve, the whole call) is left as it was, a pyr_status_t is
+ * recorded in the handle's status word and pyr_pages_status reports it. No such error makes a kernel leave its buffers.
+ *
+ * In every call `lists` (device int32 [n]) names the list of each entry; NULL means lists 0 .. n-1. n = 0 does nothing.
+ */
+typedef struct {
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* 64 or 128                                            */
+  int32_t group;       /* dimensions that share a scale: 32, 64 or 128, at most head_dim */
+  int32_t page_rows;   /* rows of a page: a multiple of 16, at most 1024       */
+  int32_t n_pages;     /* pages of the pool                                    */
+  int32_t n_lists;     /* at most 2^19                                         */
+  int32_t max_pages;   /* pages that one list can hold                         */
+  uint32_t flags;      /* 0                                                    */
+} pyr_pages_config_t;
+
+typedef struct pyr_pages pyr_pages_t;
+
+/* Size and alignment of the device buffer: status and workspace, lengths, reference counts, page tables, pool. */
+pyr_status_t pyr_pages_bytes(const pyr_pages_config_t* cfg, size_t* bytes, size_t* align);
+/* Builds a handle over `dev_buf`. Makes no CUDA call; pyr_pages_reset must come before any call that launches. */
+pyr_status_t pyr_pages_alloc(const pyr_pages_config_t* cfg, void* dev_buf, size_t bytes, pyr_pages_t** out);
+pyr_status_t pyr_pages_free(pyr_pages_t* pages);
+/* Every list empty, every page free, status and workspace cleared (on `stream`). The pool's bytes stay as they are.
+ * Not for capture: a replay would empty the cache. */
+pyr_status_t pyr_pages_reset(pyr_pages_t* pages, void* stream);
+/* Device pointers to the pool [n_pages, page bytes], the page tables [n_lists, max_pages] (page ids, -1 behind a list's
+ * pages), the lengths [n_lists] in rows and the reference counts [n_pages] (0: free). They may be saved and restored
+ * together between calls; any out pointer may be NULL. */
+pyr_status_t pyr_pages_view(const pyr_pages_t* pages, void** pool, size_t* page_bytes, int32_t** table, int32_t** lens,
+                            int32_t** refs);
+/* Synchronises `stream` and reports the first error recorded on the device since the last report: *host_status is a
+ * pyr_status_t, 0 for none, and the return value says the same. Reading clears it. */
+pyr_status_t pyr_pages_status(pyr_pages_t* pages, void* stream, int32_t* host_status);
+
+/*
+ * Room for more rows. Entry i's list gets the pages that its rows [len, len + rows_i) need and lacks: the lowest free
+ * pages, entry by entry and slot by slot (rows: device int32 [n], or NULL: rows_each for all). A part-filled last page
+ * that another list holds as well is first replaced by a page of its own into which its filled rows are copied. Lengths do
+ * not change. The reference counts that decide are those at the call's start: pages that this call gives up are free
+ * for the next one. All or nothing: a list twice, a negative count, a list that would outgrow max_pages
+ * (PYR_ERR_INVALID / PYR_ERR_CAPACITY), or too few free pages (PYR_ERR_CAPACITY) changes nothing.
+ */
+pyr_status_t pyr_pages_reserve(pyr_pages_t* pages, const int32_t* lists, int32_t n, const int32_t* rows, int32_t rows_each,
+                               void* stream);
+
+/*
+ * Stores rows. k, v (device) are [n, src_rows, n_kv_heads, head_dim], strides in elements, D contiguous, 16-byte aligned
+ * rows, dtype a pyr_dtype_t. Entry i's count_i rows (counts: device int32 [n], each in [0, n_rows]; NULL: n_rows) go to
+ * the rows [first_i, first_i + count_i) of its list (first: device int32 [n], each at most the list's length; NULL: the
+ * list's end). With idx (device int32 [n, idx_groups, n_rows] with idx_stride elements between entries; idx_groups 1 or
+ * n_kv_heads; pyr_cache_kept's first pointer is one) row x of head h is source row idx[i][h's group][x]: the Gather of
+ * Algorithm 1 straight into 4-bit pages; without, source row x. The list's length becomes max(length, first_i + count_i).
+ * Every page written must be the list's own: reserved, and held by no other list. One row per list is the decode step's
+ * append.
+ */
+pyr_status_t pyr_pages_write(pyr_pages_t* pages, const int32_t* lists, int32_t n, const int32_t* first, const void* k,
+                             const void* v, int64_t stride_b, int64_t stride_n, int64_t stride_h, int32_t src_rows,
+                             int32_t dtype, const int32_t* idx, int32_t idx_groups, int64_t idx_stride, const int32_t* counts,
+                             int32_t n_rows, void* stream);
+
+/* Reads rows back as the values they stand for: k, v (device) are [n, n_rows, n_kv_heads, head_dim], strided as above.
+ * Row x of entry i is row first_i + x of its list (first NULL: 0). Rows at or behind a list's length, and rows x >= count_i,
+ * are left as they were. */
+pyr_status_t pyr_pages_read(pyr_pages_t* pages, const int32_t* lists, int32_t n, const int32_t* first, void* k, void* v,
+                            int64_t stride_b, int64_t stride_n, int64_t stride_h, int32_t dtype, const int32_t* counts,
+                            int32_t n_rows, void* stream);
+
+/*
+ * Attention over the lists' rows. q, out (device) are [n, q_len, n_q_heads, head_dim], strides in elements, D contiguous
+ * and rows 16-byte aligned; n_q_heads a multiple of n_kv_heads. Query token t of entry i sees the first
+ * len_i - (q_len - 1 - t) rows: with q_len = 1 all of them, the row stored last included; with more, the last q_len rows are
+ * those of the query tokens themselves (a chunk of a prompt, drafted tokens). A token that sees no row gets zeros.
+ * lse (device, may be NULL) is [n, n_q_heads, q_len] fp32, the natural log of the softmax denominator, -inf for such a
+ * token. softmax_scale 0 means 1/sqrt(D). Scores, softmax statistics and sums are held in fp32. Each list is read once per
+ * 8 (bf16; 4 for fp32) query rows of a KV head; bit-reproducible. A list may appear more than once. bf16 runs on warp-level
+ * tensor-core instructions, fp32 on CUDA cores.
+ */
+pyr_status_t pyr_pages_attn(pyr_pages_t* pages, const int32_t* lists, int32_t n, const void* q, int64_t q_stride_b,
+                            int64_t q_stride_t, int64_t q_stride_h, void* out, int64_t o_stride_b, int64_t o_stride_t,
+                            int64_t o_stride_h, float* lse, int32_t q_len, int32_t n_q_heads, int32_t dtype,
+                            float softmax_scale, void* stream);
+
+/* Makes list dst_i a copy of list src_i that shares its pages. dst_i must hold no page and appear nowhere else in the call;
+ * src_i may repeat. */
+pyr_status_t pyr_pages_fork(pyr_pages_t* pages, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
+
+/* Cuts entry i's list to its first rows_i rows (rows: device int32 [n]; NULL: none, the list is emptied; a list that is
+ * shorter keeps what it has) and gives up every page behind them, reserved ones too. A page that no list holds is free. */
+pyr_status_t pyr_pages_trim(pyr_pages_t* pages, const int32_t* lists, int32_t n, const int32_t* rows, void* stream);
+
+/*
+ * Moves rows: rows 0 .. count_i - 1 of list dst_i become the rows idx[i][h's group][x] of list src_i, stored bytes as they
+ * are (idx, idx_groups, idx_stride, counts, n_rows as in pyr_pages_write; idx NULL: the first count_i rows, a copy).
+ * dst_i == src_i compacts in place: idx must ascend strictly, the pages behind the count are given up, and every page in
+ * which a row moves must be the list's own. Otherwise dst_i must have pages of its own reserved for count_i rows (what they
+ * held is overwritten) and must not be another entry's source; idx may have any order and repeats. A list must not be
+ * the destination of two entries. dst_i's length becomes count_i.
+ */
+pyr_status_t pyr_pages_compact(pyr_pages_t* pages, const int32_t* src, const int32_t* dst, int32_t n, const int32_t* idx,
+                               int32_t idx_groups, int64_t idx_stride, const int32_t* counts, int32_t n_rows, void* stream);
+
 const char* pyr_status_string(pyr_status_t status);
 
 /* Number of kernels this process has launched through the library so far. */

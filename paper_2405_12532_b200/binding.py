@@ -6,6 +6,7 @@ the library has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 
 import torch
@@ -29,6 +30,9 @@ EXPORTS = [
     "pyr_prefill_layer", "pyr_select_compact", "pyr_decode_attn", "pyr_decode_reselect", "pyr_cache_arm_wait_test", "pyr_recent_len_from_ratio", "pyr_glue_embed", "pyr_glue_rmsnorm", "pyr_glue_status", "pyr_glue_linear", "pyr_glue_linear_split", "pyr_glue_linear_swiglu", "pyr_glue_rmsnorm_rows", "pyr_glue_linear_rows",
     "pyr_glue_rope", "pyr_glue_swiglu", "pyr_glue_argmax", "pyr_status_string", "pyr_version", "pyr_launch_count",
     "pyr_decode_attn_noalloc", "pyr_decode_attn_noalloc_status",
+    "pyr_pages_bytes", "pyr_pages_alloc", "pyr_pages_free", "pyr_pages_reset", "pyr_pages_view", "pyr_pages_status",
+    "pyr_pages_reserve", "pyr_pages_write", "pyr_pages_read", "pyr_pages_attn", "pyr_pages_fork", "pyr_pages_trim",
+    "pyr_pages_compact",
 ]
 
 
@@ -40,6 +44,13 @@ class PyrConfig(C.Structure):
         ("max_new_tokens", C.c_int32),
         ("ratio", C.POINTER(C.c_double)), ("min_len", C.POINTER(C.c_int32)),
         ("recent_w", C.POINTER(C.c_float)), ("softmax_scale", C.c_float), ("flags", C.c_uint32),
+    ]
+
+
+class PyrPagesConfig(C.Structure):
+    _fields_ = [
+        ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("group", C.c_int32), ("page_rows", C.c_int32),
+        ("n_pages", C.c_int32), ("n_lists", C.c_int32), ("max_pages", C.c_int32), ("flags", C.c_uint32),
     ]
 
 
@@ -98,6 +109,19 @@ def lib() -> C.CDLL:
         L.pyr_decode_attn_noalloc.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
                                               C.c_float, vp]
         L.pyr_decode_attn_noalloc_status.argtypes = [vp, pi32]
+        L.pyr_pages_bytes.argtypes = [C.POINTER(PyrPagesConfig), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+        L.pyr_pages_alloc.argtypes = [C.POINTER(PyrPagesConfig), vp, C.c_size_t, C.POINTER(vp)]
+        L.pyr_pages_free.argtypes = [vp]
+        L.pyr_pages_reset.argtypes = [vp, vp]
+        L.pyr_pages_view.argtypes = [vp, C.POINTER(vp), C.POINTER(C.c_size_t), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp)]
+        L.pyr_pages_status.argtypes = [vp, vp, pi32]
+        L.pyr_pages_reserve.argtypes = [vp, vp, i32, vp, i32, vp]
+        L.pyr_pages_write.argtypes = [vp, vp, i32, vp, vp, vp, i64, i64, i64, i32, i32, vp, i32, i64, vp, i32, vp]
+        L.pyr_pages_read.argtypes = [vp, vp, i32, vp, vp, vp, i64, i64, i64, i32, vp, i32, vp]
+        L.pyr_pages_attn.argtypes = [vp, vp, i32, vp, i64, i64, i64, vp, i64, i64, i64, vp, i32, i32, i32, C.c_float, vp]
+        L.pyr_pages_fork.argtypes = [vp, vp, vp, i32, vp]
+        L.pyr_pages_trim.argtypes = [vp, vp, i32, vp, vp]
+        L.pyr_pages_compact.argtypes = [vp, vp, vp, i32, vp, i32, i64, vp, i32, vp]
         for name in EXPORTS:
             fn = getattr(L, name)
             if name not in ("pyr_status_string", "pyr_version", "pyr_launch_count", "pyr_recent_len_from_ratio"):
@@ -423,3 +447,176 @@ class PyrCache:
         assert q.is_contiguous() and k_new.is_contiguous() and v_new.is_contiguous() and out.is_contiguous()
         _check(lib().pyr_decode_attn(self.handle, layer, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
                                      out.data_ptr(), C.c_void_p(_stream_ptr(stream))), "pyr_decode_attn")
+
+
+def make_pages_config(*, n_kv_heads, head_dim, n_pages, n_lists, max_pages, group=64, page_rows=64, flags=0) -> PyrPagesConfig:
+    return PyrPagesConfig(n_kv_heads, head_dim, group, page_rows, n_pages, n_lists, max_pages, flags)
+
+
+def pyr_pages_bytes(cfg: PyrPagesConfig) -> tuple[int, int]:
+    b, a = C.c_size_t(0), C.c_size_t(0)
+    _check(lib().pyr_pages_bytes(C.byref(cfg), C.byref(b), C.byref(a)), "pyr_pages_bytes")
+    return b.value, a.value
+
+
+class PyrPages:
+    """A paged 4-bit cache (pyr_pages_*): the handle plus the torch buffer that backs it, emptied on creation. `lists` arguments
+    are int32 tensors of list ids, `idx` [n, groups, rows] int32 with its last two dimensions contiguous; the views `pool`
+    [n_pages, page bytes] uint8, `table`, `lens` and `refs` are the device state itself. A call runs on the current stream of
+    the cache's device, or on `stream`; device-side errors are read with status()."""
+
+    def __init__(self, device="cuda", **kw):
+        self.cfg = make_pages_config(**kw)
+        nbytes, align = pyr_pages_bytes(self.cfg)
+        self.nbytes = nbytes
+        self.buf = torch.empty(nbytes + align, dtype=torch.uint8, device=torch.device(device))
+        self.device = self.buf.device
+        off = (-self.buf.data_ptr()) % align
+        self.handle = C.c_void_p()
+        _check(lib().pyr_pages_alloc(C.byref(self.cfg), C.c_void_p(self.buf.data_ptr() + off), nbytes, C.byref(self.handle)),
+               "pyr_pages_alloc")
+        pool, table, lens, refs, page = C.c_void_p(), C.c_void_p(), C.c_void_p(), C.c_void_p(), C.c_size_t(0)
+        _check(lib().pyr_pages_view(self.handle, C.byref(pool), C.byref(page), C.byref(table), C.byref(lens), C.byref(refs)),
+               "pyr_pages_view")
+        c = self.cfg
+        self.pool = self._view(pool.value, (c.n_pages, page.value), torch.uint8)
+        self.table = self._view(table.value, (c.n_lists, c.max_pages), torch.int32)
+        self.lens = self._view(lens.value, (c.n_lists,), torch.int32)
+        self.refs = self._view(refs.value, (c.n_pages,), torch.int32)
+        self.reset()
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().pyr_pages_free(self.handle)
+            self.handle = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _view(self, ptr: int, shape, dtype):
+        off = ptr - self.buf.data_ptr()
+        nbytes = math.prod(shape) * torch.empty((), dtype=dtype).element_size()
+        return self.buf[off: off + nbytes].view(dtype).view(*shape)
+
+    def _run(self, name: str, stream, *args):
+        with torch.cuda.device(self.device):
+            _check(getattr(lib(), name)(self.handle, *args, C.c_void_p(_stream_ptr(stream))), name)
+
+    def _ids(self, t, what="lists"):
+        """Pointer to an int32 vector on the cache's device, None for NULL."""
+        if t is None:
+            return None
+        if t.dtype != torch.int32 or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{what}: expected a contiguous int32 tensor on {self.device}")
+        return t.data_ptr()
+
+    def _count(self, n, **vectors):
+        for what, t in vectors.items():
+            if t is not None and (t.dim() != 1 or t.shape[0] != n):
+                raise ValueError(f"{what}: expected {n} entries")
+
+    def _rows(self, a, b, what):
+        """Strides of a pair of [n, rows, heads, D] tensors (those of dimensions of size 1 do not count)."""
+        c = self.cfg
+        if a.dim() != 4 or a.shape[2] != c.n_kv_heads or a.shape[3] != c.head_dim or a.shape != b.shape or a.dtype != b.dtype:
+            raise ValueError(f"{what}: expected [n, rows, {c.n_kv_heads}, {c.head_dim}], keys and values alike")
+        sa, sb = self._strides(a, what), self._strides(b, what)
+        if sa != sb:
+            raise ValueError(f"{what}: keys and values need the same strides")
+        return sa
+
+    def _strides(self, t, what):
+        if t.device != self.device or t.dtype not in (torch.bfloat16, torch.float32) or (t.stride(-1) != 1 and t.shape[-1] != 1):
+            raise ValueError(f"{what}: expected bf16 or fp32 on {self.device} with a contiguous last dimension")
+        return [t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)]
+
+    def _idx(self, idx, n):
+        if idx is None:
+            return None, 1, 0
+        if idx.dim() != 3 or idx.shape[0] != n or idx.dtype != torch.int32 or idx.device != self.device:
+            raise ValueError(f"idx: expected [n, groups, rows] int32 on {self.device}")
+        g, rows = idx.shape[1], idx.shape[2]
+        if (rows > 1 and idx.stride(2) != 1) or (g > 1 and idx.stride(1) != rows):
+            raise ValueError("idx: its last two dimensions must be contiguous")
+        return idx.data_ptr(), g, idx.stride(0) if n > 1 else 0
+
+    # --- state
+    def reset(self, stream=None):
+        self._run("pyr_pages_reset", stream)
+
+    def status(self, stream=None) -> int:
+        """0, or the first device-side error since the last call (synchronises; reading clears it)."""
+        word = C.c_int32(0)
+        with torch.cuda.device(self.device):
+            st = lib().pyr_pages_status(self.handle, C.c_void_p(_stream_ptr(stream)), C.byref(word))
+        if st != word.value:
+            _check(st, "pyr_pages_status")
+        return word.value
+
+    # --- the operators
+    def reserve(self, lists, rows, stream=None):
+        """Pages for `rows` more rows (an int, or int32 [n]) of each list."""
+        n = lists.shape[0]
+        each = rows if isinstance(rows, int) else 0
+        rows = None if isinstance(rows, int) else rows
+        self._count(n, lists=lists, rows=rows)
+        self._run("pyr_pages_reserve", stream, self._ids(lists), n, self._ids(rows, "rows"), each)
+
+    def write(self, k, v, lists=None, first=None, idx=None, counts=None, stream=None):
+        """Stores rows of k, v [n, src_rows, Hkv, D] (those that idx names, or all): at the lists' ends, or from row first."""
+        n = k.shape[0]
+        sb, sn, sh = self._rows(k, v, "k, v")
+        self._count(n, lists=lists, first=first, counts=counts)
+        ip, groups, istride = self._idx(idx, n)
+        n_rows = idx.shape[2] if idx is not None else k.shape[1]
+        self._run("pyr_pages_write", stream, self._ids(lists), n, self._ids(first, "first"), k.data_ptr(), v.data_ptr(), sb, sn, sh,
+                  k.shape[1], _dt(k), ip, groups, istride, self._ids(counts, "counts"), n_rows)
+
+    def read(self, k, v, lists=None, first=None, counts=None, stream=None):
+        """Fills k, v [n, rows, Hkv, D] with the lists' rows from row first (0) on; rows a list does not have stay as they are."""
+        n = k.shape[0]
+        sb, sn, sh = self._rows(k, v, "k, v")
+        self._count(n, lists=lists, first=first, counts=counts)
+        self._run("pyr_pages_read", stream, self._ids(lists), n, self._ids(first, "first"), k.data_ptr(), v.data_ptr(), sb, sn, sh,
+                  _dt(k), self._ids(counts, "counts"), k.shape[1])
+
+    def attn(self, q, lists=None, out=None, lse=False, softmax_scale: float = 0.0, stream=None):
+        """Attention of q [n, q_len, Hq, D] over the lists' rows: out like q, and with lse=True also lse [n, Hq, q_len] fp32."""
+        if q.dim() != 4 or q.shape[3] != self.cfg.head_dim:
+            raise ValueError(f"q: expected [n, q_len, Hq, {self.cfg.head_dim}]")
+        n, t, hq, _ = q.shape
+        self._count(n, lists=lists)
+        qs = self._strides(q, "q")
+        with torch.cuda.device(self.device), torch.cuda.stream(stream):
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+            if out.shape != q.shape or out.dtype != q.dtype:
+                raise ValueError("out: expected a tensor like q")
+            stats = torch.empty(n, hq, t, dtype=torch.float32, device=self.device) if lse else None
+            self._run("pyr_pages_attn", None, self._ids(lists), n, q.data_ptr(), *qs, out.data_ptr(), *self._strides(out, "out"),
+                      stats.data_ptr() if lse else None, t, hq, _dt(q), float(softmax_scale))
+        return (out, stats) if lse else out
+
+    def fork(self, src, dst, stream=None):
+        """Lists dst become copies of lists src that share their pages."""
+        n = src.shape[0]
+        self._count(n, src=src, dst=dst)
+        self._run("pyr_pages_fork", stream, self._ids(src, "src"), self._ids(dst, "dst"), n)
+
+    def trim(self, lists, rows=None, stream=None):
+        """Cuts the lists to `rows` (int32 [n]; None: empties them) and gives up the pages behind."""
+        n = lists.shape[0]
+        self._count(n, lists=lists, rows=rows)
+        self._run("pyr_pages_trim", stream, self._ids(lists), n, self._ids(rows, "rows"))
+
+    def compact(self, src, dst, idx=None, counts=None, n_rows=None, stream=None):
+        """Rows 0 .. of lists dst become the rows idx of lists src (idx None: their first n_rows rows); src is dst: in place."""
+        n = src.shape[0]
+        self._count(n, src=src, dst=dst, counts=counts)
+        ip, groups, istride = self._idx(idx, n)
+        rows = idx.shape[2] if idx is not None else int(n_rows)
+        self._run("pyr_pages_compact", stream, self._ids(src, "src"), self._ids(dst, "dst"), n, ip, groups, istride,
+                  self._ids(counts, "counts"), rows)

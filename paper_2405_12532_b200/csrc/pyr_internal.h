@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "pages_index.h"
 #include "pyr.h"
 
 namespace pyr {
@@ -153,6 +154,57 @@ cudaError_t launch_gemm_skinny(const void* x, const void* w, const void* res, vo
 cudaError_t launch_glue_rope(void* x, const int32_t* pos, int64_t tokens, int H, int D, int dtype, cudaStream_t s);
 cudaError_t launch_glue_swiglu(const void* g, const void* u, void* out, int64_t n, int dtype, cudaStream_t s);
 cudaError_t launch_glue_argmax(const void* x, int32_t* out, int64_t rows, int n, int dtype, cudaStream_t s);
+// Paged 4-bit cache (csrc/pages_*.cu).
+struct PagesWriteArgs {
+  PagesView p;
+  const int32_t* lists; int n;
+  const int32_t* first;            // [n] or null
+  const void* k; const void* v;    // write: sources; read: destinations
+  int64_t sb, sn, sh;              // elements
+  int src_rows, dtype;
+  const int32_t* idx; int idx_groups; int64_t idx_stride;
+  const int32_t* counts; int n_rows;
+  int32_t* plan;                   // [n_lists]: the entry's first row, -1 if it is refused
+};
+struct PagesMoveArgs {
+  PagesView p;
+  const int32_t* src; const int32_t* dst; int n;
+  const int32_t* idx; int idx_groups; int64_t idx_stride;
+  const int32_t* counts; int n_rows;
+  int32_t* plan;                   // [n_lists]: rows to move, -1 if the entry is refused
+};
+struct PagesReserveArgs {
+  PagesView p;
+  const int32_t* lists; int n;
+  const int32_t* rows; int rows_each;
+  int slices;                      // of kReserveSlice pages
+  int32_t* free_ids;               // [slices * kReserveSlice]: each slice's free pages, ascending
+  int32_t* slice_first;            // [slices + 1]: free pages before each slice
+  int32_t* plan;                   // [n_lists][4]: rank of the first new page, page to copy (-1), first new slot, new slots
+  int32_t* control;                // [0] slices done, [1] 1 if the plan holds
+};
+struct PagesAttnArgs {
+  PagesView p;
+  const int32_t* lists; int n;
+  const void* q; void* out; float* lse;
+  int64_t qsb, qst, qsh, osb, ost, osh;   // elements
+  int T, Hq, rep, dtype;
+  float scale;
+  float* partial;                  // [kAttnMaxCtas][2][kAttnCols][D + 2]
+  int32_t* arrived;                // [kAttnMaxCtas], zero between calls
+};
+constexpr int kReserveSlice = 4096;
+constexpr int kAttnMaxCtas = 1024;
+constexpr int kAttnCols = 8;
+cudaError_t launch_pages_write(const PagesWriteArgs& a, int* launches, cudaStream_t s);
+cudaError_t launch_pages_read(const PagesWriteArgs& a, int* launches, cudaStream_t s);
+cudaError_t launch_pages_reserve(const PagesReserveArgs& a, int* launches, cudaStream_t s);
+cudaError_t launch_pages_fork(const PagesView& p, const int32_t* src, const int32_t* dst, int n, int* launches, cudaStream_t s);
+cudaError_t launch_pages_trim(const PagesView& p, const int32_t* lists, int n, const int32_t* rows, int* launches,
+                              cudaStream_t s);
+cudaError_t launch_pages_compact(const PagesMoveArgs& a, int* launches, cudaStream_t s);
+cudaError_t launch_pages_attn(const PagesAttnArgs& a, int* launches, cudaStream_t s);
+
 int gen_score_qtiles(int Lw);
 cudaError_t launch_gen_score(const GenScoreArgs& a, cudaStream_t s);     // two kernels
 // rows of row_bytes (a multiple of 16) per batch entry, byte strides
