@@ -129,29 +129,30 @@ __device__ __forceinline__ void write_lse(const PagesAttnArgs& a, int entry, int
 }
 
 // Shared memory of a CTA: per warp a ring of tiles, the queries of its segment and two states of [cols][D + 2].
-template <int D, int COLS>
+template <class Body>
 struct Layout {
-  static constexpr int state = COLS * (D + 2);
+  static constexpr int state = Body::COLS * (Body::kDim + 2);
   static __host__ __device__ int ring_bytes(int tile_bytes) { return kWarps * kStages * tile_bytes; }
   static __host__ __device__ int total(int tile_bytes) {
-    return 128 + ring_bytes(tile_bytes) + kWarps * (COLS * D + 2 * state) * 4;
+    return 128 + ring_bytes(tile_bytes) + kWarps * (Body::kQueryFloats + 2 * state) * 4;
   }
 };
 
 // ------------------------------------------------------------------ one warp's tiles, on CUDA cores
 // Lane 4 i + j. K: rows i and i + 8, the quarter of the dimensions that chunk j of a stored row holds. V: the eighth of the
 // dimensions that chunk i holds, of the rows j, j + 4, j + 8, j + 12.
-template <class T, int D, int GROUP, int COLS>
+template <class T, int D, int GROUP>
 struct CoreBody {
+  using Type = T;
+  static constexpr int kDim = D, COLS = 4, kBlocks = 2, kQueryFloats = COLS * D;   // queries lie in shared memory
   static constexpr int G = D / GROUP, U = GROUP / 32, X = D / 32;   // X: words of K / halves of V in a lane's chunk
   float acc[COLS][4 * X];
   float m[COLS], l[COLS], qsum[COLS][G];
   int limit[COLS];
-  int ncols;
 
   __device__ __forceinline__ void begin(const PagesAttnArgs& a, const Cursor& c, int cols_total, float* qs, int lane) {
     const int j = lane & 3, col0 = c.cg * COLS;
-    ncols = min(COLS, cols_total - col0);
+    const int ncols = min(COLS, cols_total - col0);
 #pragma unroll
     for (int x = 0; x < COLS; ++x) {
       m[x] = -INFINITY; l[x] = 0.f;
@@ -214,6 +215,7 @@ struct CoreBody {
         s[rr][x] = r < rows && row0 + r < limit[x] ? s[rr][x] * sc2 : -INFINITY;
       }
     }
+    const bool edge = row0 + kPageTile > limit[0];               // some column sees less than the whole tile
     float p[2][COLS];
 #pragma unroll
     for (int x = 0; x < COLS; ++x) {
@@ -248,7 +250,13 @@ struct CoreBody {
             const uint32_t half = codes[g * U + u];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float val = fmaf(scale, (float)((half >> (4 * k)) & 15u), zero);
+              float val = fmaf(scale, (float)((half >> (4 * k)) & 15u), zero);
+              if (edge && val != val) {      // a NaN that a column does not see must not reach it through 0 x NaN
+#pragma unroll
+                for (int x = 0; x < COLS; ++x)
+                  if (row0 + r < limit[x]) acc[x][(g * U + u) * 4 + k] = val;
+                val = 0.f;
+              }
 #pragma unroll
               for (int x = 0; x < COLS; ++x) acc[x][(g * U + u) * 4 + k] = fmaf(pr[x], val, acc[x][(g * U + u) * 4 + k]);
             }
@@ -278,9 +286,239 @@ struct CoreBody {
   }
 };
 
-template <class T, int D, int GROUP, int COLS>
-__global__ void __launch_bounds__(kThreads) attn_kernel(PagesAttnArgs a, int cgs) {
-  using L = Layout<D, COLS>;
+// ------------------------------------------------------------------ one warp's tiles, on tensor cores (bf16)
+// Rows of the cache are the 16 rows of m16n8k16, the (up to 8) query rows its 8 columns: S^T = K Q^T, O^T = V^T P^T. The
+// instruction is bound neither way here: what counts is that a register of codes becomes an operand in few steps. Lane
+// 4 i + j holds, of K's row i (and i + 8), chunk j: a word's nibbles k and k + 4 are a pair of operands, and since any order
+// of the dimensions will do as long as the queries have the same, the words are stored in the order in which lanes take
+// them. Of V it holds chunk i of four rows, two rows' halves side by side giving pairs of rows of one dimension.
+// (Legacy warp-level MMA: a decode step reads every code once, and tcgen05 would need the codes as 8- or 16-bit
+// operands in shared memory first.)
+// Row r of the matrices is row r ^ ((r >> 1) & 1) of the tile, which spreads the lanes' shared-memory reads over the banks.
+__device__ __forceinline__ void mma_full(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+               "{%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// Four pairs of codes (nibbles k and k + 4 of x) as bf16 pairs, less 8: 0x4300 | n is 128 + n.
+__device__ __forceinline__ void centred4(uint32_t x, uint32_t* y) {
+  const uint32_t bias = 0x43084308u;             // 136
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t v = ((x >> (4 * k)) & 0x000F000Fu) | 0x43004300u;
+    const __nv_bfloat162 d = __hsub2(reinterpret_cast<const __nv_bfloat162&>(v), reinterpret_cast<const __nv_bfloat162&>(bias));
+    y[k] = reinterpret_cast<const uint32_t&>(d);
+  }
+}
+
+template <int D, int GROUP>
+struct MmaBody {
+  using Type = __nv_bfloat16;
+  static constexpr int kDim = D, COLS = 8, kBlocks = 3, kQueryFloats = 0;
+  static constexpr int G = D / GROUP, U = GROUP / 32, X = D / 32;
+  static constexpr float kLazy = 8.f;            // the maximum is raised once a score is 2^8 above it
+  uint32_t qf[X][4];
+  float qsum[G][2], o[X][2][4], zacc[G][2], m[2], l[2], raise[2];
+  int limit[2], limit_min;
+
+  __device__ __forceinline__ void begin(const PagesAttnArgs& a, const Cursor& c, int cols_total, float*, int lane) {
+    const int i = lane >> 2, j = lane & 3, col0 = c.cg * COLS;
+    const int col = col0 + i, tok = col / a.rep, head = c.h * a.rep + col % a.rep;
+    const uint16_t* q = static_cast<const uint16_t*>(a.q) + (int64_t)c.entry * a.qsb + (int64_t)tok * a.qst + (int64_t)head * a.qsh;
+#pragma unroll
+    for (int w = 0; w < X; ++w) {
+      uint4 r = make_uint4(0, 0, 0, 0);
+      if (col < cols_total) r = *reinterpret_cast<const uint4*>(q + 8 * k_slot_word(D, GROUP, j * X + w));
+      qf[w][0] = __byte_perm(r.x, r.z, 0x5410); qf[w][1] = __byte_perm(r.x, r.z, 0x7632);
+      qf[w][2] = __byte_perm(r.y, r.w, 0x5410); qf[w][3] = __byte_perm(r.y, r.w, 0x7632);
+    }
+    // sums of the queries over each group, by the instruction itself: every row of a matrix of ones
+    const uint32_t ones[4] = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        mma_full(s, ones, qf[g * U + u][0], qf[g * U + u][1]);
+        mma_full(s, ones, qf[g * U + u][2], qf[g * U + u][3]);
+      }
+      qsum[g][0] = s[0]; qsum[g][1] = s[1];
+      zacc[g][0] = zacc[g][1] = 0.f;
+    }
+#pragma unroll
+    for (int x = 0; x < X; ++x)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) o[x][y][0] = o[x][y][1] = o[x][y][2] = o[x][y][3] = 0.f;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      m[x] = -INFINITY; raise[x] = -INFINITY; l[x] = 0.f;
+      limit[x] = c.len - (a.T - 1 - (col0 + 2 * j + x) / a.rep);
+    }
+    limit_min = c.len - (a.T - 1 - col0 / a.rep);
+  }
+
+  __device__ __forceinline__ void tile(const PagesAttnArgs& a, const uint8_t* tp, int row0, int rows, const float*, int lane) {
+    const int i = lane >> 2, j = lane & 3;
+    const int ri = i ^ ((i >> 1) & 1);           // tile rows of matrix rows i and i + 8
+    const float sc2 = a.scale * kLog2e;
+    const bool edge = rows < kPageTile || row0 + kPageTile > limit_min;
+
+    // S^T = K Q^T, one accumulator per group, then scale and zero
+    uint32_t kc[2][X];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(tp + tile_k_row(D, ri + 8 * r)) + j * X;
+      if constexpr (X == 4) {
+        const uint4 v = *reinterpret_cast<const uint4*>(src);
+        kc[r][0] = v.x; kc[r][1] = v.y; kc[r][2] = v.z; kc[r][3] = v.w;
+      } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(src);
+        kc[r][0] = v.x; kc[r][1] = v.y;
+      }
+    }
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        uint32_t lo[4], hi[4];
+        centred4(kc[0][g * U + u], lo);
+        centred4(kc[1][g * U + u], hi);
+        const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
+        mma_full(c, a0, qf[g * U + u][0], qf[g * U + u][1]);
+        mma_full(c, a1, qf[g * U + u][2], qf[g * U + u][3]);
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(tp + tile_k_word(D, G, ri + 8 * r, g));
+        const float scale = __uint_as_float(w << 16), zero = fmaf(8.f, scale, __uint_as_float(w & 0xffff0000u));
+#pragma unroll
+        for (int x = 0; x < 2; ++x) s[2 * r + x] += fmaf(scale, c[2 * r + x], zero * qsum[g][x]);
+      }
+    }
+    bool seen[4] = {true, true, true, true};
+    if (edge) {                                  // rows behind the end hold anything: replaced, not multiplied away
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          seen[2 * r + x] = ri + 8 * r < rows && row0 + ri + 8 * r < limit[x];
+          if (!seen[2 * r + x]) s[2 * r + x] = -INFINITY;
+        }
+    }
+    if (__any_sync(0xffffffffu, fmaxf(s[0], s[2]) > raise[0] || fmaxf(s[1], s[3]) > raise[1])) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        float mx = fmaxf(s[x], s[2 + x]);
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+        const float m_new = fmaxf(m[x], mx * sc2);
+        const float corr = m_new == -INFINITY ? 1.f : ex2(m[x] - m_new);
+        m[x] = m_new;
+        raise[x] = (m_new + kLazy) / sc2;
+        l[x] *= corr;
+#pragma unroll
+        for (int g = 0; g < G; ++g) zacc[g][x] *= corr;
+#pragma unroll
+        for (int y = 0; y < X; ++y) {
+          o[y][0][x] *= corr; o[y][0][2 + x] *= corr;
+          o[y][1][x] *= corr; o[y][1][2 + x] *= corr;
+        }
+      }
+    }
+    float p[4];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float ref = m[x] == -INFINITY ? 0.f : m[x];
+      p[x] = ex2(fmaf(s[x], sc2, -ref));
+      p[2 + x] = ex2(fmaf(s[2 + x], sc2, -ref));
+      l[x] += p[x] + p[2 + x];
+    }
+
+    // O^T += V^T P^T, the group's scale multiplied into P. P is given as the sum of two bf16 numbers: rounded to one, it
+    // would be as far off as the output's own rounding.
+    uint32_t vc[4][X / 2];                       // rows of matrix rows 2 j, 2 j + 1, 2 j + 8, 2 j + 9
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int mr = 2 * j + (r & 1), row = (mr ^ ((mr >> 1) & 1)) + 8 * (r >> 1);
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(tp + tile_v_row(D, row)) + i * (X / 2);
+      if constexpr (X == 4) {
+        const uint2 v = *reinterpret_cast<const uint2*>(src);
+        vc[r][0] = v.x; vc[r][1] = v.y;
+      } else {
+        vc[r][0] = *src;
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      uint32_t hi[2], lo[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(tp + tile_v_word(D, G, ri + 8 * r, g));
+        const float scale = __uint_as_float(w << 16), zero = fmaf(8.f, scale, __uint_as_float(w & 0xffff0000u));
+        float ps[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          ps[x] = seen[2 * r + x] ? p[2 * r + x] * scale : 0.f;
+          if (seen[2 * r + x]) zacc[g][x] = fmaf(p[2 * r + x], zero, zacc[g][x]);
+        }
+        const uint32_t h = pack_bf16(ps[0], ps[1]);
+        hi[r] = transpose8x8(h);
+        lo[r] = transpose8x8(pack_bf16(ps[0] - __uint_as_float(h << 16), ps[1] - __uint_as_float(h & 0xffff0000u)));
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int x = g * U + u;
+        const uint32_t sel = (x & 1) ? 0x7632 : 0x5410;
+        uint32_t v0[4], v1[4];
+        centred4(__byte_perm(vc[0][x >> 1], vc[1][x >> 1], sel), v0);
+        centred4(__byte_perm(vc[2][x >> 1], vc[3][x >> 1], sel), v1);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const uint32_t av[4] = {v0[2 * y], v0[2 * y + 1], v1[2 * y], v1[2 * y + 1]};
+          mma_full(o[x][y], av, hi[0], hi[1]);
+          mma_full(o[x][y], av, lo[0], lo[1]);
+        }
+      }
+    }
+  }
+
+  __device__ __forceinline__ void end(float* state, int lane) {
+    const int i = lane >> 2, j = lane & 3;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+      for (int b = 4; b < 32; b <<= 1) {
+        l[x] += __shfl_xor_sync(0xffffffffu, l[x], b);
+#pragma unroll
+        for (int g = 0; g < G; ++g) zacc[g][x] += __shfl_xor_sync(0xffffffffu, zacc[g][x], b);
+      }
+      float* st = state + (2 * j + x) * (D + 2);
+#pragma unroll
+      for (int y = 0; y < X; ++y) {
+        const int d = 4 * v_slot_half(D, GROUP, i * X + y);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) st[d + k] = o[y][k >> 1][2 * (k & 1) + x] + zacc[y / U][x];
+      }
+      if (i == 0) { st[D] = m[x]; st[D + 1] = l[x]; }
+    }
+    __syncwarp();
+  }
+};
+
+template <class Body>
+__global__ void __launch_bounds__(kThreads, Body::kBlocks) attn_kernel(PagesAttnArgs a, int cgs) {
+  using T = typename Body::Type;
+  using L = Layout<Body>;
+  constexpr int D = Body::kDim, COLS = Body::COLS;
   extern __shared__ uint8_t smem_raw[];
   __shared__ Sched sh;
   __shared__ uint64_t full[kWarps][kStages];
@@ -290,8 +528,8 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(PagesAttnArgs a, int cgs
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~uintptr_t(127));
   uint8_t* ring = base + warp * kStages * tile_bytes;
   float* floats = reinterpret_cast<float*>(base + L::ring_bytes(tile_bytes));
-  float* qs = floats + warp * COLS * D;
-  float* states = floats + kWarps * COLS * D;    // [warp][2][COLS][D + 2]
+  float* qs = floats + warp * Body::kQueryFloats;
+  float* states = floats + kWarps * Body::kQueryFloats;    // [warp][2][COLS][D + 2]
   const int cols_total = a.T * a.rep;
 
   if (lane == 0) {
@@ -372,7 +610,7 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(PagesAttnArgs a, int cgs
     };
     for (int s = 0; s < kStages && to_load > 0; ++s) issue();
 
-    CoreBody<T, D, GROUP, COLS> body;
+    Body body;
     while (left > 0) {
       // ---- a segment: the warp's tiles of one (entry, head, column group)
       const int t0 = cu.t;
@@ -506,39 +744,33 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(PagesAttnArgs a, int cgs
   }
 }
 
-template <class T, int D, int GROUP, int COLS>
+template <class Body>
 cudaError_t run_attn(const PagesAttnArgs& a, cudaStream_t s) {
-  const int cgs = (a.T * a.rep + COLS - 1) / COLS;
-  const int smem = Layout<D, COLS>::total(a.p.tile_bytes);
-  cudaError_t e = cudaFuncSetAttribute(attn_kernel<T, D, GROUP, COLS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const int cgs = (a.T * a.rep + Body::COLS - 1) / Body::COLS;
+  const int smem = Layout<Body>::total(a.p.tile_bytes);
+  cudaError_t e = cudaFuncSetAttribute(attn_kernel<Body>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const int sms = device_sm_count();
   if (sms <= 0) return cudaErrorUnknown;
   // a grid that the machine holds at once, no larger than the work can be
   const long long most = (long long)a.n * a.p.Hkv * cgs * attn_tiles(a.p.max_pages * a.p.page_rows);
   long long ctas = (most + kWarps * kMinUnits - 1) / (kWarps * kMinUnits);
-  if (ctas > 3LL * sms) ctas = 3LL * sms;
+  if (ctas > (long long)Body::kBlocks * sms) ctas = (long long)Body::kBlocks * sms;
   if (ctas > kAttnMaxCtas) ctas = kAttnMaxCtas;
-  attn_kernel<T, D, GROUP, COLS><<<(unsigned)ctas, kThreads, smem, s>>>(a, cgs);
+  attn_kernel<Body><<<(unsigned)ctas, kThreads, smem, s>>>(a, cgs);
   return cudaGetLastError();
 }
 
-template <class T>
+template <int D, int GROUP>
 cudaError_t pick(const PagesAttnArgs& a, cudaStream_t s) {
-  constexpr int C = 4;
-  if (a.p.D == 128) {
-    if (a.p.group == 32) return run_attn<T, 128, 32, C>(a, s);
-    if (a.p.group == 64) return run_attn<T, 128, 64, C>(a, s);
-    return run_attn<T, 128, 128, C>(a, s);
-  }
-  if (a.p.group == 32) return run_attn<T, 64, 32, C>(a, s);
-  return run_attn<T, 64, 64, C>(a, s);
+  return a.dtype == PYR_F32 ? run_attn<CoreBody<float, D, GROUP>>(a, s) : run_attn<MmaBody<D, GROUP>>(a, s);
 }
 
 }  // namespace
 
 cudaError_t launch_pages_attn(const PagesAttnArgs& a, int* launches, cudaStream_t s) {
-  const cudaError_t e = a.dtype == PYR_F32 ? pick<float>(a, s) : pick<__nv_bfloat16>(a, s);
+  const cudaError_t e = a.p.D == 128 ? (a.p.group == 32 ? pick<128, 32>(a, s) : a.p.group == 64 ? pick<128, 64>(a, s) : pick<128, 128>(a, s))
+                                     : (a.p.group == 32 ? pick<64, 32>(a, s) : pick<64, 64>(a, s));
   if (e == cudaSuccess) ++*launches;
   return e;
 }

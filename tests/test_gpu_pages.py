@@ -310,6 +310,27 @@ def test_attention_shows_nan_rows_where_they_are_seen(dtype):
     assert torch.equal(bad.cpu(), want) and torch.equal(torch.isnan(lse).cpu(), want.transpose(1, 2))
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_keeps_nan_values_from_tokens_that_do_not_see_them(dtype):
+    """A NaN group of V in the last row: NaN in that group's dimensions for the token that sees the row, nothing elsewhere - also
+    not through a probability of zero times NaN. Stale bytes behind a list's end (NaN scales) never count."""
+    p = _pages(1, 128, 32, 16, 8, 2, 4)
+    k, v = _rand(2, 37, 1, 128, seed=33, dtype=dtype), _rand(2, 37, 1, 128, seed=34, dtype=dtype)
+    v[0, 36, 0, 70] = float("inf")
+    p.reserve(_ids(0, 1), 37)
+    p.write(k, v)
+    q = _rand(2, 3, 5, 128, seed=35, dtype=dtype)
+    out, lse = p.attn(q, lse=True)
+    want = torch.zeros(2, 3, 5, 128, dtype=torch.bool)
+    want[0, 2, :, 64:96] = True
+    assert torch.equal(torch.isnan(out).cpu(), want) and not bool(torch.isnan(lse).any())
+    clean = v.clone()
+    clean[0, 36] = 0
+    p.write(k, clean, first=_ids(0, 0))
+    ref = p.attn(q)
+    assert torch.equal(ref[0, :2], out[0, :2]) and torch.equal(ref[1], out[1]) and p.status() == 0
+
+
 def test_attention_far_into_a_pool_beyond_four_gigabytes():
     """Pages whose byte offsets pass 2^32, written, attended, moved and read back."""
     hkv, D, pr = 32, 128, 64
