@@ -12,6 +12,7 @@
 //
 // A warp loads its tiles itself: lane 0 keeps a ring of bulk copies (a tile is one contiguous copy) in flight.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include "pyr_internal.h"
 #include "tc_common.cuh"
@@ -25,7 +26,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
-constexpr int kStages = 4;               // tiles in a warp's ring
+constexpr int kStageTiles = 2;           // a stage of a warp's ring: one copy of up to two tiles
 constexpr int kMinUnits = 4;             // a warp's share is at least this many tiles: merging costs more than they do
 
 __device__ __forceinline__ void record(int* status, int code) { atomicCAS(status, 0, code); }
@@ -51,6 +52,7 @@ struct Sched {
   int entry[kWarps];
   int abort_flag;
   int last[2];
+  float den[kAttnCols];
   Piece piece[kWarps][2];
 };
 
@@ -81,61 +83,61 @@ __device__ __forceinline__ long long entry_units(const PagesAttnArgs& a, int i, 
   return l < 0 ? 0 : (long long)attn_tiles(pages_len(a.p, l)) * a.p.Hkv * cgs;
 }
 
-// Position in the numbering of units: an entry, and a tile of one of its heads' column groups.
-struct Cursor {
-  int entry, l, len, tiles, h, cg, t;
-  long long u_entry;                     // first unit of the entry
+// The (entry, head, column group) that a warp works on. `t` is the first of its tiles that the warp takes.
+struct Place {
+  int entry, len, tiles, h, cg, t;
 
-  __device__ __forceinline__ void open(const PagesAttnArgs& a, int cgs) {
-    l = pages_list(a.p, a.lists, entry);
+  __device__ __forceinline__ int open(const PagesAttnArgs& a) {   // the entry's list
+    const int l = pages_list(a.p, a.lists, entry);
     len = l < 0 ? 0 : pages_len(a.p, l);
     tiles = l < 0 ? 0 : (int)attn_tiles(len);
-    (void)cgs;
+    return l;
   }
-  __device__ __forceinline__ void start(const PagesAttnArgs& a, int cgs, int e, long long first, long long u) {
-    entry = e; u_entry = first;
-    open(a, cgs);
-    const long long o = u - first;
+  __device__ __forceinline__ int start(const PagesAttnArgs& a, int cgs, int e, long long o) {   // unit o of entry e
+    entry = e;
+    const int l = open(a);
     t = (int)(o % tiles);
     const long long hc = o / tiles;
     cg = (int)(hc % cgs);
     h = (int)(hc / cgs);
+    return l;
   }
-  __device__ __forceinline__ void next_tile(const PagesAttnArgs& a, int cgs) {
-    if (++t < tiles) return;
+  // the next one; returns its list, or -1 if the list is the same
+  __device__ __forceinline__ int next(const PagesAttnArgs& a, int cgs) {
     t = 0;
-    if (++cg < cgs) return;
+    if (++cg < cgs) return -1;
     cg = 0;
-    if (++h < a.p.Hkv) return;
+    if (++h < a.p.Hkv) return -1;
     h = 0;
-    do {                                 // refused entries have no unit
-      u_entry += (long long)tiles * a.p.Hkv * cgs;
-      if (++entry >= a.n) { tiles = 1; len = 0; l = -1; return; }
-      open(a, cgs);
-    } while (tiles == 0);
+    int l = -1;
+    do { ++entry; l = open(a); } while (l < 0 && entry + 1 < a.n);   // refused entries have no unit
+    return l;
   }
 };
 
-// Writes column c of an entry's head: out = num / den for the D dimensions held by `lane`-strided callers.
-template <class T, int D>
-__device__ __forceinline__ void write_out(const PagesAttnArgs& a, int entry, int h, int col, int d, float value) {
-  const int tok = col / a.rep, head = h * a.rep + col % a.rep;
-  static_cast<T*>(a.out)[(int64_t)entry * a.osb + (int64_t)tok * a.ost + (int64_t)head * a.osh + d] = from_f<T>(value);
-}
-__device__ __forceinline__ void write_lse(const PagesAttnArgs& a, int entry, int h, int col, float m, float den) {
-  if (!a.lse) return;
-  const int tok = col / a.rep, head = h * a.rep + col % a.rep;
-  a.lse[((int64_t)entry * a.Hq + head) * a.T + tok] = den > 0.f ? (m + log2f(den)) * kLn2 : (den == 0.f ? -INFINITY : den);
+// Where an entry's column lies in out and lse.
+struct OutPlace {
+  int64_t out, lse;
+  __device__ __forceinline__ OutPlace(const PagesAttnArgs& a, int entry, int h, int col) {
+    const int tok = col / a.rep, head = h * a.rep + col % a.rep;
+    out = (int64_t)entry * a.osb + (int64_t)tok * a.ost + (int64_t)head * a.osh;
+    lse = ((int64_t)entry * a.Hq + head) * a.T + tok;
+  }
+};
+__device__ __forceinline__ float lse_of(float m, float den) {
+  return den > 0.f ? (m + log2f(den)) * kLn2 : (den == 0.f ? -INFINITY : den);
 }
 
-// Shared memory of a CTA: per warp a ring of tiles, the queries of its segment and two states of [cols][D + 2].
+// Shared memory of a CTA: per warp a ring of tiles, the queries of its segment and a state of [cols][D + 2]; the state that a
+// warp leaves last goes where its ring was.
 template <class Body>
 struct Layout {
   static constexpr int state = Body::COLS * (Body::kDim + 2);
-  static __host__ __device__ int ring_bytes(int tile_bytes) { return kWarps * kStages * tile_bytes; }
-  static __host__ __device__ int total(int tile_bytes) {
-    return 128 + ring_bytes(tile_bytes) + kWarps * (Body::kQueryFloats + 2 * state) * 4;
-  }
+  static constexpr int ring = Body::kStages * kStageTiles * Body::kTileBytes;
+  static constexpr int warp_bytes = (ring + (Body::kQueryFloats + state) * 4 + 127) / 128 * 128;
+  static_assert(state * 4 <= ring, "the last state fits the ring");
+  static_assert(kAttnMaxCtas * Body::COLS * 4 <= kWarps * warp_bytes, "a weight per CTA and column fits where the rings were");
+  static constexpr int total = kWarps * warp_bytes;
 };
 
 // ------------------------------------------------------------------ one warp's tiles, on CUDA cores
@@ -145,12 +147,13 @@ template <class T, int D, int GROUP>
 struct CoreBody {
   using Type = T;
   static constexpr int kDim = D, COLS = 4, kBlocks = 2, kQueryFloats = COLS * D;   // queries lie in shared memory
+  static constexpr int kStages = 2, kTileBytes = kPageTile * (D + 8 * (D / GROUP));
   static constexpr int G = D / GROUP, U = GROUP / 32, X = D / 32;   // X: words of K / halves of V in a lane's chunk
   float acc[COLS][4 * X];
   float m[COLS], l[COLS], qsum[COLS][G];
   int limit[COLS];
 
-  __device__ __forceinline__ void begin(const PagesAttnArgs& a, const Cursor& c, int cols_total, float* qs, int lane) {
+  __device__ __forceinline__ void begin(const PagesAttnArgs& a, const Place& c, int cols_total, float* qs, int lane) {
     const int j = lane & 3, col0 = c.cg * COLS;
     const int ncols = min(COLS, cols_total - col0);
 #pragma unroll
@@ -266,37 +269,61 @@ struct CoreBody {
     }
   }
 
-  // the state of the warp's segment, in dimension order
-  __device__ __forceinline__ void end(float* state, int lane) {
-    const int i = lane >> 2, j = lane & 3;
+  // sums over the lanes that share a row or a dimension
+  __device__ __forceinline__ void end() {
 #pragma unroll
     for (int x = 0; x < COLS; ++x) {
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) l[x] += __shfl_xor_sync(0xffffffffu, l[x], o);
 #pragma unroll
       for (int y = 0; y < 4 * X; ++y) {
-        float v = acc[x][y];
-        v += __shfl_xor_sync(0xffffffffu, v, 1);
-        v += __shfl_xor_sync(0xffffffffu, v, 2);
-        if (j == (y & 3)) state[x * (D + 2) + 4 * v_slot_half(D, GROUP, i * X + (y >> 2)) + (y & 3)] = v;
+        acc[x][y] += __shfl_xor_sync(0xffffffffu, acc[x][y], 1);
+        acc[x][y] += __shfl_xor_sync(0xffffffffu, acc[x][y], 2);
       }
+    }
+  }
+  __device__ __forceinline__ void keep(float* state, int lane) const {
+    const int i = lane >> 2, j = lane & 3;
+#pragma unroll
+    for (int x = 0; x < COLS; ++x) {
+#pragma unroll
+      for (int y = 0; y < 4 * X; ++y)
+        if (j == (y & 3)) state[x * (D + 2) + 4 * v_slot_half(D, GROUP, i * X + (y >> 2)) + (y & 3)] = acc[x][y];
       if (lane == 0) { state[x * (D + 2) + D] = m[x]; state[x * (D + 2) + D + 1] = l[x]; }
     }
-    __syncwarp();
+  }
+  __device__ __forceinline__ void write(const PagesAttnArgs& a, const Place& c, int cols_total, int lane) const {
+    const int i = lane >> 2, j = lane & 3;
+#pragma unroll
+    for (int x = 0; x < COLS; ++x) {
+      if (c.cg * COLS + x >= cols_total) break;
+      const OutPlace at(a, c.entry, c.h, c.cg * COLS + x);
+      const float inv = l[x] == 0.f ? 0.f : 1.f / l[x];
+#pragma unroll
+      for (int y = 0; y < 4 * X; ++y)
+        if (j == (y & 3))
+          static_cast<T*>(a.out)[at.out + 4 * v_slot_half(D, GROUP, i * X + (y >> 2)) + (y & 3)] = from_f<T>(acc[x][y] * inv);
+      if (lane == 0 && a.lse) a.lse[at.lse] = lse_of(m[x], l[x]);
+    }
   }
 };
 
 // ------------------------------------------------------------------ one warp's tiles, on tensor cores (bf16)
 // Rows of the cache are the 16 rows of m16n8k16, the (up to 8) query rows its 8 columns: S^T = K Q^T, O^T = V^T P^T. The
-// instruction is bound neither way here: what counts is that a register of codes becomes an operand in few steps. Lane
+// instruction's rate is far from a bound here; what counts is that a register of codes becomes an operand in few steps. Lane
 // 4 i + j holds, of K's row i (and i + 8), chunk j: a word's nibbles k and k + 4 are a pair of operands, and since any order
 // of the dimensions will do as long as the queries have the same, the words are stored in the order in which lanes take
 // them. Of V it holds chunk i of four rows, two rows' halves side by side giving pairs of rows of one dimension.
 // (Legacy warp-level MMA: a decode step reads every code once, and tcgen05 would need the codes as 8- or 16-bit
 // operands in shared memory first.)
 // Row r of the matrices is row r ^ ((r >> 1) & 1) of the tile, which spreads the lanes' shared-memory reads over the banks.
+//
+// Operands are f16: its 10 bits of mantissa take a nibble in two places, so that a word's eight codes need one shift, and they
+// hold P to 2^-12. What f16 lacks is range, so both factors that are not codes are normalised by powers of two: a query row
+// by its largest element (what is then below f16's smallest step is below 2^-24 of that element), and the scales that
+// multiply P by a factor per group that follows them (`norm`).
 __device__ __forceinline__ void mma_full(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
                "{%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -306,40 +333,73 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// Four pairs of codes (nibbles k and k + 4 of x) as bf16 pairs, less 8: 0x4300 | n is 128 + n.
+__device__ __forceinline__ uint32_t as_u32(__half2 x) { return reinterpret_cast<uint32_t&>(x); }
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return reinterpret_cast<__half2&>(x); }
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return as_u32(__floats2half2_rn(lo, hi)); }
+// (x & mask) | bits in one instruction
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x), "r"(mask), "r"(bits));
+  return y;
+}
+// The four pairs of codes (nibbles k and k + 4) of x as f16 pairs, less 8: 0x6400 | n is 1024 + n, 0x6400 | 16 n is
+// 1024 + 16 n.
 __device__ __forceinline__ void centred4(uint32_t x, uint32_t* y) {
-  const uint32_t bias = 0x43084308u;             // 136
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t v = ((x >> (4 * k)) & 0x000F000Fu) | 0x43004300u;
-    const __nv_bfloat162 d = __hsub2(reinterpret_cast<const __nv_bfloat162&>(v), reinterpret_cast<const __nv_bfloat162&>(bias));
-    y[k] = reinterpret_cast<const uint32_t&>(d);
-  }
+  const __half2 less = as_half2(0xE408E408u);                // -1032
+  const __half2 part = as_half2(0x2C002C00u), off = as_half2(0xD480D480u);   // 1/16, -72
+  const uint32_t z = x >> 8;
+  y[0] = as_u32(__hadd2(as_half2(and_or(x, 0x000F000Fu, 0x64006400u)), less));
+  y[1] = as_u32(__hfma2(as_half2(and_or(x, 0x00F000F0u, 0x64006400u)), part, off));
+  y[2] = as_u32(__hadd2(as_half2(and_or(z, 0x000F000Fu, 0x64006400u)), less));
+  y[3] = as_u32(__hfma2(as_half2(and_or(z, 0x00F000F0u, 0x64006400u)), part, off));
+}
+// 2^-e for the exponent e of x > 0 (clamped to what both it and its inverse can be)
+__device__ __forceinline__ float inverse_power(float x) {
+  const int e = min(max((int)(__float_as_uint(x) >> 23) - 127, -126), 126);
+  return __uint_as_float((uint32_t)(127 - e) << 23);
 }
 
 template <int D, int GROUP>
 struct MmaBody {
   using Type = __nv_bfloat16;
-  static constexpr int kDim = D, COLS = 8, kBlocks = 3, kQueryFloats = 0;
   static constexpr int G = D / GROUP, U = GROUP / 32, X = D / 32;
+  static constexpr int kDim = D, COLS = 8, kBlocks = G == 4 ? 3 : 4, kQueryFloats = 0;
+  static constexpr int kTileBytes = kPageTile * (D + 8 * G), kStages = 2;
   static constexpr float kLazy = 8.f;            // the maximum is raised once a score is 2^8 above it
   uint32_t qf[X][4];
-  float qsum[G][2], o[X][2][4], zacc[G][2], m[2], l[2], raise[2];
+  float qsum[G][2], o[X][2][4], zacc[G][2], norm[G], m[2], l[2], raise[2], sc2[2];
   int limit[2], limit_min;
 
-  __device__ __forceinline__ void begin(const PagesAttnArgs& a, const Cursor& c, int cols_total, float*, int lane) {
+  __device__ __forceinline__ void begin(const PagesAttnArgs& a, const Place& c, int cols_total, float*, int lane) {
     const int i = lane >> 2, j = lane & 3, col0 = c.cg * COLS;
-    const int col = col0 + i, tok = col / a.rep, head = c.h * a.rep + col % a.rep;
-    const uint16_t* q = static_cast<const uint16_t*>(a.q) + (int64_t)c.entry * a.qsb + (int64_t)tok * a.qst + (int64_t)head * a.qsh;
+    {
+      const int col = col0 + i, tok = col / a.rep, head = c.h * a.rep + col % a.rep;
+      const uint16_t* q = static_cast<const uint16_t*>(a.q) + (int64_t)c.entry * a.qsb + (int64_t)tok * a.qst + (int64_t)head * a.qsh;
+      float f[X][8], big = 0.f;
 #pragma unroll
-    for (int w = 0; w < X; ++w) {
-      uint4 r = make_uint4(0, 0, 0, 0);
-      if (col < cols_total) r = *reinterpret_cast<const uint4*>(q + 8 * k_slot_word(D, GROUP, j * X + w));
-      qf[w][0] = __byte_perm(r.x, r.z, 0x5410); qf[w][1] = __byte_perm(r.x, r.z, 0x7632);
-      qf[w][2] = __byte_perm(r.y, r.w, 0x5410); qf[w][3] = __byte_perm(r.y, r.w, 0x7632);
+      for (int w = 0; w < X; ++w) {
+        uint4 r = make_uint4(0, 0, 0, 0);
+        if (col < cols_total) r = *reinterpret_cast<const uint4*>(q + 8 * k_slot_word(D, GROUP, j * X + w));
+        const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          f[w][2 * k] = __uint_as_float(u[k] << 16);
+          f[w][2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
+          big = fmaxf(big, fmaxf(fabsf(f[w][2 * k]), fabsf(f[w][2 * k + 1])));
+        }
+      }
+      big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+      big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+      const float down = big > 0.f ? inverse_power(big) : 1.f;
+#pragma unroll
+      for (int w = 0; w < X; ++w)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) qf[w][k] = pack_f16(f[w][k] * down, f[w][k + 4] * down);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) sc2[x] = a.scale * kLog2e / __shfl_sync(0xffffffffu, down, (2 * j + x) * 4);
     }
     // sums of the queries over each group, by the instruction itself: every row of a matrix of ones
-    const uint32_t ones[4] = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+    const uint32_t ones[4] = {0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       float s[4] = {0.f, 0.f, 0.f, 0.f};
@@ -350,6 +410,7 @@ struct MmaBody {
       }
       qsum[g][0] = s[0]; qsum[g][1] = s[1];
       zacc[g][0] = zacc[g][1] = 0.f;
+      norm[g] = 0.f;
     }
 #pragma unroll
     for (int x = 0; x < X; ++x)
@@ -363,10 +424,35 @@ struct MmaBody {
     limit_min = c.len - (a.T - 1 - col0 / a.rep);
   }
 
+  // Brings the group's factor to the largest scale of the tile (the lanes hold two rows each): o goes with it.
+  __device__ __forceinline__ void renorm(int g, float big) {
+    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 4));
+    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 8));
+    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 16));
+    if (!(big > 0.f)) return;                    // only zeros (or NaN): any factor will do
+    const float to = inverse_power(big), by = norm[g] == 0.f ? 1.f : to / norm[g];
+    if (by > 1.f) {                              // what has been summed is beyond such small scales if it does not stay finite
+      float most = 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) most = fmaxf(most, fabsf(o[g * U + u][y][k]));
+      if (__any_sync(0xffffffffu, most > 0.f && most * by > 1e30f)) return;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[g * U + u][y][k] *= by;
+    norm[g] = to;
+  }
+
   __device__ __forceinline__ void tile(const PagesAttnArgs& a, const uint8_t* tp, int row0, int rows, const float*, int lane) {
     const int i = lane >> 2, j = lane & 3;
     const int ri = i ^ ((i >> 1) & 1);           // tile rows of matrix rows i and i + 8
-    const float sc2 = a.scale * kLog2e;
     const bool edge = rows < kPageTile || row0 + kPageTile > limit_min;
 
     // S^T = K Q^T, one accumulator per group, then scale and zero
@@ -400,30 +486,65 @@ struct MmaBody {
         const uint32_t w = *reinterpret_cast<const uint32_t*>(tp + tile_k_word(D, G, ri + 8 * r, g));
         const float scale = __uint_as_float(w << 16), zero = fmaf(8.f, scale, __uint_as_float(w & 0xffff0000u));
 #pragma unroll
-        for (int x = 0; x < 2; ++x) s[2 * r + x] += fmaf(scale, c[2 * r + x], zero * qsum[g][x]);
+        for (int x = 0; x < 2; ++x) s[2 * r + x] = fmaf(scale, c[2 * r + x], fmaf(zero, qsum[g][x], s[2 * r + x]));
       }
     }
-    bool seen[4] = {true, true, true, true};
-    if (edge) {                                  // rows behind the end hold anything: replaced, not multiplied away
+    float vs[G][2], vz[G][2];                    // V's scales and zeros (moved to the centred codes) of rows i, i + 8
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
+    for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          seen[2 * r + x] = ri + 8 * r < rows && row0 + ri + 8 * r < limit[x];
-          if (!seen[2 * r + x]) s[2 * r + x] = -INFINITY;
+      for (int r = 0; r < 2; ++r) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(tp + tile_v_word(D, G, ri + 8 * r, g));
+        vs[g][r] = __uint_as_float(w << 16);
+        vz[g][r] = fmaf(8.f, vs[g][r], __uint_as_float(w & 0xffff0000u));
+      }
+    if (edge) {
+      // Rows behind the end hold anything, rows that a token does not see may hold NaN: replaced, not multiplied away.
+      // (A NaN scale that some columns see goes into their zero sums by hand.)
+      asm volatile("");                          // a branch: as selects this would cost every tile
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int row = ri + 8 * r;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (row >= rows || row0 + row >= limit[x]) s[2 * r + x] = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          if (row < rows && vs[g][r] != vs[g][r])
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              if (row0 + row < limit[x]) zacc[g][x] = vs[g][r];
+          if (row >= rows || vs[g][r] != vs[g][r]) vs[g][r] = vz[g][r] = 0.f;
         }
+      }
     }
-    if (__any_sync(0xffffffffu, fmaxf(s[0], s[2]) > raise[0] || fmaxf(s[1], s[3]) > raise[1])) {
+    // Rare work, found by one vote: a score far above the maximum, a scale that P's f16 range no longer covers (P <= 2^8,
+    // its scaled value <= 2^15), or one so far below that P would lose bits.
+    float top = 0.f, low = INFINITY;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const float x = fmaxf(vs[g][0], vs[g][1]) * norm[g];
+      top = fmaxf(top, x);
+      low = fminf(low, x);
+    }
+    if (__any_sync(0xffffffffu, fmaxf(s[0], s[2]) > raise[0] || fmaxf(s[1], s[3]) > raise[1] || top > 64.f) ||
+        __all_sync(0xffffffffu, low < 0.015625f)) {
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const float big = fmaxf(vs[g][0], vs[g][1]);
+        const float x = big * norm[g];
+        if (__any_sync(0xffffffffu, x > 64.f) || __all_sync(0xffffffffu, !(x >= 0.015625f))) renorm(g, big);
+      }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         float mx = fmaxf(s[x], s[2 + x]);
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-        const float m_new = fmaxf(m[x], mx * sc2);
+        const float m_new = fmaxf(m[x], mx * sc2[x]);
         const float corr = m_new == -INFINITY ? 1.f : ex2(m[x] - m_new);
         m[x] = m_new;
-        raise[x] = (m_new + kLazy) / sc2;
+        raise[x] = m_new == -INFINITY ? -INFINITY : (m_new + kLazy) / sc2[x];
         l[x] *= corr;
 #pragma unroll
         for (int g = 0; g < G; ++g) zacc[g][x] *= corr;
@@ -438,13 +559,12 @@ struct MmaBody {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const float ref = m[x] == -INFINITY ? 0.f : m[x];
-      p[x] = ex2(fmaf(s[x], sc2, -ref));
-      p[2 + x] = ex2(fmaf(s[2 + x], sc2, -ref));
+      p[x] = ex2(fmaf(s[x], sc2[x], -ref));
+      p[2 + x] = ex2(fmaf(s[2 + x], sc2[x], -ref));
       l[x] += p[x] + p[2 + x];
     }
 
-    // O^T += V^T P^T, the group's scale multiplied into P. P is given as the sum of two bf16 numbers: rounded to one, it
-    // would be as far off as the output's own rounding.
+    // O^T += V^T P^T, the group's scale multiplied into P
     uint32_t vc[4][X / 2];                       // rows of matrix rows 2 j, 2 j + 1, 2 j + 8, 2 j + 9
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -459,20 +579,13 @@ struct MmaBody {
     }
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      uint32_t hi[2], lo[2];
+      uint32_t pb[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(tp + tile_v_word(D, G, ri + 8 * r, g));
-        const float scale = __uint_as_float(w << 16), zero = fmaf(8.f, scale, __uint_as_float(w & 0xffff0000u));
-        float ps[2];
+        const float f = vs[g][r] * norm[g];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          ps[x] = seen[2 * r + x] ? p[2 * r + x] * scale : 0.f;
-          if (seen[2 * r + x]) zacc[g][x] = fmaf(p[2 * r + x], zero, zacc[g][x]);
-        }
-        const uint32_t h = pack_bf16(ps[0], ps[1]);
-        hi[r] = transpose8x8(h);
-        lo[r] = transpose8x8(pack_bf16(ps[0] - __uint_as_float(h << 16), ps[1] - __uint_as_float(h & 0xffff0000u)));
+        for (int x = 0; x < 2; ++x) zacc[g][x] = fmaf(p[2 * r + x], vz[g][r], zacc[g][x]);
+        pb[r] = transpose8x8(pack_f16(p[2 * r] * f, p[2 * r + 1] * f));
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -484,15 +597,14 @@ struct MmaBody {
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           const uint32_t av[4] = {v0[2 * y], v0[2 * y + 1], v1[2 * y], v1[2 * y + 1]};
-          mma_full(o[x][y], av, hi[0], hi[1]);
-          mma_full(o[x][y], av, lo[0], lo[1]);
+          mma_full(o[x][y], av, pb[0], pb[1]);
         }
       }
     }
   }
 
-  __device__ __forceinline__ void end(float* state, int lane) {
-    const int i = lane >> 2, j = lane & 3;
+  // sums over the lanes that share a column; o without its factor, with its zeros
+  __device__ __forceinline__ void end() {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
 #pragma unroll
@@ -501,39 +613,80 @@ struct MmaBody {
 #pragma unroll
         for (int g = 0; g < G; ++g) zacc[g][x] += __shfl_xor_sync(0xffffffffu, zacc[g][x], b);
       }
+#pragma unroll
+      for (int y = 0; y < X; ++y) {
+        const float up = norm[y / U] == 0.f ? 0.f : 1.f / norm[y / U];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          o[y][k][x] = fmaf(o[y][k][x], up, zacc[y / U][x]);
+          o[y][k][2 + x] = fmaf(o[y][k][2 + x], up, zacc[y / U][x]);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void keep(float* state, int lane) const {
+    const int i = lane >> 2, j = lane & 3;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
       float* st = state + (2 * j + x) * (D + 2);
 #pragma unroll
       for (int y = 0; y < X; ++y) {
         const int d = 4 * v_slot_half(D, GROUP, i * X + y);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) st[d + k] = o[y][k >> 1][2 * (k & 1) + x] + zacc[y / U][x];
+        for (int k = 0; k < 4; ++k) st[d + k] = o[y][k >> 1][2 * (k & 1) + x];
       }
       if (i == 0) { st[D] = m[x]; st[D + 1] = l[x]; }
     }
-    __syncwarp();
+  }
+  __device__ __forceinline__ void write(const PagesAttnArgs& a, const Place& c, int cols_total, int lane) const {
+    const int i = lane >> 2, j = lane & 3;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int col = c.cg * COLS + 2 * j + x;
+      if (col >= cols_total) break;
+      const OutPlace at(a, c.entry, c.h, col);
+      const float inv = l[x] == 0.f ? 0.f : 1.f / l[x];
+#pragma unroll
+      for (int y = 0; y < X; ++y)
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + at.out + 4 * v_slot_half(D, GROUP, i * X + y)) =
+            make_uint2(pack_bf16(o[y][0][x] * inv, o[y][0][2 + x] * inv), pack_bf16(o[y][1][x] * inv, o[y][1][2 + x] * inv));
+      if (i == 0 && a.lse) a.lse[at.lse] = lse_of(m[x], l[x]);
+    }
   }
 };
+
+__device__ __forceinline__ bool try_wait_once(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n\t.reg .pred P;\n\tmbarrier.try_wait.parity.shared::cta.b64 P, [%1], %2;\n\tselp.b32 %0, 1, 0, P;\n\t}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
+}
+// one copy global -> shared that completes the phase of `bar`
+__device__ __forceinline__ void tile_load(uint32_t dst, const uint8_t* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar) : "memory");
+}
 
 template <class Body>
 __global__ void __launch_bounds__(kThreads, Body::kBlocks) attn_kernel(PagesAttnArgs a, int cgs) {
   using T = typename Body::Type;
   using L = Layout<Body>;
-  constexpr int D = Body::kDim, COLS = Body::COLS;
-  extern __shared__ uint8_t smem_raw[];
+  constexpr int D = Body::kDim, COLS = Body::COLS, S = Body::kStages, TB = Body::kTileBytes;
+  extern __shared__ __align__(128) uint8_t base[];       // (never cast through an integer: loads from it must stay shared loads)
   __shared__ Sched sh;
-  __shared__ uint64_t full[kWarps][kStages];
-  __shared__ int absent[kWarps][kStages];       // the stage's tile lies in no valid page
+  __shared__ uint64_t full[kWarps][S];
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  const int tile_bytes = a.p.tile_bytes;
-  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~uintptr_t(127));
-  uint8_t* ring = base + warp * kStages * tile_bytes;
-  float* floats = reinterpret_cast<float*>(base + L::ring_bytes(tile_bytes));
-  float* qs = floats + warp * Body::kQueryFloats;
-  float* states = floats + kWarps * Body::kQueryFloats;    // [warp][2][COLS][D + 2]
+  uint8_t* ring = base + warp * L::warp_bytes;
+  // where a warp's states lie: place 0 behind the ring and the queries, place 1 in the ring
+  auto state_of = [&](int w, int place) {
+    return reinterpret_cast<float*>(base + w * L::warp_bytes + (place ? 0 : L::ring + Body::kQueryFloats * 4));
+  };
+  float* qs = reinterpret_cast<float*>(ring + L::ring);
   const int cols_total = a.T * a.rep;
 
   if (lane == 0) {
-    for (int s = 0; s < kStages; ++s) mbar_init(&full[warp][s], 1);
+    for (int s = 0; s < S; ++s) mbar_init(&full[warp][s], 1);
     sh.piece[warp][0].valid = sh.piece[warp][1].valid = 0;
   }
   if (t == 0) sh.abort_flag = 0;
@@ -568,133 +721,147 @@ __global__ void __launch_bounds__(kThreads, Body::kBlocks) attn_kernel(PagesAttn
   __syncthreads();
 
   const long long u_warp = cta_u + warp * q;
-  long long left = total - u_warp;               // units of this warp
-  if (left > q) left = q;
-  if (left < 0) left = 0;
-  bool ok = true;
+  const int mine = (int)max(0LL, min(q, total - u_warp));    // units of this warp
 
-  if (left > 0) {
-    Cursor ld, cu;
-    ld.start(a, cgs, sh.entry[warp], sh.first_unit[warp], u_warp);
-    cu = ld;
-    long long to_load = left;
-    int win_list = -1, win0 = 0, win = -1;       // 32 page ids of the loader's list, one per lane
-    long long issued = 0, used = 0;
+  if (mine > 0) {
+    // ---- the loader's position: a tile of a list's page, and the list's next 32 page ids, one per lane
+    Place ld;
+    int ld_list = ld.start(a, cgs, sh.entry[warp], u_warp - sh.first_unit[warp] + 0LL);
+    Place cu = ld;
+    int to_load = mine, win0 = -64, win = -1, in_page = 0, in_stage = 0;
+    uint32_t loaded = 0;                         // four bits a stage: its tiles, and 8 if they lie in no valid page
+    const uint8_t* src = nullptr;
+    const uint32_t bar0 = smem_u32(&full[warp][0]), ring0 = smem_u32(ring);
 
     auto issue = [&]() {
-      const int stage = (int)(issued % kStages);
-      int page = -1;
-      const int slot = ld.t / a.p.tiles_per_page;
-      if (ld.len > 0) {
-        if (win_list != ld.l || slot < win0 || slot >= win0 + 32) {
-          win_list = ld.l;
-          win0 = slot;
-          win = pages_page(a.p, ld.l, (int64_t)win0 + lane);
+      if (in_page == 0) {
+        const int slot = ld.t / a.p.tiles_per_page, skip = ld.t - slot * a.p.tiles_per_page;
+        int page = -1;
+        if (ld.len > 0) {
+          if (slot < win0 || slot >= win0 + 32) {
+            win0 = slot;
+            win = pages_page(a.p, ld_list, (int64_t)slot + lane);
+          }
+          page = __shfl_sync(0xffffffffu, win, slot - win0);
+          if (page < 0 && lane == 0) record(a.p.status, PYR_ERR_INVALID);
         }
-        page = __shfl_sync(0xffffffffu, win, slot - win0);
+        src = page < 0 ? nullptr : a.p.pool + pages_tile(a.p, page, ld.h, skip);
+        in_page = min(a.p.tiles_per_page - skip, ld.tiles - ld.t);
       }
+      const int n = min(min(in_page, to_load), kStageTiles);
+      loaded = (loaded & ~(15u << (4 * in_stage))) | (uint32_t)(src ? n : n | 8) << (4 * in_stage);
       if (lane == 0) {
-        absent[warp][stage] = page < 0;
-        if (page >= 0) {
-          mbar_expect_tx(&full[warp][stage], tile_bytes);
-          bulk_load(ring + stage * tile_bytes, a.p.pool + pages_tile(a.p, page, ld.h, ld.t % a.p.tiles_per_page), tile_bytes,
-                    &full[warp][stage]);
-        } else {
-          mbar_arrive(&full[warp][stage]);
-          if (ld.len > 0) record(a.p.status, PYR_ERR_INVALID);
-        }
+        if (src) tile_load(ring0 + in_stage * (kStageTiles * TB), src, n * TB, bar0 + 8 * in_stage);
+        else mbar_arrive(&full[warp][in_stage]);
       }
-      ++issued;
-      --to_load;
-      if (to_load > 0) ld.next_tile(a, cgs);
+      if (src) src += n * TB;
+      in_stage ^= 1;
+      in_page -= n;
+      ld.t += n;
+      to_load -= n;
+      if (ld.t == ld.tiles && to_load > 0) {
+        const int l = ld.next(a, cgs);
+        if (l >= 0) { ld_list = l; win0 = -64; }
+      }
     };
-    for (int s = 0; s < kStages && to_load > 0; ++s) issue();
+    issue();
+    if (to_load > 0) issue();
 
     Body body;
-    while (left > 0) {
+    bool ok = true;
+    int stage = 0, left = mine;
+    uint32_t parity = 0;
+    while (true) {
       // ---- a segment: the warp's tiles of one (entry, head, column group)
-      const int t0 = cu.t;
-      const int t1 = (int)min((long long)cu.tiles, t0 + left);
+      const int t0 = cu.t, t1 = min(cu.tiles, t0 + left);
       body.begin(a, cu, cols_total, qs, lane);
-      for (int tt = t0; tt < t1; ++tt) {
-        const int stage = (int)(used % kStages);
-        if (ok) {
-          ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][stage], (uint32_t)(used / kStages) & 1, &sh.abort_flag, a.p.status, PYR_ERR_TIMEOUT));
-          if (!ok) {
-            // a wait ran out: no more copies, and those in flight must land before the shared memory is given back
-            volatile int none = 0;
-            for (long long c = used; c < issued; ++c)
-              mbar_wait_limit(&full[warp][c % kStages], (uint32_t)(c / kStages) & 1, kSpinLimit, &none, nullptr, 0);
-          }
-        }
-        if (ok) {
-          const int rows = absent[warp][stage] ? 0 : min(kPageTile, cu.len - tt * kPageTile);
-          if (rows > 0) body.tile(a, ring + stage * tile_bytes, tt * kPageTile, rows, qs, lane);
-          __syncwarp();
-          ++used;
-          if (to_load > 0) issue();
-        }
+      int tt = t0;
+#pragma unroll 1
+      while (tt < t1) {
+        if (!__all_sync(0xffffffffu, ok && try_wait_once(bar0 + 8 * stage, parity)) && ok)
+          ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][stage], parity, &sh.abort_flag, a.p.status, PYR_ERR_TIMEOUT));
+        if (!ok) break;
+        const uint32_t mine_here = loaded >> (4 * stage);
+        const int n = (int)(mine_here & 7u);
+        const uint8_t* tp = ring + stage * (kStageTiles * TB);
+        if (!(mine_here & 8u))
+#pragma unroll 1
+          for (int x = 0; x < n; ++x)
+            body.tile(a, tp + x * TB, (tt + x) * kPageTile, min(cu.len - (tt + x) * kPageTile, kPageTile), qs, lane);
+        __syncwarp();
+        tt += n;
+        if (stage) parity ^= 1;
+        stage ^= 1;
+        if (to_load > 0) issue();
+      }
+      if (!ok && to_load >= 0) {
+        // A wait ran out: the remaining work is only walked through, so that no other CTA waits for this one's share. Copies
+        // in flight must land before the shared memory is used otherwise or given back.
+        volatile int none = 0;
+        do {
+          mbar_wait_limit(&full[warp][stage], parity, kSpinLimit, &none, nullptr, 0);
+          if (stage) parity ^= 1;
+          stage ^= 1;
+        } while (stage != in_stage);
+        to_load = -1;
       }
       const bool begins = t0 == 0, ends = t1 == cu.tiles;
-      // a state that began before this warp's range waits in place 0, one that goes on behind it in place 1
-      float* state = states + (warp * 2 + (begins ? 1 : 0)) * L::state;
-      body.end(state, lane);
-      const int ncols = min(COLS, cols_total - cu.cg * COLS);
-      if (begins && ends) {
-        for (int x = 0; x < ncols; ++x) {
-          const float den = state[x * (D + 2) + D + 1], m = state[x * (D + 2) + D];
-          const float inv = den == 0.f ? 0.f : 1.f / den;
-          for (int d = lane; d < D; d += 32) write_out<T, D>(a, cu.entry, cu.h, cu.cg * COLS + x, d, state[x * (D + 2) + d] * inv);
-          if (lane == 0) write_lse(a, cu.entry, cu.h, cu.cg * COLS + x, m, den);
-        }
-        __syncwarp();
-      } else if (lane == 0) {
-        Piece& pc = sh.piece[warp][begins ? 1 : 0];
-        pc.u0 = cu.u_entry + ((long long)cu.h * cgs + cu.cg) * cu.tiles;
-        pc.u1 = pc.u0 + cu.tiles;
-        pc.entry = cu.entry; pc.h = cu.h; pc.cg = cu.cg;
-        pc.begins = begins; pc.ends = ends; pc.valid = 1;
-      }
       left -= t1 - t0;
-      cu.t = t1 - 1;
-      if (left > 0) cu.next_tile(a, cgs);
+      body.end();
+      if (begins && ends) {
+        body.write(a, cu, cols_total, lane);
+      } else {
+        // a state that began before this warp's range waits in place 0, one that goes on behind it (the last) in place 1
+        const int place = begins ? 1 : 0;
+        body.keep(state_of(warp, place), lane);
+        if (lane == 0) {
+          Piece& pc = sh.piece[warp][place];
+          pc.u0 = u_warp + (mine - left - (t1 - t0)) - t0;
+          pc.u1 = pc.u0 + cu.tiles;
+          pc.entry = cu.entry; pc.h = cu.h; pc.cg = cu.cg;
+          pc.begins = begins; pc.ends = ends; pc.valid = 1;
+        }
+      }
+      if (left == 0) break;
+      cu.next(a, cgs);
     }
   }
 
   // ---- merge the CTA's partial states: runs of consecutive ones of the same (entry, head, column group)
   __syncthreads();
   int slot_c1[2] = {-1, -1}, slot_count[2] = {0, 0};      // what the CTA leaves for others: place 0 / place 1
-  Piece left_piece[2];
+  int left_at[2] = {0, 0};                                // a piece of it
   for (int f = 0; f < kWarps * 2;) {
     if (!sh.piece[f >> 1][f & 1].valid) { ++f; continue; }
-    const Piece pc = sh.piece[f >> 1][f & 1];
-    int g = f, n = 0, members[kWarps * 2];
-    bool ends = false;
+    const Piece& pc = sh.piece[f >> 1][f & 1];
+    int g = f + 1, last = f;
     for (; g < kWarps * 2; ++g) {
       const Piece& o = sh.piece[g >> 1][g & 1];
       if (!o.valid) continue;
       if (o.u0 != pc.u0) break;
-      members[n++] = g;
-      ends = o.ends;
+      last = g;
     }
-    const bool whole = pc.begins && ends;
+    const bool whole = pc.begins && sh.piece[last >> 1][last & 1].ends;
     const int place = pc.begins ? 1 : 0;
     const int ncols = min(COLS, cols_total - pc.cg * COLS);
     for (int o = t; o < ncols * D; o += kThreads) {
       const int x = o / D, d = o % D;
       float M = -INFINITY;
-      for (int k = 0; k < n; ++k) M = fmaxf(M, states[members[k] * L::state + x * (D + 2) + D]);
+      for (int k = f; k <= last; ++k)
+        if (sh.piece[k >> 1][k & 1].valid) M = fmaxf(M, state_of(k >> 1, k & 1)[x * (D + 2) + D]);
       const float ref = M == -INFINITY ? 0.f : M;
       float num = 0.f, den = 0.f;
-      for (int k = 0; k < n; ++k) {
-        const float* st = states + members[k] * L::state + x * (D + 2);
-        const float w = exp2f(st[D] - ref);
-        num = fmaf(w, st[d], num);
-        den = fmaf(w, st[D + 1], den);
-      }
+      for (int k = f; k <= last; ++k)
+        if (sh.piece[k >> 1][k & 1].valid) {
+          const float* st = state_of(k >> 1, k & 1) + x * (D + 2);
+          const float w = ex2(st[D] - ref);
+          num = fmaf(w, st[d], num);
+          den = fmaf(w, st[D + 1], den);
+        }
       if (whole) {
-        write_out<T, D>(a, pc.entry, pc.h, pc.cg * COLS + x, d, den == 0.f ? 0.f : num / den);
-        if (d == 0) write_lse(a, pc.entry, pc.h, pc.cg * COLS + x, M, den);
+        const OutPlace at(a, pc.entry, pc.h, pc.cg * COLS + x);
+        static_cast<T*>(a.out)[at.out + d] = from_f<T>(den == 0.f ? 0.f : num / den);
+        if (d == 0 && a.lse) a.lse[at.lse] = lse_of(M, den);
       } else {
         float* dst = a.partial + ((size_t)blockIdx.x * 2 + place) * (kAttnCols * (D + 2)) + x * (D + 2);
         __stcg(dst + d, num);
@@ -702,7 +869,7 @@ __global__ void __launch_bounds__(kThreads, Body::kBlocks) attn_kernel(PagesAttn
       }
     }
     if (!whole) {
-      left_piece[place] = pc;
+      left_at[place] = f;
       slot_c1[place] = (int)(pc.u0 / cta_units);
       slot_count[place] = (int)((pc.u1 - 1) / cta_units) - slot_c1[place] + 1;
     }
@@ -719,26 +886,52 @@ __global__ void __launch_bounds__(kThreads, Body::kBlocks) attn_kernel(PagesAttn
   __threadfence();
   for (int place = 0; place < 2; ++place) {
     if (slot_c1[place] < 0 || !sh.last[place]) continue;
-    const Piece pc = left_piece[place];
+    const Piece& pc = sh.piece[left_at[place] >> 1][left_at[place] & 1];
     const int c1 = slot_c1[place], cn = slot_count[place];
     const int ncols = min(COLS, cols_total - pc.cg * COLS);
-    for (int o = t; o < ncols * D; o += kThreads) {
-      const int x = o / D, d = o % D;
-      // the first CTA holds the beginning (place 1), the others go on with it (place 0)
-      const float* src = a.partial + (size_t)c1 * 2 * (kAttnCols * (D + 2)) + x * (D + 2);
-      const size_t step = 2 * (size_t)(kAttnCols * (D + 2)), second = kAttnCols * (D + 2);
+    // the first CTA holds the beginning (place 1), the others go on with it (place 0)
+    const float* src = a.partial + (size_t)c1 * 2 * (kAttnCols * (D + 2));
+    const size_t step = 2 * (size_t)(kAttnCols * (D + 2)), second = kAttnCols * (D + 2);
+    // a column's maxima and sums are 2 cn numbers far apart: a warp a column, so that they are fetched together
+    float* weight = reinterpret_cast<float*>(base);           // [cn][COLS], where the rings were
+    __syncthreads();
+    for (int x = warp; x < ncols; x += kWarps) {
       float M = -INFINITY;
-      for (int k = 0; k < cn; ++k) M = fmaxf(M, __ldcg(src + k * step + (k == 0 ? second : 0) + D));
+      for (int k = lane; k < cn; k += 32) M = fmaxf(M, __ldcg(src + k * step + (k == 0 ? second : 0) + x * (D + 2) + D));
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
       const float ref = M == -INFINITY ? 0.f : M;
-      float num = 0.f, den = 0.f;
-      for (int k = 0; k < cn; ++k) {
-        const float* st = src + k * step + (k == 0 ? second : 0);
-        const float w = exp2f(__ldcg(st + D) - ref);
-        num = fmaf(w, __ldcg(st + d), num);
-        den = fmaf(w, __ldcg(st + D + 1), den);
+      float den = 0.f;
+      for (int k = lane; k < cn; k += 32) {
+        const float* st = src + k * step + (k == 0 ? second : 0) + x * (D + 2) + D;
+        const float w = ex2(__ldcg(st) - ref);
+        weight[k * COLS + x] = w;
+        den = fmaf(w, __ldcg(st + 1), den);
       }
-      write_out<T, D>(a, pc.entry, pc.h, pc.cg * COLS + x, d, den == 0.f ? 0.f : num / den);
-      if (d == 0) write_lse(a, pc.entry, pc.h, pc.cg * COLS + x, M, den);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+      if (lane == 0) {
+        sh.den[x] = den;
+        if (a.lse) a.lse[OutPlace(a, pc.entry, pc.h, pc.cg * COLS + x).lse] = lse_of(M, den);
+      }
+    }
+    __syncthreads();
+    static_assert(D % 4 == 0, "four dimensions a thread");
+    for (int o = t; o < ncols * (D / 4); o += kThreads) {
+      const int x = o / (D / 4), d = o % (D / 4) * 4;
+      float num[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+      for (int k = 0; k < cn; ++k) {
+        const float w = weight[k * COLS + x];
+        const float2* st = reinterpret_cast<const float2*>(src + k * step + (k == 0 ? second : 0) + x * (D + 2) + d);
+        const float2 u = __ldcg(st), v = __ldcg(st + 1);
+        num[0] = fmaf(w, u.x, num[0]); num[1] = fmaf(w, u.y, num[1]);
+        num[2] = fmaf(w, v.x, num[2]); num[3] = fmaf(w, v.y, num[3]);
+      }
+      const float den = sh.den[x], inv = den == 0.f ? 0.f : 1.f / den;
+      T* dst = static_cast<T*>(a.out) + OutPlace(a, pc.entry, pc.h, pc.cg * COLS + x).out + d;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) dst[k] = from_f<T>(num[k] * inv);
     }
     if (t == 0) a.arrived[c1] = 0;                         // as the next call expects it
   }
@@ -747,7 +940,7 @@ __global__ void __launch_bounds__(kThreads, Body::kBlocks) attn_kernel(PagesAttn
 template <class Body>
 cudaError_t run_attn(const PagesAttnArgs& a, cudaStream_t s) {
   const int cgs = (a.T * a.rep + Body::COLS - 1) / Body::COLS;
-  const int smem = Layout<Body>::total(a.p.tile_bytes);
+  constexpr int smem = Layout<Body>::total;
   cudaError_t e = cudaFuncSetAttribute(attn_kernel<Body>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const int sms = device_sm_count();

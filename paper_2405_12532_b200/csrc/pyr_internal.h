@@ -194,7 +194,7 @@ struct PagesAttnArgs {
   int32_t* arrived;                // [kAttnMaxCtas], zero between calls
 };
 constexpr int kReserveSlice = 4096;
-constexpr int kAttnMaxCtas = 1024;
+constexpr int kAttnMaxCtas = 640;
 constexpr int kAttnCols = 8;
 cudaError_t launch_pages_write(const PagesWriteArgs& a, int* launches, cudaStream_t s);
 cudaError_t launch_pages_read(const PagesWriteArgs& a, int* launches, cudaStream_t s);

@@ -331,6 +331,32 @@ def test_attention_keeps_nan_values_from_tokens_that_do_not_see_them(dtype):
     assert torch.equal(ref[0, :2], out[0, :2]) and torch.equal(ref[1], out[1]) and p.status() == 0
 
 
+@pytest.mark.parametrize("order", [1, -1])
+@pytest.mark.parametrize("D,group", FORMATS)
+def test_attention_over_scales_of_many_magnitudes(D, group, order):
+    """bf16: values whose scales run from 2^-90 to 2^90 down or up the list, group by group in other steps, and queries from
+    2^-60 to 2^60 against keys that make up for it: every dimension is held to the largest value that its group has."""
+    n, T = 96, 2
+    p = _pages(1, D, group, 32, 4, 1, 3)
+    k, v = _rand(1, n, 1, D, seed=36), _rand(1, n, 1, D, seed=37)
+    row = torch.arange(n, device=DEV).view(1, n, 1, 1) if order > 0 else torch.arange(n - 1, -1, -1, device=DEV).view(1, n, 1, 1)
+    step = torch.arange(D // group, device=DEV).repeat_interleave(group).view(1, 1, 1, D) + 1
+    v = (v * torch.exp2(((row // 16) * 12 - 36) * step.float() * (2.5 / (D // group)))).to(BF)
+    k = (k * 2.0 ** -20).to(BF)
+    p.reserve(_ids(0), n)
+    p.write(k, v)
+    q = (_rand(1, T, 8, D, seed=38) * 2.0 ** 20).to(BF)
+    out, lse = p.attn(q, lse=True)
+    assert p.status() == 0
+    K, V = _list_values(p, 0)
+    want, wl = op.attention(_wide(q[0]), K, V, D ** -0.5)
+    # P in f16 relative to the group's largest scale met: 2^-11 of a term, or 2^-25 of the largest; output 2^-9
+    big = np.abs(V).reshape(n, 1, D // group, group).max((0, 1, 3)).repeat(group)
+    err = np.abs(_wide(out[0]) - want)
+    assert (err <= (2.0 ** -9 + 1e-4) * np.abs(want) + 2.0 ** -10 * big).all()
+    assert np.abs(lse[0].cpu().double().numpy() - wl).max() <= 2e-4
+
+
 def test_attention_far_into_a_pool_beyond_four_gigabytes():
     """Pages whose byte offsets pass 2^32, written, attended, moved and read back."""
     hkv, D, pr = 32, 128, 64
