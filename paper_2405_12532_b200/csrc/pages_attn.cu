@@ -10,7 +10,9 @@
 // group) leaves a partial state; the CTA merges its warps' states in order, and what crosses CTAs goes to a workspace where
 // the CTA that finishes last merges it, again in order: results do not depend on which CTA that is.
 //
-// A warp loads its tiles itself: lane 0 keeps a ring of bulk copies (a tile is one contiguous copy) in flight.
+// One more warp loads for all of them: its lane w keeps the ring of warp w filled, a stage of which is one bulk copy of up to two
+// tiles (a head's tiles of a page are contiguous). As lanes of one warp the loaders cost an instruction each step instead of
+// one for every warp that consumes.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -24,10 +26,10 @@ using namespace tc;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
 constexpr int kStageTiles = 2;           // a stage of a warp's ring: one copy of up to two tiles
+constexpr int kStageRows = kStageTiles * kPageTile;
 constexpr int kMinUnits = 4;             // a warp's share is at least this many tiles: merging costs more than they do
+constexpr int kMaxWarps = 12;
 
 __device__ __forceinline__ void record(int* status, int code) { atomicCAS(status, 0, code); }
 
@@ -47,15 +49,16 @@ struct Piece {
 };
 
 struct Sched {
-  long long sums[kWarps + 1];
-  long long first_unit[kWarps];   // of the entry in which a warp's range starts
-  int entry[kWarps];
+  long long sums[kMaxWarps + 1];
+  long long first_unit[kMaxWarps];   // of the entry in which a warp's range starts
+  int entry[kMaxWarps];
   int abort_flag;
-  int last[2];
+  int last[2], open_c1[2], open_count[2], open_piece[2];   // what the CTA leaves for others
   float den[kAttnCols];
-  Piece piece[kWarps][2];
+  Piece piece[kMaxWarps][2];
 };
 
+template <int kWarpsAll>
 __device__ __forceinline__ long long block_scan(long long x, long long* warp_sums, long long* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   long long incl = x;
@@ -69,7 +72,7 @@ __device__ __forceinline__ long long block_scan(long long x, long long* warp_sum
   __syncthreads();
   long long before = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
+  for (int w = 0; w < kWarpsAll; ++w) {
     if (w < warp) before += warp_sums[w];
     all += warp_sums[w];
   }
@@ -96,10 +99,17 @@ struct Place {
   __device__ __forceinline__ int start(const PagesAttnArgs& a, int cgs, int e, long long o) {   // unit o of entry e
     entry = e;
     const int l = open(a);
-    t = (int)(o % tiles);
-    const long long hc = o / tiles;
-    cg = (int)(hc % cgs);
-    h = (int)(hc / cgs);
+    if (o >> 31 == 0) {                          // (64-bit divisions take a microsecond's tenth each)
+      const uint32_t hc = (uint32_t)o / (uint32_t)tiles;
+      t = (int)((uint32_t)o - hc * tiles);
+      h = (int)(hc / (uint32_t)cgs);
+      cg = (int)(hc - (uint32_t)h * cgs);
+    } else {
+      t = (int)(o % tiles);
+      const long long hc = o / tiles;
+      cg = (int)(hc % cgs);
+      h = (int)(hc / cgs);
+    }
     return l;
   }
   // the next one; returns its list, or -1 if the list is the same
@@ -136,8 +146,8 @@ struct Layout {
   static constexpr int ring = Body::kStages * kStageTiles * Body::kTileBytes;
   static constexpr int warp_bytes = (ring + (Body::kQueryFloats + state) * 4 + 127) / 128 * 128;
   static_assert(state * 4 <= ring, "the last state fits the ring");
-  static_assert(kAttnMaxCtas * Body::COLS * 4 <= kWarps * warp_bytes, "a weight per CTA and column fits where the rings were");
-  static constexpr int total = kWarps * warp_bytes;
+  static_assert(kAttnMaxCtas * Body::COLS * 4 <= Body::kWarps * warp_bytes, "a weight per CTA and column fits where the rings were");
+  static constexpr int total = Body::kWarps * warp_bytes;
 };
 
 // ------------------------------------------------------------------ one warp's tiles, on CUDA cores
@@ -146,8 +156,8 @@ struct Layout {
 template <class T, int D, int GROUP>
 struct CoreBody {
   using Type = T;
-  static constexpr int kDim = D, COLS = 4, kBlocks = 2, kQueryFloats = COLS * D;   // queries lie in shared memory
-  static constexpr int kStages = 2, kTileBytes = kPageTile * (D + 8 * (D / GROUP));
+  static constexpr int kDim = D, COLS = 4, kWarps = 7, kBlocks = 1, kQueryFloats = COLS * D;   // queries lie in shared memory
+  static constexpr int kStages = 3, kTileBytes = kPageTile * (D + 8 * (D / GROUP));
   static constexpr int G = D / GROUP, U = GROUP / 32, X = D / 32;   // X: words of K / halves of V in a lane's chunk
   float acc[COLS][4 * X];
   float m[COLS], l[COLS], qsum[COLS][G];
@@ -269,6 +279,12 @@ struct CoreBody {
     }
   }
 
+  __device__ __forceinline__ void stage(const PagesAttnArgs& a, const uint8_t* tp, int row0, int rows, const float* qs, int lane) {
+#pragma unroll 1
+    for (int x = 0; x < kStageTiles && rows > x * kPageTile; ++x)
+      tile(a, tp + x * kTileBytes, row0 + x * kPageTile, min(rows - x * kPageTile, kPageTile), qs, lane);
+  }
+
   // sums over the lanes that share a row or a dimension
   __device__ __forceinline__ void end() {
 #pragma unroll
@@ -353,6 +369,17 @@ __device__ __forceinline__ void centred4(uint32_t x, uint32_t* y) {
   y[2] = as_u32(__hadd2(as_half2(and_or(z, 0x000F000Fu, 0x64006400u)), less));
   y[3] = as_u32(__hfma2(as_half2(and_or(z, 0x00F000F0u, 0x64006400u)), part, off));
 }
+// The same for K, where the accumulator can start with what the codes have too much: nibbles 1 and 3 stay n + 64 (0x5400 | 16 n),
+// nibbles 0 and 2 become n - 8 (1024 + n would cost the accumulator bits).
+constexpr float kKeyOdd = 64.f, kKeyEven = -8.f;
+__device__ __forceinline__ void key4(uint32_t x, uint32_t* y) {
+  const __half2 less = as_half2(0xE408E408u);                // -1032
+  const uint32_t z = x >> 8;
+  y[0] = as_u32(__hadd2(as_half2(and_or(x, 0x000F000Fu, 0x64006400u)), less));
+  y[1] = and_or(x, 0x00F000F0u, 0x54005400u);
+  y[2] = as_u32(__hadd2(as_half2(and_or(z, 0x000F000Fu, 0x64006400u)), less));
+  y[3] = and_or(z, 0x00F000F0u, 0x54005400u);
+}
 // 2^-e for the exponent e of x > 0 (clamped to what both it and its inverse can be)
 __device__ __forceinline__ float inverse_power(float x) {
   const int e = min(max((int)(__float_as_uint(x) >> 23) - 127, -126), 126);
@@ -363,11 +390,12 @@ template <int D, int GROUP>
 struct MmaBody {
   using Type = __nv_bfloat16;
   static constexpr int G = D / GROUP, U = GROUP / 32, X = D / 32;
-  static constexpr int kDim = D, COLS = 8, kBlocks = G == 4 ? 3 : 4, kQueryFloats = 0;
-  static constexpr int kTileBytes = kPageTile * (D + 8 * G), kStages = 2;
+  static constexpr int kDim = D, COLS = 8, kWarps = 11, kBlocks = 1, kQueryFloats = 0;
+  static constexpr int kTileBytes = kPageTile * (D + 8 * G), kStages = kTileBytes > 2304 ? 2 : 3;
   static constexpr float kLazy = 8.f;            // the maximum is raised once a score is 2^8 above it
   uint32_t qf[X][4];
-  float qsum[G][2], o[X][2][4], zacc[G][2], norm[G], m[2], l[2], raise[2], sc2[2];
+  float qsum[G][2], bias[G][2];                  // sums of the queries over a group; what the codes' offsets would add to a score
+  float o[X][2][4], zacc[G][2], norm[G], m[2], ref[2], l[2], raise[2], sc2[2];
   int limit[2], limit_min;
 
   __device__ __forceinline__ void begin(const PagesAttnArgs& a, const Place& c, int cols_total, float*, int lane) {
@@ -398,17 +426,24 @@ struct MmaBody {
 #pragma unroll
       for (int x = 0; x < 2; ++x) sc2[x] = a.scale * kLog2e / __shfl_sync(0xffffffffu, down, (2 * j + x) * 4);
     }
-    // sums of the queries over each group, by the instruction itself: every row of a matrix of ones
-    const uint32_t ones[4] = {0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
+    // sums of the queries over each group, by the instruction itself: every row of a matrix of ones (zeros for one half of
+    // the dimensions at a time: operands 0, 1 go with nibbles 0 and 2 of a code word, operands 2, 3 with nibbles 1 and 3)
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
+      const uint32_t ones = 0x3C003C00u, even[4] = {ones, ones, 0, 0}, odd[4] = {0, 0, ones, ones};
+      float s[4] = {0.f, 0.f, 0.f, 0.f}, z[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        mma_full(s, ones, qf[g * U + u][0], qf[g * U + u][1]);
-        mma_full(s, ones, qf[g * U + u][2], qf[g * U + u][3]);
+        mma_full(s, even, qf[g * U + u][0], qf[g * U + u][1]);
+        mma_full(s, even, qf[g * U + u][2], qf[g * U + u][3]);
+        mma_full(z, odd, qf[g * U + u][0], qf[g * U + u][1]);
+        mma_full(z, odd, qf[g * U + u][2], qf[g * U + u][3]);
       }
-      qsum[g][0] = s[0]; qsum[g][1] = s[1];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        qsum[g][x] = s[x] + z[x];
+        bias[g][x] = -(kKeyEven * s[x] + kKeyOdd * z[x]);
+      }
       zacc[g][0] = zacc[g][1] = 0.f;
       norm[g] = 0.f;
     }
@@ -418,7 +453,7 @@ struct MmaBody {
       for (int y = 0; y < 2; ++y) o[x][y][0] = o[x][y][1] = o[x][y][2] = o[x][y][3] = 0.f;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      m[x] = -INFINITY; raise[x] = -INFINITY; l[x] = 0.f;
+      m[x] = -INFINITY; raise[x] = -INFINITY; ref[x] = 0.f; l[x] = 0.f;
       limit[x] = c.len - (a.T - 1 - (col0 + 2 * j + x) / a.rep);
     }
     limit_min = c.len - (a.T - 1 - col0 / a.rep);
@@ -450,100 +485,119 @@ struct MmaBody {
     norm[g] = to;
   }
 
-  __device__ __forceinline__ void tile(const PagesAttnArgs& a, const uint8_t* tp, int row0, int rows, const float*, int lane) {
+  // Up to two tiles (those of a stage): `rows` of their 32 rows belong to the list, the first of them is its row `row0`.
+  __device__ __forceinline__ void stage(const PagesAttnArgs& a, const uint8_t* tp, int row0, int rows, const float*, int lane) {
     const int i = lane >> 2, j = lane & 3;
     const int ri = i ^ ((i >> 1) & 1);           // tile rows of matrix rows i and i + 8
-    const bool edge = rows < kPageTile || row0 + kPageTile > limit_min;
+    const bool edge = rows < kStageRows || row0 + kStageRows > limit_min;
 
     // S^T = K Q^T, one accumulator per group, then scale and zero
-    uint32_t kc[2][X];
+    float s[kStageTiles][4];
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const uint32_t* src = reinterpret_cast<const uint32_t*>(tp + tile_k_row(D, ri + 8 * r)) + j * X;
-      if constexpr (X == 4) {
-        const uint4 v = *reinterpret_cast<const uint4*>(src);
-        kc[r][0] = v.x; kc[r][1] = v.y; kc[r][2] = v.z; kc[r][3] = v.w;
-      } else {
-        const uint2 v = *reinterpret_cast<const uint2*>(src);
-        kc[r][0] = v.x; kc[r][1] = v.y;
-      }
-    }
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      float c[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        uint32_t lo[4], hi[4];
-        centred4(kc[0][g * U + u], lo);
-        centred4(kc[1][g * U + u], hi);
-        const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
-        mma_full(c, a0, qf[g * U + u][0], qf[g * U + u][1]);
-        mma_full(c, a1, qf[g * U + u][2], qf[g * U + u][3]);
-      }
+    for (int b = 0; b < kStageTiles; ++b) {
+      const uint8_t* tile = tp + b * kTileBytes;
+      uint32_t kc[2][X];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(tp + tile_k_word(D, G, ri + 8 * r, g));
-        const float scale = __uint_as_float(w << 16), zero = fmaf(8.f, scale, __uint_as_float(w & 0xffff0000u));
-#pragma unroll
-        for (int x = 0; x < 2; ++x) s[2 * r + x] = fmaf(scale, c[2 * r + x], fmaf(zero, qsum[g][x], s[2 * r + x]));
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(tile + tile_k_row(D, ri + 8 * r)) + j * X;
+        if constexpr (X == 4) {
+          const uint4 v = *reinterpret_cast<const uint4*>(src);
+          kc[r][0] = v.x; kc[r][1] = v.y; kc[r][2] = v.z; kc[r][3] = v.w;
+        } else {
+          const uint2 v = *reinterpret_cast<const uint2*>(src);
+          kc[r][0] = v.x; kc[r][1] = v.y;
+        }
       }
-    }
-    float vs[G][2], vz[G][2];                    // V's scales and zeros (moved to the centred codes) of rows i, i + 8
 #pragma unroll
-    for (int g = 0; g < G; ++g)
+      for (int g = 0; g < G; ++g) {
+        float c[4] = {bias[g][0], bias[g][1], bias[g][0], bias[g][1]};
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(tp + tile_v_word(D, G, ri + 8 * r, g));
-        vs[g][r] = __uint_as_float(w << 16);
-        vz[g][r] = fmaf(8.f, vs[g][r], __uint_as_float(w & 0xffff0000u));
-      }
-    if (edge) {
-      // Rows behind the end hold anything, rows that a token does not see may hold NaN: replaced, not multiplied away.
-      // (A NaN scale that some columns see goes into their zero sums by hand.)
-      asm volatile("");                          // a branch: as selects this would cost every tile
+        for (int u = 0; u < U; ++u) {
+          uint32_t lo[4], hi[4];
+          key4(kc[0][g * U + u], lo);
+          key4(kc[1][g * U + u], hi);
+          const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
+          mma_full(c, a0, qf[g * U + u][0], qf[g * U + u][1]);
+          mma_full(c, a1, qf[g * U + u][2], qf[g * U + u][3]);
+        }
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int row = ri + 8 * r;
+        for (int r = 0; r < 2; ++r) {
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(tile + tile_k_word(D, G, ri + 8 * r, g));
+          const float scale = __uint_as_float(w << 16), zero = __uint_as_float(w & 0xffff0000u);
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-          if (row >= rows || row0 + row >= limit[x]) s[2 * r + x] = -INFINITY;
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          if (row < rows && vs[g][r] != vs[g][r])
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-              if (row0 + row < limit[x]) zacc[g][x] = vs[g][r];
-          if (row >= rows || vs[g][r] != vs[g][r]) vs[g][r] = vz[g][r] = 0.f;
+          for (int x = 0; x < 2; ++x) {
+            const float zq = g == 0 ? zero * qsum[g][x] : fmaf(zero, qsum[g][x], s[b][2 * r + x]);
+            s[b][2 * r + x] = fmaf(scale, c[2 * r + x], zq);
+          }
         }
       }
     }
+    uint32_t vw[kStageTiles][G][2];              // V's (scale, zero) of rows i, i + 8
+#pragma unroll
+    for (int b = 0; b < kStageTiles; ++b)
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          vw[b][g][r] = *reinterpret_cast<const uint32_t*>(tp + b * kTileBytes + tile_v_word(D, G, ri + 8 * r, g));
+    if (edge) {
+      // Rows behind the end hold anything, rows that a token does not see may hold NaN: replaced, not multiplied away.
+      // (A NaN scale that some columns see goes into their zero sums by hand.)
+      asm volatile("");                          // a branch: as selects this would cost every stage
+#pragma unroll
+      for (int b = 0; b < kStageTiles; ++b)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int row = b * kPageTile + ri + 8 * r;
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            if (row >= rows || row0 + row >= limit[x]) s[b][2 * r + x] = -INFINITY;
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const float scale = __uint_as_float(vw[b][g][r] << 16);
+            if (row < rows && scale != scale)
+#pragma unroll
+              for (int x = 0; x < 2; ++x)
+                if (row0 + row < limit[x]) zacc[g][x] = scale;
+            if (row >= rows || scale != scale) vw[b][g][r] = 0;
+          }
+        }
+    }
     // Rare work, found by one vote: a score far above the maximum, a scale that P's f16 range no longer covers (P <= 2^8,
-    // its scaled value <= 2^15), or one so far below that P would lose bits.
+    // its scaled value <= 2^15), or only scales so far below that P would lose bits.
     float top = 0.f, low = INFINITY;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      const float x = fmaxf(vs[g][0], vs[g][1]) * norm[g];
-      top = fmaxf(top, x);
-      low = fminf(low, x);
+      float big = __uint_as_float(vw[0][g][0] << 16);
+#pragma unroll
+      for (int y = 1; y < 2 * kStageTiles; ++y) big = fmaxf(big, __uint_as_float(vw[y >> 1][g][y & 1] << 16));
+      big *= norm[g];
+      top = fmaxf(top, big);
+      low = fminf(low, big);
     }
-    if (__any_sync(0xffffffffu, fmaxf(s[0], s[2]) > raise[0] || fmaxf(s[1], s[3]) > raise[1] || top > 64.f) ||
+    float ms[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) ms[x] = fmaxf(fmaxf(s[0][x], s[0][2 + x]), fmaxf(s[1][x], s[1][2 + x]));
+    if (__any_sync(0xffffffffu, ms[0] > raise[0] || ms[1] > raise[1] || top > 64.f) ||
         __all_sync(0xffffffffu, low < 0.015625f)) {
 #pragma unroll
       for (int g = 0; g < G; ++g) {
-        const float big = fmaxf(vs[g][0], vs[g][1]);
+        float big = 0.f;
+#pragma unroll
+        for (int y = 0; y < 2 * kStageTiles; ++y) big = fmaxf(big, __uint_as_float(vw[y >> 1][g][y & 1] << 16));
         const float x = big * norm[g];
         if (__any_sync(0xffffffffu, x > 64.f) || __all_sync(0xffffffffu, !(x >= 0.015625f))) renorm(g, big);
       }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        float mx = fmaxf(s[x], s[2 + x]);
+        float mx = ms[x];
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
         const float m_new = fmaxf(m[x], mx * sc2[x]);
         const float corr = m_new == -INFINITY ? 1.f : ex2(m[x] - m_new);
         m[x] = m_new;
+        ref[x] = m_new == -INFINITY ? 0.f : m_new;               // nothing seen yet: every term is zero
         raise[x] = m_new == -INFINITY ? -INFINITY : (m_new + kLazy) / sc2[x];
         l[x] *= corr;
 #pragma unroll
@@ -555,49 +609,53 @@ struct MmaBody {
         }
       }
     }
-    float p[4];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const float ref = m[x] == -INFINITY ? 0.f : m[x];
-      p[x] = ex2(fmaf(s[x], sc2[x], -ref));
-      p[2 + x] = ex2(fmaf(s[2 + x], sc2[x], -ref));
-      l[x] += p[x] + p[2 + x];
-    }
 
-    // O^T += V^T P^T, the group's scale multiplied into P
-    uint32_t vc[4][X / 2];                       // rows of matrix rows 2 j, 2 j + 1, 2 j + 8, 2 j + 9
+    // P, and O^T += V^T P^T with the group's scale multiplied into P
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int mr = 2 * j + (r & 1), row = (mr ^ ((mr >> 1) & 1)) + 8 * (r >> 1);
-      const uint32_t* src = reinterpret_cast<const uint32_t*>(tp + tile_v_row(D, row)) + i * (X / 2);
-      if constexpr (X == 4) {
-        const uint2 v = *reinterpret_cast<const uint2*>(src);
-        vc[r][0] = v.x; vc[r][1] = v.y;
-      } else {
-        vc[r][0] = *src;
+    for (int b = 0; b < kStageTiles; ++b) {
+      const uint8_t* tile = tp + b * kTileBytes;
+      float p[4];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        p[x] = ex2(fmaf(s[b][x], sc2[x], -ref[x]));
+        p[2 + x] = ex2(fmaf(s[b][2 + x], sc2[x], -ref[x]));
+        l[x] += p[x] + p[2 + x];
       }
-    }
+      uint32_t vc[4][X / 2];                     // rows of matrix rows 2 j, 2 j + 1, 2 j + 8, 2 j + 9
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      uint32_t pb[2];
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const float f = vs[g][r] * norm[g];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) zacc[g][x] = fmaf(p[2 * r + x], vz[g][r], zacc[g][x]);
-        pb[r] = transpose8x8(pack_f16(p[2 * r] * f, p[2 * r + 1] * f));
+      for (int r = 0; r < 4; ++r) {
+        const int row = ((2 * j + (r & 1)) ^ (j & 1)) + 8 * (r >> 1);
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(tile + tile_v_row(D, row)) + i * (X / 2);
+        if constexpr (X == 4) {
+          const uint2 v = *reinterpret_cast<const uint2*>(src);
+          vc[r][0] = v.x; vc[r][1] = v.y;
+        } else {
+          vc[r][0] = *src;
+        }
       }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int x = g * U + u;
-        const uint32_t sel = (x & 1) ? 0x7632 : 0x5410;
-        uint32_t v0[4], v1[4];
-        centred4(__byte_perm(vc[0][x >> 1], vc[1][x >> 1], sel), v0);
-        centred4(__byte_perm(vc[2][x >> 1], vc[3][x >> 1], sel), v1);
+      for (int g = 0; g < G; ++g) {
+        uint32_t pb[2];
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const uint32_t av[4] = {v0[2 * y], v0[2 * y + 1], v1[2 * y], v1[2 * y + 1]};
-          mma_full(o[x][y], av, pb[0], pb[1]);
+        for (int r = 0; r < 2; ++r) {
+          const float scale = __uint_as_float(vw[b][g][r] << 16);
+          const float zero = fmaf(8.f, scale, __uint_as_float(vw[b][g][r] & 0xffff0000u)), f = scale * norm[g];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) zacc[g][x] = fmaf(p[2 * r + x], zero, zacc[g][x]);
+          pb[r] = transpose8x8(pack_f16(p[2 * r] * f, p[2 * r + 1] * f));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int x = g * U + u;
+          const uint32_t sel = (x & 1) ? 0x7632 : 0x5410;
+          uint32_t v0[4], v1[4];
+          centred4(__byte_perm(vc[0][x >> 1], vc[1][x >> 1], sel), v0);
+          centred4(__byte_perm(vc[2][x >> 1], vc[3][x >> 1], sel), v1);
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const uint32_t av[4] = {v0[2 * y], v0[2 * y + 1], v1[2 * y], v1[2 * y + 1]};
+            mma_full(o[x][y], av, pb[0], pb[1]);
+          }
         }
       }
     }
@@ -661,6 +719,15 @@ __device__ __forceinline__ bool try_wait_once(uint32_t bar, uint32_t parity) {
                : "=r"(done) : "r"(bar), "r"(parity) : "memory");
   return done != 0;
 }
+__device__ __forceinline__ bool test_wait_once(uint32_t bar, uint32_t parity) {        // does not suspend
+  uint32_t done;
+  asm volatile("{\n\t.reg .pred P;\n\tmbarrier.test_wait.parity.shared::cta.b64 P, [%1], %2;\n\tselp.b32 %0, 1, 0, P;\n\t}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
+}
+__device__ __forceinline__ void arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 // one copy global -> shared that completes the phase of `bar`
 __device__ __forceinline__ void tile_load(uint32_t dst, const uint8_t* src, uint32_t bytes, uint32_t bar) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -668,50 +735,86 @@ __device__ __forceinline__ void tile_load(uint32_t dst, const uint8_t* src, uint
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar) : "memory");
 }
 
+// Merge, by one warp, of the states [x][D + 2] that the bits of `members` number (`at` gives a state's address), columns
+// x < ncols. f gets (column, first of four dimensions, their sums, maximum, denominator).
+template <int D, class At, class F>
+__device__ __forceinline__ void merge_states(uint32_t members, int ncols, int lane, At at, F f) {
+  for (int o = lane; o < ncols * (D / 4); o += 32) {
+    const int x = o / (D / 4), d = o % (D / 4) * 4;
+    float M = -INFINITY;
+    for (uint32_t b = members; b; b &= b - 1) M = fmaxf(M, at(__ffs(b) - 1)[x * (D + 2) + D]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    float num[4] = {0.f, 0.f, 0.f, 0.f}, den = 0.f;
+    for (uint32_t b = members; b; b &= b - 1) {
+      const float* st = at(__ffs(b) - 1) + x * (D + 2);
+      const float w = ex2(st[D] - ref);
+      const float2 u = *reinterpret_cast<const float2*>(st + d), v = *reinterpret_cast<const float2*>(st + d + 2);
+      num[0] = fmaf(w, u.x, num[0]); num[1] = fmaf(w, u.y, num[1]);
+      num[2] = fmaf(w, v.x, num[2]); num[3] = fmaf(w, v.y, num[3]);
+      den = fmaf(w, st[D + 1], den);
+    }
+    f(x, d, num, M, den);
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void write4(const PagesAttnArgs& a, const Piece& pc, int col, int d, const float* num, float M,
+                                       float den, bool stats) {
+  const OutPlace at(a, pc.entry, pc.h, col);
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  T* dst = static_cast<T*>(a.out) + at.out + d;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) dst[k] = from_f<T>(num[k] * inv);
+  if (stats && a.lse) a.lse[at.lse] = lse_of(M, den);
+}
+
 template <class Body>
-__global__ void __launch_bounds__(kThreads, Body::kBlocks) attn_kernel(PagesAttnArgs a, int cgs) {
+__global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_kernel(PagesAttnArgs a, int cgs) {
   using T = typename Body::Type;
   using L = Layout<Body>;
   constexpr int D = Body::kDim, COLS = Body::COLS, S = Body::kStages, TB = Body::kTileBytes;
+  constexpr int kWarps = Body::kWarps, kThreads = (kWarps + 1) * 32;
+  static_assert(kWarps <= kMaxWarps, "tables in Sched");
   extern __shared__ __align__(128) uint8_t base[];       // (never cast through an integer: loads from it must stay shared loads)
   __shared__ Sched sh;
-  __shared__ uint64_t full[kWarps][S];
+  __shared__ uint64_t full[kWarps][S], empty[kWarps][S];
+  __shared__ int loaded[kWarps][S];              // a stage's tiles, 0 if they lie in no valid page
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  uint8_t* ring = base + warp * L::warp_bytes;
   // where a warp's states lie: place 0 behind the ring and the queries, place 1 in the ring
   auto state_of = [&](int w, int place) {
     return reinterpret_cast<float*>(base + w * L::warp_bytes + (place ? 0 : L::ring + Body::kQueryFloats * 4));
   };
-  float* qs = reinterpret_cast<float*>(ring + L::ring);
   const int cols_total = a.T * a.rep;
 
-  if (lane == 0) {
-    for (int s = 0; s < S; ++s) mbar_init(&full[warp][s], 1);
+  if (warp < kWarps && lane == 0) {
+    for (int s = 0; s < S; ++s) { mbar_init(&full[warp][s], 1); mbar_init(&empty[warp][s], 1); }
     sh.piece[warp][0].valid = sh.piece[warp][1].valid = 0;
   }
-  if (t == 0) sh.abort_flag = 0;
+  if (t == 0) { sh.abort_flag = 0; sh.open_c1[0] = sh.open_c1[1] = -1; }
   fence_barrier_init();
 
   // ---- this CTA's share: total units, units per warp, and the entries in which the warps' ranges start
-  long long total = 0, part;
+  long long total = 0, part, u_mine = 0, lo_mine = 0;
   for (int i0 = 0; i0 < a.n; i0 += kThreads) {
     const int i = i0 + t;
-    const long long u = i < a.n ? entry_units(a, i, cgs) : 0;
-    if (blockIdx.x == 0 && i < a.n && u == 0) record(a.p.status, PYR_ERR_INVALID);
-    block_scan(u, sh.sums, &part);
+    u_mine = i < a.n ? entry_units(a, i, cgs) : 0;
+    if (blockIdx.x == 0 && i < a.n && u_mine == 0) record(a.p.status, PYR_ERR_INVALID);
+    lo_mine = block_scan<kWarps + 1>(u_mine, sh.sums, &part);
     total += part;
   }
   const long long workers = (long long)gridDim.x * kWarps;
-  long long q = (total + workers - 1) / workers;
+  long long q = total >> 31 ? (total + workers - 1) / workers : (long long)(((uint32_t)total + (uint32_t)workers - 1u) / (uint32_t)workers);
   if (q < kMinUnits) q = kMinUnits;
   const long long cta_units = q * kWarps, cta_u = blockIdx.x * cta_units;
   if (cta_u >= total) return;                    // the whole CTA: nothing is in flight
   long long run = 0;
   for (int i0 = 0; i0 < a.n && run < cta_u + cta_units; i0 += kThreads) {
     const int i = i0 + t;
-    const long long u = i < a.n ? entry_units(a, i, cgs) : 0;
-    const long long lo = run + block_scan(u, sh.sums, &part);
-#pragma unroll
+    long long u = u_mine, lo = lo_mine;
+    if (a.n > kThreads) {
+      u = i < a.n ? entry_units(a, i, cgs) : 0;
+      lo = run + block_scan<kWarps + 1>(u, sh.sums, &part);
+    }
     for (int w = 0; w < kWarps; ++w) {
       const long long s = cta_u + w * q;
       if (s >= lo && s < lo + u) { sh.entry[w] = i; sh.first_unit[w] = lo; }
@@ -720,53 +823,91 @@ __global__ void __launch_bounds__(kThreads, Body::kBlocks) attn_kernel(PagesAttn
   }
   __syncthreads();
 
-  const long long u_warp = cta_u + warp * q;
-  const int mine = (int)max(0LL, min(q, total - u_warp));    // units of this warp
+  const int w_of = warp < kWarps ? warp : lane;          // the warp whose range this thread works on or loads for
+  const long long u_warp = cta_u + w_of * q;
+  const int mine = w_of < kWarps ? (int)max(0LL, min(q, total - u_warp)) : 0;    // its units
 
-  if (mine > 0) {
-    // ---- the loader's position: a tile of a list's page, and the list's next 32 page ids, one per lane
-    Place ld;
-    int ld_list = ld.start(a, cgs, sh.entry[warp], u_warp - sh.first_unit[warp] + 0LL);
-    Place cu = ld;
-    int to_load = mine, win0 = -64, win = -1, in_page = 0, in_stage = 0;
-    uint32_t loaded = 0;                         // four bits a stage: its tiles, and 8 if they lie in no valid page
+  if (warp == kWarps) {
+    // ------------------------------------------------------------ loaders: lane w for warp w
+    Place ld{};
+    int list = -1, slot = 0, skip = 0, in_page = 0, in_stage = 0, issued = 0, to_load = mine;
+    int page_first = -1, page_next = -1;         // page ids as the table has them: of slot 0, and of slot `slot`
+    const int tpp = a.p.tiles_per_page, head_bytes = tpp * TB;
     const uint8_t* src = nullptr;
-    const uint32_t bar0 = smem_u32(&full[warp][0]), ring0 = smem_u32(ring);
-
-    auto issue = [&]() {
-      if (in_page == 0) {
-        const int slot = ld.t / a.p.tiles_per_page, skip = ld.t - slot * a.p.tiles_per_page;
-        int page = -1;
-        if (ld.len > 0) {
-          if (slot < win0 || slot >= win0 + 32) {
-            win0 = slot;
-            win = pages_page(a.p, ld_list, (int64_t)slot + lane);
+    uint32_t parity = 1;                         // of the wait for an empty stage: the first ones are
+    const int32_t* row = a.p.table;
+    if (mine > 0) {
+      list = ld.start(a, cgs, sh.entry[w_of], u_warp - sh.first_unit[w_of]);
+      slot = ld.t / tpp;
+      skip = ld.t - slot * tpp;
+      row = a.p.table + (size_t)list * a.p.max_pages;
+      page_first = row[0];
+      page_next = row[slot];
+    }
+    (void)list;
+    const uint32_t full0 = smem_u32(&full[w_of < kWarps ? w_of : 0][0]), empty0 = smem_u32(&empty[w_of < kWarps ? w_of : 0][0]);
+    const uint32_t ring0 = smem_u32(base) + (w_of < kWarps ? w_of : 0) * L::warp_bytes;
+    volatile int* abort_flag = &sh.abort_flag;
+    for (uint32_t idle = 0; __any_sync(0xffffffffu, to_load > 0);) {
+      const bool go = to_load > 0 && test_wait_once(empty0 + 8 * in_stage, parity);
+      if (go) {
+        if (in_page == 0) {
+          src = nullptr;
+          if (ld.len > 0) {
+            if (page_next >= 0 && page_next < a.p.n_pages)
+              src = a.p.pool + ((size_t)page_next * a.p.Hkv + ld.h) * head_bytes + skip * TB;
+            else
+              record(a.p.status, PYR_ERR_INVALID);
           }
-          page = __shfl_sync(0xffffffffu, win, slot - win0);
-          if (page < 0 && lane == 0) record(a.p.status, PYR_ERR_INVALID);
+          in_page = min(tpp - skip, ld.tiles - ld.t);
+          skip = 0;
+          // the id after this one is fetched now and looked at when its page is opened
+          if (++slot < a.p.max_pages) page_next = row[slot];
         }
-        src = page < 0 ? nullptr : a.p.pool + pages_tile(a.p, page, ld.h, skip);
-        in_page = min(a.p.tiles_per_page - skip, ld.tiles - ld.t);
+        const int n = min(min(in_page, to_load), kStageTiles);
+        loaded[w_of][in_stage] = src ? n : -n;
+        if (src) {
+          tile_load(ring0 + in_stage * (kStageTiles * TB), src, n * TB, full0 + 8 * in_stage);
+          src += n * TB;
+        } else {
+          arrive(full0 + 8 * in_stage);
+        }
+        if (++in_stage == S) { in_stage = 0; parity ^= 1; }
+        ++issued;
+        in_page -= n;
+        ld.t += n;
+        to_load -= n;
+        if (ld.t == ld.tiles && to_load > 0) {
+          const int l = ld.next(a, cgs);
+          if (l >= 0) {
+            row = a.p.table + (size_t)l * a.p.max_pages;
+            page_first = row[0];
+          }
+          slot = 0;
+          page_next = page_first;
+        }
       }
-      const int n = min(min(in_page, to_load), kStageTiles);
-      loaded = (loaded & ~(15u << (4 * in_stage))) | (uint32_t)(src ? n : n | 8) << (4 * in_stage);
-      if (lane == 0) {
-        if (src) tile_load(ring0 + in_stage * (kStageTiles * TB), src, n * TB, bar0 + 8 * in_stage);
-        else mbar_arrive(&full[warp][in_stage]);
+      if (__any_sync(0xffffffffu, go)) {
+        idle = 0;
+      } else if (++idle > kSpinLimit || *abort_flag) {
+        if (lane == 0 && !*abort_flag) { *abort_flag = 1; record(a.p.status, PYR_ERR_TIMEOUT); }
+        break;
       }
-      if (src) src += n * TB;
-      in_stage ^= 1;
-      in_page -= n;
-      ld.t += n;
-      to_load -= n;
-      if (ld.t == ld.tiles && to_load > 0) {
-        const int l = ld.next(a, cgs);
-        if (l >= 0) { ld_list = l; win0 = -64; }
-      }
-    };
-    issue();
-    if (to_load > 0) issue();
-
+    }
+    __syncwarp();
+    if (*abort_flag && w_of < kWarps) {
+      // nobody consumes any more: the copies in flight must land before the CTA gives its shared memory back
+      volatile int none = 0;
+      for (int u = max(0, issued - S); u < issued; ++u)
+        mbar_wait_limit(&full[w_of][u % S], (uint32_t)(u / S) & 1, kSpinLimit, &none, nullptr, 0);
+    }
+  } else if (mine > 0) {
+    // ------------------------------------------------------------ consumers
+    Place cu{};
+    cu.start(a, cgs, sh.entry[warp], u_warp - sh.first_unit[warp]);
+    uint8_t* ring = base + warp * L::warp_bytes;
+    float* qs = reinterpret_cast<float*>(ring + L::ring);
+    const uint32_t full0 = smem_u32(&full[warp][0]), empty0 = smem_u32(&empty[warp][0]);
     Body body;
     bool ok = true;
     int stage = 0, left = mine;
@@ -775,35 +916,19 @@ __global__ void __launch_bounds__(kThreads, Body::kBlocks) attn_kernel(PagesAttn
       // ---- a segment: the warp's tiles of one (entry, head, column group)
       const int t0 = cu.t, t1 = min(cu.tiles, t0 + left);
       body.begin(a, cu, cols_total, qs, lane);
-      int tt = t0;
 #pragma unroll 1
-      while (tt < t1) {
-        if (!__all_sync(0xffffffffu, ok && try_wait_once(bar0 + 8 * stage, parity)) && ok)
+      for (int tt = t0; tt < t1 && ok;) {
+        if (!__all_sync(0xffffffffu, try_wait_once(full0 + 8 * stage, parity))) {
           ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][stage], parity, &sh.abort_flag, a.p.status, PYR_ERR_TIMEOUT));
-        if (!ok) break;
-        const uint32_t mine_here = loaded >> (4 * stage);
-        const int n = (int)(mine_here & 7u);
-        const uint8_t* tp = ring + stage * (kStageTiles * TB);
-        if (!(mine_here & 8u))
-#pragma unroll 1
-          for (int x = 0; x < n; ++x)
-            body.tile(a, tp + x * TB, (tt + x) * kPageTile, min(cu.len - (tt + x) * kPageTile, kPageTile), qs, lane);
+          if (!ok) break;        // the remaining work is only walked through, so that no other CTA waits for this one's share
+        }
+        const int n = loaded[warp][stage];
+        if (n > 0)
+          body.stage(a, ring + stage * (kStageTiles * TB), tt * kPageTile, min(cu.len - tt * kPageTile, n * kPageTile), qs, lane);
+        tt += n < 0 ? -n : n;
         __syncwarp();
-        tt += n;
-        if (stage) parity ^= 1;
-        stage ^= 1;
-        if (to_load > 0) issue();
-      }
-      if (!ok && to_load >= 0) {
-        // A wait ran out: the remaining work is only walked through, so that no other CTA waits for this one's share. Copies
-        // in flight must land before the shared memory is used otherwise or given back.
-        volatile int none = 0;
-        do {
-          mbar_wait_limit(&full[warp][stage], parity, kSpinLimit, &none, nullptr, 0);
-          if (stage) parity ^= 1;
-          stage ^= 1;
-        } while (stage != in_stage);
-        to_load = -1;
+        if (lane == 0) arrive(empty0 + 8 * stage);
+        if (++stage == S) { stage = 0; parity ^= 1; }
       }
       const bool begins = t0 == 0, ends = t1 == cu.tiles;
       left -= t1 - t0;
@@ -827,67 +952,59 @@ __global__ void __launch_bounds__(kThreads, Body::kBlocks) attn_kernel(PagesAttn
     }
   }
 
-  // ---- merge the CTA's partial states: runs of consecutive ones of the same (entry, head, column group)
+  // ---- merge the CTA's partial states: runs of consecutive ones of the same (entry, head, column group), a warp a run
   __syncthreads();
-  int slot_c1[2] = {-1, -1}, slot_count[2] = {0, 0};      // what the CTA leaves for others: place 0 / place 1
-  int left_at[2] = {0, 0};                                // a piece of it
-  for (int f = 0; f < kWarps * 2;) {
+  for (int f = 0, r = 0; f < kWarps * 2;) {
     if (!sh.piece[f >> 1][f & 1].valid) { ++f; continue; }
     const Piece& pc = sh.piece[f >> 1][f & 1];
     int g = f + 1, last = f;
+    uint32_t members = 1;                        // bit k: piece f + k
     for (; g < kWarps * 2; ++g) {
       const Piece& o = sh.piece[g >> 1][g & 1];
       if (!o.valid) continue;
       if (o.u0 != pc.u0) break;
       last = g;
+      members |= 1u << (g - f);
     }
-    const bool whole = pc.begins && sh.piece[last >> 1][last & 1].ends;
-    const int place = pc.begins ? 1 : 0;
-    const int ncols = min(COLS, cols_total - pc.cg * COLS);
-    for (int o = t; o < ncols * D; o += kThreads) {
-      const int x = o / D, d = o % D;
-      float M = -INFINITY;
-      for (int k = f; k <= last; ++k)
-        if (sh.piece[k >> 1][k & 1].valid) M = fmaxf(M, state_of(k >> 1, k & 1)[x * (D + 2) + D]);
-      const float ref = M == -INFINITY ? 0.f : M;
-      float num = 0.f, den = 0.f;
-      for (int k = f; k <= last; ++k)
-        if (sh.piece[k >> 1][k & 1].valid) {
-          const float* st = state_of(k >> 1, k & 1) + x * (D + 2);
-          const float w = ex2(st[D] - ref);
-          num = fmaf(w, st[d], num);
-          den = fmaf(w, st[D + 1], den);
-        }
+    if (r % (kWarps + 1) == warp) {
+      const bool whole = pc.begins && sh.piece[last >> 1][last & 1].ends;
+      const int place = pc.begins ? 1 : 0;
+      const int ncols = min(COLS, cols_total - pc.cg * COLS);
+      auto at = [&](int k) { return (const float*)state_of((f + k) >> 1, (f + k) & 1); };
       if (whole) {
-        const OutPlace at(a, pc.entry, pc.h, pc.cg * COLS + x);
-        static_cast<T*>(a.out)[at.out + d] = from_f<T>(den == 0.f ? 0.f : num / den);
-        if (d == 0 && a.lse) a.lse[at.lse] = lse_of(M, den);
+        merge_states<D>(members, ncols, lane, at, [&](int x, int d, const float* num, float M, float den) {
+          write4<T>(a, pc, pc.cg * COLS + x, d, num, M, den, d == 0);
+        });
       } else {
-        float* dst = a.partial + ((size_t)blockIdx.x * 2 + place) * (kAttnCols * (D + 2)) + x * (D + 2);
-        __stcg(dst + d, num);
-        if (d == 0) { __stcg(dst + D, M); __stcg(dst + D + 1, den); }
+        float* dst = a.partial + ((size_t)blockIdx.x * 2 + place) * (kAttnCols * (D + 2));
+        merge_states<D>(members, ncols, lane, at, [&](int x, int d, const float* num, float M, float den) {
+          __stcg(reinterpret_cast<float2*>(dst + x * (D + 2) + d), make_float2(num[0], num[1]));
+          __stcg(reinterpret_cast<float2*>(dst + x * (D + 2) + d + 2), make_float2(num[2], num[3]));
+          if (d == 0) __stcg(reinterpret_cast<float2*>(dst + x * (D + 2) + D), make_float2(M, den));
+        });
+        if (lane == 0) {
+          sh.open_piece[place] = f;
+          sh.open_c1[place] = (int)(pc.u0 / cta_units);
+          sh.open_count[place] = (int)((pc.u1 - 1) / cta_units) - (int)(pc.u0 / cta_units) + 1;
+        }
+        __threadfence();
       }
     }
-    if (!whole) {
-      left_at[place] = f;
-      slot_c1[place] = (int)(pc.u0 / cta_units);
-      slot_count[place] = (int)((pc.u1 - 1) / cta_units) - slot_c1[place] + 1;
-    }
+    ++r;
     f = g;
   }
-  if (slot_c1[0] < 0 && slot_c1[1] < 0) return;           // uniform over the CTA
-  __threadfence();
   __syncthreads();
+  if (sh.open_c1[0] < 0 && sh.open_c1[1] < 0) return;     // uniform over the CTA
   if (t < 2) {
     sh.last[t] = 0;
-    if (slot_c1[t] >= 0) sh.last[t] = atomicAdd(&a.arrived[slot_c1[t]], 1) == slot_count[t] - 1;
+    if (sh.open_c1[t] >= 0) sh.last[t] = atomicAdd(&a.arrived[sh.open_c1[t]], 1) == sh.open_count[t] - 1;
+    __threadfence();
   }
   __syncthreads();
-  __threadfence();
   for (int place = 0; place < 2; ++place) {
-    if (slot_c1[place] < 0 || !sh.last[place]) continue;
-    const Piece& pc = sh.piece[left_at[place] >> 1][left_at[place] & 1];
-    const int c1 = slot_c1[place], cn = slot_count[place];
+    if (sh.open_c1[place] < 0 || !sh.last[place]) continue;
+    const Piece& pc = sh.piece[sh.open_piece[place] >> 1][sh.open_piece[place] & 1];
+    const int c1 = sh.open_c1[place], cn = sh.open_count[place];
     const int ncols = min(COLS, cols_total - pc.cg * COLS);
     // the first CTA holds the beginning (place 1), the others go on with it (place 0)
     const float* src = a.partial + (size_t)c1 * 2 * (kAttnCols * (D + 2));
@@ -895,7 +1012,7 @@ __global__ void __launch_bounds__(kThreads, Body::kBlocks) attn_kernel(PagesAttn
     // a column's maxima and sums are 2 cn numbers far apart: a warp a column, so that they are fetched together
     float* weight = reinterpret_cast<float*>(base);           // [cn][COLS], where the rings were
     __syncthreads();
-    for (int x = warp; x < ncols; x += kWarps) {
+    for (int x = warp; x < ncols; x += kWarps + 1) {
       float M = -INFINITY;
       for (int k = lane; k < cn; k += 32) M = fmaxf(M, __ldcg(src + k * step + (k == 0 ? second : 0) + x * (D + 2) + D));
 #pragma unroll
@@ -928,10 +1045,7 @@ __global__ void __launch_bounds__(kThreads, Body::kBlocks) attn_kernel(PagesAttn
         num[0] = fmaf(w, u.x, num[0]); num[1] = fmaf(w, u.y, num[1]);
         num[2] = fmaf(w, v.x, num[2]); num[3] = fmaf(w, v.y, num[3]);
       }
-      const float den = sh.den[x], inv = den == 0.f ? 0.f : 1.f / den;
-      T* dst = static_cast<T*>(a.out) + OutPlace(a, pc.entry, pc.h, pc.cg * COLS + x).out + d;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) dst[k] = from_f<T>(num[k] * inv);
+      write4<T>(a, pc, pc.cg * COLS + x, d, num, 0.f, sh.den[x], false);
     }
     if (t == 0) a.arrived[c1] = 0;                         // as the next call expects it
   }
@@ -947,10 +1061,11 @@ cudaError_t run_attn(const PagesAttnArgs& a, cudaStream_t s) {
   if (sms <= 0) return cudaErrorUnknown;
   // a grid that the machine holds at once, no larger than the work can be
   const long long most = (long long)a.n * a.p.Hkv * cgs * attn_tiles(a.p.max_pages * a.p.page_rows);
-  long long ctas = (most + kWarps * kMinUnits - 1) / (kWarps * kMinUnits);
+  constexpr int per_cta = Body::kWarps * kMinUnits;
+  long long ctas = (most + per_cta - 1) / per_cta;
   if (ctas > (long long)Body::kBlocks * sms) ctas = (long long)Body::kBlocks * sms;
   if (ctas > kAttnMaxCtas) ctas = kAttnMaxCtas;
-  attn_kernel<Body><<<(unsigned)ctas, kThreads, smem, s>>>(a, cgs);
+  attn_kernel<Body><<<(unsigned)ctas, (Body::kWarps + 1) * 32, smem, s>>>(a, cgs);
   return cudaGetLastError();
 }
 
