@@ -28,7 +28,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kStageTiles = 2;           // a stage of a warp's ring: one copy of up to two tiles
 constexpr int kStageRows = kStageTiles * kPageTile;
-constexpr int kMinUnits = 4;             // a warp's share is at least this many tiles: merging costs more than they do
+constexpr int kSegmentUnits = 2;         // what beginning and ending a (entry, head, column group) costs, in tiles
+constexpr int kMinUnits = 6;             // a warp's share is at least this much: merging costs more than that
 constexpr int kMaxWarps = 12;
 
 __device__ __forceinline__ void record(int* status, int code) { atomicCAS(status, 0, code); }
@@ -42,7 +43,7 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float
 
 // A partial state's place in the call.
 struct Piece {
-  long long u0, u1;      // units of its (entry, head, column group)
+  long long u0, u1;      // units of its (entry, head, column group) that stand for tiles
   int entry, h, cg;
   int begins, ends;      // whether it holds the first / the last of them
   int valid;
@@ -80,48 +81,61 @@ __device__ __forceinline__ long long block_scan(long long x, long long* warp_sum
   return before + incl - x;
 }
 
-// Units of entry i: 0 if its list id is out of range (the entry is refused).
+// Units of entry i: 0 if its list id is out of range (the entry is refused). A (head, column group) has kSegmentUnits units
+// that stand for no tile before those that do: short lists cost more than their tiles, and a warp's share must say so.
 __device__ __forceinline__ long long entry_units(const PagesAttnArgs& a, int i, int cgs) {
   const int l = pages_list(a.p, a.lists, i);
-  return l < 0 ? 0 : (long long)attn_tiles(pages_len(a.p, l)) * a.p.Hkv * cgs;
+  return l < 0 ? 0 : (long long)(attn_tiles(pages_len(a.p, l)) + kSegmentUnits) * a.p.Hkv * cgs;
 }
 
-// The (entry, head, column group) that a warp works on. `t` is the first of its tiles that the warp takes.
+// The (entry, head, column group) that a warp works on, and the tiles [t, t1) of it that are the warp's.
 struct Place {
-  int entry, len, tiles, h, cg, t;
+  int entry, len, tiles, h, cg, t, t1;
+  int list;
 
-  __device__ __forceinline__ int open(const PagesAttnArgs& a) {   // the entry's list
-    const int l = pages_list(a.p, a.lists, entry);
-    len = l < 0 ? 0 : pages_len(a.p, l);
-    tiles = l < 0 ? 0 : (int)attn_tiles(len);
-    return l;
+  __device__ __forceinline__ void open(const PagesAttnArgs& a) {       // the entry's list
+    list = pages_list(a.p, a.lists, entry);
+    len = list < 0 ? 0 : pages_len(a.p, list);
+    tiles = list < 0 ? 0 : (int)attn_tiles(len);
   }
-  __device__ __forceinline__ int start(const PagesAttnArgs& a, int cgs, int e, long long o) {   // unit o of entry e
+  // Takes units from `left` on, of which `r` of this (head, column group) lie before the warp's.
+  __device__ __forceinline__ void take(int r, int* left) {
+    const int n = min(*left, tiles + kSegmentUnits - r);
+    t = max(0, r - kSegmentUnits);
+    t1 = max(0, r + n - kSegmentUnits);
+    *left -= n;
+  }
+  __device__ __forceinline__ void start(const PagesAttnArgs& a, int cgs, int e, long long o, int* left) {   // unit o of entry e
     entry = e;
-    const int l = open(a);
-    if (o >> 31 == 0) {                          // (64-bit divisions take a microsecond's tenth each)
-      const uint32_t hc = (uint32_t)o / (uint32_t)tiles;
-      t = (int)((uint32_t)o - hc * tiles);
+    open(a);
+    const int per = tiles + kSegmentUnits;
+    int r;
+    if (o >> 31 == 0) {                          // (64-bit divisions take a tenth of a microsecond each)
+      const uint32_t hc = (uint32_t)o / (uint32_t)per;
+      r = (int)((uint32_t)o - hc * per);
       h = (int)(hc / (uint32_t)cgs);
       cg = (int)(hc - (uint32_t)h * cgs);
     } else {
-      t = (int)(o % tiles);
-      const long long hc = o / tiles;
+      r = (int)(o % per);
+      const long long hc = o / per;
       cg = (int)(hc % cgs);
       h = (int)(hc / cgs);
     }
-    return l;
+    take(r, left);
   }
-  // the next one; returns its list, or -1 if the list is the same
-  __device__ __forceinline__ int next(const PagesAttnArgs& a, int cgs) {
-    t = 0;
-    if (++cg < cgs) return -1;
-    cg = 0;
-    if (++h < a.p.Hkv) return -1;
-    h = 0;
-    int l = -1;
-    do { ++entry; l = open(a); } while (l < 0 && entry + 1 < a.n);   // refused entries have no unit
-    return l;
+  // The next one. Returns whether its list is another.
+  __device__ __forceinline__ bool next(const PagesAttnArgs& a, int cgs, int* left) {
+    bool other = false;
+    if (++cg >= cgs) {
+      cg = 0;
+      if (++h >= a.p.Hkv) {
+        h = 0;
+        other = true;
+        do { ++entry; open(a); } while (list < 0 && entry + 1 < a.n);  // refused entries have no unit
+      }
+    }
+    take(0, left);
+    return other;
   }
 };
 
@@ -830,26 +844,34 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
   if (warp == kWarps) {
     // ------------------------------------------------------------ loaders: lane w for warp w
     Place ld{};
-    int list = -1, slot = 0, skip = 0, in_page = 0, in_stage = 0, issued = 0, to_load = mine;
+    int slot = 0, skip = 0, in_page = 0, in_stage = 0, issued = 0, left = mine;
     int page_first = -1, page_next = -1;         // page ids as the table has them: of slot 0, and of slot `slot`
     const int tpp = a.p.tiles_per_page, head_bytes = tpp * TB;
     const uint8_t* src = nullptr;
     uint32_t parity = 1;                         // of the wait for an empty stage: the first ones are
     const int32_t* row = a.p.table;
     if (mine > 0) {
-      list = ld.start(a, cgs, sh.entry[w_of], u_warp - sh.first_unit[w_of]);
+      ld.start(a, cgs, sh.entry[w_of], u_warp - sh.first_unit[w_of], &left);
       slot = ld.t / tpp;
       skip = ld.t - slot * tpp;
-      row = a.p.table + (size_t)list * a.p.max_pages;
+      row = a.p.table + (size_t)ld.list * a.p.max_pages;
       page_first = row[0];
       page_next = row[slot];
     }
-    (void)list;
     const uint32_t full0 = smem_u32(&full[w_of < kWarps ? w_of : 0][0]), empty0 = smem_u32(&empty[w_of < kWarps ? w_of : 0][0]);
     const uint32_t ring0 = smem_u32(base) + (w_of < kWarps ? w_of : 0) * L::warp_bytes;
     volatile int* abort_flag = &sh.abort_flag;
-    for (uint32_t idle = 0; __any_sync(0xffffffffu, to_load > 0);) {
-      const bool go = to_load > 0 && test_wait_once(empty0 + 8 * in_stage, parity);
+    for (uint32_t idle = 0; __any_sync(0xffffffffu, ld.t < ld.t1 || left > 0);) {
+      if (ld.t == ld.t1 && left > 0) {           // on to the next (entry, head, column group)
+        if (ld.next(a, cgs, &left)) {
+          row = a.p.table + (size_t)ld.list * a.p.max_pages;
+          page_first = row[0];
+        }
+        slot = 0;
+        in_page = 0;
+        page_next = page_first;
+      }
+      const bool go = ld.t < ld.t1 && test_wait_once(empty0 + 8 * in_stage, parity);
       if (go) {
         if (in_page == 0) {
           src = nullptr;
@@ -859,12 +881,12 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
             else
               record(a.p.status, PYR_ERR_INVALID);
           }
-          in_page = min(tpp - skip, ld.tiles - ld.t);
+          in_page = min(tpp - skip, ld.t1 - ld.t);
           skip = 0;
           // the id after this one is fetched now and looked at when its page is opened
           if (++slot < a.p.max_pages) page_next = row[slot];
         }
-        const int n = min(min(in_page, to_load), kStageTiles);
+        const int n = min(in_page, kStageTiles);
         loaded[w_of][in_stage] = src ? n : -n;
         if (src) {
           tile_load(ring0 + in_stage * (kStageTiles * TB), src, n * TB, full0 + 8 * in_stage);
@@ -876,16 +898,6 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
         ++issued;
         in_page -= n;
         ld.t += n;
-        to_load -= n;
-        if (ld.t == ld.tiles && to_load > 0) {
-          const int l = ld.next(a, cgs);
-          if (l >= 0) {
-            row = a.p.table + (size_t)l * a.p.max_pages;
-            page_first = row[0];
-          }
-          slot = 0;
-          page_next = page_first;
-        }
       }
       if (__any_sync(0xffffffffu, go)) {
         idle = 0;
@@ -904,17 +916,22 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
   } else if (mine > 0) {
     // ------------------------------------------------------------ consumers
     Place cu{};
-    cu.start(a, cgs, sh.entry[warp], u_warp - sh.first_unit[warp]);
+    int stage = 0, left = mine;
+    cu.start(a, cgs, sh.entry[warp], u_warp - sh.first_unit[warp], &left);
     uint8_t* ring = base + warp * L::warp_bytes;
     float* qs = reinterpret_cast<float*>(ring + L::ring);
     const uint32_t full0 = smem_u32(&full[warp][0]), empty0 = smem_u32(&empty[warp][0]);
     Body body;
     bool ok = true;
-    int stage = 0, left = mine;
     uint32_t parity = 0;
     while (true) {
       // ---- a segment: the warp's tiles of one (entry, head, column group)
-      const int t0 = cu.t, t1 = min(cu.tiles, t0 + left);
+      const int t0 = cu.t, t1 = cu.t1;
+      if (t0 == t1) {                            // only units without a tile
+        if (left == 0) break;
+        cu.next(a, cgs, &left);
+        continue;
+      }
       body.begin(a, cu, cols_total, qs, lane);
 #pragma unroll 1
       for (int tt = t0; tt < t1 && ok;) {
@@ -931,7 +948,6 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
         if (++stage == S) { stage = 0; parity ^= 1; }
       }
       const bool begins = t0 == 0, ends = t1 == cu.tiles;
-      left -= t1 - t0;
       body.end();
       if (begins && ends) {
         body.write(a, cu, cols_total, lane);
@@ -941,14 +957,14 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
         body.keep(state_of(warp, place), lane);
         if (lane == 0) {
           Piece& pc = sh.piece[warp][place];
-          pc.u0 = u_warp + (mine - left - (t1 - t0)) - t0;
+          pc.u0 = u_warp + (mine - left) - t1;    // (the warp's units up to here end with tile t1 - 1)
           pc.u1 = pc.u0 + cu.tiles;
           pc.entry = cu.entry; pc.h = cu.h; pc.cg = cu.cg;
           pc.begins = begins; pc.ends = ends; pc.valid = 1;
         }
       }
       if (left == 0) break;
-      cu.next(a, cgs);
+      cu.next(a, cgs, &left);
     }
   }
 
