@@ -449,6 +449,10 @@ class PyrCache:
                                      out.data_ptr(), C.c_void_p(_stream_ptr(stream))), "pyr_decode_attn")
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
+
+
 def make_pages_config(*, n_kv_heads, head_dim, n_pages, n_lists, max_pages, group=64, page_rows=64, flags=0) -> PyrPagesConfig:
     return PyrPagesConfig(n_kv_heads, head_dim, group, page_rows, n_pages, n_lists, max_pages, flags)
 
@@ -471,6 +475,8 @@ class PyrPages:
         self.nbytes = nbytes
         self.buf = torch.empty(nbytes + align, dtype=torch.uint8, device=torch.device(device))
         self.device = self.buf.device
+        self._index, self._heads, self._dim = self.device.index, self.cfg.n_kv_heads, self.cfg.head_dim
+        self._fn = {name: getattr(lib(), name) for name in EXPORTS if name.startswith("pyr_pages_")}
         off = (-self.buf.data_ptr()) % align
         self.handle = C.c_void_p()
         _check(lib().pyr_pages_alloc(C.byref(self.cfg), C.c_void_p(self.buf.data_ptr() + off), nbytes, C.byref(self.handle)),
@@ -502,41 +508,45 @@ class PyrPages:
         return self.buf[off: off + nbytes].view(dtype).view(*shape)
 
     def _run(self, name: str, stream, *args):
-        with torch.cuda.device(self.device):
-            _check(getattr(lib(), name)(self.handle, *args, C.c_void_p(_stream_ptr(stream))), name)
+        # (a decode step makes several of these calls a layer: nothing here that a call can do without)
+        i = self._index
+        ptr = _raw_stream(i) if stream is None else stream.cuda_stream
+        if _current_device() == i:
+            st = self._fn[name](self.handle, *args, ptr)
+        else:
+            with torch.cuda.device(i):
+                st = self._fn[name](self.handle, *args, ptr)
+        if st:
+            _check(st, name)
 
-    def _ids(self, t, what="lists"):
-        """Pointer to an int32 vector on the cache's device, None for NULL."""
+    def _ids(self, t, n, what="lists"):
+        """Pointer to an int32 vector of n entries on the cache's device, None for NULL."""
         if t is None:
             return None
-        if t.dtype != torch.int32 or t.device != self.device or not t.is_contiguous():
-            raise ValueError(f"{what}: expected a contiguous int32 tensor on {self.device}")
+        if t.dtype is not torch.int32 or t.get_device() != self._index or t.shape != (n,) or not t.is_contiguous():
+            raise ValueError(f"{what}: expected {n} contiguous int32 entries on {self.device}")
         return t.data_ptr()
 
-    def _count(self, n, **vectors):
-        for what, t in vectors.items():
-            if t is not None and (t.dim() != 1 or t.shape[0] != n):
-                raise ValueError(f"{what}: expected {n} entries")
-
-    def _rows(self, a, b, what):
+    def _rows(self, a, b):
         """Strides of a pair of [n, rows, heads, D] tensors (those of dimensions of size 1 do not count)."""
-        c = self.cfg
-        if a.dim() != 4 or a.shape[2] != c.n_kv_heads or a.shape[3] != c.head_dim or a.shape != b.shape or a.dtype != b.dtype:
-            raise ValueError(f"{what}: expected [n, rows, {c.n_kv_heads}, {c.head_dim}], keys and values alike")
-        sa, sb = self._strides(a, what), self._strides(b, what)
-        if sa != sb:
-            raise ValueError(f"{what}: keys and values need the same strides")
+        shape = a.shape
+        if len(shape) != 4 or shape[2] != self._heads or shape[3] != self._dim or b.shape != shape or a.dtype is not b.dtype:
+            raise ValueError(f"k, v: expected [n, rows, {self._heads}, {self._dim}], keys and values alike")
+        sa = self._strides(a, "k, v")
+        if self._strides(b, "k, v") != sa:
+            raise ValueError("k, v: keys and values need the same strides")
         return sa
 
     def _strides(self, t, what):
-        if t.device != self.device or t.dtype not in (torch.bfloat16, torch.float32) or (t.stride(-1) != 1 and t.shape[-1] != 1):
+        (n, r, h, _), (sb, sr, sh, sd) = t.shape, t.stride()
+        if t.get_device() != self._index or (t.dtype is not torch.bfloat16 and t.dtype is not torch.float32) or sd != 1:
             raise ValueError(f"{what}: expected bf16 or fp32 on {self.device} with a contiguous last dimension")
-        return [t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)]
+        return (sb if n > 1 else 0, sr if r > 1 else 0, sh if h > 1 else 0)
 
     def _idx(self, idx, n):
         if idx is None:
             return None, 1, 0
-        if idx.dim() != 3 or idx.shape[0] != n or idx.dtype != torch.int32 or idx.device != self.device:
+        if idx.dim() != 3 or idx.shape[0] != n or idx.dtype is not torch.int32 or idx.get_device() != self._index:
             raise ValueError(f"idx: expected [n, groups, rows] int32 on {self.device}")
         g, rows = idx.shape[1], idx.shape[2]
         if (rows > 1 and idx.stride(2) != 1) or (g > 1 and idx.stride(1) != rows):
@@ -560,63 +570,58 @@ class PyrPages:
     def reserve(self, lists, rows, stream=None):
         """Pages for `rows` more rows (an int, or int32 [n]) of each list."""
         n = lists.shape[0]
-        each = rows if isinstance(rows, int) else 0
-        rows = None if isinstance(rows, int) else rows
-        self._count(n, lists=lists, rows=rows)
-        self._run("pyr_pages_reserve", stream, self._ids(lists), n, self._ids(rows, "rows"), each)
+        if isinstance(rows, int):
+            self._run("pyr_pages_reserve", stream, self._ids(lists, n), n, None, rows)
+        else:
+            self._run("pyr_pages_reserve", stream, self._ids(lists, n), n, self._ids(rows, n, "rows"), 0)
 
     def write(self, k, v, lists=None, first=None, idx=None, counts=None, stream=None):
         """Stores rows of k, v [n, src_rows, Hkv, D] (those that idx names, or all): at the lists' ends, or from row first."""
-        n = k.shape[0]
-        sb, sn, sh = self._rows(k, v, "k, v")
-        self._count(n, lists=lists, first=first, counts=counts)
+        sb, sn, sh = self._rows(k, v)
+        n, src = k.shape[0], k.shape[1]
         ip, groups, istride = self._idx(idx, n)
-        n_rows = idx.shape[2] if idx is not None else k.shape[1]
-        self._run("pyr_pages_write", stream, self._ids(lists), n, self._ids(first, "first"), k.data_ptr(), v.data_ptr(), sb, sn, sh,
-                  k.shape[1], _dt(k), ip, groups, istride, self._ids(counts, "counts"), n_rows)
+        self._run("pyr_pages_write", stream, self._ids(lists, n), n, self._ids(first, n, "first"), k.data_ptr(), v.data_ptr(), sb, sn,
+                  sh, src, _dt(k), ip, groups, istride, self._ids(counts, n, "counts"), src if idx is None else idx.shape[2])
 
     def read(self, k, v, lists=None, first=None, counts=None, stream=None):
         """Fills k, v [n, rows, Hkv, D] with the lists' rows from row first (0) on; rows a list does not have stay as they are."""
+        sb, sn, sh = self._rows(k, v)
         n = k.shape[0]
-        sb, sn, sh = self._rows(k, v, "k, v")
-        self._count(n, lists=lists, first=first, counts=counts)
-        self._run("pyr_pages_read", stream, self._ids(lists), n, self._ids(first, "first"), k.data_ptr(), v.data_ptr(), sb, sn, sh,
-                  _dt(k), self._ids(counts, "counts"), k.shape[1])
+        self._run("pyr_pages_read", stream, self._ids(lists, n), n, self._ids(first, n, "first"), k.data_ptr(), v.data_ptr(), sb, sn,
+                  sh, _dt(k), self._ids(counts, n, "counts"), k.shape[1])
 
     def attn(self, q, lists=None, out=None, lse=False, softmax_scale: float = 0.0, stream=None):
         """Attention of q [n, q_len, Hq, D] over the lists' rows: out like q, and with lse=True also lse [n, Hq, q_len] fp32."""
-        if q.dim() != 4 or q.shape[3] != self.cfg.head_dim:
-            raise ValueError(f"q: expected [n, q_len, Hq, {self.cfg.head_dim}]")
-        n, t, hq, _ = q.shape
-        self._count(n, lists=lists)
+        shape = q.shape
+        if len(shape) != 4 or shape[3] != self._dim:
+            raise ValueError(f"q: expected [n, q_len, Hq, {self._dim}]")
+        if stream is not None:
+            with torch.cuda.device(self._index), torch.cuda.stream(stream):    # what is allocated here is used on that stream
+                return self.attn(q, lists, out, lse, softmax_scale)
+        n, t, hq, _ = shape
         qs = self._strides(q, "q")
-        with torch.cuda.device(self.device), torch.cuda.stream(stream):
-            if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
-            if out.shape != q.shape or out.dtype != q.dtype:
-                raise ValueError("out: expected a tensor like q")
-            stats = torch.empty(n, hq, t, dtype=torch.float32, device=self.device) if lse else None
-            self._run("pyr_pages_attn", None, self._ids(lists), n, q.data_ptr(), *qs, out.data_ptr(), *self._strides(out, "out"),
-                      stats.data_ptr() if lse else None, t, hq, _dt(q), float(softmax_scale))
+        if out is None:
+            out = torch.empty(shape, dtype=q.dtype, device=self.device)
+        elif out.shape != shape or out.dtype is not q.dtype:
+            raise ValueError("out: expected a tensor like q")
+        stats = torch.empty(n, hq, t, dtype=torch.float32, device=self.device) if lse else None
+        self._run("pyr_pages_attn", None, self._ids(lists, n), n, q.data_ptr(), *qs, out.data_ptr(), *self._strides(out, "out"),
+                  stats.data_ptr() if lse else None, t, hq, _dt(q), softmax_scale)
         return (out, stats) if lse else out
 
     def fork(self, src, dst, stream=None):
         """Lists dst become copies of lists src that share their pages."""
         n = src.shape[0]
-        self._count(n, src=src, dst=dst)
-        self._run("pyr_pages_fork", stream, self._ids(src, "src"), self._ids(dst, "dst"), n)
+        self._run("pyr_pages_fork", stream, self._ids(src, n, "src"), self._ids(dst, n, "dst"), n)
 
     def trim(self, lists, rows=None, stream=None):
         """Cuts the lists to `rows` (int32 [n]; None: empties them) and gives up the pages behind."""
         n = lists.shape[0]
-        self._count(n, lists=lists, rows=rows)
-        self._run("pyr_pages_trim", stream, self._ids(lists), n, self._ids(rows, "rows"))
+        self._run("pyr_pages_trim", stream, self._ids(lists, n), n, self._ids(rows, n, "rows"))
 
     def compact(self, src, dst, idx=None, counts=None, n_rows=None, stream=None):
         """Rows 0 .. of lists dst become the rows idx of lists src (idx None: their first n_rows rows); src is dst: in place."""
         n = src.shape[0]
-        self._count(n, src=src, dst=dst, counts=counts)
         ip, groups, istride = self._idx(idx, n)
-        rows = idx.shape[2] if idx is not None else int(n_rows)
-        self._run("pyr_pages_compact", stream, self._ids(src, "src"), self._ids(dst, "dst"), n, ip, groups, istride,
-                  self._ids(counts, "counts"), rows)
+        self._run("pyr_pages_compact", stream, self._ids(src, n, "src"), self._ids(dst, n, "dst"), n, ip, groups, istride,
+                  self._ids(counts, n, "counts"), int(n_rows) if idx is None else idx.shape[2])

@@ -367,9 +367,10 @@ __device__ __forceinline__ uint32_t as_u32(__half2 x) { return reinterpret_cast<
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return reinterpret_cast<__half2&>(x); }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return as_u32(__floats2half2_rn(lo, hi)); }
 // (x & mask) | bits in one instruction
-__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {
+template <uint32_t kMask>
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t bits) {
   uint32_t y;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x), "r"(mask), "r"(bits));
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x), "n"(kMask), "r"(bits));
   return y;
 }
 // The four pairs of codes (nibbles k and k + 4) of x as f16 pairs, less 8: 0x6400 | n is 1024 + n, 0x6400 | 16 n is
@@ -378,10 +379,10 @@ __device__ __forceinline__ void centred4(uint32_t x, uint32_t* y) {
   const __half2 less = as_half2(0xE408E408u);                // -1032
   const __half2 part = as_half2(0x2C002C00u), off = as_half2(0xD480D480u);   // 1/16, -72
   const uint32_t z = x >> 8;
-  y[0] = as_u32(__hadd2(as_half2(and_or(x, 0x000F000Fu, 0x64006400u)), less));
-  y[1] = as_u32(__hfma2(as_half2(and_or(x, 0x00F000F0u, 0x64006400u)), part, off));
-  y[2] = as_u32(__hadd2(as_half2(and_or(z, 0x000F000Fu, 0x64006400u)), less));
-  y[3] = as_u32(__hfma2(as_half2(and_or(z, 0x00F000F0u, 0x64006400u)), part, off));
+  y[0] = as_u32(__hadd2(as_half2(and_or<0x000F000Fu>(x, 0x64006400u)), less));
+  y[1] = as_u32(__hfma2(as_half2(and_or<0x00F000F0u>(x, 0x64006400u)), part, off));
+  y[2] = as_u32(__hadd2(as_half2(and_or<0x000F000Fu>(z, 0x64006400u)), less));
+  y[3] = as_u32(__hfma2(as_half2(and_or<0x00F000F0u>(z, 0x64006400u)), part, off));
 }
 // The same for K, where the accumulator can start with what the codes have too much: nibbles 1 and 3 stay n + 64 (0x5400 | 16 n),
 // nibbles 0 and 2 become n - 8 (1024 + n would cost the accumulator bits).
@@ -389,10 +390,10 @@ constexpr float kKeyOdd = 64.f, kKeyEven = -8.f;
 __device__ __forceinline__ void key4(uint32_t x, uint32_t* y) {
   const __half2 less = as_half2(0xE408E408u);                // -1032
   const uint32_t z = x >> 8;
-  y[0] = as_u32(__hadd2(as_half2(and_or(x, 0x000F000Fu, 0x64006400u)), less));
-  y[1] = and_or(x, 0x00F000F0u, 0x54005400u);
-  y[2] = as_u32(__hadd2(as_half2(and_or(z, 0x000F000Fu, 0x64006400u)), less));
-  y[3] = and_or(z, 0x00F000F0u, 0x54005400u);
+  y[0] = as_u32(__hadd2(as_half2(and_or<0x000F000Fu>(x, 0x64006400u)), less));
+  y[1] = and_or<0x00F000F0u>(x, 0x54005400u);
+  y[2] = as_u32(__hadd2(as_half2(and_or<0x000F000Fu>(z, 0x64006400u)), less));
+  y[3] = and_or<0x00F000F0u>(z, 0x54005400u);
 }
 // 2^-e for the exponent e of x > 0 (clamped to what both it and its inverse can be)
 __device__ __forceinline__ float inverse_power(float x) {
@@ -749,11 +750,11 @@ __device__ __forceinline__ void tile_load(uint32_t dst, const uint8_t* src, uint
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar) : "memory");
 }
 
-// Merge, by one warp, of the states [x][D + 2] that the bits of `members` number (`at` gives a state's address), columns
-// x < ncols. f gets (column, first of four dimensions, their sums, maximum, denominator).
+// Merge of the states [x][D + 2] that the bits of `members` number (`at` gives a state's address), columns x < ncols: the o-th
+// four dimensions of them. f gets (column, first dimension, four sums, maximum, denominator).
 template <int D, class At, class F>
-__device__ __forceinline__ void merge_states(uint32_t members, int ncols, int lane, At at, F f) {
-  for (int o = lane; o < ncols * (D / 4); o += 32) {
+__device__ __forceinline__ void merge_states(uint32_t members, int ncols, int o, At at, F f) {
+  if (o < ncols * (D / 4)) {
     const int x = o / (D / 4), d = o % (D / 4) * 4;
     float M = -INFINITY;
     for (uint32_t b = members; b; b &= b - 1) M = fmaxf(M, at(__ffs(b) - 1)[x * (D + 2) + D]);
@@ -982,33 +983,33 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
       last = g;
       members |= 1u << (g - f);
     }
-    if (r % (kWarps + 1) == warp) {
-      const bool whole = pc.begins && sh.piece[last >> 1][last & 1].ends;
-      const int place = pc.begins ? 1 : 0;
-      const int ncols = min(COLS, cols_total - pc.cg * COLS);
-      auto at = [&](int k) { return (const float*)state_of((f + k) >> 1, (f + k) & 1); };
-      if (whole) {
-        merge_states<D>(members, ncols, lane, at, [&](int x, int d, const float* num, float M, float den) {
+    // (32 times four dimensions at a time, dealt to the warps run by run)
+    const bool whole = pc.begins && sh.piece[last >> 1][last & 1].ends;
+    const int place = pc.begins ? 1 : 0;
+    const int ncols = min(COLS, cols_total - pc.cg * COLS);
+    auto at = [&](int k) { return (const float*)state_of((f + k) >> 1, (f + k) & 1); };
+    float* dst = a.partial + ((size_t)blockIdx.x * 2 + place) * (kAttnCols * (D + 2));
+    for (int o = 0; o < ncols * (D / 4); o += 32, r = r == kWarps ? 0 : r + 1) {
+      if (r != warp) continue;
+      if (whole)
+        merge_states<D>(members, ncols, o + lane, at, [&](int x, int d, const float* num, float M, float den) {
           write4<T>(a, pc, pc.cg * COLS + x, d, num, M, den, d == 0);
         });
-      } else {
-        float* dst = a.partial + ((size_t)blockIdx.x * 2 + place) * (kAttnCols * (D + 2));
-        merge_states<D>(members, ncols, lane, at, [&](int x, int d, const float* num, float M, float den) {
+      else
+        merge_states<D>(members, ncols, o + lane, at, [&](int x, int d, const float* num, float M, float den) {
           __stcg(reinterpret_cast<float2*>(dst + x * (D + 2) + d), make_float2(num[0], num[1]));
           __stcg(reinterpret_cast<float2*>(dst + x * (D + 2) + d + 2), make_float2(num[2], num[3]));
           if (d == 0) __stcg(reinterpret_cast<float2*>(dst + x * (D + 2) + D), make_float2(M, den));
         });
-        if (lane == 0) {
-          sh.open_piece[place] = f;
-          sh.open_c1[place] = (int)(pc.u0 / cta_units);
-          sh.open_count[place] = (int)((pc.u1 - 1) / cta_units) - (int)(pc.u0 / cta_units) + 1;
-        }
-        __threadfence();
-      }
     }
-    ++r;
+    if (!whole && t == 0) {
+      sh.open_piece[place] = f;
+      sh.open_c1[place] = (int)(pc.u0 / cta_units);
+      sh.open_count[place] = (int)((pc.u1 - 1) / cta_units) - (int)(pc.u0 / cta_units) + 1;
+    }
     f = g;
   }
+  __threadfence();
   __syncthreads();
   if (sh.open_c1[0] < 0 && sh.open_c1[1] < 0) return;     // uniform over the CTA
   if (t < 2) {
@@ -1025,6 +1026,37 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
     // the first CTA holds the beginning (place 1), the others go on with it (place 0)
     const float* src = a.partial + (size_t)c1 * 2 * (kAttnCols * (D + 2));
     const size_t step = 2 * (size_t)(kAttnCols * (D + 2)), second = kAttnCols * (D + 2);
+    constexpr int kFew = 8;
+    if (cn <= kFew) {                            // everything a thread needs in one round of loads
+      for (int o = t; o < ncols * (D / 4); o += kThreads) {
+        const int x = o / (D / 4), d = o % (D / 4) * 4;
+        float2 ml[kFew], u[kFew], v[kFew];
+#pragma unroll
+        for (int k = 0; k < kFew; ++k)
+          if (k < cn) {
+            const float* st = src + k * step + (k == 0 ? second : 0) + x * (D + 2);
+            ml[k] = __ldcg(reinterpret_cast<const float2*>(st + D));
+            u[k] = __ldcg(reinterpret_cast<const float2*>(st + d));
+            v[k] = __ldcg(reinterpret_cast<const float2*>(st + d + 2));
+          }
+        float M = -INFINITY, num[4] = {0.f, 0.f, 0.f, 0.f}, den = 0.f;
+#pragma unroll
+        for (int k = 0; k < kFew; ++k)
+          if (k < cn) M = fmaxf(M, ml[k].x);
+        const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int k = 0; k < kFew; ++k)
+          if (k < cn) {
+            const float w = ex2(ml[k].x - ref);
+            num[0] = fmaf(w, u[k].x, num[0]); num[1] = fmaf(w, u[k].y, num[1]);
+            num[2] = fmaf(w, v[k].x, num[2]); num[3] = fmaf(w, v[k].y, num[3]);
+            den = fmaf(w, ml[k].y, den);
+          }
+        write4<T>(a, pc, pc.cg * COLS + x, d, num, M, den, d == 0);
+      }
+      if (t == 0) a.arrived[c1] = 0;
+      continue;
+    }
     // a column's maxima and sums are 2 cn numbers far apart: a warp a column, so that they are fetched together
     float* weight = reinterpret_cast<float*>(base);           // [cn][COLS], where the rings were
     __syncthreads();
@@ -1071,7 +1103,7 @@ template <class Body>
 cudaError_t run_attn(const PagesAttnArgs& a, cudaStream_t s) {
   const int cgs = (a.T * a.rep + Body::COLS - 1) / Body::COLS;
   constexpr int smem = Layout<Body>::total;
-  cudaError_t e = cudaFuncSetAttribute(attn_kernel<Body>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = allow_shared<attn_kernel<Body>>(smem);
   if (e != cudaSuccess) return e;
   const int sms = device_sm_count();
   if (sms <= 0) return cudaErrorUnknown;

@@ -406,7 +406,7 @@ cudaError_t run_move(const PagesMoveArgs& a, int tiles, cudaStream_t s) {
 
 cudaError_t launch_pages_reserve(const PagesReserveArgs& a, int* launches, cudaStream_t s) {
   const int words = (a.p.n_lists + 31) / 32;
-  cudaError_t e = cudaFuncSetAttribute(reserve_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxLists / 32 * 4);
+  cudaError_t e = allow_shared<reserve_plan_kernel>(kMaxLists / 32 * 4);
   if (e != cudaSuccess) return e;
   reserve_plan_kernel<<<a.slices, kScanThreads, words * sizeof(uint32_t), s>>>(a, words);
   e = cudaGetLastError();

@@ -258,7 +258,7 @@ cudaError_t launch_pages_write(const PagesWriteArgs& a, int* launches, cudaStrea
   const int64_t items = (int64_t)a.n * a.p.Hkv * blocks;
   const int64_t grid = (items + kRowThreads / 32 - 1) / (kRowThreads / 32);
   if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
-  cudaError_t e = cudaFuncSetAttribute(write_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (kMaxLists / 32) * 4);
+  cudaError_t e = allow_shared<write_plan_kernel>(2 * (kMaxLists / 32) * 4);
   if (e != cudaSuccess) return e;
   write_plan_kernel<<<1, kPlanThreads, 2 * words * sizeof(uint32_t), s>>>(a, words);
   e = cudaGetLastError();

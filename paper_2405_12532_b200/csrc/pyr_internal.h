@@ -3,6 +3,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "pages_index.h"
 #include "pyr.h"
 
@@ -154,6 +156,20 @@ cudaError_t launch_gemm_skinny(const void* x, const void* w, const void* res, vo
 cudaError_t launch_glue_rope(void* x, const int32_t* pos, int64_t tokens, int H, int D, int dtype, cudaStream_t s);
 cudaError_t launch_glue_swiglu(const void* g, const void* u, void* out, int64_t n, int dtype, cudaStream_t s);
 cudaError_t launch_glue_argmax(const void* x, int32_t* out, int64_t rows, int n, int dtype, cudaStream_t s);
+// Lets a kernel use `bytes` of dynamic shared memory; asked of the runtime once per device.
+template <auto kKernel>
+cudaError_t allow_shared(int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = -1;
+  const cudaError_t g = cudaGetDevice(&dev);
+  if (g != cudaSuccess) return g;
+  const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+  if (done.load() & bit) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit);
+  return e;
+}
+
 // Paged 4-bit cache (csrc/pages_*.cu).
 struct PagesWriteArgs {
   PagesView p;
