@@ -11,7 +11,7 @@ constexpr size_t kAlign = 256;
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 struct PagesLayout {
-  size_t status, control, arrived, lens, refs, table, plan, free_ids, slice_first, partial, pool, total;
+  size_t status, control, arrived, refused, lens, refs, table, plan, free_ids, slice_first, partial, pool, total;
   int slices;
 };
 
@@ -38,6 +38,7 @@ void plan(const pyr_pages_config_t* c, PagesLayout* l) {
   l->status = take(pyr::kStatusWords * 4);
   l->control = take(64 * 4);
   l->arrived = take((size_t)pyr::kAttnMaxCtas * 4);
+  l->refused = take((size_t)c->n_lists * 4);
   l->lens = take((size_t)c->n_lists * 4);
   l->refs = take((size_t)c->n_pages * 4);
   l->table = take((size_t)c->n_lists * c->max_pages * 4);
@@ -161,7 +162,7 @@ pyr_status_t pyr_pages_reset(pyr_pages_t* h, void* stream) {
     return PYR_ERR_CUDA;
   if (major != 10) return PYR_ERR_UNSUPPORTED;
   const PagesLayout& l = h->lay;
-  // status, control words, arrival counters, lengths and reference counts lie one behind the other
+  // status, control words, arrival counters, refusals, lengths and reference counts lie one behind the other
   if (cudaMemsetAsync(h->base + l.status, 0, l.table - l.status, s) != cudaSuccess) return PYR_ERR_CUDA;
   if (cudaMemsetAsync(h->base + l.table, 0xff, l.plan - l.table, s) != cudaSuccess) return PYR_ERR_CUDA;
   h->ready = true;
@@ -304,7 +305,7 @@ pyr_status_t pyr_pages_compact(pyr_pages_t* h, const int32_t* src, const int32_t
   a.p = view(h);
   a.src = src; a.dst = dst; a.n = n; a.idx = idx; a.idx_groups = idx ? idx_groups : 1; a.idx_stride = idx_stride;
   a.counts = counts; a.n_rows = n_rows;
-  a.plan = at<int32_t>(h, h->lay.plan);
+  a.refused = at<int32_t>(h, h->lay.refused);
   PYR_PAGES(pyr::launch_pages_compact(a, &launches, static_cast<cudaStream_t>(stream)));
 }
 

@@ -43,12 +43,43 @@ __device__ __forceinline__ long long block_scan(long long x, long long* warp_sum
 // Every CTA lists the free pages of its slice of the pool; the CTA that finishes last knows how many lie before each slice
 // and plans the entries: how many pages each needs and the rank of its first one among the free pages. (One pass over the
 // reference counts by the whole machine; one CTA reading them alone would take over ten times as long for a large pool.)
+struct Need { int err, old, slot, fresh; };        // fresh pages from slot `slot` on, and one more to copy page `old` to
+
+__device__ __forceinline__ Need entry_need(const PagesReserveArgs& a, int i) {
+  Need d{0, -1, 0, 0};
+  const int l = pages_list(a.p, a.lists, i);
+  const int add = a.rows ? a.rows[i] : a.rows_each;
+  if (l < 0 || add < 0) {
+    d.err = PYR_ERR_INVALID;
+  } else if (add > 0) {
+    const int len = pages_len(a.p, l);
+    const int64_t rows = (int64_t)len + add;
+    if (rows > (int64_t)a.p.max_pages * a.p.page_rows) {
+      d.err = PYR_ERR_CAPACITY;
+    } else {
+      const int s1 = (int)((rows + a.p.page_rows - 1) / a.p.page_rows);
+      if (len % a.p.page_rows) {               // the part-filled last page: a copy if others hold it too
+        const int page = pages_page(a.p, l, len / a.p.page_rows);
+        if (page < 0) d.err = PYR_ERR_INVALID;
+        else if (a.p.refs[page] > 1) d.old = page;
+      }
+      d.slot = (len + a.p.page_rows - 1) / a.p.page_rows;
+      while (d.slot < s1 && a.p.table[(size_t)l * a.p.max_pages + d.slot] >= 0) ++d.slot;   // reserved before
+      d.fresh = s1 - d.slot;
+    }
+  }
+  return d;
+}
+
 __global__ void __launch_bounds__(kScanThreads) reserve_plan_kernel(PagesReserveArgs a, int words) {
   extern __shared__ uint32_t seen[];     // a bit per list
   __shared__ long long sums[33];
   __shared__ int is_last, errors;
   const int t = threadIdx.x;
   long long total;
+  let_next_start();
+  // (looked up here, beside the pages, by every CTA: the one that plans then has it at hand)
+  const Need first = t < a.n ? entry_need(a, t) : Need{0, -1, 0, 0};
   {
     const int64_t p0 = (int64_t)blockIdx.x * kReserveSlice + t * 4;
     uint32_t free4 = 0;
@@ -62,20 +93,22 @@ __global__ void __launch_bounds__(kScanThreads) reserve_plan_kernel(PagesReserve
       if (free4 >> i & 1u) ids[at++] = (int32_t)(p0 + i);
     if (t == 0) a.slice_first[blockIdx.x + 1] = (int32_t)total;
   }
-  __threadfence();
-  __syncthreads();
-  if (t == 0) is_last = atomicAdd(&a.control[0], 1) == a.slices - 1;
-  __syncthreads();
-  if (!is_last) return;
-  __threadfence();
-
-  long long free_pages = 0;
-  for (int s0 = 0; s0 < a.slices; s0 += kScanThreads) {
-    const int s = s0 + t;
-    const long long c = s < a.slices ? __ldcg(a.slice_first + s + 1) : 0;
-    const long long before = free_pages + block_scan(c, sums, &total);
-    if (s < a.slices) a.slice_first[s + 1] = (int32_t)(before + c);
-    free_pages += total;
+  long long free_pages = total;
+  if (a.slices > 1) {
+    __threadfence();
+    __syncthreads();
+    if (t == 0) is_last = atomicAdd(&a.control[0], 1) == a.slices - 1;
+    __syncthreads();
+    if (!is_last) return;
+    __threadfence();
+    free_pages = 0;
+    for (int s0 = 0; s0 < a.slices; s0 += kScanThreads) {
+      const int s = s0 + t;
+      const long long c = s < a.slices ? __ldcg(a.slice_first + s + 1) : 0;
+      const long long before = free_pages + block_scan(c, sums, &total);
+      if (s < a.slices) a.slice_first[s + 1] = (int32_t)(before + c);
+      free_pages += total;
+    }
   }
   for (int i = t; i < words; i += kScanThreads) seen[i] = 0;
   if (t == 0) { a.slice_first[0] = 0; a.control[0] = 0; errors = 0; }
@@ -84,40 +117,17 @@ __global__ void __launch_bounds__(kScanThreads) reserve_plan_kernel(PagesReserve
   long long taken = 0;
   for (int i0 = 0; i0 < a.n; i0 += kScanThreads) {
     const int i = i0 + t;
-    long long need = 0;
-    int err = 0, old = -1, slot = 0, fresh = 0;
+    Need d = i0 == 0 ? first : (i < a.n ? entry_need(a, i) : Need{0, -1, 0, 0});
     if (i < a.n) {
       const int l = pages_list(a.p, a.lists, i);
-      const int add = a.rows ? a.rows[i] : a.rows_each;
-      if (l < 0 || add < 0 || (atomicOr(&seen[l >> 5], 1u << (l & 31)) >> (l & 31) & 1u)) {
-        err = PYR_ERR_INVALID;
-      } else if (add > 0) {
-        const int len = pages_len(a.p, l);
-        const int64_t rows = (int64_t)len + add;
-        if (rows > (int64_t)a.p.max_pages * a.p.page_rows) {
-          err = PYR_ERR_CAPACITY;
-        } else {
-          const int s1 = (int)((rows + a.p.page_rows - 1) / a.p.page_rows);
-          if (len % a.p.page_rows) {               // the part-filled last page: a copy if others hold it too
-            const int page = pages_page(a.p, l, len / a.p.page_rows);
-            if (page < 0) err = PYR_ERR_INVALID;
-            else if (a.p.refs[page] > 1) old = page;
-          }
-          slot = (len + a.p.page_rows - 1) / a.p.page_rows;
-          while (slot < s1 && a.p.table[(size_t)l * a.p.max_pages + slot] >= 0) ++slot;   // reserved before
-          fresh = s1 - slot;
-          need = fresh + (old >= 0 ? 1 : 0);
-        }
-      }
+      if (l >= 0 && (atomicOr(&seen[l >> 5], 1u << (l & 31)) >> (l & 31) & 1u)) d.err = PYR_ERR_INVALID;
     }
-    if (err) atomicCAS(&errors, 0, err);
+    if (d.err) atomicCAS(&errors, 0, d.err);
+    const long long need = d.err ? 0 : d.fresh + (d.old >= 0 ? 1 : 0);
     const long long base = taken + block_scan(need, sums, &total);
     taken += total;
-    if (i < a.n) {
-      int32_t* pl = a.plan + (int64_t)i * 4;
-      pl[0] = (int32_t)(base < 0x7fffffff ? base : 0x7fffffff);
-      pl[1] = old; pl[2] = slot; pl[3] = fresh;
-    }
+    if (i < a.n)
+      reinterpret_cast<int4*>(a.plan)[i] = make_int4((int)(base < 0x7fffffff ? base : 0x7fffffff), d.old, d.slot, d.fresh);
   }
   __syncthreads();
   if (t == 0) {
@@ -139,34 +149,43 @@ __device__ __forceinline__ int free_page(const PagesReserveArgs& a, int rank) {
   return a.free_ids[(int64_t)lo * kReserveSlice + (rank - a.slice_first[lo])];
 }
 
-// Copies the first `rows` rows of one head of a page to another page: whole tiles as they lie, of a part-filled tile the
-// rows' codes and words.
-__device__ __forceinline__ void copy_head_rows(const PagesView& p, int from, int to, int h, int rows) {
-  const int G = p.D / p.group, half = kPageTile * p.D / 2;
-  const uint8_t* s = p.pool + pages_tile(p, from, h, 0);
-  uint8_t* d = p.pool + pages_tile(p, to, h, 0);
-  const int whole = rows / kPageTile * p.tile_bytes;
-  for (int o = threadIdx.x * 16; o < whole; o += blockDim.x * 16)
-    *reinterpret_cast<uint4*>(d + o) = *reinterpret_cast<const uint4*>(s + o);
-  const int left = rows % kPageTile;
-  s += whole; d += whole;
+// Copies the first `rows` rows of the heads [h0, h1) of a page to another page, 16 bytes a thread at a time whatever the head:
+// whole tiles as they lie, of a part-filled tile the rows' codes and (4 bytes at a time) words.
+__device__ __forceinline__ void copy_rows_of_page(const PagesView& p, int from, int to, int h0, int h1, int rows) {
+  const int G = p.D / p.group, half = kPageTile * p.D / 2, heads = h1 - h0;
+  const size_t head_bytes = (size_t)p.tiles_per_page * p.tile_bytes;
+  const uint8_t* s = p.pool + pages_tile(p, from, h0, 0);
+  uint8_t* d = p.pool + pages_tile(p, to, h0, 0);
+  const int whole = rows / kPageTile * p.tile_bytes, left = rows % kPageTile;
   const int codes = left * p.D / 2, words = left * G * 4;
-  for (int o = threadIdx.x * 16; o < 2 * codes; o += blockDim.x * 16) {
-    const int at = o < codes ? o : half + o - codes;
+  const int per16 = whole / 16 + 2 * codes / 16, per4 = 2 * words / 4;
+  auto place = [&](int x) {                      // of the x-th 16-byte piece of a head
+    const int o = x * 16;
+    if (o < whole) return o;
+    const int c = o - whole;
+    return whole + (c < codes ? c : half + c - codes);
+  };
+#pragma unroll 4
+  for (int x = threadIdx.x; x < heads * per16; x += kThreads) {
+    const int h = x / per16;
+    const size_t at = h * head_bytes + place(x - h * per16);
     *reinterpret_cast<uint4*>(d + at) = *reinterpret_cast<const uint4*>(s + at);
   }
-  for (int o = threadIdx.x * 4; o < 2 * words; o += blockDim.x * 4) {
-    const int at = 2 * half + (o < words ? o : kPageTile * G * 4 + o - words);
+#pragma unroll 2
+  for (int x = threadIdx.x; x < heads * per4; x += kThreads) {
+    const int h = x / per4, o = (x - h * per4) * 4;
+    const size_t at = h * head_bytes + whole + 2 * half + (o < words ? o : kPageTile * G * 4 + o - words);
     *reinterpret_cast<uint32_t*>(d + at) = *reinterpret_cast<const uint32_t*>(s + at);
   }
 }
 
 // grid (entries, parts): part 0 writes the entry's table and counts, every part copies its share of the heads.
 __global__ void __launch_bounds__(kThreads) reserve_take_kernel(PagesReserveArgs a) {
-  if (a.control[1] == 0) return;
+  wait_for_previous();
   const int i = blockIdx.x;
-  const int32_t* pl = a.plan + (int64_t)i * 4;
-  const int base = pl[0], old = pl[1], slot = pl[2], fresh = pl[3];
+  const int4 pl = reinterpret_cast<const int4*>(a.plan)[i];
+  if (a.control[1] == 0) return;
+  const int base = pl.x, old = pl.y, slot = pl.z, fresh = pl.w;
   if (old < 0 && (fresh == 0 || blockIdx.y != 0)) return;
   const int l = pages_list(a.p, a.lists, i);
   const int copies = old >= 0 ? 1 : 0;
@@ -181,7 +200,8 @@ __global__ void __launch_bounds__(kThreads) reserve_take_kernel(PagesReserveArgs
   if (copies) {
     const int to = free_page(a, base);
     const int len = pages_len(a.p, l);
-    for (int h = blockIdx.y; h < a.p.Hkv; h += gridDim.y) copy_head_rows(a.p, old, to, h, len % a.p.page_rows);
+    const int share = (a.p.Hkv + gridDim.y - 1) / gridDim.y, h0 = blockIdx.y * share, h1 = min(h0 + share, a.p.Hkv);
+    if (h0 < h1) copy_rows_of_page(a.p, old, to, h0, h1, len % a.p.page_rows);
     if (blockIdx.y == 0 && threadIdx.x == 0) {
       a.p.table[(size_t)l * a.p.max_pages + len / a.p.page_rows] = to;
       a.p.refs[to] = 1;
@@ -197,7 +217,8 @@ __global__ void __launch_bounds__(kThreads) fork_kernel(PagesView p, const int32
   const int e = blockIdx.x;
   const int s = pages_list(p, src, e), d = pages_list(p, dst, e);
   bool bad = s < 0 || d < 0;
-  for (int x = threadIdx.x; x < n; x += kThreads) bad = bad || (x != e && dst[x] == d) || src[x] == d;
+#pragma unroll 4
+  for (int x = threadIdx.x; x < n; x += kThreads) bad |= (x != e && dst[x] == d) | (src[x] == d);
   int pages = 0, len = 0;
   if (s >= 0 && d >= 0) {
     len = pages_len(p, s);
@@ -246,48 +267,64 @@ __global__ void __launch_bounds__(kThreads) trim_kernel(PagesView p, const int32
 }
 
 // ------------------------------------------------------------------ compact
-// Checks an entry as a whole: plan[e] = rows to move, -1 if it is refused.
-__global__ void __launch_bounds__(kThreads) compact_plan_kernel(PagesMoveArgs a) {
+__device__ __forceinline__ int entry_count(const PagesMoveArgs& a, int e) { return a.counts ? a.counts[e] : a.n_rows; }
+
+// Checks every entry before a row moves; grid (entries, index lists of an entry). Whatever is wrong sets refused[e].
+__global__ void __launch_bounds__(kThreads) compact_check_kernel(PagesMoveArgs a) {
   const int e = blockIdx.x, t = threadIdx.x;
   const PagesView& p = a.p;
+  let_next_start();
   const int s = pages_list(p, a.src, e), d = pages_list(p, a.dst, e);
-  const int cnt = a.counts ? a.counts[e] : a.n_rows;
-  bool bad = s < 0 || d < 0 || cnt < 0 || cnt > a.n_rows;
+  const int cnt = entry_count(a, e);
+  bool bad = s < 0 || d < 0 || cnt < 0 || cnt > a.n_rows || (int64_t)cnt > (int64_t)p.max_pages * p.page_rows;
   if (!bad) {
     const bool in_place = s == d;
     const int len = pages_len(p, s);
-    for (int x = t; x < a.n; x += kThreads) bad = bad || (x != e && (a.dst[x] == d || a.src[x] == d));
-    bad = bad || (int64_t)cnt > (int64_t)p.max_pages * p.page_rows || (!a.idx && cnt > len);
-    const int pages = (cnt + p.page_rows - 1) / p.page_rows;
-    const int from = (len + p.page_rows - 1) / p.page_rows;
-    if (!bad)
-      for (int x = t; x < pages; x += kThreads) {
-        const int id = pages_page(p, d, x);
-        bad = bad || id < 0 || (!in_place && p.refs[id] != 1);
-      }
-    for (int x = t; x < from; x += kThreads) bad = bad || pages_page(p, s, x) < 0;
-    if (!bad && a.idx) {
-      const int32_t* idx = a.idx + (int64_t)e * a.idx_stride;
-      for (int g = 0; g < a.idx_groups; ++g)
-        for (int x = t; x < cnt; x += kThreads) {
-          const int32_t* row = idx + (int64_t)g * a.n_rows;
-          const int v = row[x];
-          bad = bad || v < 0 || v >= len;
-          if (in_place) {
-            bad = bad || (x > 0 && row[x - 1] >= v);
-            if (v != x) {
-              const int id = pages_page(p, d, x / p.page_rows);
-              bad = bad || id < 0 || p.refs[id] != 1;
-            }
+    if (a.idx) {
+      const int32_t* row = a.idx + (int64_t)e * a.idx_stride + (int64_t)blockIdx.y * a.n_rows;
+#pragma unroll 4
+      for (int x = t; x < cnt; x += kThreads) {
+        const int v = row[x];
+        bad |= v < 0 || v >= len;
+        if (in_place) {
+          bad |= x > 0 && row[x - 1] >= v;
+          if (v != x) {
+            const int id = pages_page(p, d, x / p.page_rows);
+            bad |= id < 0 || p.refs[id] != 1;
           }
         }
+      }
+    } else {
+      bad = cnt > len;
+    }
+    if (blockIdx.y == 0) {
+#pragma unroll 4
+      for (int x = t; x < a.n; x += kThreads) bad |= x != e && (a.dst[x] == d || a.src[x] == d);
+      const int pages = (cnt + p.page_rows - 1) / p.page_rows, from = (len + p.page_rows - 1) / p.page_rows;
+      for (int x = t; x < pages; x += kThreads) {
+        const int id = pages_page(p, d, x);
+        bad |= id < 0 || (!in_place && p.refs[id] != 1);
+      }
+      for (int x = t; x < from; x += kThreads) bad |= pages_page(p, s, x) < 0;
     }
   }
-  bad = __syncthreads_or(bad);
-  if (t == 0) {
-    a.plan[e] = bad ? -1 : cnt;
-    if (bad) record(p.status, PYR_ERR_INVALID);
+  if (__syncthreads_or(bad) && t == 0) {
+    a.refused[e] = 1;
+    record(p.status, PYR_ERR_INVALID);
   }
+}
+
+// Where a list's row lies: its tile (0: nowhere) and its row there.
+struct RowPlace { unsigned long long tile; int row; };
+__device__ __forceinline__ RowPlace row_place(const PagesView& p, int l, int h, int row) {
+  RowPlace r{0, 0};
+  if (row < 0) return r;
+  const int slot = row / p.page_rows, in = row - slot * p.page_rows;
+  const int page = pages_page(p, l, slot);
+  if (page < 0) return r;
+  r.tile = reinterpret_cast<unsigned long long>(p.pool + pages_tile(p, page, h, in / kPageTile));
+  r.row = in % kPageTile;
+  return r;
 }
 
 // The bytes that one warp moves for a tile of destination rows, held in registers between the reads and the writes.
@@ -299,20 +336,13 @@ struct TileRows {
   uint4 k[CP], v[CP];
   uint32_t kw[WP], vw[WP];
 
-  __device__ __forceinline__ void load(const PagesView& p, int l, int h, int src, int lane) {
-    // lane r (< 16) knows source row r of the tile (-1: none)
-    const uint8_t* base = nullptr;
-    int r = 0;
-    if (src >= 0) {
-      const int page = pages_page(p, l, src / p.page_rows);
-      if (page >= 0) { base = p.pool + pages_tile(p, page, h, src % p.page_rows / kPageTile); r = src % kPageTile; }
-    }
-    const unsigned long long addr = reinterpret_cast<unsigned long long>(base);
+  // lanes first .. first + 15 know the source rows of the tile
+  __device__ __forceinline__ void load(const RowPlace& from, int first, int lane) {
 #pragma unroll
     for (int i = 0; i < CP; ++i) {
       const int piece = i * 32 + lane, row = piece / C, c = piece % C;
-      const uint8_t* b = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, addr, row));
-      const int rr = __shfl_sync(0xffffffffu, r, row);
+      const uint8_t* b = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, from.tile, first + row));
+      const int rr = __shfl_sync(0xffffffffu, from.row, first + row);
       if (b) {
         k[i] = *reinterpret_cast<const uint4*>(b + tile_k_row(D, rr) + 16 * c);
         v[i] = *reinterpret_cast<const uint4*>(b + tile_v_row(D, rr) + 16 * c);
@@ -321,8 +351,8 @@ struct TileRows {
 #pragma unroll
     for (int i = 0; i < WP; ++i) {
       const int piece = i * 32 + lane, row = piece / G < kPageTile ? piece / G : 0, g = piece % G;
-      const uint8_t* b = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, addr, row));
-      const int rr = __shfl_sync(0xffffffffu, r, row);
+      const uint8_t* b = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, from.tile, first + row));
+      const int rr = __shfl_sync(0xffffffffu, from.row, first + row);
       if (b && piece < kPageTile * G) {
         kw[i] = *reinterpret_cast<const uint32_t*>(b + tile_k_word(D, G, rr, g));
         vw[i] = *reinterpret_cast<const uint32_t*>(b + tile_v_word(D, G, rr, g));
@@ -349,57 +379,122 @@ struct TileRows {
   }
 };
 
-// One warp per (entry, KV head, destination tile); where source and destination are one list, the first tile's warp takes
-// all of the head's tiles in order. In place, idx ascends strictly, so row x comes from a row >= x: a tile's sources, and
-// those of the tiles behind it, lie at or above its first row, and once a tile has been read nothing that is still to be
-// read lies in it.
+// Into another list: one warp per (entry, KV head, run of kRun destination tiles), the next tile's rows on their way while one
+// is stored. (An entry whose list is its own destination is left to the first run's warp, tile by tile, see below.)
+constexpr int kRun = 4;
+
 template <int D, int G>
-__global__ void __launch_bounds__(kThreads) compact_move_kernel(PagesMoveArgs a, int tiles, int64_t items) {
+__global__ void __launch_bounds__(kThreads) compact_move_kernel(PagesMoveArgs a, int runs, int64_t items) {
+  wait_for_previous();
+  let_next_start();
   const int lane = threadIdx.x & 31;
   const int64_t item = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   if (item >= items) return;
-  int tile = (int)(item % tiles);
-  const int h = (int)(item / tiles % a.p.Hkv);
-  const int e = (int)(item / tiles / a.p.Hkv);
-  const int cnt = a.plan[e];
-  if (cnt <= 0) return;
+  const int run = (int)(item % runs);
+  const int h = (int)(item / runs % a.p.Hkv);
+  const int e = (int)(item / runs / a.p.Hkv);
+  const int cnt = entry_count(a, e), x0 = run * kRun * kPageTile;
+  if (x0 >= cnt || a.refused[e]) return;
   const int s = pages_list(a.p, a.src, e), d = pages_list(a.p, a.dst, e);
-  const bool in_place = s == d;
-  if (in_place && tile > 0) return;
   const int32_t* idx = a.idx ? a.idx + (int64_t)e * a.idx_stride + (int64_t)(a.idx_groups == 1 ? 0 : h) * a.n_rows : nullptr;
-  if (in_place && !idx) return;
-  const int end = in_place ? (cnt + kPageTile - 1) / kPageTile : min(tile + 1, (cnt + kPageTile - 1) / kPageTile);
-  for (; tile < end; ++tile) {
-    const int x = tile * kPageTile + lane;
-    const int src = lane < kPageTile && x < cnt ? (idx ? idx[x] : x) : -1;
-    const int rows = min(cnt - tile * kPageTile, kPageTile);
-    if (in_place && __all_sync(0xffffffffu, src < 0 || src == x)) continue;      // nothing moves (and the page may be shared)
-    TileRows<D, G> t;
-    t.load(a.p, s, h, src, lane);
-    __syncwarp();
-    const int row0 = tile * kPageTile;
-    const int page = pages_page(a.p, d, row0 / a.p.page_rows);
-    if (page >= 0) t.store(a.p.pool + pages_tile(a.p, page, h, row0 % a.p.page_rows / kPageTile), rows, lane);
-    __syncwarp();
+  if (s == d) {
+    if (run != 0 || !idx) return;                // (a copy of a list to itself is done)
+    for (int row0 = 0; row0 < cnt; row0 += kPageTile) {
+      const int x = row0 + lane, src = lane < kPageTile && x < cnt ? idx[x] : -1;
+      if (!__any_sync(0xffffffffu, src >= 0 && src != x)) continue;
+      TileRows<D, G> rows;
+      rows.load(row_place(a.p, s, h, src), 0, lane);
+      __syncwarp();
+      const int page = pages_page(a.p, d, row0 / a.p.page_rows);
+      if (page >= 0) rows.store(a.p.pool + pages_tile(a.p, page, h, row0 % a.p.page_rows / kPageTile), min(cnt - row0, kPageTile), lane);
+      __syncwarp();
+    }
+    return;
+  }
+  // source rows of the run (lane l: rows l and l + 32 of it) and the pages that its tiles go to (lane t: tile t), looked up
+  // together: what follows needs no address that is still to be fetched
+  static_assert(kRun * kPageTile == 64, "two rows a lane");
+  RowPlace from[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int x = x0 + 32 * k + lane;
+    from[k] = row_place(a.p, s, h, x < cnt ? (idx ? idx[x] : x) : -1);
+  }
+  const int to_row = x0 + (lane & (kRun - 1)) * kPageTile;
+  const int to_page = to_row < cnt ? pages_page(a.p, d, to_row / a.p.page_rows) : -1;
+  const unsigned long long to = to_page < 0 ? 0 : reinterpret_cast<unsigned long long>(
+      a.p.pool + pages_tile(a.p, to_page, h, to_row % a.p.page_rows / kPageTile));
+  TileRows<D, G> rows[2];
+  rows[0].load(from[0], 0, lane);
+#pragma unroll
+  for (int t = 0; t < kRun; ++t) {
+    if (t + 1 < kRun && x0 + (t + 1) * kPageTile < cnt) rows[(t + 1) & 1].load(from[(t + 1) >> 1], ((t + 1) & 1) * kPageTile, lane);
+    uint8_t* tile = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, to, t));
+    const int n = cnt - x0 - t * kPageTile;
+    if (n > 0 && tile) rows[t & 1].store(tile, min(n, kPageTile), lane);
+  }
+}
+
+// In place: one CTA per (entry, KV head), a tile a warp, front to back. idx ascends strictly, so row x comes from a row >= x:
+// once the rows of a step's tiles have been read, nothing that later steps read lies in those tiles, and one barrier a step
+// (between its reads and its writes) is enough.
+template <int D, int G>
+__global__ void __launch_bounds__(kThreads) compact_inplace_kernel(PagesMoveArgs a) {
+  wait_for_previous();
+  let_next_start();
+  constexpr int kStep = kThreads / 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int e = blockIdx.x / a.p.Hkv, h = blockIdx.x % a.p.Hkv;
+  const int cnt = entry_count(a, e);
+  if (cnt <= 0 || a.refused[e]) return;
+  const int l = pages_list(a.p, a.dst, e);
+  const int32_t* idx = a.idx + (int64_t)e * a.idx_stride + (int64_t)(a.idx_groups == 1 ? 0 : h) * a.n_rows;
+  const int tiles = (cnt + kPageTile - 1) / kPageTile;
+  TileRows<D, G> rows;
+  for (int t0 = 0; t0 < tiles; t0 += kStep) {
+    const int row0 = (t0 + warp) * kPageTile, x = row0 + lane;
+    const int src = lane < kPageTile && x < cnt ? idx[x] : -1;
+    // (a tile of which no row moves is not written: its page may be shared)
+    const bool moves = __any_sync(0xffffffffu, src >= 0 && src != x);
+    const int page = moves ? pages_page(a.p, l, row0 / a.p.page_rows) : -1;
+    if (moves) rows.load(row_place(a.p, l, h, src), 0, lane);
+    __syncthreads();
+    if (page >= 0)
+      rows.store(a.p.pool + pages_tile(a.p, page, h, row0 % a.p.page_rows / kPageTile), min(cnt - row0, kPageTile), lane);
   }
 }
 
 __global__ void __launch_bounds__(kThreads) compact_finish_kernel(PagesMoveArgs a) {
+  wait_for_previous();
   const int e = blockIdx.x;
-  const int cnt = a.plan[e];
-  if (cnt < 0) return;
+  if (a.refused[e]) {
+    __syncthreads();
+    if (threadIdx.x == 0) a.refused[e] = 0;        // as the next call expects it
+    return;
+  }
+  const int cnt = entry_count(a, e);
   const int s = pages_list(a.p, a.src, e), d = pages_list(a.p, a.dst, e);
   if (threadIdx.x == 0) a.p.lens[d] = cnt;
   if (s == d) drop_pages(a.p, d, (cnt + a.p.page_rows - 1) / a.p.page_rows);
 }
 
 template <int D, int G>
-cudaError_t run_move(const PagesMoveArgs& a, int tiles, cudaStream_t s) {
-  const int64_t items = (int64_t)a.n * a.p.Hkv * tiles;
-  const int64_t grid = (items + kThreads / 32 - 1) / (kThreads / 32);
-  if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
-  compact_move_kernel<D, G><<<(unsigned)grid, kThreads, 0, s>>>(a, tiles, items);
-  return cudaGetLastError();
+cudaError_t run_move(const PagesMoveArgs& a, int* launches, cudaStream_t s) {
+  cudaError_t e;
+  if (a.src == a.dst) {                          // one array for both: every entry is compacted in place
+    if (!a.idx) return cudaSuccess;
+    const int64_t heads = (int64_t)a.n * a.p.Hkv;
+    if (heads > 0x7fffffffLL) return cudaErrorInvalidValue;
+    e = launch_behind(compact_inplace_kernel<D, G>, dim3((unsigned)heads), dim3(kThreads), 0, s, a);
+  } else {
+    const int runs = (a.n_rows + kRun * kPageTile - 1) / (kRun * kPageTile);
+    const int64_t items = (int64_t)a.n * a.p.Hkv * runs;
+    const int64_t grid = (items + kThreads / 32 - 1) / (kThreads / 32);
+    if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
+    e = launch_behind(compact_move_kernel<D, G>, dim3((unsigned)grid), dim3(kThreads), 0, s, a, runs, items);
+  }
+  if (e == cudaSuccess) ++*launches;
+  return e;
 }
 
 }  // namespace
@@ -415,8 +510,7 @@ cudaError_t launch_pages_reserve(const PagesReserveArgs& a, int* launches, cudaS
   // enough CTAs to share out the heads when there are few lists to copy for
   int parts = 1;
   while (parts < 16 && parts < a.p.Hkv && (int64_t)a.n * parts < 256) parts *= 2;
-  reserve_take_kernel<<<dim3(a.n, parts), kThreads, 0, s>>>(a);
-  e = cudaGetLastError();
+  e = launch_behind(reserve_take_kernel, dim3(a.n, parts), dim3(kThreads), 0, s, a);
   if (e == cudaSuccess) ++*launches;
   return e;
 }
@@ -437,21 +531,17 @@ cudaError_t launch_pages_trim(const PagesView& p, const int32_t* lists, int n, c
 }
 
 cudaError_t launch_pages_compact(const PagesMoveArgs& a, int* launches, cudaStream_t s) {
-  compact_plan_kernel<<<a.n, kThreads, 0, s>>>(a);
+  compact_check_kernel<<<dim3(a.n, a.idx ? a.idx_groups : 1), kThreads, 0, s>>>(a);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   ++*launches;
-  // a call whose two list arrays are one array compacts every entry in place: a warp per head is all it can use
-  const int tiles = a.src == a.dst ? 1 : (a.n_rows + kPageTile - 1) / kPageTile;
   if (a.n_rows > 0) {
     const int G = a.p.D / a.p.group;
-    if (a.p.D == 128) e = G == 4 ? run_move<128, 4>(a, tiles, s) : G == 2 ? run_move<128, 2>(a, tiles, s) : run_move<128, 1>(a, tiles, s);
-    else e = G == 2 ? run_move<64, 2>(a, tiles, s) : run_move<64, 1>(a, tiles, s);
+    if (a.p.D == 128) e = G == 4 ? run_move<128, 4>(a, launches, s) : G == 2 ? run_move<128, 2>(a, launches, s) : run_move<128, 1>(a, launches, s);
+    else e = G == 2 ? run_move<64, 2>(a, launches, s) : run_move<64, 1>(a, launches, s);
     if (e != cudaSuccess) return e;
-    ++*launches;
   }
-  compact_finish_kernel<<<a.n, kThreads, 0, s>>>(a);
-  e = cudaGetLastError();
+  e = launch_behind(compact_finish_kernel, dim3(a.n), dim3(kThreads), 0, s, a);
   if (e == cudaSuccess) ++*launches;
   return e;
 }

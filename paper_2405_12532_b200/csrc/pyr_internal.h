@@ -170,6 +170,23 @@ cudaError_t allow_shared(int bytes) {
   return e;
 }
 
+#ifdef __CUDACC__
+// Launches a kernel that may start while the one before it on the stream still runs: it must call wait_for_previous() before it
+// touches anything the other writes, and the other let_next_start() (early: only the launch overlaps then).
+template <class... P, class... A>
+cudaError_t launch_behind(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = s;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+#endif
+
 // Paged 4-bit cache (csrc/pages_*.cu).
 struct PagesWriteArgs {
   PagesView p;
@@ -187,7 +204,7 @@ struct PagesMoveArgs {
   const int32_t* src; const int32_t* dst; int n;
   const int32_t* idx; int idx_groups; int64_t idx_stride;
   const int32_t* counts; int n_rows;
-  int32_t* plan;                   // [n_lists]: rows to move, -1 if the entry is refused
+  int32_t* refused;                // [n_lists]: set where an entry is refused; zero between calls
 };
 struct PagesReserveArgs {
   PagesView p;
