@@ -28,8 +28,12 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kStageTiles = 2;           // a stage of a warp's ring: one copy of up to two tiles
 constexpr int kStageRows = kStageTiles * kPageTile;
-constexpr int kSegmentUnits = 2;         // what beginning and ending a (entry, head, column group) costs, in tiles
-constexpr int kMinUnits = 6;             // a warp's share is at least this much: merging costs more than that
+// What beginning and ending a (entry, head, column group) costs a warp, in tiles: its queries, a first step that sets the maximum
+// and the scales' factors, its sums (64 ragged lists of 32 heads: 102 us with 2, 96 with 3, 92 with 4, 90 with 6 and 8).
+constexpr int kSegmentUnits = 6;
+// A warp's share is at least this much: next to nothing, since small calls are bound by a warp's own latency, 2 us a step
+// (with 2 instead of 4 and 8: 385 rows of 32 heads 20.5, 22.5 and 24.6 us, the small fp32 model 21, 26 and 32 us).
+constexpr int kMinUnits = 2;
 constexpr int kMaxWarps = 12;
 
 __device__ __forceinline__ void record(int* status, int code) { atomicCAS(status, 0, code); }
@@ -52,7 +56,7 @@ struct Piece {
 struct Sched {
   long long sums[kMaxWarps + 1];
   long long first_unit[kMaxWarps];   // of the entry in which a warp's range starts
-  int entry[kMaxWarps];
+  int entry[kMaxWarps], list[kMaxWarps], len[kMaxWarps];
   int abort_flag;
   int last[2], open_c1[2], open_count[2], open_piece[2];   // what the CTA leaves for others
   float den[kAttnCols];
@@ -83,9 +87,10 @@ __device__ __forceinline__ long long block_scan(long long x, long long* warp_sum
 
 // Units of entry i: 0 if its list id is out of range (the entry is refused). A (head, column group) has kSegmentUnits units
 // that stand for no tile before those that do: short lists cost more than their tiles, and a warp's share must say so.
-__device__ __forceinline__ long long entry_units(const PagesAttnArgs& a, int i, int cgs) {
-  const int l = pages_list(a.p, a.lists, i);
-  return l < 0 ? 0 : (long long)(attn_tiles(pages_len(a.p, l)) + kSegmentUnits) * a.p.Hkv * cgs;
+__device__ __forceinline__ long long entry_units(const PagesAttnArgs& a, int i, int cgs, int* list, int* len) {
+  *list = pages_list(a.p, a.lists, i);
+  *len = *list < 0 ? 0 : pages_len(a.p, *list);
+  return *list < 0 ? 0 : (long long)(attn_tiles(*len) + kSegmentUnits) * a.p.Hkv * cgs;
 }
 
 // The (entry, head, column group) that a warp works on, and the tiles [t, t1) of it that are the warp's.
@@ -105,9 +110,10 @@ struct Place {
     t1 = max(0, r + n - kSegmentUnits);
     *left -= n;
   }
-  __device__ __forceinline__ void start(const PagesAttnArgs& a, int cgs, int e, long long o, int* left) {   // unit o of entry e
-    entry = e;
-    open(a);
+  // unit o of entry e, whose list and length are at hand
+  __device__ __forceinline__ void start(const PagesAttnArgs& a, int cgs, int e, int l, int n, long long o, int* left) {
+    entry = e; list = l; len = n;
+    tiles = (int)attn_tiles(len);
     const int per = tiles + kSegmentUnits;
     int r;
     if (o >> 31 == 0) {                          // (64-bit divisions take a tenth of a microsecond each)
@@ -810,9 +816,10 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
 
   // ---- this CTA's share: total units, units per warp, and the entries in which the warps' ranges start
   long long total = 0, part, u_mine = 0, lo_mine = 0;
+  int l_mine = 0, len_mine = 0;
   for (int i0 = 0; i0 < a.n; i0 += kThreads) {
     const int i = i0 + t;
-    u_mine = i < a.n ? entry_units(a, i, cgs) : 0;
+    u_mine = i < a.n ? entry_units(a, i, cgs, &l_mine, &len_mine) : 0;
     if (blockIdx.x == 0 && i < a.n && u_mine == 0) record(a.p.status, PYR_ERR_INVALID);
     lo_mine = block_scan<kWarps + 1>(u_mine, sh.sums, &part);
     total += part;
@@ -827,12 +834,12 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
     const int i = i0 + t;
     long long u = u_mine, lo = lo_mine;
     if (a.n > kThreads) {
-      u = i < a.n ? entry_units(a, i, cgs) : 0;
+      u = i < a.n ? entry_units(a, i, cgs, &l_mine, &len_mine) : 0;
       lo = run + block_scan<kWarps + 1>(u, sh.sums, &part);
     }
     for (int w = 0; w < kWarps; ++w) {
       const long long s = cta_u + w * q;
-      if (s >= lo && s < lo + u) { sh.entry[w] = i; sh.first_unit[w] = lo; }
+      if (s >= lo && s < lo + u) { sh.entry[w] = i; sh.first_unit[w] = lo; sh.list[w] = l_mine; sh.len[w] = len_mine; }
     }
     run += part;
   }
@@ -852,7 +859,7 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
     uint32_t parity = 1;                         // of the wait for an empty stage: the first ones are
     const int32_t* row = a.p.table;
     if (mine > 0) {
-      ld.start(a, cgs, sh.entry[w_of], u_warp - sh.first_unit[w_of], &left);
+      ld.start(a, cgs, sh.entry[w_of], sh.list[w_of], sh.len[w_of], u_warp - sh.first_unit[w_of], &left);
       slot = ld.t / tpp;
       skip = ld.t - slot * tpp;
       row = a.p.table + (size_t)ld.list * a.p.max_pages;
@@ -918,7 +925,7 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
     // ------------------------------------------------------------ consumers
     Place cu{};
     int stage = 0, left = mine;
-    cu.start(a, cgs, sh.entry[warp], u_warp - sh.first_unit[warp], &left);
+    cu.start(a, cgs, sh.entry[warp], sh.list[warp], sh.len[warp], u_warp - sh.first_unit[warp], &left);
     uint8_t* ring = base + warp * L::warp_bytes;
     float* qs = reinterpret_cast<float*>(ring + L::ring);
     const uint32_t full0 = smem_u32(&full[warp][0]), empty0 = smem_u32(&empty[warp][0]);
@@ -971,20 +978,20 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
 
   // ---- merge the CTA's partial states: runs of consecutive ones of the same (entry, head, column group), a warp a run
   __syncthreads();
-  for (int f = 0, r = 0; f < kWarps * 2;) {
-    if (!sh.piece[f >> 1][f & 1].valid) { ++f; continue; }
+  static_assert(kWarps * 2 <= 32, "a lane a piece");
+  const bool there = lane < kWarps * 2 && sh.piece[lane >> 1][lane & 1].valid;
+  uint32_t pieces = __ballot_sync(0xffffffffu, there);
+  const uint32_t ending = __ballot_sync(0xffffffffu, there && sh.piece[lane >> 1][lane & 1].ends);
+  for (int r = 0; pieces;) {
+    // the run: from the first piece left to the next one that ends
+    const int f = __ffs(pieces) - 1;
+    const uint32_t from = ending >> f << f, upto = from ? (from & -from) * 2 - 1 : 0xffffffffu;
+    const uint32_t members = (pieces & upto) >> f;                // bit k: piece f + k
+    const bool ends = from != 0;
+    pieces &= ~upto;
     const Piece& pc = sh.piece[f >> 1][f & 1];
-    int g = f + 1, last = f;
-    uint32_t members = 1;                        // bit k: piece f + k
-    for (; g < kWarps * 2; ++g) {
-      const Piece& o = sh.piece[g >> 1][g & 1];
-      if (!o.valid) continue;
-      if (o.u0 != pc.u0) break;
-      last = g;
-      members |= 1u << (g - f);
-    }
     // (32 times four dimensions at a time, dealt to the warps run by run)
-    const bool whole = pc.begins && sh.piece[last >> 1][last & 1].ends;
+    const bool whole = pc.begins && ends;
     const int place = pc.begins ? 1 : 0;
     const int ncols = min(COLS, cols_total - pc.cg * COLS);
     auto at = [&](int k) { return (const float*)state_of((f + k) >> 1, (f + k) & 1); };
@@ -1007,9 +1014,8 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
       sh.open_c1[place] = (int)(pc.u0 / cta_units);
       sh.open_count[place] = (int)((pc.u1 - 1) / cta_units) - (int)(pc.u0 / cta_units) + 1;
     }
-    f = g;
+    if (!whole) __threadfence();                 // (what another CTA will read)
   }
-  __threadfence();
   __syncthreads();
   if (sh.open_c1[0] < 0 && sh.open_c1[1] < 0) return;     // uniform over the CTA
   if (t < 2) {
