@@ -354,10 +354,15 @@ struct CoreBody {
 // operands in shared memory first.)
 // Row r of the matrices is row r ^ ((r >> 1) & 1) of the tile, which spreads the lanes' shared-memory reads over the banks.
 //
-// Operands are f16: its 10 bits of mantissa take a nibble in two places, so that a word's eight codes need one shift, and they
-// hold P to 2^-12. What f16 lacks is range, so both factors that are not codes are normalised by powers of two: a query row
-// by its largest element (what is then below f16's smallest step is below 2^-24 of that element), and the scales that
-// multiply P by a factor per group that follows them (`norm`).
+// Operands are f16. A code masked in place is an operand already: as the bits of an f16 number a nibble n in bits 0 .. 3 is the
+// subnormal n 2^-24, in bits 4 .. 7 it is n 2^-20, both exact, so that a word's eight codes take one shift and four masks
+// and nothing is added or converted. (The factors go into the queries for K, into the sums at the end for V.) What f16 lacks
+// is range, so both factors that are not codes are normalised by powers of two: a query row by its largest element (what is
+// then below f16's smallest step is below 2^-24 of that element), and the scales that multiply P, which f16 holds to 2^-12,
+// by a factor per group that follows them (`norm`).
+// V's codes have a mean of 7.5, so that o grows with the number of rows while what matters in it grows with its root. The
+// instruction truncates its sums, and an o far above what matters would let that show (relative 2^-25 a tile): every
+// kCentre steps what a group's o have in common is moved to the group's sum of zeros, which is kept apart and rounded.
 __device__ __forceinline__ void mma_full(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
                "{%0, %1, %2, %3};"
@@ -372,34 +377,13 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 __device__ __forceinline__ uint32_t as_u32(__half2 x) { return reinterpret_cast<uint32_t&>(x); }
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return reinterpret_cast<__half2&>(x); }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return as_u32(__floats2half2_rn(lo, hi)); }
-// (x & mask) | bits in one instruction
-template <uint32_t kMask>
-__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t bits) {
-  uint32_t y;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x), "n"(kMask), "r"(bits));
-  return y;
-}
-// The four pairs of codes (nibbles k and k + 4) of x as f16 pairs, less 8: 0x6400 | n is 1024 + n, 0x6400 | 16 n is
-// 1024 + 16 n.
-__device__ __forceinline__ void centred4(uint32_t x, uint32_t* y) {
-  const __half2 less = as_half2(0xE408E408u);                // -1032
-  const __half2 part = as_half2(0x2C002C00u), off = as_half2(0xD480D480u);   // 1/16, -72
+// The four pairs of codes (nibbles k and k + 4) of x as f16 pairs: times 2^-24 for k = 0 and 2, times 2^-20 for k = 1 and 3.
+__device__ __forceinline__ void codes4(uint32_t x, uint32_t* y) {
   const uint32_t z = x >> 8;
-  y[0] = as_u32(__hadd2(as_half2(and_or<0x000F000Fu>(x, 0x64006400u)), less));
-  y[1] = as_u32(__hfma2(as_half2(and_or<0x00F000F0u>(x, 0x64006400u)), part, off));
-  y[2] = as_u32(__hadd2(as_half2(and_or<0x000F000Fu>(z, 0x64006400u)), less));
-  y[3] = as_u32(__hfma2(as_half2(and_or<0x00F000F0u>(z, 0x64006400u)), part, off));
-}
-// The same for K, where the accumulator can start with what the codes have too much: nibbles 1 and 3 stay n + 64 (0x5400 | 16 n),
-// nibbles 0 and 2 become n - 8 (1024 + n would cost the accumulator bits).
-constexpr float kKeyOdd = 64.f, kKeyEven = -8.f;
-__device__ __forceinline__ void key4(uint32_t x, uint32_t* y) {
-  const __half2 less = as_half2(0xE408E408u);                // -1032
-  const uint32_t z = x >> 8;
-  y[0] = as_u32(__hadd2(as_half2(and_or<0x000F000Fu>(x, 0x64006400u)), less));
-  y[1] = and_or<0x00F000F0u>(x, 0x54005400u);
-  y[2] = as_u32(__hadd2(as_half2(and_or<0x000F000Fu>(z, 0x64006400u)), less));
-  y[3] = and_or<0x00F000F0u>(z, 0x54005400u);
+  y[0] = x & 0x000F000Fu;
+  y[1] = x & 0x00F000F0u;
+  y[2] = z & 0x000F000Fu;
+  y[3] = z & 0x00F000F0u;
 }
 // 2^-e for the exponent e of x > 0 (clamped to what both it and its inverse can be)
 __device__ __forceinline__ float inverse_power(float x) {
@@ -414,10 +398,11 @@ struct MmaBody {
   static constexpr int kDim = D, COLS = 8, kWarps = 11, kBlocks = 1, kQueryFloats = 0;
   static constexpr int kTileBytes = kPageTile * (D + 8 * G), kStages = kTileBytes > 2304 ? 2 : 3;
   static constexpr float kLazy = 8.f;            // the maximum is raised once a score is 2^8 above it
+  static constexpr int kCentre = 64;
   uint32_t qf[X][4];
-  float qsum[G][2], bias[G][2];                  // sums of the queries over a group; what the codes' offsets would add to a score
+  float qsum[G][2];                              // sums of the queries over a group
   float o[X][2][4], zacc[G][2], norm[G], m[2], ref[2], l[2], raise[2], sc2[2];
-  int limit[2], limit_min;
+  int limit[2], limit_min, steps;
 
   __device__ __forceinline__ void begin(const PagesAttnArgs& a, const Place& c, int cols_total, float*, int lane) {
     const int i = lane >> 2, j = lane & 3, col0 = c.cg * COLS;
@@ -443,28 +428,27 @@ struct MmaBody {
 #pragma unroll
       for (int w = 0; w < X; ++w)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) qf[w][k] = pack_f16(f[w][k] * down, f[w][k + 4] * down);
+        for (int k = 0; k < 4; ++k) {
+          const float by = k & 1 ? down : 16.f * down;           // for codes times 2^-20 and 2^-24
+          qf[w][k] = pack_f16(f[w][k] * by, f[w][k + 4] * by);
+        }
+      // scores come out times 2^-20
 #pragma unroll
-      for (int x = 0; x < 2; ++x) sc2[x] = a.scale * kLog2e / __shfl_sync(0xffffffffu, down, (2 * j + x) * 4);
+      for (int x = 0; x < 2; ++x) sc2[x] = a.scale * kLog2e * 0x1p20f / __shfl_sync(0xffffffffu, down, (2 * j + x) * 4);
     }
-    // sums of the queries over each group, by the instruction itself: every row of a matrix of ones (zeros for one half of
-    // the dimensions at a time: operands 0, 1 go with nibbles 0 and 2 of a code word, operands 2, 3 with nibbles 1 and 3)
+    // sums of the queries over each group, by the instruction itself (every row of a matrix of constants that undo the queries'
+    // factors: operands 0, 1 go with nibbles 0 and 2 of a code word, operands 2, 3 with nibbles 1 and 3)
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      const uint32_t ones = 0x3C003C00u, even[4] = {ones, ones, 0, 0}, odd[4] = {0, 0, ones, ones};
-      float s[4] = {0.f, 0.f, 0.f, 0.f}, z[4] = {0.f, 0.f, 0.f, 0.f};
+      const uint32_t undo[4] = {0x2C002C00u, 0x2C002C00u, 0x3C003C00u, 0x3C003C00u};       // 1/16, 1
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        mma_full(s, even, qf[g * U + u][0], qf[g * U + u][1]);
-        mma_full(s, even, qf[g * U + u][2], qf[g * U + u][3]);
-        mma_full(z, odd, qf[g * U + u][0], qf[g * U + u][1]);
-        mma_full(z, odd, qf[g * U + u][2], qf[g * U + u][3]);
+        mma_full(s, undo, qf[g * U + u][0], qf[g * U + u][1]);
+        mma_full(s, undo, qf[g * U + u][2], qf[g * U + u][3]);
       }
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        qsum[g][x] = s[x] + z[x];
-        bias[g][x] = -(kKeyEven * s[x] + kKeyOdd * z[x]);
-      }
+      qsum[g][0] = s[0] * 0x1p-20f;
+      qsum[g][1] = s[1] * 0x1p-20f;
       zacc[g][0] = zacc[g][1] = 0.f;
       norm[g] = 0.f;
     }
@@ -478,6 +462,7 @@ struct MmaBody {
       limit[x] = c.len - (a.T - 1 - (col0 + 2 * j + x) / a.rep);
     }
     limit_min = c.len - (a.T - 1 - col0 / a.rep);
+    steps = 0;
   }
 
   // Brings the group's factor to the largest scale of the tile (the lanes hold two rows each): o goes with it.
@@ -506,11 +491,33 @@ struct MmaBody {
     norm[g] = to;
   }
 
+  // Moves what a group's o have in common (one of them, that is) to the group's sum of zeros.
+  __device__ __forceinline__ void centre(int lane) {
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const float c = __shfl_sync(0xffffffffu, o[g * U][0][x], lane & 3);
+        if (lane < 4 && norm[g] != 0.f) zacc[g][x] += c * (0x1p24f / norm[g]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            o[g * U + u][y][x] -= c;
+            o[g * U + u][y][2 + x] -= 16.f * c;
+          }
+      }
+  }
+
   // Up to two tiles (those of a stage): `rows` of their 32 rows belong to the list, the first of them is its row `row0`.
   __device__ __forceinline__ void stage(const PagesAttnArgs& a, const uint8_t* tp, int row0, int rows, const float*, int lane) {
     const int i = lane >> 2, j = lane & 3;
     const int ri = i ^ ((i >> 1) & 1);           // tile rows of matrix rows i and i + 8
     const bool edge = rows < kStageRows || row0 + kStageRows > limit_min;
+    if (++steps == kCentre) {
+      steps = 0;
+      centre(lane);
+    }
 
     // S^T = K Q^T, one accumulator per group, then scale and zero
     float s[kStageTiles][4];
@@ -531,12 +538,12 @@ struct MmaBody {
       }
 #pragma unroll
       for (int g = 0; g < G; ++g) {
-        float c[4] = {bias[g][0], bias[g][1], bias[g][0], bias[g][1]};
+        float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           uint32_t lo[4], hi[4];
-          key4(kc[0][g * U + u], lo);
-          key4(kc[1][g * U + u], hi);
+          codes4(kc[0][g * U + u], lo);
+          codes4(kc[1][g * U + u], hi);
           const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
           mma_full(c, a0, qf[g * U + u][0], qf[g * U + u][1]);
           mma_full(c, a1, qf[g * U + u][2], qf[g * U + u][3]);
@@ -660,7 +667,7 @@ struct MmaBody {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const float scale = __uint_as_float(vw[b][g][r] << 16);
-          const float zero = fmaf(8.f, scale, __uint_as_float(vw[b][g][r] & 0xffff0000u)), f = scale * norm[g];
+          const float zero = __uint_as_float(vw[b][g][r] & 0xffff0000u), f = scale * norm[g];
 #pragma unroll
           for (int x = 0; x < 2; ++x) zacc[g][x] = fmaf(p[2 * r + x], zero, zacc[g][x]);
           pb[r] = transpose8x8(pack_f16(p[2 * r] * f, p[2 * r + 1] * f));
@@ -670,8 +677,8 @@ struct MmaBody {
           const int x = g * U + u;
           const uint32_t sel = (x & 1) ? 0x7632 : 0x5410;
           uint32_t v0[4], v1[4];
-          centred4(__byte_perm(vc[0][x >> 1], vc[1][x >> 1], sel), v0);
-          centred4(__byte_perm(vc[2][x >> 1], vc[3][x >> 1], sel), v1);
+          codes4(__byte_perm(vc[0][x >> 1], vc[1][x >> 1], sel), v0);
+          codes4(__byte_perm(vc[2][x >> 1], vc[3][x >> 1], sel), v1);
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             const uint32_t av[4] = {v0[2 * y], v0[2 * y + 1], v1[2 * y], v1[2 * y + 1]};
@@ -694,10 +701,10 @@ struct MmaBody {
       }
 #pragma unroll
       for (int y = 0; y < X; ++y) {
-        const float up = norm[y / U] == 0.f ? 0.f : 1.f / norm[y / U];
+        const float up = norm[y / U] == 0.f ? 0.f : 0x1p20f / norm[y / U];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          o[y][k][x] = fmaf(o[y][k][x], up, zacc[y / U][x]);
+          o[y][k][x] = fmaf(o[y][k][x], 16.f * up, zacc[y / U][x]);
           o[y][k][2 + x] = fmaf(o[y][k][2 + x], up, zacc[y / U][x]);
         }
       }
