@@ -284,10 +284,10 @@ struct CoreBody {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               float val = fmaf(scale, (float)((half >> (4 * k)) & 15u), zero);
-              if (edge && val != val) {      // a NaN that a column does not see must not reach it through 0 x NaN
+              if (edge && !(fabsf(val) <= 3.402823466e38f)) {      // what a column does not see must not reach it as 0 x NaN
 #pragma unroll
                 for (int x = 0; x < COLS; ++x)
-                  if (row0 + r < limit[x]) acc[x][(g * U + u) * 4 + k] = val;
+                  if (row0 + r < limit[x]) acc[x][(g * U + u) * 4 + k] = fmaf(pr[x], val, acc[x][(g * U + u) * 4 + k]);
                 val = 0.f;
               }
 #pragma unroll
@@ -357,8 +357,8 @@ struct CoreBody {
 // Operands are f16. A code masked in place is an operand already: as the bits of an f16 number a nibble n in bits 0 .. 3 is the
 // subnormal n 2^-24, in bits 4 .. 7 it is n 2^-20, both exact, so that a word's eight codes take one shift and four masks
 // and nothing is added or converted. (The factors go into the queries for K, into the sums at the end for V.) What f16 lacks
-// is range, so both factors that are not codes are normalised by powers of two: a query row by its largest element (what is
-// then below f16's smallest step is below 2^-24 of that element), and the scales that multiply P, which f16 holds to 2^-12,
+// is range, so both factors that are not codes are normalised by powers of two: a query row so that its largest element is near
+// f16's (what is then below f16's smallest step is below 2^-35 of that element), and the scales that multiply P, which f16 holds to 2^-12,
 // by a factor per group that follows them (`norm`).
 // V's codes have a mean of 7.5, so that o grows with the number of rows while what matters in it grows with its root. The
 // instruction truncates its sums, and an o far above what matters would let that show (relative 2^-25 a tile): every
@@ -385,9 +385,9 @@ __device__ __forceinline__ void codes4(uint32_t x, uint32_t* y) {
   y[2] = z & 0x000F000Fu;
   y[3] = z & 0x00F000F0u;
 }
-// 2^-e for the exponent e of x > 0 (clamped to what both it and its inverse can be)
+// 2^-e for the exponent e of x > 0 (clamped so that it, 2^11 times it and its inverse are numbers)
 __device__ __forceinline__ float inverse_power(float x) {
-  const int e = min(max((int)(__float_as_uint(x) >> 23) - 127, -126), 126);
+  const int e = min(max((int)(__float_as_uint(x) >> 23) - 127, -114), 126);
   return __uint_as_float((uint32_t)(127 - e) << 23);
 }
 
@@ -429,12 +429,12 @@ struct MmaBody {
       for (int w = 0; w < X; ++w)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const float by = k & 1 ? down : 16.f * down;           // for codes times 2^-20 and 2^-24
+          const float by = k & 1 ? 0x1p11f * down : 0x1p15f * down;      // for codes times 2^-20 and 2^-24
           qf[w][k] = pack_f16(f[w][k] * by, f[w][k + 4] * by);
         }
-      // scores come out times 2^-20
+      // scores come out times 2^-9 down
 #pragma unroll
-      for (int x = 0; x < 2; ++x) sc2[x] = a.scale * kLog2e * 0x1p20f / __shfl_sync(0xffffffffu, down, (2 * j + x) * 4);
+      for (int x = 0; x < 2; ++x) sc2[x] = a.scale * kLog2e * 0x1p9f / __shfl_sync(0xffffffffu, down, (2 * j + x) * 4);
     }
     // sums of the queries over each group, by the instruction itself (every row of a matrix of constants that undo the queries'
     // factors: operands 0, 1 go with nibbles 0 and 2 of a code word, operands 2, 3 with nibbles 1 and 3)
@@ -498,7 +498,7 @@ struct MmaBody {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const float c = __shfl_sync(0xffffffffu, o[g * U][0][x], lane & 3);
-        if (lane < 4 && norm[g] != 0.f) zacc[g][x] += c * (0x1p24f / norm[g]);
+        if (lane < 4 && norm[g] != 0.f) zacc[g][x] += c * 0x1p24f * (1.f / norm[g]);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -701,11 +701,11 @@ struct MmaBody {
       }
 #pragma unroll
       for (int y = 0; y < X; ++y) {
-        const float up = norm[y / U] == 0.f ? 0.f : 0x1p20f / norm[y / U];
+        const float up = norm[y / U] == 0.f ? 0.f : 1.f / norm[y / U];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          o[y][k][x] = fmaf(o[y][k][x], 16.f * up, zacc[y / U][x]);
-          o[y][k][2 + x] = fmaf(o[y][k][2 + x], up, zacc[y / U][x]);
+          o[y][k][x] = fmaf(o[y][k][x] * 0x1p24f, up, zacc[y / U][x]);
+          o[y][k][2 + x] = fmaf(o[y][k][2 + x] * 0x1p20f, up, zacc[y / U][x]);
         }
       }
     }
@@ -1121,11 +1121,12 @@ cudaError_t run_attn(const PagesAttnArgs& a, cudaStream_t s) {
   const int sms = device_sm_count();
   if (sms <= 0) return cudaErrorUnknown;
   // a grid that the machine holds at once, no larger than the work can be
-  const long long most = (long long)a.n * a.p.Hkv * cgs * attn_tiles(a.p.max_pages * a.p.page_rows);
+  const long long most = (long long)a.n * a.p.Hkv * cgs * (attn_tiles(a.p.max_pages * a.p.page_rows) + kSegmentUnits);
   constexpr int per_cta = Body::kWarps * kMinUnits;
   long long ctas = (most + per_cta - 1) / per_cta;
   if (ctas > (long long)Body::kBlocks * sms) ctas = (long long)Body::kBlocks * sms;
   if (ctas > kAttnMaxCtas) ctas = kAttnMaxCtas;
+  if (most / ctas > (1 << 30)) return cudaErrorInvalidValue;   // a CTA's share is counted in 32 bits
   attn_kernel<Body><<<(unsigned)ctas, (Body::kWarps + 1) * 32, smem, s>>>(a, cgs);
   return cudaGetLastError();
 }

@@ -7,6 +7,7 @@ namespace pyr {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kListThreads = 128;        // of a CTA that serves one list's table
 constexpr int kScanThreads = 1024;
 static_assert(kReserveSlice == kScanThreads * 4, "a thread of the scan owns four pages");
 
@@ -165,14 +166,14 @@ __device__ __forceinline__ void copy_rows_of_page(const PagesView& p, int from, 
     const int c = o - whole;
     return whole + (c < codes ? c : half + c - codes);
   };
-#pragma unroll 4
-  for (int x = threadIdx.x; x < heads * per16; x += kThreads) {
+#pragma unroll 8
+  for (int x = threadIdx.x; x < heads * per16; x += kListThreads) {
     const int h = x / per16;
     const size_t at = h * head_bytes + place(x - h * per16);
     *reinterpret_cast<uint4*>(d + at) = *reinterpret_cast<const uint4*>(s + at);
   }
 #pragma unroll 2
-  for (int x = threadIdx.x; x < heads * per4; x += kThreads) {
+  for (int x = threadIdx.x; x < heads * per4; x += kListThreads) {
     const int h = x / per4, o = (x - h * per4) * 4;
     const size_t at = h * head_bytes + whole + 2 * half + (o < words ? o : kPageTile * G * 4 + o - words);
     *reinterpret_cast<uint32_t*>(d + at) = *reinterpret_cast<const uint32_t*>(s + at);
@@ -180,7 +181,7 @@ __device__ __forceinline__ void copy_rows_of_page(const PagesView& p, int from, 
 }
 
 // grid (entries, parts): part 0 writes the entry's table and counts, every part copies its share of the heads.
-__global__ void __launch_bounds__(kThreads) reserve_take_kernel(PagesReserveArgs a) {
+__global__ void __launch_bounds__(kListThreads) reserve_take_kernel(PagesReserveArgs a) {
   wait_for_previous();
   const int i = blockIdx.x;
   const int4 pl = reinterpret_cast<const int4*>(a.plan)[i];
@@ -191,7 +192,7 @@ __global__ void __launch_bounds__(kThreads) reserve_take_kernel(PagesReserveArgs
   const int copies = old >= 0 ? 1 : 0;
   if (blockIdx.y == 0) {
     int32_t* row = a.p.table + (size_t)l * a.p.max_pages;
-    for (int x = threadIdx.x; x < fresh; x += kThreads) {
+    for (int x = threadIdx.x; x < fresh; x += kListThreads) {
       const int id = free_page(a, base + copies + x);
       row[slot + x] = id;
       a.p.refs[id] = 1;
@@ -213,24 +214,24 @@ __global__ void __launch_bounds__(kThreads) reserve_take_kernel(PagesReserveArgs
 // ------------------------------------------------------------------ fork, trim
 // One CTA per entry. An entry whose destination appears elsewhere in the call is refused by every CTA that sees it, so the
 // outcome does not depend on their order.
-__global__ void __launch_bounds__(kThreads) fork_kernel(PagesView p, const int32_t* src, const int32_t* dst, int n) {
+__global__ void __launch_bounds__(kListThreads) fork_kernel(PagesView p, const int32_t* src, const int32_t* dst, int n) {
   const int e = blockIdx.x;
   const int s = pages_list(p, src, e), d = pages_list(p, dst, e);
   bool bad = s < 0 || d < 0;
 #pragma unroll 4
-  for (int x = threadIdx.x; x < n; x += kThreads) bad |= (x != e && dst[x] == d) | (src[x] == d);
+  for (int x = threadIdx.x; x < n; x += kListThreads) bad |= (x != e && dst[x] == d) | (src[x] == d);
   int pages = 0, len = 0;
   if (s >= 0 && d >= 0) {
     len = pages_len(p, s);
     pages = (len + p.page_rows - 1) / p.page_rows;
     bad = bad || p.lens[d] != 0 || p.table[(size_t)d * p.max_pages] >= 0;
-    for (int x = threadIdx.x; x < pages; x += kThreads) bad = bad || pages_page(p, s, x) < 0;
+    for (int x = threadIdx.x; x < pages; x += kListThreads) bad = bad || pages_page(p, s, x) < 0;
   }
   if (__syncthreads_or(bad)) {
     if (threadIdx.x == 0) record(p.status, PYR_ERR_INVALID);
     return;
   }
-  for (int x = threadIdx.x; x < pages; x += kThreads) {
+  for (int x = threadIdx.x; x < pages; x += kListThreads) {
     const int id = pages_page(p, s, x);
     p.table[(size_t)d * p.max_pages + x] = id;
     atomicAdd(&p.refs[id], 1);
@@ -249,7 +250,7 @@ __device__ __forceinline__ void drop_pages(const PagesView& p, int l, int first)
   }
 }
 
-__global__ void __launch_bounds__(kThreads) trim_kernel(PagesView p, const int32_t* lists, int n, const int32_t* rows) {
+__global__ void __launch_bounds__(kListThreads) trim_kernel(PagesView p, const int32_t* lists, int n, const int32_t* rows) {
   const int e = blockIdx.x;
   const int l = pages_list(p, lists, e);
   const int want = rows ? rows[e] : 0;
@@ -510,13 +511,13 @@ cudaError_t launch_pages_reserve(const PagesReserveArgs& a, int* launches, cudaS
   // enough CTAs to share out the heads when there are few lists to copy for
   int parts = 1;
   while (parts < 16 && parts < a.p.Hkv && (int64_t)a.n * parts < 256) parts *= 2;
-  e = launch_behind(reserve_take_kernel, dim3(a.n, parts), dim3(kThreads), 0, s, a);
+  e = launch_behind(reserve_take_kernel, dim3(a.n, parts), dim3(kListThreads), 0, s, a);
   if (e == cudaSuccess) ++*launches;
   return e;
 }
 
 cudaError_t launch_pages_fork(const PagesView& p, const int32_t* src, const int32_t* dst, int n, int* launches, cudaStream_t s) {
-  fork_kernel<<<n, kThreads, 0, s>>>(p, src, dst, n);
+  fork_kernel<<<n, kListThreads, 0, s>>>(p, src, dst, n);
   const cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess) ++*launches;
   return e;
@@ -524,7 +525,7 @@ cudaError_t launch_pages_fork(const PagesView& p, const int32_t* src, const int3
 
 cudaError_t launch_pages_trim(const PagesView& p, const int32_t* lists, int n, const int32_t* rows, int* launches,
                               cudaStream_t s) {
-  trim_kernel<<<n, kThreads, 0, s>>>(p, lists, n, rows);
+  trim_kernel<<<n, kListThreads, 0, s>>>(p, lists, n, rows);
   const cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess) ++*launches;
   return e;

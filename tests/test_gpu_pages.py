@@ -357,6 +357,51 @@ def test_attention_over_scales_of_many_magnitudes(D, group, order):
     assert np.abs(lse[0].cpu().double().numpy() - wl).max() <= 2e-4
 
 
+def test_attention_over_many_rows_a_warp():
+    """64 lists of 16384 rows (the same pages, queries of their own): each warp sums over thousands of rows of one head, whose
+    codes all have the same sign."""
+    n, rows, hkv, D = 64, 16384, 4, 128
+    p = _pages(hkv, D, 64, 256, 64, n, 64)
+    k, v = _rand(1, rows, hkv, D, seed=44, dtype=BF, scale=0.2), _rand(1, rows, hkv, D, seed=45, dtype=BF)
+    p.reserve(_ids(0), rows)
+    p.write(k, v, _ids(0))
+    p.table.copy_(p.table[:1].expand(n, -1).clone())
+    p.lens.fill_(rows)
+    q = _rand(n, 1, hkv, D, seed=46, dtype=BF)
+    out, lse = p.attn(q, lse=True)
+    assert p.status() == 0
+    kd = torch.from_numpy(_quantised(k[0], 64)).to(DEV)
+    vd = torch.from_numpy(_quantised(v[0], 64)).to(DEV)
+    z = torch.einsum("nhd,rhd->nhr", q[:, 0].double(), kd) * D ** -0.5
+    want = torch.einsum("nhr,rhd->nhd", torch.softmax(z, -1), vd)
+    err = (out[:, 0].double() - want).abs()
+    # P in f16 (2^-12 of a term, sums of 16384 of them about 2^-12 15 step / 128), the output's rounding, the sums' truncation
+    # (64 steps of 2^-24 relative to 15 steps of the scale)
+    step = (vd.max() - vd.min()) / 15
+    assert bool((err <= 2.0 ** -9 * want.abs() + 15 * step * (2.0 ** -12 / 128 * 8 + 64 * 2.0 ** -24)).all())
+    assert float((lse[:, :, 0].double() - torch.logsumexp(z, -1)).abs().max()) <= 1e-5
+
+
+def test_attention_with_queries_and_values_near_the_ends_of_their_range():
+    """Queries of 2^100 against keys of 2^-100, and the other way round; values of 2^120 and 2^-90."""
+    p = _pages(1, 128, 32, 16, 8, 4, 2)
+    k, v = _rand(4, 30, 1, 128, seed=47), _rand(4, 30, 1, 128, seed=48)
+    e = torch.tensor([-100.0, 90.0, 0.0, 0.0], device=DEV).view(4, 1, 1, 1)
+    w = torch.tensor([0.0, 0.0, 120.0, -90.0], device=DEV).view(4, 1, 1, 1)
+    k, v = (k * torch.exp2(e)).to(BF), (v * torch.exp2(w)).to(BF)
+    p.reserve(_ids(0, 1, 2, 3), 30)
+    p.write(k, v)
+    q = (_rand(4, 1, 3, 128, seed=49) * torch.exp2(-e)).to(BF)
+    out, lse = p.attn(q, lse=True)
+    assert p.status() == 0
+    for i in range(4):
+        K, V = _list_values(p, i)
+        want, wl = op.attention(_wide(q[i]), K, V, 128 ** -0.5)
+        tol = 2.0 ** -9 * np.abs(want) + 2.0 ** -10 * np.abs(V).max()
+        assert (np.abs(_wide(out[i]) - want) <= tol).all(), i
+        assert np.abs(lse[i].cpu().double().numpy() - wl).max() <= 1e-4, i
+
+
 def test_attention_far_into_a_pool_beyond_four_gigabytes():
     """Pages whose byte offsets pass 2^32, written, attended, moved and read back."""
     hkv, D, pr = 32, 128, 64
