@@ -451,6 +451,7 @@ class PyrCache:
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _current_device = torch._C._cuda_getDevice
+_PAGES_DTYPES = {torch.bfloat16: PYR_BF16, torch.float32: PYR_F32}
 
 
 def make_pages_config(*, n_kv_heads, head_dim, n_pages, n_lists, max_pages, group=64, page_rows=64, flags=0) -> PyrPagesConfig:
@@ -523,25 +524,26 @@ class PyrPages:
         """Pointer to an int32 vector of n entries on the cache's device, None for NULL."""
         if t is None:
             return None
-        if t.dtype is not torch.int32 or t.get_device() != self._index or t.shape != (n,) or not t.is_contiguous():
+        if t.dtype is not torch.int32 or t.get_device() != self._index or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
             raise ValueError(f"{what}: expected {n} contiguous int32 entries on {self.device}")
         return t.data_ptr()
 
-    def _rows(self, a, b):
-        """Strides of a pair of [n, rows, heads, D] tensors (those of dimensions of size 1 do not count)."""
-        shape = a.shape
-        if len(shape) != 4 or shape[2] != self._heads or shape[3] != self._dim or b.shape != shape or a.dtype is not b.dtype:
-            raise ValueError(f"k, v: expected [n, rows, {self._heads}, {self._dim}], keys and values alike")
-        sa = self._strides(a, "k, v")
-        if self._strides(b, "k, v") != sa:
-            raise ValueError("k, v: keys and values need the same strides")
-        return sa
+    def _tensor(self, t, what):
+        """(shape, strides, pyr_dtype_t) of a [n, rows, heads, D] tensor."""
+        shape, strides, dtype = t.shape, t.stride(), _PAGES_DTYPES.get(t.dtype)
+        if dtype is None or len(shape) != 4 or shape[3] != self._dim or strides[3] != 1 or t.get_device() != self._index:
+            raise ValueError(f"{what}: expected a bf16 or fp32 tensor [n, rows, heads, {self._dim}] on {self.device}, the last "
+                             "dimension contiguous")
+        return shape, strides, dtype
 
-    def _strides(self, t, what):
-        (n, r, h, _), (sb, sr, sh, sd) = t.shape, t.stride()
-        if t.get_device() != self._index or (t.dtype is not torch.bfloat16 and t.dtype is not torch.float32) or sd != 1:
-            raise ValueError(f"{what}: expected bf16 or fp32 on {self.device} with a contiguous last dimension")
-        return (sb if n > 1 else 0, sr if r > 1 else 0, sh if h > 1 else 0)
+    def _rows(self, k, v):
+        """The same of a pair of tensors that are laid out alike (strides of dimensions of size 1 do not count)."""
+        shape, strides, dtype = self._tensor(k, "k")
+        shape_v, strides_v, dtype_v = self._tensor(v, "v")
+        if shape[2] != self._heads or shape_v != shape or dtype_v != dtype or (
+                strides_v != strides and any(n > 1 and x != y for n, x, y in zip(shape, strides, strides_v))):
+            raise ValueError(f"k, v: expected {self._heads} heads, and keys and values alike in shape, type and strides")
+        return shape, strides, dtype
 
     def _idx(self, idx, n):
         if idx is None:
@@ -577,36 +579,32 @@ class PyrPages:
 
     def write(self, k, v, lists=None, first=None, idx=None, counts=None, stream=None):
         """Stores rows of k, v [n, src_rows, Hkv, D] (those that idx names, or all): at the lists' ends, or from row first."""
-        sb, sn, sh = self._rows(k, v)
-        n, src = k.shape[0], k.shape[1]
+        (n, src, _, _), (sb, sn, sh, _), dtype = self._rows(k, v)
         ip, groups, istride = self._idx(idx, n)
         self._run("pyr_pages_write", stream, self._ids(lists, n), n, self._ids(first, n, "first"), k.data_ptr(), v.data_ptr(), sb, sn,
-                  sh, src, _dt(k), ip, groups, istride, self._ids(counts, n, "counts"), src if idx is None else idx.shape[2])
+                  sh, src, dtype, ip, groups, istride, self._ids(counts, n, "counts"), src if idx is None else idx.shape[2])
 
     def read(self, k, v, lists=None, first=None, counts=None, stream=None):
         """Fills k, v [n, rows, Hkv, D] with the lists' rows from row first (0) on; rows a list does not have stay as they are."""
-        sb, sn, sh = self._rows(k, v)
-        n = k.shape[0]
+        (n, rows, _, _), (sb, sn, sh, _), dtype = self._rows(k, v)
         self._run("pyr_pages_read", stream, self._ids(lists, n), n, self._ids(first, n, "first"), k.data_ptr(), v.data_ptr(), sb, sn,
-                  sh, _dt(k), self._ids(counts, n, "counts"), k.shape[1])
+                  sh, dtype, self._ids(counts, n, "counts"), rows)
 
     def attn(self, q, lists=None, out=None, lse=False, softmax_scale: float = 0.0, stream=None):
         """Attention of q [n, q_len, Hq, D] over the lists' rows: out like q, and with lse=True also lse [n, Hq, q_len] fp32."""
-        shape = q.shape
-        if len(shape) != 4 or shape[3] != self._dim:
-            raise ValueError(f"q: expected [n, q_len, Hq, {self._dim}]")
         if stream is not None:
             with torch.cuda.device(self._index), torch.cuda.stream(stream):    # what is allocated here is used on that stream
                 return self.attn(q, lists, out, lse, softmax_scale)
+        shape, (qb, qt, qh, _), dtype = self._tensor(q, "q")
         n, t, hq, _ = shape
-        qs = self._strides(q, "q")
         if out is None:
-            out = torch.empty(shape, dtype=q.dtype, device=self.device)
-        elif out.shape != shape or out.dtype is not q.dtype:
+            out = torch.empty_like(q)
+        shape_o, (ob, ot, oh, _), dtype_o = self._tensor(out, "out")
+        if shape_o != shape or dtype_o != dtype:
             raise ValueError("out: expected a tensor like q")
         stats = torch.empty(n, hq, t, dtype=torch.float32, device=self.device) if lse else None
-        self._run("pyr_pages_attn", None, self._ids(lists, n), n, q.data_ptr(), *qs, out.data_ptr(), *self._strides(out, "out"),
-                  stats.data_ptr() if lse else None, t, hq, _dt(q), softmax_scale)
+        self._run("pyr_pages_attn", None, self._ids(lists, n), n, q.data_ptr(), qb, qt, qh, out.data_ptr(), ob, ot, oh,
+                  stats.data_ptr() if lse else None, t, hq, dtype, softmax_scale)
         return (out, stats) if lse else out
 
     def fork(self, src, dst, stream=None):

@@ -92,12 +92,16 @@ pyr_status_t check_call(const pyr_pages* h, int32_t n, bool distinct) {
 // With lists == NULL entry i is list i, so there cannot be more entries than lists.
 bool default_lists_fit(const pyr_pages* h, const int32_t* lists, int32_t n) { return lists || n <= h->cfg.n_lists; }
 
-// rows of [n, rows, Hkv, D] tensors: 16-byte aligned, innermost dimension contiguous
+// rows of [n, rows, heads, D] tensors: 16-byte aligned, innermost dimension contiguous (the stride of a dimension of size 1 is not
+// looked at)
 pyr_status_t check_rows(const pyr_pages* h, const void* a, const void* b, int32_t dtype, int64_t sb, int64_t sn, int64_t sh,
-                        int heads) {
+                        int64_t n, int64_t rows, int heads) {
   if (!a || !b) return PYR_ERR_NULL;
   if (dtype != PYR_BF16 && dtype != PYR_F32) return PYR_ERR_UNSUPPORTED;
   const int D = h->cfg.head_dim, eb = dtype == PYR_BF16 ? 2 : 4;
+  if (n <= 1) sb = 0;
+  if (rows <= 1) sn = 0;
+  if (heads <= 1) sh = 0;
   if (sb < 0 || sn < 0 || sh < 0 || (heads > 1 && sh < D)) return PYR_ERR_INVALID;
   if ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % 16 || (sb * eb) % 16 || (sn * eb) % 16 ||
       (sh * eb) % 16)
@@ -218,7 +222,7 @@ pyr_status_t pyr_pages_write(pyr_pages_t* h, const int32_t* lists, int32_t n, co
                              const int32_t* idx, int32_t idx_groups, int64_t idx_stride, const int32_t* counts,
                              int32_t n_rows, void* stream) {
   pyr_status_t st = check_call(h, n, true);
-  if (st == PYR_OK) st = check_rows(h, k, v, dtype, sb, sn, sh, h->cfg.n_kv_heads);
+  if (st == PYR_OK) st = check_rows(h, k, v, dtype, sb, sn, sh, n, src_rows, h->cfg.n_kv_heads);
   if (st == PYR_OK) st = check_idx(h, idx, idx_groups, idx_stride, n_rows);
   if (st != PYR_OK) return st;
   if (n_rows < 0 || src_rows < 0 || (!idx && n_rows > src_rows)) return PYR_ERR_INVALID;
@@ -236,7 +240,7 @@ pyr_status_t pyr_pages_read(pyr_pages_t* h, const int32_t* lists, int32_t n, con
                             int64_t sb, int64_t sn, int64_t sh, int32_t dtype, const int32_t* counts, int32_t n_rows,
                             void* stream) {
   pyr_status_t st = check_call(h, n, false);
-  if (st == PYR_OK) st = check_rows(h, k, v, dtype, sb, sn, sh, h->cfg.n_kv_heads);
+  if (st == PYR_OK) st = check_rows(h, k, v, dtype, sb, sn, sh, n, n_rows, h->cfg.n_kv_heads);
   if (st != PYR_OK) return st;
   if (n_rows < 0 || !default_lists_fit(h, lists, n)) return PYR_ERR_INVALID;
   // rows that overlap would be written by several threads
@@ -259,8 +263,8 @@ pyr_status_t pyr_pages_attn(pyr_pages_t* h, const int32_t* lists, int32_t n, con
   if (st != PYR_OK) return st;
   if (q_len < 1 || n_q_heads < 1 || n_q_heads % h->cfg.n_kv_heads || !default_lists_fit(h, lists, n)) return PYR_ERR_INVALID;
   if (!(softmax_scale >= 0.0f) || !std::isfinite(softmax_scale)) return PYR_ERR_INVALID;
-  st = check_rows(h, q, q, dtype, qsb, qst, qsh, n_q_heads);
-  if (st == PYR_OK) st = check_rows(h, out, out, dtype, osb, ost, osh, n_q_heads);
+  st = check_rows(h, q, q, dtype, qsb, qst, qsh, n, q_len, n_q_heads);
+  if (st == PYR_OK) st = check_rows(h, out, out, dtype, osb, ost, osh, n, q_len, n_q_heads);
   if (st != PYR_OK) return st;
   if ((q_len > 1 && ost < h->cfg.head_dim) || (n > 1 && osb < h->cfg.head_dim)) return PYR_ERR_INVALID;
   const int64_t cols = (int64_t)q_len * (n_q_heads / h->cfg.n_kv_heads);

@@ -5,6 +5,7 @@
 // clamp, and a code's value scale * c + zero is within scale / 2 of x. The product scale * c is exact in fp32 (8 + 4 bits).
 // Arithmetic is plain IEEE single precision, never contracted, so that the stored bytes are the same everywhere.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include "pyr_internal.h"
 
@@ -382,11 +383,21 @@ __global__ void __launch_bounds__(kRowThreads) write_few_kernel(PagesWriteArgs a
   }
 }
 
-// The values of eight codes: scale * code + zero, the product exact.
+// The values of eight codes: scale * code + zero, the product exact. Codes become numbers two at a time: 0x6400 | n is the f16
+// number 1024 + n, 0x6400 | 16 n is 1024 + 16 n (integer conversions, a quarter of the rate, were the bound before: 70 us for
+// 640 k rows of 128 dimensions, K and V).
 __device__ __forceinline__ void values8(uint32_t codes, uint32_t word, float* x) {
   const float scale = __uint_as_float(word << 16), zero = __uint_as_float(word & 0xFFFF0000u);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) x[k] = __fmaf_rn(scale, (float)((codes >> (4 * k)) & 15u), zero);
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t bits = k < 2 ? codes : codes >> 8, mask = k & 1 ? 0x00F000F0u : 0x000F000Fu;
+    const uint32_t y = (bits & mask) | 0x64006400u;
+    const __half2 v = reinterpret_cast<const __half2&>(y);
+    const float2 n = __half22float2(k & 1 ? __hfma2(v, __float2half2_rn(0.0625f), __float2half2_rn(-64.f))
+                                          : __hsub2(v, __float2half2_rn(1024.f)));
+    x[k] = __fmaf_rn(scale, n.x, zero);
+    x[k + 4] = __fmaf_rn(scale, n.y, zero);
+  }
 }
 
 // One warp per (entry, KV head, tile of its list), as for writing.
