@@ -408,6 +408,8 @@ pyr_status_t pyr_glue_argmax(const void* x, int32_t* out, int64_t rows, int32_t 
  * page out of range, no free page, the same list twice where it would be written twice) cannot be returned by an
  * asynchronous call: the list concerned (or, in pyr_pages_reserve, the whole call) is left as it was, a pyr_status_t is
  * recorded in the handle's status word and pyr_pages_status reports it. No such error makes a kernel leave its buffers.
+ * Rows in a slot whose page id is out of range take no part in attention and are not read back.
+ * The GPU that holds the buffer must be the current one in every call. At most 2^30 rows an entry and call.
  *
  * In every call `lists` (device int32 [n]) names the list of each entry; NULL means lists 0 .. n-1. n = 0 does nothing.
  */
@@ -458,7 +460,8 @@ pyr_status_t pyr_pages_reserve(pyr_pages_t* pages, const int32_t* lists, int32_t
  * the rows [first_i, first_i + count_i) of its list (first: device int32 [n], each at most the list's length; NULL: the
  * list's end). With idx (device int32 [n, idx_groups, n_rows] with idx_stride elements between entries; idx_groups 1 or
  * n_kv_heads; pyr_cache_kept's first pointer is one) row x of head h is source row idx[i][h's group][x]: the Gather of
- * Algorithm 1 straight into 4-bit pages; without, source row x. The list's length becomes max(length, first_i + count_i).
+ * Algorithm 1 straight into 4-bit pages; without, source row x (an index out of range stores a row of NaN and is reported).
+ * The list's length becomes max(length, first_i + count_i).
  * Every page written must be the list's own: reserved, and held by no other list. One row per list is the decode step's
  * append.
  */
@@ -481,8 +484,8 @@ pyr_status_t pyr_pages_read(pyr_pages_t* pages, const int32_t* lists, int32_t n,
  * those of the query tokens themselves (a chunk of a prompt, drafted tokens). A token that sees no row gets zeros.
  * lse (device, may be NULL) is [n, n_q_heads, q_len] fp32, the natural log of the softmax denominator, -inf for such a
  * token. softmax_scale 0 means 1/sqrt(D). Scores, softmax statistics and sums are held in fp32. Each list is read once per
- * 8 (bf16; 4 for fp32) query rows of a KV head; bit-reproducible. A list may appear more than once. bf16 runs on warp-level
- * tensor-core instructions, fp32 on CUDA cores.
+ * 8 (bf16; 4 for fp32) query rows of a KV head; bit-reproducible. A list may appear more than once; an entry whose list id
+ * is out of range writes nothing. bf16 runs on warp-level tensor-core instructions, fp32 on CUDA cores.
  */
 pyr_status_t pyr_pages_attn(pyr_pages_t* pages, const int32_t* lists, int32_t n, const void* q, int64_t q_stride_b,
                             int64_t q_stride_t, int64_t q_stride_h, void* out, int64_t o_stride_b, int64_t o_stride_t,

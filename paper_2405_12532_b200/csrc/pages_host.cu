@@ -8,10 +8,11 @@
 namespace {
 
 constexpr size_t kAlign = 256;
+constexpr int32_t kMaxRows = 1 << 30;      // of a call's entry: row arithmetic stays within 32 bits
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 struct PagesLayout {
-  size_t status, control, arrived, refused, lens, refs, table, plan, free_ids, slice_first, partial, pool, total;
+  size_t status, control, arrived, refused, moved, lens, refs, table, plan, free_ids, slice_first, partial, pool, total;
   int slices;
 };
 
@@ -39,6 +40,7 @@ void plan(const pyr_pages_config_t* c, PagesLayout* l) {
   l->control = take(64 * 4);
   l->arrived = take((size_t)pyr::kAttnMaxCtas * 4);
   l->refused = take((size_t)c->n_lists * 4);
+  l->moved = take((size_t)c->n_lists * 4);
   l->lens = take((size_t)c->n_lists * 4);
   l->refs = take((size_t)c->n_pages * 4);
   l->table = take((size_t)c->n_lists * c->max_pages * 4);
@@ -84,7 +86,6 @@ pyr::PagesView view(const pyr_pages* h) {
 // has more entries than there are lists except attention, reading and forking from, which may repeat them
 pyr_status_t check_call(const pyr_pages* h, int32_t n, bool distinct) {
   if (!h) return PYR_ERR_NULL;
-  if (!h->ready) return PYR_ERR_ORDER;
   if (n < 0 || (distinct && n > h->cfg.n_lists)) return PYR_ERR_INVALID;
   return PYR_OK;
 }
@@ -117,6 +118,8 @@ pyr_status_t check_idx(const pyr_pages* h, const int32_t* idx, int32_t groups, i
 
 }  // namespace
 
+// The last check of a launching call: everything that the arguments alone decide has been refused before it.
+#define PYR_PAGES_READY(h) do { if (!(h)->ready) return PYR_ERR_ORDER; } while (0)
 #define PYR_PAGES(call) do { int launches = 0; const cudaError_t e_ = (call); pyr::count_launches(launches); \
                              return e_ == cudaSuccess ? PYR_OK : PYR_ERR_CUDA; } while (0)
 
@@ -166,7 +169,7 @@ pyr_status_t pyr_pages_reset(pyr_pages_t* h, void* stream) {
     return PYR_ERR_CUDA;
   if (major != 10) return PYR_ERR_UNSUPPORTED;
   const PagesLayout& l = h->lay;
-  // status, control words, arrival counters, refusals, lengths and reference counts lie one behind the other
+  // status, control words, arrival counters, refusals, move counters, lengths and reference counts lie one behind the other
   if (cudaMemsetAsync(h->base + l.status, 0, l.table - l.status, s) != cudaSuccess) return PYR_ERR_CUDA;
   if (cudaMemsetAsync(h->base + l.table, 0xff, l.plan - l.table, s) != cudaSuccess) return PYR_ERR_CUDA;
   h->ready = true;
@@ -205,6 +208,7 @@ pyr_status_t pyr_pages_reserve(pyr_pages_t* h, const int32_t* lists, int32_t n, 
   const pyr_status_t st = check_call(h, n, true);
   if (st != PYR_OK) return st;
   if (!rows && rows_each < 0) return PYR_ERR_INVALID;
+  PYR_PAGES_READY(h);
   if (n == 0) return PYR_OK;
   pyr::PagesReserveArgs a;
   a.p = view(h);
@@ -226,6 +230,8 @@ pyr_status_t pyr_pages_write(pyr_pages_t* h, const int32_t* lists, int32_t n, co
   if (st == PYR_OK) st = check_idx(h, idx, idx_groups, idx_stride, n_rows);
   if (st != PYR_OK) return st;
   if (n_rows < 0 || src_rows < 0 || (!idx && n_rows > src_rows)) return PYR_ERR_INVALID;
+  if (n_rows > kMaxRows) return PYR_ERR_UNSUPPORTED;
+  PYR_PAGES_READY(h);
   if (n == 0 || n_rows == 0) return PYR_OK;
   pyr::PagesWriteArgs a;
   a.p = view(h);
@@ -246,6 +252,8 @@ pyr_status_t pyr_pages_read(pyr_pages_t* h, const int32_t* lists, int32_t n, con
   // rows that overlap would be written by several threads
   if (n_rows > 1 && sn < h->cfg.head_dim) return PYR_ERR_INVALID;
   if (n > 1 && sb < h->cfg.head_dim) return PYR_ERR_INVALID;
+  if (n_rows > kMaxRows) return PYR_ERR_UNSUPPORTED;
+  PYR_PAGES_READY(h);
   if (n == 0 || n_rows == 0) return PYR_OK;
   pyr::PagesWriteArgs a;
   a.p = view(h);
@@ -269,6 +277,7 @@ pyr_status_t pyr_pages_attn(pyr_pages_t* h, const int32_t* lists, int32_t n, con
   if ((q_len > 1 && ost < h->cfg.head_dim) || (n > 1 && osb < h->cfg.head_dim)) return PYR_ERR_INVALID;
   const int64_t cols = (int64_t)q_len * (n_q_heads / h->cfg.n_kv_heads);
   if (cols > (1 << 20)) return PYR_ERR_UNSUPPORTED;
+  PYR_PAGES_READY(h);
   if (n == 0) return PYR_OK;
   pyr::PagesAttnArgs a;
   a.p = view(h);
@@ -284,8 +293,9 @@ pyr_status_t pyr_pages_attn(pyr_pages_t* h, const int32_t* lists, int32_t n, con
 pyr_status_t pyr_pages_fork(pyr_pages_t* h, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
   const pyr_status_t st = check_call(h, n, true);
   if (st != PYR_OK) return st;
+  if (n > 0 && (!src || !dst)) return PYR_ERR_NULL;
+  PYR_PAGES_READY(h);
   if (n == 0) return PYR_OK;
-  if (!src || !dst) return PYR_ERR_NULL;
   PYR_PAGES(pyr::launch_pages_fork(view(h), src, dst, n, &launches, static_cast<cudaStream_t>(stream)));
 }
 
@@ -293,6 +303,7 @@ pyr_status_t pyr_pages_trim(pyr_pages_t* h, const int32_t* lists, int32_t n, con
   const pyr_status_t st = check_call(h, n, false);
   if (st != PYR_OK) return st;
   if (!default_lists_fit(h, lists, n)) return PYR_ERR_INVALID;
+  PYR_PAGES_READY(h);
   if (n == 0) return PYR_OK;
   PYR_PAGES(pyr::launch_pages_trim(view(h), lists, n, rows, &launches, static_cast<cudaStream_t>(stream)));
 }
@@ -303,13 +314,16 @@ pyr_status_t pyr_pages_compact(pyr_pages_t* h, const int32_t* src, const int32_t
   if (st == PYR_OK) st = check_idx(h, idx, idx_groups, idx_stride, n_rows);
   if (st != PYR_OK) return st;
   if (n_rows < 0) return PYR_ERR_INVALID;
+  if (n_rows > kMaxRows) return PYR_ERR_UNSUPPORTED;
+  if (n > 0 && (!src || !dst)) return PYR_ERR_NULL;
+  PYR_PAGES_READY(h);
   if (n == 0) return PYR_OK;
-  if (!src || !dst) return PYR_ERR_NULL;
   pyr::PagesMoveArgs a;
   a.p = view(h);
   a.src = src; a.dst = dst; a.n = n; a.idx = idx; a.idx_groups = idx ? idx_groups : 1; a.idx_stride = idx_stride;
   a.counts = counts; a.n_rows = n_rows;
   a.refused = at<int32_t>(h, h->lay.refused);
+  a.moved = at<int32_t>(h, h->lay.moved);
   PYR_PAGES(pyr::launch_pages_compact(a, &launches, static_cast<cudaStream_t>(stream)));
 }
 

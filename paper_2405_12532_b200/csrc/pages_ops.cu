@@ -7,7 +7,7 @@ namespace pyr {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kListThreads = 128;        // of a CTA that serves one list's table
+constexpr int kListThreads = 128;        // of a CTA that serves one list's table (1280 lists: 6.0 us to fork, 7.4 with 256)
 constexpr int kScanThreads = 1024;
 static_assert(kReserveSlice == kScanThreads * 4, "a thread of the scan owns four pages");
 
@@ -166,14 +166,14 @@ __device__ __forceinline__ void copy_rows_of_page(const PagesView& p, int from, 
     const int c = o - whole;
     return whole + (c < codes ? c : half + c - codes);
   };
-#pragma unroll 8
-  for (int x = threadIdx.x; x < heads * per16; x += kListThreads) {
+#pragma unroll 4
+  for (int x = threadIdx.x; x < heads * per16; x += kThreads) {
     const int h = x / per16;
     const size_t at = h * head_bytes + place(x - h * per16);
     *reinterpret_cast<uint4*>(d + at) = *reinterpret_cast<const uint4*>(s + at);
   }
 #pragma unroll 2
-  for (int x = threadIdx.x; x < heads * per4; x += kListThreads) {
+  for (int x = threadIdx.x; x < heads * per4; x += kThreads) {
     const int h = x / per4, o = (x - h * per4) * 4;
     const size_t at = h * head_bytes + whole + 2 * half + (o < words ? o : kPageTile * G * 4 + o - words);
     *reinterpret_cast<uint32_t*>(d + at) = *reinterpret_cast<const uint32_t*>(s + at);
@@ -181,7 +181,7 @@ __device__ __forceinline__ void copy_rows_of_page(const PagesView& p, int from, 
 }
 
 // grid (entries, parts): part 0 writes the entry's table and counts, every part copies its share of the heads.
-__global__ void __launch_bounds__(kListThreads) reserve_take_kernel(PagesReserveArgs a) {
+__global__ void __launch_bounds__(kThreads) reserve_take_kernel(PagesReserveArgs a) {
   wait_for_previous();
   const int i = blockIdx.x;
   const int4 pl = reinterpret_cast<const int4*>(a.plan)[i];
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kListThreads) reserve_take_kernel(PagesReserve
   const int copies = old >= 0 ? 1 : 0;
   if (blockIdx.y == 0) {
     int32_t* row = a.p.table + (size_t)l * a.p.max_pages;
-    for (int x = threadIdx.x; x < fresh; x += kListThreads) {
+    for (int x = threadIdx.x; x < fresh; x += kThreads) {
       const int id = free_page(a, base + copies + x);
       row[slot + x] = id;
       a.p.refs[id] = 1;
@@ -241,9 +241,9 @@ __global__ void __launch_bounds__(kListThreads) fork_kernel(PagesView p, const i
 
 // Gives up the pages of list l from slot `first` on. A table entry is taken by exchange, so that a list named twice gives
 // a page up once.
-__device__ __forceinline__ void drop_pages(const PagesView& p, int l, int first) {
+__device__ __forceinline__ void drop_pages(const PagesView& p, int l, int first, int index, int threads) {
   int32_t* row = p.table + (size_t)l * p.max_pages;
-  for (int x = first + threadIdx.x; x < p.max_pages; x += blockDim.x) {
+  for (int x = first + index; x < p.max_pages; x += threads) {
     if (row[x] < 0) continue;
     const int id = atomicExch(&row[x], -1);
     if (id >= 0 && id < p.n_pages) atomicSub(&p.refs[id], 1);
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kListThreads) trim_kernel(PagesView p, const i
     keep = len < want ? (len < 0 ? 0 : len) : want;
   }
   __syncthreads();
-  drop_pages(p, l, (keep + p.page_rows - 1) / p.page_rows);
+  drop_pages(p, l, (keep + p.page_rows - 1) / p.page_rows, threadIdx.x, kListThreads);
 }
 
 // ------------------------------------------------------------------ compact
@@ -380,20 +380,28 @@ struct TileRows {
   }
 };
 
+// What is left to do for an entry once its rows have moved, by `threads` threads: the length, and in place the pages behind it.
+__device__ __forceinline__ void finish_entry(const PagesMoveArgs& a, int e, int index, int threads) {
+  if (a.refused[e]) return;
+  const int cnt = entry_count(a, e);
+  const int s = pages_list(a.p, a.src, e), d = pages_list(a.p, a.dst, e);
+  if (index == 0) a.p.lens[d] = cnt;
+  if (s == d) drop_pages(a.p, d, (cnt + a.p.page_rows - 1) / a.p.page_rows, index, threads);
+}
+
+// Where no row moves.
+__global__ void __launch_bounds__(kThreads) compact_finish_kernel(PagesMoveArgs a) {
+  wait_for_previous();
+  const int e = blockIdx.x;
+  finish_entry(a, e, threadIdx.x, kThreads);
+  __syncthreads();
+  if (threadIdx.x == 0) a.refused[e] = 0;          // as the next call expects it
+}
+
 // Into another list: one warp per (entry, KV head, run of kRun destination tiles), the next tile's rows on their way while one
 // is stored. (An entry whose list is its own destination is left to the first run's warp, tile by tile, see below.)
-constexpr int kRun = 4;
-
-template <int D, int G>
-__global__ void __launch_bounds__(kThreads) compact_move_kernel(PagesMoveArgs a, int runs, int64_t items) {
-  wait_for_previous();
-  let_next_start();
-  const int lane = threadIdx.x & 31;
-  const int64_t item = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-  if (item >= items) return;
-  const int run = (int)(item % runs);
-  const int h = (int)(item / runs % a.p.Hkv);
-  const int e = (int)(item / runs / a.p.Hkv);
+template <int D, int G, int kRun>
+__device__ __forceinline__ void move_run(const PagesMoveArgs& a, int e, int h, int run, int lane) {
   const int cnt = entry_count(a, e), x0 = run * kRun * kPageTile;
   if (x0 >= cnt || a.refused[e]) return;
   const int s = pages_list(a.p, a.src, e), d = pages_list(a.p, a.dst, e);
@@ -412,14 +420,14 @@ __global__ void __launch_bounds__(kThreads) compact_move_kernel(PagesMoveArgs a,
     }
     return;
   }
-  // source rows of the run (lane l: rows l and l + 32 of it) and the pages that its tiles go to (lane t: tile t), looked up
+  // source rows of the run (lane l: rows l, l + 32, .. of it) and the pages that its tiles go to (lane t: tile t), looked up
   // together: what follows needs no address that is still to be fetched
-  static_assert(kRun * kPageTile == 64, "two rows a lane");
-  RowPlace from[2];
+  constexpr int kRows = kRun * kPageTile, kPlaces = (kRows + 31) / 32;
+  RowPlace from[kPlaces];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int x = x0 + 32 * k + lane;
-    from[k] = row_place(a.p, s, h, x < cnt ? (idx ? idx[x] : x) : -1);
+  for (int k = 0; k < kPlaces; ++k) {
+    const int in = 32 * k + lane, x = x0 + in;
+    from[k] = row_place(a.p, s, h, in < kRows && x < cnt ? (idx ? idx[x] : x) : -1);
   }
   const int to_row = x0 + (lane & (kRun - 1)) * kPageTile;
   const int to_page = to_row < cnt ? pages_page(a.p, d, to_row / a.p.page_rows) : -1;
@@ -436,18 +444,37 @@ __global__ void __launch_bounds__(kThreads) compact_move_kernel(PagesMoveArgs a,
   }
 }
 
+// The warp that is the last of its entry finishes it: no other looks at the entry's table any more.
+template <int D, int G, int kRun>
+__global__ void __launch_bounds__(kThreads) compact_move_kernel(PagesMoveArgs a, int runs, int64_t items) {
+  wait_for_previous();
+  const int lane = threadIdx.x & 31;
+  const int64_t item = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  if (item >= items) return;
+  const int run = (int)(item % runs);
+  const int h = (int)(item / runs % a.p.Hkv);
+  const int e = (int)(item / runs / a.p.Hkv);
+  move_run<D, G, kRun>(a, e, h, run, lane);
+  __syncwarp();
+  int order = 0;
+  if (lane == 0) order = atomicAdd(&a.moved[e], 1);
+  if (__shfl_sync(0xffffffffu, order, 0) != a.p.Hkv * runs - 1) return;
+  finish_entry(a, e, lane, 32);
+  __syncwarp();
+  if (lane == 0) a.refused[e] = a.moved[e] = 0;    // as the next call expects them
+}
+
 // In place: one CTA per (entry, KV head), a tile a warp, front to back. idx ascends strictly, so row x comes from a row >= x:
 // once the rows of a step's tiles have been read, nothing that later steps read lies in those tiles, and one barrier a step
 // (between its reads and its writes) is enough.
 template <int D, int G>
 __global__ void __launch_bounds__(kThreads) compact_inplace_kernel(PagesMoveArgs a) {
   wait_for_previous();
-  let_next_start();
   constexpr int kStep = kThreads / 32;
+  __shared__ int is_last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int e = blockIdx.x / a.p.Hkv, h = blockIdx.x % a.p.Hkv;
-  const int cnt = entry_count(a, e);
-  if (cnt <= 0 || a.refused[e]) return;
+  const int cnt = a.refused[e] ? 0 : entry_count(a, e);
   const int l = pages_list(a.p, a.dst, e);
   const int32_t* idx = a.idx + (int64_t)e * a.idx_stride + (int64_t)(a.idx_groups == 1 ? 0 : h) * a.n_rows;
   const int tiles = (cnt + kPageTile - 1) / kPageTile;
@@ -463,39 +490,38 @@ __global__ void __launch_bounds__(kThreads) compact_inplace_kernel(PagesMoveArgs
     if (page >= 0)
       rows.store(a.p.pool + pages_tile(a.p, page, h, row0 % a.p.page_rows / kPageTile), min(cnt - row0, kPageTile), lane);
   }
+  // the CTA that is the last of its entry finishes it: no other looks at the entry's table any more
+  __syncthreads();
+  if (threadIdx.x == 0) is_last = atomicAdd(&a.moved[e], 1) == a.p.Hkv - 1;
+  __syncthreads();
+  if (!is_last) return;
+  finish_entry(a, e, threadIdx.x, kThreads);
+  __syncthreads();
+  if (threadIdx.x == 0) a.refused[e] = a.moved[e] = 0;   // as the next call expects them
 }
 
-__global__ void __launch_bounds__(kThreads) compact_finish_kernel(PagesMoveArgs a) {
-  wait_for_previous();
-  const int e = blockIdx.x;
-  if (a.refused[e]) {
-    __syncthreads();
-    if (threadIdx.x == 0) a.refused[e] = 0;        // as the next call expects it
-    return;
-  }
-  const int cnt = entry_count(a, e);
-  const int s = pages_list(a.p, a.src, e), d = pages_list(a.p, a.dst, e);
-  if (threadIdx.x == 0) a.p.lens[d] = cnt;
-  if (s == d) drop_pages(a.p, d, (cnt + a.p.page_rows - 1) / a.p.page_rows);
+template <int D, int G, int kRun>
+cudaError_t run_runs(const PagesMoveArgs& a, cudaStream_t s) {
+  const int runs = (a.n_rows + kRun * kPageTile - 1) / (kRun * kPageTile);
+  const int64_t items = (int64_t)a.n * a.p.Hkv * runs;
+  const int64_t grid = (items + kThreads / 32 - 1) / (kThreads / 32);
+  if (grid > 0x7fffffffLL || (int64_t)a.p.Hkv * runs > 0x7fffffffLL) return cudaErrorInvalidValue;
+  return launch_behind(compact_move_kernel<D, G, kRun>, dim3((unsigned)grid), dim3(kThreads), 0, s, a, runs, items);
 }
 
 template <int D, int G>
-cudaError_t run_move(const PagesMoveArgs& a, int* launches, cudaStream_t s) {
-  cudaError_t e;
+cudaError_t run_move(const PagesMoveArgs& a, cudaStream_t s) {
   if (a.src == a.dst) {                          // one array for both: every entry is compacted in place
-    if (!a.idx) return cudaSuccess;
     const int64_t heads = (int64_t)a.n * a.p.Hkv;
     if (heads > 0x7fffffffLL) return cudaErrorInvalidValue;
-    e = launch_behind(compact_inplace_kernel<D, G>, dim3((unsigned)heads), dim3(kThreads), 0, s, a);
-  } else {
-    const int runs = (a.n_rows + kRun * kPageTile - 1) / (kRun * kPageTile);
-    const int64_t items = (int64_t)a.n * a.p.Hkv * runs;
-    const int64_t grid = (items + kThreads / 32 - 1) / (kThreads / 32);
-    if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
-    e = launch_behind(compact_move_kernel<D, G>, dim3((unsigned)grid), dim3(kThreads), 0, s, a, runs, items);
+    return launch_behind(compact_inplace_kernel<D, G>, dim3((unsigned)heads), dim3(kThreads), 0, s, a);
   }
-  if (e == cudaSuccess) ++*launches;
-  return e;
+  // Runs of four tiles where there are enough of them to give every SM 32 warps (64 lists of 32 heads: 148 us), else a tile a
+  // warp: then a warp's own latency is what counts (4 lists of 8 heads, 717 rows: 6.6 us, 11 with runs of four).
+  const int sms = device_sm_count();
+  if (sms <= 0) return cudaErrorUnknown;
+  const int64_t runs = (int64_t)a.n * a.p.Hkv * ((a.n_rows + 4 * kPageTile - 1) / (4 * kPageTile));
+  return runs >= 32LL * sms ? run_runs<D, G, 4>(a, s) : run_runs<D, G, 1>(a, s);
 }
 
 }  // namespace
@@ -511,7 +537,7 @@ cudaError_t launch_pages_reserve(const PagesReserveArgs& a, int* launches, cudaS
   // enough CTAs to share out the heads when there are few lists to copy for
   int parts = 1;
   while (parts < 16 && parts < a.p.Hkv && (int64_t)a.n * parts < 256) parts *= 2;
-  e = launch_behind(reserve_take_kernel, dim3(a.n, parts), dim3(kListThreads), 0, s, a);
+  e = launch_behind(reserve_take_kernel, dim3(a.n, parts), dim3(kThreads), 0, s, a);
   if (e == cudaSuccess) ++*launches;
   return e;
 }
@@ -536,13 +562,10 @@ cudaError_t launch_pages_compact(const PagesMoveArgs& a, int* launches, cudaStre
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   ++*launches;
-  if (a.n_rows > 0) {
-    const int G = a.p.D / a.p.group;
-    if (a.p.D == 128) e = G == 4 ? run_move<128, 4>(a, launches, s) : G == 2 ? run_move<128, 2>(a, launches, s) : run_move<128, 1>(a, launches, s);
-    else e = G == 2 ? run_move<64, 2>(a, launches, s) : run_move<64, 1>(a, launches, s);
-    if (e != cudaSuccess) return e;
-  }
-  e = launch_behind(compact_finish_kernel, dim3(a.n), dim3(kThreads), 0, s, a);
+  const int G = a.p.D / a.p.group;
+  if (a.n_rows == 0 || (a.src == a.dst && !a.idx)) e = launch_behind(compact_finish_kernel, dim3(a.n), dim3(kThreads), 0, s, a);
+  else if (a.p.D == 128) e = G == 4 ? run_move<128, 4>(a, s) : G == 2 ? run_move<128, 2>(a, s) : run_move<128, 1>(a, s);
+  else e = G == 2 ? run_move<64, 2>(a, s) : run_move<64, 1>(a, s);
   if (e == cudaSuccess) ++*launches;
   return e;
 }

@@ -205,6 +205,7 @@ struct PagesMoveArgs {
   const int32_t* idx; int idx_groups; int64_t idx_stride;
   const int32_t* counts; int n_rows;
   int32_t* refused;                // [n_lists]: set where an entry is refused; zero between calls
+  int32_t* moved;                  // [n_lists]: warps or CTAs done with an entry; zero between calls
 };
 struct PagesReserveArgs {
   PagesView p;

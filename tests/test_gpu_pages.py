@@ -605,6 +605,45 @@ def test_compact_in_place_keeps_a_shared_prefix_shared():
     assert p.refs.tolist()[:4] == [2, 2, 1, 0]
 
 
+def test_compact_of_nothing_and_of_many_entries_at_once():
+    """No rows, a copy of a list to itself, and calls whose entries are partly in place, partly not, partly refused: every entry
+    is finished by itself, and the counters are left as the next call needs them."""
+    n, hkv, D, pr = 6, 3, 64, 16
+    p = _pages(hkv, D, 32, pr, 80, 2 * n, 8)
+    k, v = _rand(n, 100, hkv, D, seed=75), _rand(n, 100, hkv, D, seed=76)
+    src = _ids(*range(n))
+    p.reserve(src, 100)
+    p.write(k, v, src)
+    p.reserve(_ids(6, 7, 8), 40)
+    kq = _quantised(k, 32)
+    idx = torch.stack([torch.arange(i, 100, 2 + i % 2)[:30] for i in range(n)]).to(torch.int32).view(n, 1, 30).to(DEV)
+    for _ in range(2):
+        dst = _ids(6, 1, 7, 3, 9, 8)                   # 1 and 3 in place; 9 has no pages
+        if _ == 0:
+            p.compact(src, dst, idx=idx)
+            assert p.status() == pb.PYR_ERR_INVALID
+            assert p.lens.tolist() == [100, 30, 100, 30, 100, 100, 30, 30, 30, 0, 0, 0]
+        else:                                          # again: the refused entry given pages, the others as they are by now
+            p.reserve(_ids(9), 30)
+            p.compact(_ids(0, 2, 4, 5), _ids(6, 7, 9, 8), idx=idx[[0, 2, 4, 5]].contiguous())
+            assert p.status() == 0 and p.lens.tolist() == [100, 30, 100, 30, 100, 100, 30, 30, 30, 30, 0, 0]
+        for i, l in enumerate(dst.tolist()):
+            if _ == 0 and l == 9:
+                continue
+            np.testing.assert_array_equal(_list_values(p, l)[0], kq[i, idx[i, 0].cpu().numpy()])
+    p.compact(_ids(0), _ids(0), n_rows=50)             # a list's own first rows: only the length and the pages change
+    assert p.status() == 0 and int(p.lens[0]) == 50 and int((p.table[0] >= 0).sum()) == 4
+    two = _ids(2, 4)
+    p.compact(two, two, n_rows=17)
+    p.compact(_ids(5), _ids(6), n_rows=0)
+    assert p.status() == 0 and p.lens[[2, 4, 6]].tolist() == [17, 17, 0]
+    np.testing.assert_array_equal(_list_values(p, 2)[0], kq[2, :17])
+    held = torch.zeros_like(p.refs)
+    t = p.table[p.table >= 0].long()
+    held.index_add_(0, t, torch.ones_like(t, dtype=torch.int32))
+    assert torch.equal(held, p.refs)
+
+
 # ------------------------------------------------------------------ refusals
 
 def test_refused_entries_change_nothing_and_are_reported():

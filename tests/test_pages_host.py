@@ -92,6 +92,46 @@ def test_pages_calls_need_a_reset_first():
     L.pyr_pages_free(h)
 
 
+def test_pages_arguments_are_refused_before_any_launch():
+    """What the arguments alone decide: null pointers, types, counts, strides that overlap or break the 16-byte rows, head counts,
+    scales. (A valid call on the same handle is only out of order: it has not been reset.)"""
+    L, h, P, N = pb.lib(), _handle(), C.c_void_p(FAKE), None
+    before = pb.launch_count()
+    INV, NUL, UNS, ORD = pb.PYR_ERR_INVALID, pb.PYR_ERR_NULL, pb.PYR_ERR_UNSUPPORTED, pb.PYR_ERR_ORDER
+
+    def write(n=2, k=P, v=P, sb=5120, sn=512, sh=128, src=10, dtype=pb.PYR_BF16, idx=N, groups=1, istride=0, rows=10):
+        return L.pyr_pages_write(h, N, n, N, k, v, sb, sn, sh, src, dtype, idx, groups, istride, N, rows, N)
+
+    assert write() == ORD and write(idx=P, groups=4, istride=40, rows=99) == ORD and write(n=1, sb=7) == ORD
+    assert write(k=N) == NUL and write(v=N) == NUL and write(dtype=5) == UNS
+    assert write(n=-1) == INV and write(n=6) == INV and write(rows=-1) == INV and write(src=-1) == INV and write(rows=11) == INV
+    assert write(idx=P, groups=2) == INV and write(idx=P, istride=-1) == INV and write(sh=64) == INV and write(sn=-512) == INV
+    assert write(sn=516) == INV and write(k=C.c_void_p(FAKE + 8)) == INV and write(idx=P, rows=(1 << 30) + 1) == UNS
+
+    def read(n=2, k=P, v=P, sb=5120, sn=512, sh=128, dtype=pb.PYR_F32, rows=10):
+        return L.pyr_pages_read(h, N, n, N, k, v, sb, sn, sh, dtype, N, rows, N)
+
+    assert read() == ORD and read(k=N) == NUL and read(dtype=9) == UNS and read(rows=-1) == INV and read(n=6) == INV
+    assert read(sn=64) == INV and read(sb=64) == INV and read(n=1, sb=64) == ORD and read(rows=1, sn=64) == ORD
+
+    def attn(n=2, q=P, out=P, qb=1024, qt=1024, qh=128, ob=1024, ot=1024, oh=128, lse=N, t=1, hq=8, dtype=pb.PYR_BF16, scale=0.0):
+        return L.pyr_pages_attn(h, N, n, q, qb, qt, qh, out, ob, ot, oh, lse, t, hq, dtype, scale, N)
+
+    assert attn() == ORD and attn(lse=P, scale=0.5) == ORD and attn(n=6) == INV and attn(n=-1) == INV
+    assert attn(q=N) == NUL and attn(out=N) == NUL and attn(dtype=3) == UNS and attn(hq=6) == INV and attn(hq=0) == INV and attn(t=0) == INV
+    assert attn(scale=-1.0) == INV and attn(scale=float("inf")) == INV and attn(scale=float("nan")) == INV
+    assert attn(oh=64) == INV and attn(ob=64) == INV and attn(t=2, ot=64) == INV and attn(qh=132) == INV and attn(t=1 << 20) == UNS
+
+    assert L.pyr_pages_reserve(h, N, 2, N, -1, N) == INV and L.pyr_pages_reserve(h, N, 6, N, 1, N) == INV
+    assert L.pyr_pages_reserve(h, N, 2, P, -1, N) == ORD
+    assert L.pyr_pages_fork(h, N, P, 1, N) == NUL and L.pyr_pages_fork(h, P, N, 1, N) == NUL and L.pyr_pages_fork(h, P, P, 6, N) == INV
+    assert L.pyr_pages_trim(h, N, 6, N, N) == INV and L.pyr_pages_trim(h, P, -2, N, N) == INV
+    assert L.pyr_pages_compact(h, N, P, 1, N, 1, 0, N, 1, N) == NUL and L.pyr_pages_compact(h, P, P, 1, P, 3, 0, N, 1, N) == INV
+    assert L.pyr_pages_compact(h, P, P, 1, N, 1, 0, N, -1, N) == INV and L.pyr_pages_compact(h, P, P, 6, N, 1, 0, N, 1, N) == INV
+    assert pb.launch_count() == before
+    L.pyr_pages_free(h)
+
+
 HARNESS = r"""
 #include "pages_index.h"
 using namespace pyr;
