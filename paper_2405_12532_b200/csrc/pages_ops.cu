@@ -328,6 +328,14 @@ __device__ __forceinline__ RowPlace row_place(const PagesView& p, int l, int h, 
   return r;
 }
 
+// A row's codes are 64 bytes (32 with 64 dimensions), and rows between kept ones are not wanted: without the hint the L2 cache
+// fetches lines of 128 bytes (64 lists of 32 heads, 1155 of 2176 rows: 170 us, 162 with it; 1.56 times the kept rows' bytes read).
+__device__ __forceinline__ uint4 load_codes(const uint8_t* p) {
+  uint4 r;
+  asm volatile("ld.global.L2::64B.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
+  return r;
+}
+
 // The bytes that one warp moves for a tile of destination rows, held in registers between the reads and the writes.
 template <int D, int G>
 struct TileRows {
@@ -345,8 +353,8 @@ struct TileRows {
       const uint8_t* b = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, from.tile, first + row));
       const int rr = __shfl_sync(0xffffffffu, from.row, first + row);
       if (b) {
-        k[i] = *reinterpret_cast<const uint4*>(b + tile_k_row(D, rr) + 16 * c);
-        v[i] = *reinterpret_cast<const uint4*>(b + tile_v_row(D, rr) + 16 * c);
+        k[i] = load_codes(b + tile_k_row(D, rr) + 16 * c);
+        v[i] = load_codes(b + tile_v_row(D, rr) + 16 * c);
       }
     }
 #pragma unroll
