@@ -357,12 +357,18 @@ struct CoreBody {
 // Operands are f16. A code masked in place is an operand already: as the bits of an f16 number a nibble n in bits 0 .. 3 is the
 // subnormal n 2^-24, in bits 4 .. 7 it is n 2^-20, both exact, so that a word's eight codes take one shift and four masks
 // and nothing is added or converted. (The factors go into the queries for K, into the sums at the end for V.) What f16 lacks
-// is range, so both factors that are not codes are normalised by powers of two: a query row so that its largest element is near
-// f16's (what is then below f16's smallest step is below 2^-35 of that element), and the scales that multiply P, which f16 holds to 2^-12,
-// by a factor per group that follows them (`norm`).
+// is range, so both factors that are not codes are normalised by powers of two: a query row so that its largest element is
+// near f16's (what is then below f16's smallest step is below 2^-35 of that element), and the scales that multiply P, which
+// f16 holds to 2^-11, by a factor per group that follows them (`norm`).
 // V's codes have a mean of 7.5, so that o grows with the number of rows while what matters in it grows with its root. The
-// instruction truncates its sums, and an o far above what matters would let that show (relative 2^-25 a tile): every
-// kCentre steps what a group's o have in common is moved to the group's sum of zeros, which is kept apart and rounded.
+// instruction truncates its sums, and an o far above what matters would let that show: every kCentre steps what a group's o
+// have in common is moved to the group's sum of zeros, which is kept apart and rounded. (100 k rows a list, error against 64
+// bits: 1.65e-3 is the output's own rounding, 1.77e-3 with 4 or 8, 1.78e-3 with 16, 1.90e-3 with 64; the rest is P's.)
+//
+// What bounds it: 273 instructions a tile and warp, 88 of them to take codes out of words, half of all on the integer pipe (64 % busy
+// in the main loop) and the rest waiting for one another in 11 warps an SM: 158 registers allow no more (15 warps with 128,
+// some of them spilled, are as fast). Measured with an idle start (64 lists of 1088 rows, 32 heads, 321 MB): 77 us = 4.2 TB/s;
+// 5 us pass before the first tile is there and 7 from the last tile to the end (merging).
 __device__ __forceinline__ void mma_full(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
                "{%0, %1, %2, %3};"
@@ -398,7 +404,7 @@ struct MmaBody {
   static constexpr int kDim = D, COLS = 8, kWarps = 11, kBlocks = 1, kQueryFloats = 0;
   static constexpr int kTileBytes = kPageTile * (D + 8 * G), kStages = kTileBytes > 2304 ? 2 : 3;
   static constexpr float kLazy = 8.f;            // the maximum is raised once a score is 2^8 above it
-  static constexpr int kCentre = 64;
+  static constexpr int kCentre = 8;
   uint32_t qf[X][4];
   float qsum[G][2];                              // sums of the queries over a group
   float o[X][2][4], zacc[G][2], norm[G], m[2], ref[2], l[2], raise[2], sc2[2];
