@@ -38,9 +38,6 @@ constexpr int kMaxWarps = 12;
 
 __device__ __forceinline__ void record(int* status, int code) { atomicCAS(status, 0, code); }
 
-template <class T> __device__ __forceinline__ float to_f(T x);
-template <> __device__ __forceinline__ float to_f<float>(float x) { return x; }
-template <> __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
 template <class T> __device__ __forceinline__ T from_f(float x);
 template <> __device__ __forceinline__ float from_f<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
@@ -170,12 +167,13 @@ struct Layout {
   static constexpr int total = Body::kWarps * warp_bytes;
 };
 
-// ------------------------------------------------------------------ one warp's tiles, on CUDA cores
-// Lane 4 i + j. K: rows i and i + 8, the quarter of the dimensions that chunk j of a stored row holds. V: the eighth of the
+// ------------------------------------------------------------------ one warp's tiles, on CUDA cores (fp32)
+// Every product in fp32: fp32 outputs are held to what fp32 can do, which operands of fewer bits cannot. Bound by its
+// multiply-adds where a KV head has several query rows (2 x 128 of them a row and column). Lane 4 i + j. K: rows i and i + 8, the quarter of the dimensions that chunk j of a stored row holds. V: the eighth of the
 // dimensions that chunk i holds, of the rows j, j + 4, j + 8, j + 12.
-template <class T, int D, int GROUP>
+template <int D, int GROUP>
 struct CoreBody {
-  using Type = T;
+  using Type = float;
   static constexpr int kDim = D, COLS = 4, kWarps = 7, kBlocks = 1, kQueryFloats = COLS * D;   // queries lie in shared memory
   static constexpr int kStages = 3, kTileBytes = kPageTile * (D + 8 * (D / GROUP));
   static constexpr int G = D / GROUP, U = GROUP / 32, X = D / 32;   // X: words of K / halves of V in a lane's chunk
@@ -195,10 +193,10 @@ struct CoreBody {
       for (int g = 0; g < G; ++g) qsum[x][g] = 0.f;
       const int col = col0 + x, tok = col / a.rep, head = c.h * a.rep + col % a.rep;
       limit[x] = c.len - (a.T - 1 - tok);
-      const T* q = static_cast<const T*>(a.q) + (int64_t)c.entry * a.qsb + (int64_t)tok * a.qst + (int64_t)head * a.qsh;
+      const float* q = static_cast<const float*>(a.q) + (int64_t)c.entry * a.qsb + (int64_t)tok * a.qst + (int64_t)head * a.qsh;
       // queries in the order of the stored codes
       for (int p = lane; p < D; p += 32)
-        qs[x * D + p] = x < ncols ? to_f(q[8 * k_slot_word(D, GROUP, p >> 3) + (p & 7)]) : 0.f;
+        qs[x * D + p] = x < ncols ? q[8 * k_slot_word(D, GROUP, p >> 3) + (p & 7)] : 0.f;
     }
     __syncwarp();
 #pragma unroll
@@ -338,7 +336,7 @@ struct CoreBody {
 #pragma unroll
       for (int y = 0; y < 4 * X; ++y)
         if (j == (y & 3))
-          static_cast<T*>(a.out)[at.out + 4 * v_slot_half(D, GROUP, i * X + (y >> 2)) + (y & 3)] = from_f<T>(acc[x][y] * inv);
+          static_cast<float*>(a.out)[at.out + 4 * v_slot_half(D, GROUP, i * X + (y >> 2)) + (y & 3)] = acc[x][y] * inv;
       if (lane == 0 && a.lse) a.lse[at.lse] = lse_of(m[x], l[x]);
     }
   }
@@ -381,7 +379,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   return y;
 }
 __device__ __forceinline__ uint32_t as_u32(__half2 x) { return reinterpret_cast<uint32_t&>(x); }
-__device__ __forceinline__ __half2 as_half2(uint32_t x) { return reinterpret_cast<__half2&>(x); }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return as_u32(__floats2half2_rn(lo, hi)); }
 // The four pairs of codes (nibbles k and k + 4) of x as f16 pairs: times 2^-24 for k = 0 and 2, times 2^-20 for k = 1 and 3.
 __device__ __forceinline__ void codes4(uint32_t x, uint32_t* y) {
@@ -1139,7 +1136,7 @@ cudaError_t run_attn(const PagesAttnArgs& a, cudaStream_t s) {
 
 template <int D, int GROUP>
 cudaError_t pick(const PagesAttnArgs& a, cudaStream_t s) {
-  return a.dtype == PYR_F32 ? run_attn<CoreBody<float, D, GROUP>>(a, s) : run_attn<MmaBody<D, GROUP>>(a, s);
+  return a.dtype == PYR_F32 ? run_attn<CoreBody<D, GROUP>>(a, s) : run_attn<MmaBody<D, GROUP>>(a, s);
 }
 
 }  // namespace
