@@ -171,10 +171,10 @@ struct Layout {
 // Every product in fp32: fp32 outputs are held to what fp32 can do, which operands of fewer bits cannot. Bound by its
 // multiply-adds where a KV head has several query rows (2 x 128 of them a row and column). Lane 4 i + j. K: rows i and i + 8, the quarter of the dimensions that chunk j of a stored row holds. V: the eighth of the
 // dimensions that chunk i holds, of the rows j, j + 4, j + 8, j + 12.
-template <int D, int GROUP>
+template <int D, int GROUP, int kCols>
 struct CoreBody {
   using Type = float;
-  static constexpr int kDim = D, COLS = 4, kWarps = 7, kBlocks = 1, kQueryFloats = COLS * D;   // queries lie in shared memory
+  static constexpr int kDim = D, COLS = kCols, kWarps = 7, kBlocks = 1, kQueryFloats = COLS * D;   // queries lie in shared memory
   static constexpr int kStages = 3, kTileBytes = kPageTile * (D + 8 * (D / GROUP));
   static constexpr int G = D / GROUP, U = GROUP / 32, X = D / 32;   // X: words of K / halves of V in a lane's chunk
   float acc[COLS][4 * X];
@@ -1136,7 +1136,12 @@ cudaError_t run_attn(const PagesAttnArgs& a, cudaStream_t s) {
 
 template <int D, int GROUP>
 cudaError_t pick(const PagesAttnArgs& a, cudaStream_t s) {
-  return a.dtype == PYR_F32 ? run_attn<CoreBody<D, GROUP>>(a, s) : run_attn<MmaBody<D, GROUP>>(a, s);
+  if (a.dtype != PYR_F32) return run_attn<MmaBody<D, GROUP>>(a, s);
+  // fp32 pays for every column whether it is there or not: 16 lists of 1088 rows, 32 heads, one column: 207 us with four, 92 with
+  // one; two: 118 and 57
+  const int cols = a.T * a.rep;
+  return cols == 1 ? run_attn<CoreBody<D, GROUP, 1>>(a, s) : cols == 2 ? run_attn<CoreBody<D, GROUP, 2>>(a, s)
+                                                                       : run_attn<CoreBody<D, GROUP, 4>>(a, s);
 }
 
 }  // namespace

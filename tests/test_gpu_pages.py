@@ -274,6 +274,18 @@ def test_attention_against_fp64(D, group, page_rows, hq, hkv, q_len, lens, dtype
     _check_attn(p, q, range(len(lens)), out, lse, D ** -0.5)
 
 
+@pytest.mark.parametrize("hq,q_len", [(2, 2), (4, 1), (2, 1), (6, 1)])
+@pytest.mark.parametrize("D,group", FORMATS)
+def test_fp32_attention_with_one_two_and_more_columns(D, group, hq, q_len):
+    lens = [70, 3, 1, 0, 200]
+    p = _pages(2, D, group, 32, 16, 5, 7)
+    _fill(p, lens, seed=24, dtype=F32)
+    q = _rand(5, q_len, hq, D, seed=25)
+    out, lse = p.attn(q, lse=True)
+    assert p.status() == 0
+    _check_attn(p, q, range(5), out, lse, D ** -0.5)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_attention_strides_lists_scale(dtype):
     """Lists in any order and more than once, token-major and head-major tensors, a scale of the caller's, scores that are far
