@@ -34,6 +34,7 @@ constexpr int kSegmentUnits = 6;
 // A warp's share is at least this much: next to nothing, since small calls are bound by a warp's own latency, 2 us a step
 // (with 2 instead of 4 and 8: 385 rows of 32 heads 20.5, 22.5 and 24.6 us, the small fp32 model 21, 26 and 32 us).
 constexpr int kMinUnits = 2;
+constexpr int kCtaTiles = 8;             // a (entry, head, column group) of up to this many tiles a warp may be a CTA's alone
 constexpr int kMaxWarps = 12;
 
 __device__ __forceinline__ void record(int* status, int code) { atomicCAS(status, 0, code); }
@@ -53,6 +54,7 @@ struct Piece {
 struct Sched {
   long long sums[kMaxWarps + 1];
   long long first_unit[kMaxWarps];   // of the entry in which a warp's range starts
+  long long share_u, share_units;    // the CTA's units, where it takes one (entry, head, column group)
   int entry[kMaxWarps], list[kMaxWarps], len[kMaxWarps];
   int abort_flag;
   int last[2], open_c1[2], open_count[2], open_piece[2];   // what the CTA leaves for others
@@ -834,30 +836,59 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
     lo_mine = block_scan<kWarps + 1>(u_mine, sh.sums, &part);
     total += part;
   }
-  const long long workers = (long long)gridDim.x * kWarps;
-  long long q = total >> 31 ? (total + workers - 1) / workers : (long long)(((uint32_t)total + (uint32_t)workers - 1u) / (uint32_t)workers);
-  if (q < kMinUnits) q = kMinUnits;
-  const long long cta_units = q * kWarps, cta_u = blockIdx.x * cta_units;
-  if (cta_u >= total) return;                    // the whole CTA: nothing is in flight
-  long long run = 0;
-  for (int i0 = 0; i0 < a.n && run < cta_u + cta_units; i0 += kThreads) {
-    const int i = i0 + t;
-    long long u = u_mine, lo = lo_mine;
-    if (a.n > kThreads) {
-      u = i < a.n ? entry_units(a, i, cgs, &l_mine, &len_mine) : 0;
-      lo = run + block_scan<kWarps + 1>(u, sh.sums, &part);
+  // With no more (entry, head, column group)s than CTAs, and none long, each CTA takes one: no state crosses CTAs then, which
+  // would cost more than the shorter way to the end saves (a step in a graph, us, even shares -> one a CTA; heads of queries
+  // and of keys: 1 list x 385 rows, 32/32: 13.8 -> 9.8; 4 x 700, 32/32: 15.2 -> 10.9; 16 x 1300, 64/8: 19.3 -> 14.9; but
+  // 1 x 2500, 32/32, 14 tiles a warp: 16.4 -> 18.2).
+  long long cta_u = 0, cta_units = 0;
+  bool whole_ones = false;
+  if (a.n <= kThreads) {
+    const bool there = u_mine > 0;
+    const bool any_long = __syncthreads_or(there && attn_tiles(len_mine) > kCtaTiles * kWarps);
+    const int per_entry = a.p.Hkv * cgs;
+    const long long all = (long long)__syncthreads_count(there) * per_entry;
+    whole_ones = !any_long && all <= gridDim.x;
+    if (whole_ones) {
+      if (blockIdx.x >= all) return;             // the whole CTA: nothing is in flight
+      const int e = blockIdx.x / per_entry;
+      const long long order = block_scan<kWarps + 1>(there, sh.sums, &part);
+      if (there && order == e) {
+        const int tiles = (int)attn_tiles(len_mine);
+        sh.share_u = lo_mine + (long long)(blockIdx.x - e * per_entry) * (tiles + kSegmentUnits) + kSegmentUnits;
+        sh.share_units = tiles;
+        for (int w = 0; w < kWarps; ++w) { sh.entry[w] = t; sh.first_unit[w] = lo_mine; sh.list[w] = l_mine; sh.len[w] = len_mine; }
+      }
+      __syncthreads();
+      cta_u = sh.share_u;
+      cta_units = sh.share_units;
     }
-    for (int w = 0; w < kWarps; ++w) {
-      const long long s = cta_u + w * q;
-      if (s >= lo && s < lo + u) { sh.entry[w] = i; sh.first_unit[w] = lo; sh.list[w] = l_mine; sh.len[w] = len_mine; }
-    }
-    run += part;
   }
-  __syncthreads();
+  if (!whole_ones) {
+    const long long workers = (long long)gridDim.x * kWarps;
+    const long long q = total >> 31 ? (total + workers - 1) / workers : (long long)(((uint32_t)total + (uint32_t)workers - 1u) / (uint32_t)workers);
+    cta_units = max(q, (long long)kMinUnits) * kWarps;
+    cta_u = blockIdx.x * cta_units;
+    if (cta_u >= total) return;                  // the whole CTA: nothing is in flight
+    long long run = 0;
+    for (int i0 = 0; i0 < a.n && run < cta_u + cta_units; i0 += kThreads) {
+      const int i = i0 + t;
+      long long u = u_mine, lo = lo_mine;
+      if (a.n > kThreads) {
+        u = i < a.n ? entry_units(a, i, cgs, &l_mine, &len_mine) : 0;
+        lo = run + block_scan<kWarps + 1>(u, sh.sums, &part);
+      }
+      for (int w = 0; w < kWarps; ++w) {
+        const long long s = cta_u + cta_units * w / kWarps;
+        if (s >= lo && s < lo + u) { sh.entry[w] = i; sh.first_unit[w] = lo; sh.list[w] = l_mine; sh.len[w] = len_mine; }
+      }
+      run += part;
+    }
+    __syncthreads();
+  }
 
   const int w_of = warp < kWarps ? warp : lane;          // the warp whose range this thread works on or loads for
-  const long long u_warp = cta_u + w_of * q;
-  const int mine = w_of < kWarps ? (int)max(0LL, min(q, total - u_warp)) : 0;    // its units
+  const long long u_warp = cta_u + cta_units * min(w_of, kWarps) / kWarps;
+  const int mine = w_of < kWarps ? (int)max(0LL, min(cta_u + cta_units * (w_of + 1) / kWarps, total) - u_warp) : 0;    // its units
 
   if (warp == kWarps) {
     // ------------------------------------------------------------ loaders: lane w for warp w
