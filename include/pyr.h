@@ -418,7 +418,7 @@ typedef struct {
   int32_t head_dim;    /* 64 or 128                                            */
   int32_t group;       /* dimensions that share a scale: 32, 64 or 128, at most head_dim */
   int32_t page_rows;   /* rows of a page: a multiple of 16, at most 1024       */
-  int32_t n_pages;     /* pages of the pool                                    */
+  int32_t n_pages;     /* pages of the pool (2^56 bytes at most)               */
   int32_t n_lists;     /* at most 2^19                                         */
   int32_t max_pages;   /* pages that one list can hold                         */
   uint32_t flags;      /* 0                                                    */

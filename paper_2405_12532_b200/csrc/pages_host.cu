@@ -9,6 +9,7 @@ namespace {
 
 constexpr size_t kAlign = 256;
 constexpr int32_t kMaxRows = 1 << 30;      // of a call's entry: row arithmetic stays within 32 bits
+constexpr uint64_t kMaxPool = 1ull << 56;  // bytes of a pool
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 struct PagesLayout {
@@ -29,6 +30,9 @@ pyr_status_t validate(const pyr_pages_config_t* c) {
   // a list's length is an int32, and so is every page id that the reserve scan rounds up to whole slices
   if ((int64_t)c->max_pages * c->page_rows > 0x7fffffff - pyr::kMaxPageRows || c->n_pages > 0x7fffffff - pyr::kReserveSlice)
     return PYR_ERR_UNSUPPORTED;
+  // the buffer's size in bytes must be a number of 64 bits with room to spare (the table's is: 2^19 lists of 2^27 pages)
+  const uint64_t page_bytes = (uint64_t)c->n_kv_heads * (c->page_rows / pyr::kPageTile) * pyr::pages_tile_bytes(c->head_dim, c->group);
+  if (page_bytes > kMaxPool / (uint64_t)c->n_pages) return PYR_ERR_UNSUPPORTED;
   return PYR_OK;
 }
 

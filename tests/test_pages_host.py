@@ -72,6 +72,18 @@ def test_pages_bytes_alloc_and_view():
     assert L.pyr_pages_free(h) == pb.PYR_OK and L.pyr_pages_free(None) == pb.PYR_ERR_NULL
 
 
+@pytest.mark.parametrize("over", [dict(n_pages=0x7fffffff - 4096, n_kv_heads=65535, page_rows=1024, group=32, max_pages=1),
+                                  dict(n_pages=0x7fffffff - 4096, n_kv_heads=52429, page_rows=1024, group=32, max_pages=1),
+                                  dict(n_pages=1 << 30, n_kv_heads=512, page_rows=1024, max_pages=1)])
+def test_pools_whose_size_would_not_fit_are_refused(over):
+    """(2^64 and more bytes would come out as a small number, and a small buffer would pass for such a pool.)"""
+    b, h = C.c_size_t(0), C.c_void_p()
+    assert pb.lib().pyr_pages_bytes(C.byref(_cfg(**over)), C.byref(b), None) == pb.PYR_ERR_UNSUPPORTED
+    assert pb.lib().pyr_pages_alloc(C.byref(_cfg(**over)), C.c_void_p(FAKE), (1 << 64) - 1, C.byref(h)) == pb.PYR_ERR_UNSUPPORTED
+    nbytes, _ = pb.pyr_pages_bytes(_cfg(n_pages=1 << 30, n_kv_heads=64, page_rows=32, max_pages=1))
+    assert nbytes > (1 << 30) * 64 * 2 * op.tile_bytes(128, 64)
+
+
 def test_pages_calls_need_a_reset_first():
     """Every launching call before pyr_pages_reset is out of order; nothing is launched."""
     L, h, P = pb.lib(), _handle(), C.c_void_p(FAKE)
