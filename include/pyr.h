@@ -470,7 +470,8 @@ pyr_status_t pyr_pages_write(pyr_pages_t* pages, const int32_t* lists, int32_t n
                              int32_t dtype, const int32_t* idx, int32_t idx_groups, int64_t idx_stride, const int32_t* counts,
                              int32_t n_rows, void* stream);
 
-/* Reads rows back as the values they stand for: k, v (device) are [n, n_rows, n_kv_heads, head_dim], strided as above.
+/* Reads rows back as the values they stand for: k, v (device) are [n, n_rows, n_kv_heads, head_dim], strided as above, no two rows
+ * over one another (each stride passes what the smaller ones span).
  * Row x of entry i is row first_i + x of its list (first NULL: 0). Rows at or behind a list's length, and rows x >= count_i,
  * are left as they were. */
 pyr_status_t pyr_pages_read(pyr_pages_t* pages, const int32_t* lists, int32_t n, const int32_t* first, void* k, void* v,
@@ -479,7 +480,7 @@ pyr_status_t pyr_pages_read(pyr_pages_t* pages, const int32_t* lists, int32_t n,
 
 /*
  * Attention over the lists' rows. q, out (device) are [n, q_len, n_q_heads, head_dim], strides in elements, D contiguous
- * and rows 16-byte aligned; n_q_heads a multiple of n_kv_heads. Query token t of entry i sees the first
+ * and rows 16-byte aligned, out's rows apart as in pyr_pages_read; n_q_heads a multiple of n_kv_heads. Query token t of entry i sees the first
  * len_i - (q_len - 1 - t) rows: with q_len = 1 all of them, the row stored last included; with more, the last q_len rows are
  * those of the query tokens themselves (a chunk of a prompt, drafted tokens). A token that sees no row gets zeros.
  * lse (device, may be NULL) is [n, n_q_heads, q_len] fp32, the natural log of the softmax denominator, -inf for such a

@@ -2,6 +2,7 @@
 // reads device memory: lengths and tables live on the device, and what depends on them is checked by the kernels.
 #include <cmath>
 #include <new>
+#include <utility>
 
 #include "pyr_internal.h"
 
@@ -112,6 +113,21 @@ pyr_status_t check_rows(const pyr_pages* h, const void* a, const void* b, int32_
       (sh * eb) % 16)
     return PYR_ERR_INVALID;
   return PYR_OK;
+}
+
+// Whether the rows of a tensor that is written lie apart: each stride passes everything that the smaller ones span.
+bool rows_apart(const pyr_pages* h, int64_t sb, int64_t sn, int64_t sh, int64_t n, int64_t rows, int64_t heads) {
+  struct { int64_t stride, size; } d[3] = {{sh, heads}, {sn, rows}, {sb, n}};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2 - i; ++j)
+      if (d[j].stride > d[j + 1].stride) std::swap(d[j], d[j + 1]);
+  __int128 span = h->cfg.head_dim;
+  for (const auto& x : d) {
+    if (x.size <= 1) continue;
+    if (x.stride < span) return false;
+    span += (__int128)x.stride * (x.size - 1);
+  }
+  return true;
 }
 
 pyr_status_t check_idx(const pyr_pages* h, const int32_t* idx, int32_t groups, int64_t stride, int32_t n_rows) {
@@ -254,8 +270,7 @@ pyr_status_t pyr_pages_read(pyr_pages_t* h, const int32_t* lists, int32_t n, con
   if (st != PYR_OK) return st;
   if (n_rows < 0 || !default_lists_fit(h, lists, n)) return PYR_ERR_INVALID;
   // rows that overlap would be written by several threads
-  if (n_rows > 1 && sn < h->cfg.head_dim) return PYR_ERR_INVALID;
-  if (n > 1 && sb < h->cfg.head_dim) return PYR_ERR_INVALID;
+  if (!rows_apart(h, sb, sn, sh, n, n_rows, h->cfg.n_kv_heads)) return PYR_ERR_INVALID;
   if (n_rows > kMaxRows) return PYR_ERR_UNSUPPORTED;
   PYR_PAGES_READY(h);
   if (n == 0 || n_rows == 0) return PYR_OK;
@@ -278,9 +293,9 @@ pyr_status_t pyr_pages_attn(pyr_pages_t* h, const int32_t* lists, int32_t n, con
   st = check_rows(h, q, q, dtype, qsb, qst, qsh, n, q_len, n_q_heads);
   if (st == PYR_OK) st = check_rows(h, out, out, dtype, osb, ost, osh, n, q_len, n_q_heads);
   if (st != PYR_OK) return st;
-  if ((q_len > 1 && ost < h->cfg.head_dim) || (n > 1 && osb < h->cfg.head_dim)) return PYR_ERR_INVALID;
   const int64_t cols = (int64_t)q_len * (n_q_heads / h->cfg.n_kv_heads);
   if (cols > (1 << 20)) return PYR_ERR_UNSUPPORTED;
+  if (!rows_apart(h, osb, ost, osh, n, q_len, n_q_heads)) return PYR_ERR_INVALID;
   PYR_PAGES_READY(h);
   if (n == 0) return PYR_OK;
   pyr::PagesAttnArgs a;

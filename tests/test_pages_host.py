@@ -144,6 +144,28 @@ def test_pages_arguments_are_refused_before_any_launch():
     L.pyr_pages_free(h)
 
 
+def test_tensors_to_be_written_must_not_overlap_themselves():
+    """(Two threads would write one place, in any order.) Dimensions in any order of strides, and dimensions of size 1, are fine."""
+    L, h, P, N = pb.lib(), _handle(), C.c_void_p(FAKE), None
+    INV, ORD = pb.PYR_ERR_INVALID, pb.PYR_ERR_ORDER
+
+    def read(sb, sn, sh, n=2, rows=10):
+        return L.pyr_pages_read(h, N, n, N, P, P, sb, sn, sh, pb.PYR_BF16, N, rows, N)
+
+    def attn(sb, st, sh, n=2, t=3, hq=8):
+        return L.pyr_pages_attn(h, N, n, P, 0, 0, 128, P, sb, st, sh, N, t, hq, pb.PYR_BF16, 0.0, N)
+
+    # 4 heads of 128: rows then heads, heads then rows, entries innermost, padded
+    assert read(5120, 512, 128) == ORD and read(5120, 128, 1280) == ORD and read(128, 1024, 256) == ORD and read(9000, 640, 136) == ORD
+    assert read(5120, 128, 128) == INV and read(512, 512, 128) == INV and read(5112, 512, 128) == INV and read(5120, 504, 128) == INV
+    assert read(5120, 128, 1272) == INV and read(0, 512, 128) == INV and read(0, 512, 128, n=1) == ORD and read(512, 0, 128, rows=1) == ORD
+    # 8 heads of 128, 3 tokens
+    assert attn(3 * 1024, 1024, 128) == ORD and attn(3 * 1024, 128, 384) == ORD and attn(1024, 2048, 128) == ORD
+    assert attn(1024, 1024, 128) == INV and attn(3 * 1024, 128, 128) == INV and attn(2 * 1024, 1024, 128) == INV
+    assert attn(1024, 0, 128, t=1) == ORD and attn(0, 1024, 128, n=1) == ORD
+    L.pyr_pages_free(h)
+
+
 HARNESS = r"""
 #include "pages_index.h"
 using namespace pyr;
