@@ -409,7 +409,8 @@ pyr_status_t pyr_glue_argmax(const void* x, int32_t* out, int64_t rows, int32_t 
  * asynchronous call: the list concerned (or, in pyr_pages_reserve, the whole call) is left as it was, a pyr_status_t is
  * recorded in the handle's status word and pyr_pages_status reports it. No such error makes a kernel leave its buffers.
  * Rows in a slot whose page id is out of range take no part in attention and are not read back.
- * The GPU that holds the buffer must be the current one in every call. At most 2^30 rows an entry and call.
+ * The GPU that holds the buffer must be the current one in every call. At most 2^30 rows an entry and call, and 2^31 - 1 tiles
+ * of 16 rows over a call's entries and KV heads.
  *
  * In every call `lists` (device int32 [n]) names the list of each entry; NULL means lists 0 .. n-1. n = 0 does nothing.
  */

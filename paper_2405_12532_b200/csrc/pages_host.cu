@@ -115,6 +115,12 @@ pyr_status_t check_rows(const pyr_pages* h, const void* a, const void* b, int32_
   return PYR_OK;
 }
 
+// Whether a call's tiles, of all entries and heads, can be counted in 31 bits (a launch has a warp for each).
+bool tiles_fit(const pyr_pages* h, int64_t n, int32_t n_rows) {
+  const int64_t tiles = ((int64_t)n_rows + 2 * pyr::kPageTile - 2) / pyr::kPageTile;
+  return tiles == 0 || n * h->cfg.n_kv_heads <= 0x7fffffff / tiles;
+}
+
 // Whether the rows of a tensor that is written lie apart: each stride passes everything that the smaller ones span.
 bool rows_apart(const pyr_pages* h, int64_t sb, int64_t sn, int64_t sh, int64_t n, int64_t rows, int64_t heads) {
   struct { int64_t stride, size; } d[3] = {{sh, heads}, {sn, rows}, {sb, n}};
@@ -250,7 +256,7 @@ pyr_status_t pyr_pages_write(pyr_pages_t* h, const int32_t* lists, int32_t n, co
   if (st == PYR_OK) st = check_idx(h, idx, idx_groups, idx_stride, n_rows);
   if (st != PYR_OK) return st;
   if (n_rows < 0 || src_rows < 0 || (!idx && n_rows > src_rows)) return PYR_ERR_INVALID;
-  if (n_rows > kMaxRows) return PYR_ERR_UNSUPPORTED;
+  if (n_rows > kMaxRows || !tiles_fit(h, n, n_rows)) return PYR_ERR_UNSUPPORTED;
   PYR_PAGES_READY(h);
   if (n == 0 || n_rows == 0) return PYR_OK;
   pyr::PagesWriteArgs a;
@@ -271,7 +277,7 @@ pyr_status_t pyr_pages_read(pyr_pages_t* h, const int32_t* lists, int32_t n, con
   if (n_rows < 0 || !default_lists_fit(h, lists, n)) return PYR_ERR_INVALID;
   // rows that overlap would be written by several threads
   if (!rows_apart(h, sb, sn, sh, n, n_rows, h->cfg.n_kv_heads)) return PYR_ERR_INVALID;
-  if (n_rows > kMaxRows) return PYR_ERR_UNSUPPORTED;
+  if (n_rows > kMaxRows || !tiles_fit(h, n, n_rows)) return PYR_ERR_UNSUPPORTED;
   PYR_PAGES_READY(h);
   if (n == 0 || n_rows == 0) return PYR_OK;
   pyr::PagesWriteArgs a;
@@ -333,7 +339,7 @@ pyr_status_t pyr_pages_compact(pyr_pages_t* h, const int32_t* src, const int32_t
   if (st == PYR_OK) st = check_idx(h, idx, idx_groups, idx_stride, n_rows);
   if (st != PYR_OK) return st;
   if (n_rows < 0) return PYR_ERR_INVALID;
-  if (n_rows > kMaxRows) return PYR_ERR_UNSUPPORTED;
+  if (n_rows > kMaxRows || !tiles_fit(h, n, n_rows)) return PYR_ERR_UNSUPPORTED;
   if (n > 0 && (!src || !dst)) return PYR_ERR_NULL;
   PYR_PAGES_READY(h);
   if (n == 0) return PYR_OK;

@@ -166,6 +166,16 @@ def test_tensors_to_be_written_must_not_overlap_themselves():
     L.pyr_pages_free(h)
 
 
+def test_calls_with_more_tiles_than_a_launch_has_warps_are_refused_whole():
+    """(Refused by the second launch of a call, the first one's work would stay behind and spoil the next call.)"""
+    L, h, P, N = pb.lib(), _handle(n_kv_heads=64), C.c_void_p(FAKE), None
+    for rows, want in [(1 << 28, pb.PYR_ERR_ORDER), (1 << 30, pb.PYR_ERR_UNSUPPORTED)]:
+        assert L.pyr_pages_write(h, N, 1, N, P, P, 0, 8192, 128, 10, pb.PYR_BF16, P, 1, 0, N, rows, N) == want
+        assert L.pyr_pages_read(h, N, 1, N, P, P, 0, 8192, 128, pb.PYR_BF16, N, rows, N) == want
+        assert L.pyr_pages_compact(h, P, C.c_void_p(FAKE + 64), 1, P, 1, 0, N, rows, N) == want
+    L.pyr_pages_free(h)
+
+
 HARNESS = r"""
 #include "pages_index.h"
 using namespace pyr;
