@@ -274,6 +274,34 @@ def test_attention_against_fp64(D, group, page_rows, hq, hkv, q_len, lens, dtype
     _check_attn(p, q, range(len(lens)), out, lse, D ** -0.5)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lens", [[1408, 1, 0, 700], [1409, 1, 0, 700], [176, 176, 1408, 177], [16 * 8 * 11 - 1] * 3])
+@pytest.mark.parametrize("entries", [4, 18, 19, 37, 38, 74])
+def test_attention_on_both_sides_of_the_rules_that_deal_out_the_work(entries, lens, dtype):
+    """About as many (entry, head, column group)s as a B200 has SMs (148), and lists about as long as a CTA takes whole; some
+    entries name no list, and lists repeat."""
+    hkv, hq, D, T = 4, 12, 64, 3                    # 9 columns: 2 groups (bf16), 3 (fp32)
+    p = _pages(hkv, D, 32, 64, sum(-(-x // 64) for x in lens), len(lens), 23)
+    _fill(p, lens, seed=26, dtype=dtype)
+    q = _rand(entries, T, hq, D, seed=27, dtype=dtype)
+    lists = [(7 * i) % len(lens) for i in range(entries)]
+    named = list(lists)
+    for i in range(3, entries, 16):
+        named[i] = -1 if i % 32 == 3 else len(lens)
+    out = torch.full_like(q, -5.0)
+    got, lse = p.attn(q, _ids(*named), out=out, lse=True)
+    assert p.status() == (pb.PYR_ERR_INVALID if named != lists else 0)
+    first = {}
+    for i in range(entries):
+        if named[i] != lists[i]:
+            assert bool((out[i] == -5).all())
+        else:
+            first.setdefault(lists[i], []).append(i)
+    for l, at in first.items():
+        at = sorted({at[0], at[len(at) // 2], at[-1]})
+        _check_attn(p, q[at], [l] * len(at), out[at], lse[at], D ** -0.5)
+
+
 @pytest.mark.parametrize("hq,q_len", [(2, 2), (4, 1), (2, 1), (6, 1)])
 @pytest.mark.parametrize("D,group", FORMATS)
 def test_fp32_attention_with_one_two_and_more_columns(D, group, hq, q_len):
