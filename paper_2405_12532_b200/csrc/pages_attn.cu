@@ -1169,10 +1169,16 @@ template <int D, int GROUP>
 cudaError_t pick(const PagesAttnArgs& a, cudaStream_t s) {
   if (a.dtype != PYR_F32) return run_attn<MmaBody<D, GROUP>>(a, s);
   // fp32 pays for every column whether it is there or not: 16 lists of 1088 rows, 32 heads, one column: 207 us with four, 92 with
-  // one; two: 118 and 57
-  const int cols = a.T * a.rep;
-  return cols == 1 ? run_attn<CoreBody<D, GROUP, 1>>(a, s) : cols == 2 ? run_attn<CoreBody<D, GROUP, 2>>(a, s)
-                                                                       : run_attn<CoreBody<D, GROUP, 4>>(a, s);
+  // one; two: 118 and 57. Where lists cannot be long and there are SMs for it, columns go to CTAs of their own: the list is
+  // read once for each then, but a step, of which a warp has one or two, is that much shorter (7 lists x 4 heads, 272 rows,
+  // 4 columns: 13.8 us with four a CTA, 8.6 with one; 128 dimensions: 26.8 and 13.4).
+  const int sms = device_sm_count();
+  if (sms <= 0) return cudaErrorUnknown;
+  const long long cols = (long long)a.T * a.rep, pairs = (long long)a.n * a.p.Hkv;
+  const bool small = attn_tiles(a.p.max_pages * a.p.page_rows) <= kCtaTiles * CoreBody<D, GROUP, 4>::kWarps;
+  if (cols == 1 || (small && pairs * cols <= sms)) return run_attn<CoreBody<D, GROUP, 1>>(a, s);
+  if (cols == 2 || (small && pairs * ((cols + 1) / 2) <= sms)) return run_attn<CoreBody<D, GROUP, 2>>(a, s);
+  return run_attn<CoreBody<D, GROUP, 4>>(a, s);
 }
 
 }  // namespace
