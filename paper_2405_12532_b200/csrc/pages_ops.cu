@@ -8,6 +8,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kListThreads = 128;        // of a CTA that serves one list's table (1280 lists: 6.0 us to fork, 7.4 with 256)
+constexpr int kMoveThreads = 64;         // warps come and go on their own (64 lists of 32 heads, 1155 of 2176 rows: 160 us with 256, 152, 151)
 constexpr int kScanThreads = 1024;
 static_assert(kReserveSlice == kScanThreads * 4, "a thread of the scan owns four pages");
 
@@ -329,7 +330,8 @@ __device__ __forceinline__ RowPlace row_place(const PagesView& p, int l, int h, 
 }
 
 // A row's codes are 64 bytes (32 with 64 dimensions), and rows between kept ones are not wanted: without the hint the L2 cache
-// fetches lines of 128 bytes (64 lists of 32 heads, 1155 of 2176 rows: 170 us, 162 with it; 1.56 times the kept rows' bytes read).
+// fetches lines of 128 bytes (64 lists of 32 heads, 1155 of 2176 rows: 170 us and 1.56 times the kept rows' bytes read, 162 us and 1.13
+// times with it).
 __device__ __forceinline__ uint4 load_codes(const uint8_t* p) {
   uint4 r;
   asm volatile("ld.global.L2::64B.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
@@ -454,10 +456,10 @@ __device__ __forceinline__ void move_run(const PagesMoveArgs& a, int e, int h, i
 
 // The warp that is the last of its entry finishes it: no other looks at the entry's table any more.
 template <int D, int G, int kRun>
-__global__ void __launch_bounds__(kThreads) compact_move_kernel(PagesMoveArgs a, int runs, int64_t items) {
+__global__ void __launch_bounds__(kMoveThreads) compact_move_kernel(PagesMoveArgs a, int runs, int64_t items) {
   wait_for_previous();
   const int lane = threadIdx.x & 31;
-  const int64_t item = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  const int64_t item = (int64_t)blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5);
   if (item >= items) return;
   const int run = (int)(item % runs);
   const int h = (int)(item / runs % a.p.Hkv);
@@ -512,9 +514,9 @@ template <int D, int G, int kRun>
 cudaError_t run_runs(const PagesMoveArgs& a, cudaStream_t s) {
   const int runs = (a.n_rows + kRun * kPageTile - 1) / (kRun * kPageTile);
   const int64_t items = (int64_t)a.n * a.p.Hkv * runs;
-  const int64_t grid = (items + kThreads / 32 - 1) / (kThreads / 32);
+  const int64_t grid = (items + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
   if (grid > 0x7fffffffLL || (int64_t)a.p.Hkv * runs > 0x7fffffffLL) return cudaErrorInvalidValue;
-  return launch_behind(compact_move_kernel<D, G, kRun>, dim3((unsigned)grid), dim3(kThreads), 0, s, a, runs, items);
+  return launch_behind(compact_move_kernel<D, G, kRun>, dim3((unsigned)grid), dim3(kMoveThreads), 0, s, a, runs, items);
 }
 
 template <int D, int G>
@@ -524,7 +526,7 @@ cudaError_t run_move(const PagesMoveArgs& a, cudaStream_t s) {
     if (heads > 0x7fffffffLL) return cudaErrorInvalidValue;
     return launch_behind(compact_inplace_kernel<D, G>, dim3((unsigned)heads), dim3(kThreads), 0, s, a);
   }
-  // Runs of four tiles where there are enough of them to give every SM 32 warps (64 lists of 32 heads: 148 us), else a tile a
+  // Runs of four tiles where there are enough of them to give every SM 32 warps (64 lists of 32 heads: 151 us), else a tile a
   // warp: then a warp's own latency is what counts (4 lists of 8 heads, 717 rows: 6.6 us, 11 with runs of four).
   const int sms = device_sm_count();
   if (sms <= 0) return cudaErrorUnknown;
