@@ -13,7 +13,9 @@ namespace pyr {
 namespace {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 256;                 // of a CTA that writes an entry's few rows
+constexpr int kTileThreads = 64;                 // of one whose warps take a tile each and come and go on their own (8 x 2005 rows
+                                                 // of 40 heads written and read: 167.5 us with 256, 164.9, 163.2)
 constexpr int kFewRows = 512;                    // rows times heads of an entry that one CTA writes as fast as many
 constexpr uint32_t kNanWord = 0x7FC07FC0u;       // (scale, zero) of a group that has no finite range
 constexpr float kScaleMin = 7.888609052210118e-31f;   // 2^-100
@@ -292,10 +294,10 @@ __device__ __forceinline__ const int32_t* entry_idx(const PagesWriteArgs& a, int
 // rows of 128 dimensions, K and V, from bf16: 92 us = 4.6 TB/s of 420 MB, three quarters of the issue slots taken (eleven
 // instructions a value), with loads of four rows and both tensors in flight a warp and 32 warps an SM.
 template <class T, int D, int GROUP>
-__global__ void __launch_bounds__(kRowThreads, sizeof(T) == 2 ? 4 : 2) write_rows_kernel(PagesWriteArgs a, int blocks, int64_t items) {
+__global__ void __launch_bounds__(kTileThreads, sizeof(T) == 2 ? 16 : 8) write_rows_kernel(PagesWriteArgs a, int blocks, int64_t items) {
   wait_for_previous();
   const int lane = threadIdx.x & 31;
-  const int64_t item = (int64_t)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+  const int64_t item = (int64_t)blockIdx.x * (kTileThreads / 32) + (threadIdx.x >> 5);
   if (item >= items) return;
   const int blk = (int)(item % blocks);
   const int h = (int)(item / blocks % a.p.Hkv);
@@ -395,10 +397,10 @@ __device__ __forceinline__ void values8(uint32_t codes, uint32_t word, float* x)
 
 // One warp per (entry, KV head, tile of its list), as for writing.
 template <class T, int D, int GROUP>
-__global__ void __launch_bounds__(kRowThreads) read_rows_kernel(PagesWriteArgs a, int blocks, int64_t items) {
+__global__ void __launch_bounds__(kTileThreads) read_rows_kernel(PagesWriteArgs a, int blocks, int64_t items) {
   constexpr int LPR = D / 8, RPP = 32 / LPR, G = D / GROUP, P = kPageTile / RPP;
   const int lane = threadIdx.x & 31, sub = lane / LPR, wi = lane % LPR;
-  const int64_t item = (int64_t)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+  const int64_t item = (int64_t)blockIdx.x * (kTileThreads / 32) + (threadIdx.x >> 5);
   if (item >= items) return;
   const int blk = (int)(item % blocks);
   const int h = (int)(item / blocks % a.p.Hkv);
@@ -459,7 +461,7 @@ cudaError_t by_format(const PagesView& p, int dtype, F f) {
 struct RunWrite {
   const PagesWriteArgs& a; int blocks; int64_t items; unsigned grid; cudaStream_t s;
   template <class T, int D, int G> cudaError_t run() {
-    return launch_behind(write_rows_kernel<T, D, G>, dim3(grid), dim3(kRowThreads), 0, s, a, blocks, items);
+    return launch_behind(write_rows_kernel<T, D, G>, dim3(grid), dim3(kTileThreads), 0, s, a, blocks, items);
   }
 };
 struct RunFew {
@@ -472,7 +474,7 @@ struct RunFew {
 struct RunRead {
   const PagesWriteArgs& a; int blocks; int64_t items; unsigned grid; cudaStream_t s;
   template <class T, int D, int G> cudaError_t run() {
-    read_rows_kernel<T, D, G><<<grid, kRowThreads, 0, s>>>(a, blocks, items);
+    read_rows_kernel<T, D, G><<<grid, kTileThreads, 0, s>>>(a, blocks, items);
     return cudaGetLastError();
   }
 };
@@ -492,7 +494,7 @@ cudaError_t launch_pages_write(const PagesWriteArgs& a, int* launches, cudaStrea
   }
   const int words = (a.p.n_lists + 31) / 32;
   const int64_t items = (int64_t)a.n * a.p.Hkv * blocks;
-  const int64_t grid = (items + kRowThreads / 32 - 1) / (kRowThreads / 32);
+  const int64_t grid = (items + kTileThreads / 32 - 1) / (kTileThreads / 32);
   if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
   e = allow_shared<write_plan_kernel>(2 * (kMaxLists / 32) * 4);
   if (e != cudaSuccess) return e;
@@ -508,7 +510,7 @@ cudaError_t launch_pages_write(const PagesWriteArgs& a, int* launches, cudaStrea
 cudaError_t launch_pages_read(const PagesWriteArgs& a, int* launches, cudaStream_t s) {
   const int blocks = tiles_over(a.n_rows);
   const int64_t items = (int64_t)a.n * a.p.Hkv * blocks;
-  const int64_t grid = (items + kRowThreads / 32 - 1) / (kRowThreads / 32);
+  const int64_t grid = (items + kTileThreads / 32 - 1) / (kTileThreads / 32);
   if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
   const cudaError_t e = by_format(a.p, a.dtype, RunRead{a, blocks, items, (unsigned)grid, s});
   if (e == cudaSuccess) ++*launches;
