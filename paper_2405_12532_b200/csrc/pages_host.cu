@@ -102,7 +102,7 @@ bool default_lists_fit(const pyr_pages* h, const int32_t* lists, int32_t n) { re
 // looked at)
 pyr_status_t check_rows(const pyr_pages* h, const void* a, const void* b, int32_t dtype, int64_t sb, int64_t sn, int64_t sh,
                         int64_t n, int64_t rows, int heads) {
-  if (!a || !b) return PYR_ERR_NULL;
+  if ((!a || !b) && n > 0 && rows > 0) return PYR_ERR_NULL;      // (a tensor without elements needs no address)
   if (dtype != PYR_BF16 && dtype != PYR_F32) return PYR_ERR_UNSUPPORTED;
   const int D = h->cfg.head_dim, eb = dtype == PYR_BF16 ? 2 : 4;
   if (n <= 1) sb = 0;

@@ -792,6 +792,28 @@ def test_binding_refuses_what_it_can_see():
 
 # ------------------------------------------------------------------ together
 
+def test_calls_with_nothing_to_do():
+    p = _pages(2, 64, 32, 32, 4, 3, 2)
+    _fill(p, [5, 0, 40], seed=40)
+    state = _state(p)
+    none = torch.zeros(0, dtype=torch.int32, device=DEV)
+    kv = torch.zeros(0, 4, 2, 64, dtype=BF, device=DEV)
+    p.reserve(none, 3)
+    p.write(kv, kv, none)
+    p.read(kv, kv, none)
+    out, lse = p.attn(torch.zeros(0, 1, 4, 64, dtype=BF, device=DEV), none, lse=True)
+    assert out.shape == (0, 1, 4, 64) and lse.shape == (0, 4, 1)
+    p.fork(none, none)
+    p.trim(none)
+    p.compact(none, none, n_rows=4)
+    empty = torch.zeros(3, 0, 2, 64, dtype=BF, device=DEV)
+    p.write(empty, empty)
+    p.read(empty, empty)
+    assert p.status() == 0 and _unchanged(p, state)
+    p.compact(_ids(0), _ids(0), idx=torch.zeros(1, 1, 0, dtype=torch.int32, device=DEV))
+    assert p.status() == 0 and p.lens.tolist() == [0, 0, 40] and int(p.table[0].max()) == -1
+
+
 def test_calls_run_on_the_stream_they_are_given():
     p = _pages(2, 128, 64, 16, 20, 2, 8)
     s = torch.cuda.Stream()

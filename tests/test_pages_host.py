@@ -176,6 +176,19 @@ def test_calls_with_more_tiles_than_a_launch_has_warps_are_refused_whole():
     L.pyr_pages_free(h)
 
 
+def test_tensors_without_elements_need_no_address():
+    """(An empty torch tensor's address is null.) The calls get past the checks of their arguments."""
+    L, h, N, ORD = pb.lib(), _handle(), None, pb.PYR_ERR_ORDER
+    bf = pb.PYR_BF16
+    assert L.pyr_pages_write(h, N, 0, N, N, N, 0, 512, 128, 10, bf, N, 1, 0, N, 10, N) == ORD
+    assert L.pyr_pages_write(h, N, 2, N, N, N, 0, 512, 128, 0, bf, N, 1, 0, N, 0, N) == ORD
+    assert L.pyr_pages_read(h, N, 0, N, N, N, 0, 512, 128, bf, N, 10, N) == ORD
+    assert L.pyr_pages_read(h, N, 2, N, N, N, 512, 512, 128, bf, N, 0, N) == ORD
+    assert L.pyr_pages_attn(h, N, 0, N, 0, 0, 128, N, 0, 0, 128, N, 1, 8, bf, 0.0, N) == ORD
+    assert L.pyr_pages_attn(h, N, 1, N, 0, 0, 128, N, 0, 0, 128, N, 1, 8, bf, 0.0, N) == pb.PYR_ERR_NULL
+    L.pyr_pages_free(h)
+
+
 HARNESS = r"""
 #include "pages_index.h"
 using namespace pyr;
