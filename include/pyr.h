@@ -486,7 +486,7 @@ pyr_status_t pyr_pages_read(pyr_pages_t* pages, const int32_t* lists, int32_t n,
  * those of the query tokens themselves (a chunk of a prompt, drafted tokens). A token that sees no row gets zeros.
  * lse (device, may be NULL) is [n, n_q_heads, q_len] fp32, the natural log of the softmax denominator, -inf for such a
  * token. softmax_scale 0 means 1/sqrt(D). Scores, softmax statistics and sums are held in fp32. Each list is read once per
- * 8 (bf16; 4 for fp32) query rows of a KV head; bit-reproducible. A list may appear more than once; an entry whose list id
+ * 8 (bf16; 1 to 4 for fp32) query rows of a KV head; bit-reproducible. A list may appear more than once; an entry whose list id
  * is out of range writes nothing. bf16 runs on warp-level tensor-core instructions, fp32 on CUDA cores.
  */
 pyr_status_t pyr_pages_attn(pyr_pages_t* pages, const int32_t* lists, int32_t n, const void* q, int64_t q_stride_b,
