@@ -16,6 +16,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <climits>
+
 #include "pyr_internal.h"
 #include "tc_common.cuh"
 
@@ -359,7 +361,9 @@ struct CoreBody {
 // and nothing is added or converted. (The factors go into the queries for K, into the sums at the end for V.) What f16 lacks
 // is range, so both factors that are not codes are normalised by powers of two: a query row so that its largest element is
 // near f16's (what is then below f16's smallest step is below 2^-35 of that element), and the scales that multiply P, which
-// f16 holds to 2^-11, by a factor per group that follows them (`norm`).
+// f16 holds to 2^-11, by a factor per group that follows them (`norm`). The factor that a score needs to undo the first, 2^e for
+// a row whose largest element has the exponent e, times 2^9 and the softmax scale, passes fp32 from about e = 122 on:
+// part of it is then multiplied in by itself (`up`), in the stages' branch for edges, which such a segment always takes.
 // V's codes have a mean of 7.5, so that o grows with the number of rows while what matters in it grows with its root. The
 // instruction truncates its sums, and an o far above what matters would let that show: every kCentre steps what a group's o
 // have in common is moved to the group's sum of zeros, which is kept apart and rounded. (100 k rows a list, error against 64
@@ -390,10 +394,15 @@ __device__ __forceinline__ void codes4(uint32_t x, uint32_t* y) {
   y[2] = z & 0x000F000Fu;
   y[3] = z & 0x00F000F0u;
 }
-// 2^-e for the exponent e of x > 0 (clamped so that it, 2^11 times it and its inverse are numbers)
+// 2^k, -127 <= k <= 127
+__device__ __forceinline__ float power_of_two(int k) {
+  return __uint_as_float(k > -127 ? (uint32_t)(k + 127) << 23 : 0x00400000u);
+}
+// The exponent of x > 0 (-127 for 0 and subnormals).
+__device__ __forceinline__ int exponent_of(float x) { return (int)(__float_as_uint(x) >> 23) - 127; }
+// 2^-e for the exponent e of x > 0 (clamped so that it and its inverse are numbers)
 __device__ __forceinline__ float inverse_power(float x) {
-  const int e = min(max((int)(__float_as_uint(x) >> 23) - 127, -114), 126);
-  return __uint_as_float((uint32_t)(127 - e) << 23);
+  return power_of_two(-min(max(exponent_of(x), -114), 126));
 }
 
 template <int D, int GROUP>
@@ -406,11 +415,12 @@ struct MmaBody {
   static constexpr int kCentre = 8;
   uint32_t qf[X][4];
   float qsum[G][2];                              // sums of the queries over a group
-  float o[X][2][4], zacc[G][2], norm[G], m[2], ref[2], l[2], raise[2], sc2[2];
+  float o[X][2][4], zacc[G][2], norm[G], m[2], ref[2], l[2], raise[2], sc2[2], up[2];
   int limit[2], limit_min, steps;
 
   __device__ __forceinline__ void begin(const PagesAttnArgs& a, const Place& c, int cols_total, float*, int lane) {
     const int i = lane >> 2, j = lane & 3, col0 = c.cg * COLS;
+    bool far = false;
     {
       const int col = col0 + i, tok = col / a.rep, head = c.h * a.rep + col % a.rep;
       const uint16_t* q = static_cast<const uint16_t*>(a.q) + (int64_t)c.entry * a.qsb + (int64_t)tok * a.qst + (int64_t)head * a.qsh;
@@ -429,7 +439,9 @@ struct MmaBody {
       }
       big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
       big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-      const float down = big > 0.f ? inverse_power(big) : 1.f;
+      // 2^-e, of a row that is smaller still 2^112: with 2^15 a number, and bf16's smallest, 2^-133, keeps all its bits
+      const int e = min(max(exponent_of(big), -112), 127);
+      const float down = power_of_two(-e);
 #pragma unroll
       for (int w = 0; w < X; ++w)
 #pragma unroll
@@ -437,9 +449,18 @@ struct MmaBody {
           const float by = k & 1 ? 0x1p11f * down : 0x1p15f * down;      // for codes times 2^-20 and 2^-24
           qf[w][k] = pack_f16(f[w][k] * by, f[w][k + 4] * by);
         }
-      // scores come out times 2^-9 down
+      // Scores come out times 2^-9 down, so they take `scale` times 2^(9 + e): up to 2^96 of it in sc2, the rest in up. (At least
+      // 2^-149, at most the largest number: a row that a column does not see is -Inf times it.)
+      const float scale = a.scale * kLog2e;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) sc2[x] = a.scale * kLog2e * 0x1p9f / __shfl_sync(0xffffffffu, down, (2 * j + x) * 4);
+      for (int x = 0; x < 2; ++x) {
+        const int all = 9 + __shfl_sync(0xffffffffu, e, (2 * j + x) * 4);
+        const int apart = min(max(all + exponent_of(scale) - 96, 0), 127), k = all - apart;
+        sc2[x] = fminf(fmaxf(scale * power_of_two(k / 2) * power_of_two(k - k / 2), 0x1p-149f), 3.402823466e38f);
+        up[x] = power_of_two(apart);
+        far |= apart > 0;
+      }
+      far = __any_sync(0xffffffffu, far);
     }
     // sums of the queries over each group, by the instruction itself (every row of a matrix of constants that undo the queries'
     // factors: operands 0, 1 go with nibbles 0 and 2 of a code word, operands 2, 3 with nibbles 1 and 3)
@@ -466,7 +487,7 @@ struct MmaBody {
       m[x] = -INFINITY; raise[x] = -INFINITY; ref[x] = 0.f; l[x] = 0.f;
       limit[x] = c.len - (a.T - 1 - (col0 + 2 * j + x) / a.rep);
     }
-    limit_min = c.len - (a.T - 1 - col0 / a.rep);
+    limit_min = far ? INT_MIN / 2 : c.len - (a.T - 1 - col0 / a.rep);
     steps = 0;
   }
 
@@ -584,7 +605,7 @@ struct MmaBody {
           const int row = b * kPageTile + ri + 8 * r;
 #pragma unroll
           for (int x = 0; x < 2; ++x)
-            if (row >= rows || row0 + row >= limit[x]) s[b][2 * r + x] = -INFINITY;
+            s[b][2 * r + x] = row >= rows || row0 + row >= limit[x] ? -INFINITY : s[b][2 * r + x] * up[x];
 #pragma unroll
           for (int g = 0; g < G; ++g) {
             const float scale = __uint_as_float(vw[b][g][r] << 16);

@@ -1,0 +1,110 @@
+"""Attention over the paged 4-bit cache where numbers are large, small or far apart, against fp64 (oracle/pages.py): query rows
+over the whole range of their type."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages as op
+from paper_2405_12532_b200 import binding as pb
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _ids(*x):
+    return torch.tensor(list(x), dtype=torch.int32, device=DEV)
+
+
+def _wide(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def _parts(p, l):
+    """K values, then V's codes, scales and zeros per dimension, of a list's rows, all [rows, Hkv, D] in fp64."""
+    c = p.cfg
+    D, g, pr = c.head_dim, c.group, c.page_rows
+    pool = p.pool.cpu().numpy().reshape(c.n_pages, c.n_kv_heads, pr // 16, -1)
+    table, n = p.table[l].cpu().numpy(), int(p.lens[l])
+    out = [np.zeros((n, c.n_kv_heads, D)) for _ in range(4)]
+    for r0 in range(0, n, 16):
+        m = min(16, n - r0)
+        for h in range(c.n_kv_heads):
+            kc, ks, kz, vc, vs, vz = op.unpack(pool[table[r0 // pr], h, r0 % pr // 16], D, g)
+            for o, x in zip(out, (op.values(kc, ks, kz), vc, np.repeat(vs, g, -1), np.repeat(vz, g, -1))):
+                o[r0:r0 + m, h] = x[:m]
+    return out
+
+
+def _score_error(q, K, scale):
+    """Of one query row's scores: a code times a query value, summed in fp32 and multiplied by the row's (scale, zero), is off by
+    at most (D + 8) 2^-23 of scale sum |q| (15 s + |zero|), and 15 s + |zero| is at most 3 times the row's largest |K| (a group
+    that straddles zero has 15 s up to twice that, |zero| up to it) and the two roundings of the format."""
+    return (K.shape[1] + 8) * 2.0 ** -23 * scale * np.abs(q).sum() * 3.1 * np.abs(K).max()
+
+
+# ------------------------------------------------------------------ queries over the range of their type
+
+# every binade where a factor of the kernels could leave fp32 or f16, both ends of bf16 (2^-133 is its smallest number) among them
+EXPONENTS = [-133, -130, -127, -126, -125, -115, -114, -113, -112, -111, -100, -60, 0, 60, 96, 99, 100, 101, 113, 117, 118, 119, 121,
+             122, 124, 126, 127]
+
+
+@pytest.mark.parametrize("softmax_scale", [0.0, 1.0, 2.0 ** -30])
+@pytest.mark.parametrize("dtype", [BF])
+@pytest.mark.parametrize("D,group", [(64, 32), (128, 32), (128, 64), (128, 128)])
+def test_query_rows_over_the_whole_range_of_bf16(D, group, dtype, softmax_scale):
+    """List i's keys are of about 2^-e / softmax_scale (as far as numbers go), so that query rows of 2^e give scores of about 1;
+    the first two KV rows are zeros. Every query head has a power of two of its own, e, e - 1, e - 40 and so on (columns of one
+    matrix with factors of their own), some elements are zeros, one row is all zeros, and the largest element is the largest of
+    its binade: at 127 that of bf16."""
+    rows, T, hq = 45, 2, 6
+    n = len(EXPONENTS)
+    p = pb.PyrPages(n_kv_heads=1, head_dim=D, group=group, page_rows=32, n_pages=2 * n, n_lists=n, max_pages=2)
+    g = torch.Generator().manual_seed(D + group)
+    scale = softmax_scale or D ** -0.5
+    e = torch.tensor(EXPONENTS, dtype=torch.float64).view(n, 1, 1, 1)
+    k = torch.randn(n, rows, 1, D, generator=g, dtype=torch.float64).clamp(-1.9, 1.9)
+    # the largest key is below 2^126: neither it nor its group's 15 steps leave the range
+    k = (k * torch.exp2((-e + (30 if softmax_scale == 2.0 ** -30 else 0)).clamp(-140, 125))).float()
+    k[:, :2] = 0
+    v = torch.randn(n, rows, 1, D, generator=g)
+    base = torch.randn(n, T, hq, D, generator=g, dtype=torch.float64).clamp(-1.9, 1.9)
+    base[..., 3::7] = 0
+    base[..., 5] = 1.9921875
+    base[..., 9] = -1.9921875
+    less = torch.tensor([0, 1, 40, 0, 7, 0], dtype=torch.float64).view(1, 1, hq, 1)
+    q = (base * torch.exp2(e - less)).float().to(BF)           # (on the CPU: small numbers stay)
+    q[:, 1, 3] = 0
+    q = q.to(dtype)
+    assert bool(torch.isfinite(q).all()) and float(q[-1].abs().max()) == float(torch.finfo(BF).max)
+    p.reserve(_ids(*range(n)), rows)
+    p.write(k.to(DEV), v.to(DEV))
+    out, lse = p.attn(q.to(DEV), lse=True, softmax_scale=softmax_scale)
+    assert p.status() == 0
+    for i in range(n):
+        K, vc, vs, vz = (x[:, 0] for x in _parts(p, i))
+        V = vc * vs + vz
+        for t in range(T):
+            see = rows - (T - 1 - t)
+            for h in range(hq):
+                x = _wide(q[i, t, h])
+                z = K[:see] @ x * scale
+                want_lse = z.max() + np.log(np.exp(z - z.max()).sum())
+                w = np.exp(z - want_lse)
+                want = w @ V[:see]
+                # fp32: the scores' error moves a weight by that factor; exponential and sums 2^-20. bf16 besides: weights
+                # times a scale in f16 before they meet the codes, 2^-11 and what f16 cannot hold of a small one, 2^-25 a row (the
+                # zeros' part stays in fp32), the output 2^-8
+                ds = _score_error(x, K, scale) + 2.0 ** -22 * np.abs(z).max()
+                rel = 2 * ds + 2.0 ** -20
+                tol = rel * (w @ np.abs(V[:see]) + np.abs(want)) + 2.0 ** -24 * np.abs(want)
+                if dtype == BF:
+                    tol = tol + 2.0 ** -11 * (w @ (vc * vs)[:see]) + 2.0 ** -8 * np.abs(want) + 2.0 ** -25 * rows * 15 * vs.max()
+                if rel > 0.5:                                  # scores so large that fp32 cannot tell the rows apart
+                    assert bool(torch.isfinite(out[i, t, h]).all()), (EXPONENTS[i], t, h)
+                    continue
+                err = np.abs(_wide(out[i, t, h]) - want)
+                assert (err <= tol).all(), (EXPONENTS[i], t, h, float(err.max()), float(tol.flat[err.argmax()]))
+                lerr = abs(float(lse[i, h, t]) - want_lse)
+                assert lerr <= ds + 2.0 ** -20 * (1 + abs(want_lse)), (EXPONENTS[i], t, h, lerr)
