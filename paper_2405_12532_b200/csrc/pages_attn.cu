@@ -172,15 +172,18 @@ struct Layout {
 };
 
 // ------------------------------------------------------------------ one warp's tiles, on CUDA cores (fp32)
-// Every product in fp32: fp32 outputs are held to what fp32 can do, which operands of fewer bits cannot. Bound by its
-// multiply-adds where a KV head has several query rows (2 x 128 of them a row and column). Lane 4 i + j. K: rows i and i + 8, the quarter of the dimensions that chunk j of a stored row holds. V: the eighth of the
+// Every product in fp32: fp32 outputs are held to what fp32 can do, which operands of fewer bits cannot. A sum of codes times
+// queries (up to 15 of them each) leaves fp32 before q . K does: a query row with an element of 2^100 or more is taken times 2^-64, its
+// scores times 2^64. Bound by its multiply-adds where a KV head has several query rows (2 x 128 of them a row and column).
+// Lane 4 i + j. K: rows i and i + 8, the quarter of the dimensions that chunk j of a stored row holds. V: the eighth of the
 // dimensions that chunk i holds, of the rows j, j + 4, j + 8, j + 12.
 template <int D, int GROUP, int kCols>
 struct CoreBody {
   using Type = float;
-  static constexpr int kDim = D, COLS = kCols, kWarps = 7, kBlocks = 1, kQueryFloats = COLS * D;   // queries lie in shared memory
+  static constexpr int kDim = D, COLS = kCols, kWarps = 7, kBlocks = 1, kQueryFloats = COLS * D + 4;   // queries and their scores' factors lie in shared memory
   static constexpr int kStages = 3, kTileBytes = kPageTile * (D + 8 * (D / GROUP));
   static constexpr int G = D / GROUP, U = GROUP / 32, X = D / 32;   // X: words of K / halves of V in a lane's chunk
+  static_assert(COLS <= 4, "a factor a column");
   float acc[COLS][4 * X];
   float m[COLS], l[COLS], qsum[COLS][G];
   int limit[COLS];
@@ -199,8 +202,16 @@ struct CoreBody {
       limit[x] = c.len - (a.T - 1 - tok);
       const float* q = static_cast<const float*>(a.q) + (int64_t)c.entry * a.qsb + (int64_t)tok * a.qst + (int64_t)head * a.qsh;
       // queries in the order of the stored codes
-      for (int p = lane; p < D; p += 32)
-        qs[x * D + p] = x < ncols ? q[8 * k_slot_word(D, GROUP, p >> 3) + (p & 7)] : 0.f;
+      bool far = false;
+      for (int p = lane; p < D; p += 32) {
+        const float v = x < ncols ? q[8 * k_slot_word(D, GROUP, p >> 3) + (p & 7)] : 0.f;
+        qs[x * D + p] = v;
+        far |= fabsf(v) >= 0x1p100f;
+      }
+      far = __any_sync(0xffffffffu, far);
+      if (lane == 0) qs[COLS * D + x] = far ? 0x1p64f : 1.f;
+      if (far)
+        for (int p = lane; p < D; p += 32) qs[x * D + p] *= 0x1p-64f;
     }
     __syncwarp();
 #pragma unroll
@@ -247,7 +258,7 @@ struct CoreBody {
         s[rr][x] += __shfl_xor_sync(0xffffffffu, s[rr][x], 1);
         s[rr][x] += __shfl_xor_sync(0xffffffffu, s[rr][x], 2);
         // rows behind the list's end hold anything: replaced, not multiplied away
-        s[rr][x] = r < rows && row0 + r < limit[x] ? s[rr][x] * sc2 : -INFINITY;
+        s[rr][x] = r < rows && row0 + r < limit[x] ? s[rr][x] * qs[COLS * D + x] * sc2 : -INFINITY;
       }
     }
     const bool edge = row0 + kPageTile > limit[0];               // some column sees less than the whole tile

@@ -51,7 +51,7 @@ EXPONENTS = [-133, -130, -127, -126, -125, -115, -114, -113, -112, -111, -100, -
 
 
 @pytest.mark.parametrize("softmax_scale", [0.0, 1.0, 2.0 ** -30])
-@pytest.mark.parametrize("dtype", [BF])
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("D,group", [(64, 32), (128, 32), (128, 64), (128, 128)])
 def test_query_rows_over_the_whole_range_of_bf16(D, group, dtype, softmax_scale):
     """List i's keys are of about 2^-e / softmax_scale (as far as numbers go), so that query rows of 2^e give scores of about 1;
