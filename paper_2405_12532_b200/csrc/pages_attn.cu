@@ -426,7 +426,8 @@ struct MmaBody {
   static constexpr int kCentre = 8;
   uint32_t qf[X][4];
   float qsum[G][2];                              // sums of the queries over a group
-  float o[X][2][4], zacc[G][2], norm[G], m[2], ref[2], l[2], raise[2], sc2[2], up[2];
+  float o[X][2][4], zacc[G][2], norm[G], l[2], sc2[2], up[2];
+  float ref[2], raise[2];                        // the maximum (0 and raise = -Inf: nothing seen) and what raises it, before sc2
   int limit[2], limit_min, steps;
 
   __device__ __forceinline__ void begin(const PagesAttnArgs& a, const Place& c, int cols_total, float*, int lane) {
@@ -495,12 +496,14 @@ struct MmaBody {
       for (int y = 0; y < 2; ++y) o[x][y][0] = o[x][y][1] = o[x][y][2] = o[x][y][3] = 0.f;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      m[x] = -INFINITY; raise[x] = -INFINITY; ref[x] = 0.f; l[x] = 0.f;
+      raise[x] = -INFINITY; ref[x] = 0.f; l[x] = 0.f;
       limit[x] = c.len - (a.T - 1 - (col0 + 2 * j + x) / a.rep);
     }
     limit_min = far ? INT_MIN / 2 : c.len - (a.T - 1 - col0 / a.rep);
     steps = 0;
   }
+
+  __device__ __forceinline__ float top_score(int x) const { return raise[x] == -INFINITY ? -INFINITY : ref[x]; }
 
   // Brings the group's factor to the largest scale of the tile (the lanes hold two rows each): o goes with it.
   __device__ __forceinline__ void renorm(int g, float big) {
@@ -659,11 +662,10 @@ struct MmaBody {
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-        const float m_new = fmaxf(m[x], mx * sc2[x]);
-        const float corr = m_new == -INFINITY ? 1.f : ex2(m[x] - m_new);
-        m[x] = m_new;
-        ref[x] = m_new == -INFINITY ? 0.f : m_new;               // nothing seen yet: every term is zero
-        raise[x] = m_new == -INFINITY ? -INFINITY : (m_new + kLazy) / sc2[x];
+        const float m_old = top_score(x), m_new = fmaxf(m_old, mx);
+        const float corr = m_new == -INFINITY ? 1.f : ex2((m_old - m_new) * sc2[x]);
+        ref[x] = m_new == -INFINITY ? 0.f : m_new;
+        raise[x] = m_new == -INFINITY ? -INFINITY : m_new + kLazy / sc2[x];
         l[x] *= corr;
 #pragma unroll
         for (int g = 0; g < G; ++g) zacc[g][x] *= corr;
@@ -679,11 +681,13 @@ struct MmaBody {
 #pragma unroll
     for (int b = 0; b < kStageTiles; ++b) {
       const uint8_t* tile = tp + b * kTileBytes;
+      // (the difference first: a product that is rounded in one place and not in the other is off by 2^-24 of a score, which
+      // for scores beyond 2^30 is beyond an exponential's range)
       float p[4];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        p[x] = ex2(fmaf(s[b][x], sc2[x], -ref[x]));
-        p[2 + x] = ex2(fmaf(s[b][2 + x], sc2[x], -ref[x]));
+        p[x] = ex2((s[b][x] - ref[x]) * sc2[x]);
+        p[2 + x] = ex2((s[b][2 + x] - ref[x]) * sc2[x]);
         l[x] += p[x] + p[2 + x];
       }
       uint32_t vc[4][X / 2];                     // rows of matrix rows 2 j, 2 j + 1, 2 j + 8, 2 j + 9
@@ -758,7 +762,7 @@ struct MmaBody {
 #pragma unroll
         for (int k = 0; k < 4; ++k) st[d + k] = o[y][k >> 1][2 * (k & 1) + x];
       }
-      if (i == 0) { st[D] = m[x]; st[D + 1] = l[x]; }
+      if (i == 0) { st[D] = top_score(x) * sc2[x]; st[D + 1] = l[x]; }
     }
   }
   __device__ __forceinline__ void write(const PagesAttnArgs& a, const Place& c, int cols_total, int lane) const {
@@ -773,7 +777,7 @@ struct MmaBody {
       for (int y = 0; y < X; ++y)
         *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + at.out + 4 * v_slot_half(D, GROUP, i * X + y)) =
             make_uint2(pack_bf16(o[y][0][x] * inv, o[y][0][2 + x] * inv), pack_bf16(o[y][1][x] * inv, o[y][1][2 + x] * inv));
-      if (i == 0 && a.lse) a.lse[at.lse] = lse_of(m[x], l[x]);
+      if (i == 0 && a.lse) a.lse[at.lse] = lse_of(top_score(x) * sc2[x], l[x]);
     }
   }
 };

@@ -108,3 +108,51 @@ def test_query_rows_over_the_whole_range_of_bf16(D, group, dtype, softmax_scale)
                 assert (err <= tol).all(), (EXPONENTS[i], t, h, float(err.max()), float(tol.flat[err.argmax()]))
                 lerr = abs(float(lse[i, h, t]) - want_lse)
                 assert lerr <= ds + 2.0 ** -20 * (1 + abs(want_lse)), (EXPONENTS[i], t, h, lerr)
+
+
+# ------------------------------------------------------------------ weights and scales far apart
+
+def _attn_bound(z, w, c, s, zero, ds, small):
+    """Of one bf16 output row: softmax weights w [rows], V's codes, scales, zeros [rows, D]. Weights off by 2 ds + 2^-20 and by
+    their sums (each of a lane's adds 2^-24 over an eighth of the rows, each matrix instruction's 2^-23 over a sixteenth), the
+    weights that meet the codes rounded to f16 (2^-11), `small` for what f16 cannot hold of them, the output's rounding."""
+    v = c * s + zero
+    rel = 2 * ds + 2.0 ** -20 + w.shape[0] * 2.0 ** -26
+    want = w @ v
+    return want, rel * (w @ v.abs() + want.abs()) + 2.0 ** -11 * (w @ (c * s)) + small + 2.0 ** -8 * want.abs()
+
+
+@pytest.mark.parametrize("order", [1, -1])
+@pytest.mark.parametrize("D,group", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
+def test_columns_with_magnitudes_of_their_own_over_scales_of_many(D, group, order):
+    """The eight query heads of one column group are of 2^-60 to 2^60, the keys of three lists 2^-60, 1 and 2^60, and the scales of
+    V run from 2^-90 to 2^90 up or down each list: held to the largest scale of the group (small = 2^-25 a row of it)."""
+    n, rows, hq = 3, 96, 8
+    p = pb.PyrPages(n_kv_heads=1, head_dim=D, group=group, page_rows=32, n_pages=9, n_lists=n, max_pages=3)
+    g = torch.Generator().manual_seed(D + group + order)
+    e = torch.tensor([-60.0, 0.0, 60.0]).view(n, 1, 1, 1)
+    k = (torch.randn(n, rows, 1, D, generator=g) * torch.exp2(e)).to(BF)
+    block = torch.arange(rows).view(1, rows, 1, 1) // 16
+    v = (torch.randn(n, rows, 1, D, generator=g) * torch.exp2(order * (block * 36.0 - 90.0))).to(BF)
+    q = (torch.randn(n, 1, hq, D, generator=g) * torch.exp2(torch.linspace(-60, 60, hq).round()).view(1, 1, hq, 1)).to(BF)
+    p.reserve(_ids(0, 1, 2), rows)
+    p.write(k.to(DEV), v.to(DEV))
+    out, lse = p.attn(q.to(DEV), lse=True)
+    assert p.status() == 0
+    told = 0
+    for i in range(n):
+        K, c, s, z0 = (torch.from_numpy(x[:, 0]) for x in _parts(p, i))
+        for h in range(hq):
+            x = q[i, 0, h].double()
+            z = K @ x * D ** -0.5
+            ds = _score_error(x.numpy(), K.numpy(), D ** -0.5)
+            assert bool(torch.isfinite(out[i, 0, h]).all())
+            if ds > 0.1:
+                continue
+            told += 1
+            w = torch.softmax(z, 0)
+            want, tol = _attn_bound(z, w, c, s, z0, ds, 2.0 ** -25 * rows * 15 * s.max(0).values)
+            err = (out[i, 0, h].double().cpu() - want).abs()
+            assert bool((err <= tol).all()), (i, h, float((err / tol).max()))
+            assert abs(float(lse[i, h, 0]) - float(torch.logsumexp(z, 0))) <= ds + 2.0 ** -20 * (1 + float(z.abs().max()))
+    assert told >= 12
