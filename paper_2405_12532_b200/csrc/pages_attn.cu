@@ -372,7 +372,9 @@ struct CoreBody {
 // and nothing is added or converted. (The factors go into the queries for K, into the sums at the end for V.) What f16 lacks
 // is range, so both factors that are not codes are normalised by powers of two: a query row so that its largest element is
 // near f16's (what is then below f16's smallest step is below 2^-35 of that element), and the scales that multiply P, which
-// f16 holds to 2^-11, by a factor per group that follows them (`norm`). The factor that a score needs to undo the first, 2^e for
+// f16 holds to 2^-11, by a factor per group that follows them (`norm`) and keeps the products near f16's top: many rows of
+// little weight behind one of much add up, and what f16 drops of them is the same for all. (16384 rows of 2^-17.5 of the first one's
+// weight, one of the first 32 with scales 50 times the others': off by up to 0.013 of values of 1.2 with factors near 1.) The factor that a score needs to undo the first, 2^e for
 // a row whose largest element has the exponent e, times 2^9 and the softmax scale, passes fp32 from about e = 122 on:
 // part of it is then multiplied in by itself (`up`), in the stages' branch for edges, which such a segment always takes.
 // V's codes have a mean of 7.5, so that o grows with the number of rows while what matters in it grows with its root. The
@@ -422,7 +424,11 @@ struct MmaBody {
   static constexpr int G = D / GROUP, U = GROUP / 32, X = D / 32;
   static constexpr int kDim = D, COLS = 8, kWarps = 11, kBlocks = 1, kQueryFloats = 0;
   static constexpr int kTileBytes = kPageTile * (D + 8 * G), kStages = kTileBytes > 2304 ? 2 : 3;
-  static constexpr float kLazy = 8.f;            // the maximum is raised once a score is 2^8 above it
+  static constexpr float kLazy = 4.f;            // the maximum is raised once a score is 2^4 above it
+  // The largest scale of a group times its factor is set to 2^8 .. 2^9 and set anew above 2^11, or where all rows of a stage are below
+  // 2^4: P times that stays below 2^15 (f16 ends at 2^16), is held to 2^-11 down to weights of 2^-18 of the largest, and what
+  // is smaller to 2^-29 of it.
+  static constexpr float kScaleTop = 0x1p11f, kScaleSet = 0x1p8f, kScaleLow = 0x1p4f;
   static constexpr int kCentre = 8;
   uint32_t qf[X][4];
   float qsum[G][2];                              // sums of the queries over a group
@@ -511,7 +517,7 @@ struct MmaBody {
     big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 8));
     big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 16));
     if (!(big > 0.f)) return;                    // only zeros (or NaN): any factor will do
-    const float to = inverse_power(big), by = norm[g] == 0.f ? 1.f : to / norm[g];
+    const float to = inverse_power(big) * kScaleSet, by = norm[g] == 0.f ? 1.f : to / norm[g];
     if (by > 1.f) {                              // what has been summed is beyond such small scales if it does not stay finite
       float most = 0.f;
 #pragma unroll
@@ -631,8 +637,8 @@ struct MmaBody {
           }
         }
     }
-    // Rare work, found by one vote: a score far above the maximum, a scale that P's f16 range no longer covers (P <= 2^8,
-    // its scaled value <= 2^15), or only scales so far below that P would lose bits.
+    // Rare work, found by one vote: a score far above the maximum, a scale that P's f16 range no longer covers, or only scales so
+    // far below that P would lose bits.
     float top = 0.f, low = INFINITY;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
@@ -646,15 +652,15 @@ struct MmaBody {
     float ms[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) ms[x] = fmaxf(fmaxf(s[0][x], s[0][2 + x]), fmaxf(s[1][x], s[1][2 + x]));
-    if (__any_sync(0xffffffffu, ms[0] > raise[0] || ms[1] > raise[1] || top > 64.f) ||
-        __all_sync(0xffffffffu, low < 0.015625f)) {
+    if (__any_sync(0xffffffffu, ms[0] > raise[0] || ms[1] > raise[1] || top > kScaleTop) ||
+        __all_sync(0xffffffffu, low < kScaleLow)) {
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         float big = 0.f;
 #pragma unroll
         for (int y = 0; y < 2 * kStageTiles; ++y) big = fmaxf(big, __uint_as_float(vw[y >> 1][g][y & 1] << 16));
         const float x = big * norm[g];
-        if (__any_sync(0xffffffffu, x > 64.f) || __all_sync(0xffffffffu, !(x >= 0.015625f))) renorm(g, big);
+        if (__any_sync(0xffffffffu, x > kScaleTop) || __all_sync(0xffffffffu, !(x >= kScaleLow))) renorm(g, big);
       }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {

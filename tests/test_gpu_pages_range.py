@@ -122,6 +122,40 @@ def _attn_bound(z, w, c, s, zero, ds, small):
     return want, rel * (w @ v.abs() + want.abs()) + 2.0 ** -11 * (w @ (c * s)) + small + 2.0 ** -8 * want.abs()
 
 
+@pytest.mark.parametrize("rows,outlier", [(16384, 50.0), (16384, 1.0), (65536, 8.0), (4096, 700.0)])
+@pytest.mark.parametrize("D,group", [(64, 32), (128, 32), (128, 64), (128, 128)])
+def test_many_small_weights_behind_a_large_one(D, group, rows, outlier):
+    """Row 0 takes most of the weight, thousands of rows behind it 2^-16 to 2^-20.5 of its weight each (all alike: whatever
+    is lost of one is lost of all), and one of the first 32 rows has values far above the others'. 407 entries of 4 heads are a
+    (entry, head) a warp on 148 SMs, so that a warp meets all of it in order. f16 holds a weight times its normalised scale to
+    2^-25, and that scale is at least 2^4 for the largest of any 32 rows read together: small = 2^-29 times code and that scale."""
+    hkv, n = 4, 407
+    p = pb.PyrPages(n_kv_heads=hkv, head_dim=D, group=group, page_rows=256, n_pages=rows // 256, n_lists=1, max_pages=rows // 256)
+    g = torch.Generator().manual_seed(rows + D + group)
+    k = torch.zeros(1, rows, hkv, D)
+    k[0, 0] = (torch.tensor([16.0, 17.5, 19.5, 20.5]) * np.log(2.0) * D ** -0.5).view(hkv, 1)
+    v = 1.2 * torch.randn(1, rows, hkv, D, generator=g)
+    v[0, 5] *= outlier
+    k, v = k.to(BF), v.to(BF)
+    p.reserve(_ids(0), rows)
+    p.write(k.to(DEV), v.to(DEV))
+    q = torch.ones(n, 1, hkv, D, dtype=BF, device=DEV)
+    out, lse = p.attn(q, _ids(*[0] * n), lse=True)
+    assert p.status() == 0
+    code, scale, zero = (torch.from_numpy(x).to(DEV) for x in op.quantise(v[0].float().numpy(), group))
+    for h in range(hkv):
+        c, s, z0 = code[:, h].double(), scale[:, h].double(), zero[:, h].double()
+        near = torch.nn.functional.max_pool1d(s.T.unsqueeze(0), 63, 1, 31)[0].T
+        small = 2.0 ** -29 * (c * near.repeat_interleave(group, 1)).sum(0)
+        s, z0 = s.repeat_interleave(group, 1), z0.repeat_interleave(group, 1)
+        z = k[0, :, h].double().sum(1).to(DEV) * D ** -0.5
+        ds = (D + 8) * 2.0 ** -23 * float(z.max())
+        want, tol = _attn_bound(z, torch.softmax(z, 0), c, s, z0, ds, small)
+        err = (out[:, 0, h].double() - want).abs()
+        assert bool((err <= tol).all()), (h, float(err.max()), float(tol.min()), float((err / tol).max()))
+        assert float((lse[:, h, 0].double() - torch.logsumexp(z, 0)).abs().max()) <= ds + 2.0 ** -20 * 16 + rows * 2.0 ** -27
+
+
 @pytest.mark.parametrize("order", [1, -1])
 @pytest.mark.parametrize("D,group", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
 def test_columns_with_magnitudes_of_their_own_over_scales_of_many(D, group, order):
