@@ -517,7 +517,8 @@ struct MmaBody {
     big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 8));
     big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 16));
     if (!(big > 0.f)) return;                    // only zeros (or NaN): any factor will do
-    const float to = inverse_power(big) * kScaleSet, by = norm[g] == 0.f ? 1.f : to / norm[g];
+    const float to = inverse_power(big) * kScaleSet;
+    float by = norm[g] == 0.f ? 1.f : to / norm[g];
     if (by > 1.f) {                              // what has been summed is beyond such small scales if it does not stay finite
       float most = 0.f;
 #pragma unroll
@@ -527,6 +528,7 @@ struct MmaBody {
 #pragma unroll
           for (int k = 0; k < 4; ++k) most = fmaxf(most, fabsf(o[g * U + u][y][k]));
       if (__any_sync(0xffffffffu, most > 0.f && most * by > 1e30f)) return;
+      by = fminf(by, 3.402823466e38f);           // (Inf, where nothing has been summed: it stays zero)
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)

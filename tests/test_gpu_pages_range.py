@@ -190,3 +190,28 @@ def test_columns_with_magnitudes_of_their_own_over_scales_of_many(D, group, orde
             assert bool((err <= tol).all()), (i, h, float((err / tol).max()))
             assert abs(float(lse[i, h, 0]) - float(torch.logsumexp(z, 0))) <= ds + 2.0 ** -20 * (1 + float(z.abs().max()))
     assert told >= 12
+
+
+def test_tokens_that_see_no_row_get_zeros_whatever_the_values():
+    """48 tokens over 40 rows: the first eight, a column group of their own, see nothing, while the scales of V fall from 2^113 to
+    2^-22 between two reads of 32 rows (a ratio beyond fp32)."""
+    D, rows, T, n = 64, 40, 48, 300
+    p = pb.PyrPages(n_kv_heads=1, head_dim=D, group=64, page_rows=64, n_pages=1, n_lists=1, max_pages=1)
+    g = torch.Generator().manual_seed(3)
+    k, v = torch.randn(1, rows, 1, D, generator=g), torch.randn(1, rows, 1, D, generator=g)
+    v[:, :32] *= 2.0 ** 115
+    v[:, 32:] *= 2.0 ** -20
+    p.reserve(_ids(0), rows)
+    p.write(k.to(BF).to(DEV), v.to(BF).to(DEV))
+    q = torch.randn(1, T, 1, D, generator=g).to(BF).expand(n, -1, -1, -1).contiguous()
+    out, lse = p.attn(q.to(DEV), _ids(*[0] * n), lse=True)
+    assert p.status() == 0
+    assert not bool(out[:, :8].any()) and bool(torch.isneginf(lse[:, :, :8]).all())
+    K, c, s, z0 = (torch.from_numpy(x[:, 0]) for x in _parts(p, 0))
+    for t in range(8, T):
+        see = t - 7
+        x = q[0, t, 0].double()
+        z = K[:see] @ x * D ** -0.5
+        want, tol = _attn_bound(z, torch.softmax(z, 0), c[:see], s[:see], z0[:see], _score_error(x.numpy(), K.numpy(), D ** -0.5),
+                                2.0 ** -25 * rows * 15 * s.max(0).values)
+        assert bool(((out[:, t, 0].double().cpu() - want).abs() <= tol).all()), t
