@@ -490,7 +490,8 @@ pyr_status_t pyr_pages_read(pyr_pages_t* pages, const int32_t* lists, int32_t n,
  * the weight by which a row's V codes are multiplied is rounded by 2^-11 of itself, one below 2^-18 of the column's largest by up to 2^-29
  * of that, times the largest scale that a group has in 32 neighbouring rows (V's zeros and the denominator take it in fp32).
  * Each list is read once per 8 (bf16; 1 to 4 for fp32) query rows of a KV head; bit-reproducible. A list may appear more than once; an entry whose list id
- * is out of range writes nothing. bf16 runs on warp-level tensor-core instructions, fp32 on CUDA cores.
+ * is out of range writes nothing. A call whose lists come to more than 2^30 tiles of 16 rows (times KV heads and times eighths of the
+ * query rows) for each warp of the machine writes nothing and records PYR_ERR_UNSUPPORTED. bf16 runs on warp-level tensor-core instructions, fp32 on CUDA cores.
  */
 pyr_status_t pyr_pages_attn(pyr_pages_t* pages, const int32_t* lists, int32_t n, const void* q, int64_t q_stride_b,
                             int64_t q_stride_t, int64_t q_stride_h, void* out, int64_t o_stride_b, int64_t o_stride_t,

@@ -32,7 +32,7 @@ constexpr int kStageTiles = 2;           // a stage of a warp's ring: one copy o
 constexpr int kStageRows = kStageTiles * kPageTile;
 // What beginning and ending a (entry, head, column group) costs a warp, in tiles: its queries, a first step that sets the maximum
 // and the scales' factors, its sums (64 ragged lists of 32 heads: 102 us with 2, 96 with 3, 92 with 4, 90 with 6 and 8).
-constexpr int kSegmentUnits = 6;
+constexpr int kSegmentUnits = kAttnSegmentUnits;
 // A warp's share is at least this much: next to nothing, since small calls are bound by a warp's own latency, 2 us a step
 // (with 2 instead of 4 and 8: 385 rows of 32 heads 20.5, 22.5 and 24.6 us, the small fp32 model 21, 26 and 32 us).
 constexpr int kMinUnits = 2;
@@ -908,9 +908,12 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
     }
   }
   if (!whole_ones) {
-    const long long workers = (long long)gridDim.x * kWarps;
-    const long long q = total >> 31 ? (total + workers - 1) / workers : (long long)(((uint32_t)total + (uint32_t)workers - 1u) / (uint32_t)workers);
-    cta_units = max(q, (long long)kMinUnits) * kWarps;
+    const long long q = attn_share(total, (long long)gridDim.x * kWarps, kMinUnits);
+    if (q < 0) {                                 // (in every CTA)
+      if (blockIdx.x == 0 && t == 0) record(a.p.status, PYR_ERR_UNSUPPORTED);
+      return;
+    }
+    cta_units = q * kWarps;
     cta_u = blockIdx.x * cta_units;
     if (cta_u >= total) return;                  // the whole CTA: nothing is in flight
     long long run = 0;
@@ -1198,13 +1201,8 @@ cudaError_t run_attn(const PagesAttnArgs& a, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   const int sms = device_sm_count();
   if (sms <= 0) return cudaErrorUnknown;
-  // a grid that the machine holds at once, no larger than the work can be
-  const long long most = (long long)a.n * a.p.Hkv * cgs * (attn_tiles(a.p.max_pages * a.p.page_rows) + kSegmentUnits);
-  constexpr int per_cta = Body::kWarps * kMinUnits;
-  long long ctas = (most + per_cta - 1) / per_cta;
-  if (ctas > (long long)Body::kBlocks * sms) ctas = (long long)Body::kBlocks * sms;
-  if (ctas > kAttnMaxCtas) ctas = kAttnMaxCtas;
-  if (most / ctas > (1 << 30)) return cudaErrorInvalidValue;   // a CTA's share is counted in 32 bits
+  const int at_once = Body::kBlocks * sms < kAttnMaxCtas ? Body::kBlocks * sms : kAttnMaxCtas;
+  const int ctas = attn_ctas(a.p, a.n, cgs, Body::kWarps * kMinUnits, at_once);
   attn_kernel<Body><<<(unsigned)ctas, (Body::kWarps + 1) * 32, smem, s>>>(a, cgs);
   return cudaGetLastError();
 }

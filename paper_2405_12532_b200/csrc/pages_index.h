@@ -77,8 +77,25 @@ PYR_HD int v_slot_half(int D, int group, int slot) {
 }
 
 // How the attention's work is dealt out. A unit is one tile of one (entry, KV head, column group); an entry without rows
-// still has one tile per head, so that its zeros get written. Units are numbered entry by entry, head by head, column
-// group by column group, tile by tile, and worker w of `q` units takes [w q, (w + 1) q).
+// still has one tile per head, so that its zeros get written. Before its tiles each (entry, KV head, column group) has
+// kAttnSegmentUnits units that stand for no tile, for what beginning and ending it costs. Units are numbered entry by entry,
+// head by head, column group by column group, tile by tile. Where there are no more (entry, KV head, column group)s than CTAs
+// and none is long, a CTA takes one of them and its warps share the tiles; else every warp takes the same number of consecutive units.
+constexpr int kAttnSegmentUnits = 6;
 PYR_HD int64_t attn_tiles(int len) { return len > 0 ? (len + kPageTile - 1) / kPageTile : 1; }
+// The units of each of `workers` warps (at least `least`), -1 where they are more than a warp counts in 32 bits.
+PYR_HD int64_t attn_share(int64_t total, int64_t workers, int64_t least) {
+  // (64-bit divisions take a tenth of a microsecond each)
+  const int64_t q = total >> 31 ? (total + workers - 1) / workers : (int64_t)(((uint32_t)total + (uint32_t)workers - 1u) / (uint32_t)workers);
+  return q > (1 << 30) ? -1 : (q < least ? least : q);
+}
+// CTAs of a launch: as many as the machine holds at once, `most`, but no more than have `least` units each if every list were as
+// long as its table.
+inline int attn_ctas(const PagesView& p, int64_t n, int64_t column_groups, int64_t least, int64_t most) {
+  const int64_t tiles = attn_tiles(p.max_pages * p.page_rows) + kAttnSegmentUnits;
+  const unsigned __int128 units = (unsigned __int128)n * (uint64_t)p.Hkv * (uint64_t)column_groups * (uint64_t)tiles;
+  const unsigned __int128 ctas = (units + (uint64_t)least - 1) / (uint64_t)least;
+  return ctas < (uint64_t)most ? (int)ctas : (int)most;
+}
 
 }  // namespace pyr

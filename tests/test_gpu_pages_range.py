@@ -215,3 +215,23 @@ def test_tokens_that_see_no_row_get_zeros_whatever_the_values():
         want, tol = _attn_bound(z, torch.softmax(z, 0), c[:see], s[:see], z0[:see], _score_error(x.numpy(), K.numpy(), D ** -0.5),
                                 2.0 ** -25 * rows * 15 * s.max(0).values)
         assert bool(((out[:, t, 0].double().cpu() - want).abs() <= tol).all()), t
+
+
+# ------------------------------------------------------------------ tables with room to grow
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_what_a_list_could_hold_does_not_refuse_a_call(dtype):
+    """Tables for 2^31 rows, lists of 100: the same outputs, bit for bit, as with tables of one page."""
+    hkv, hq, D, T, lens = 8, 64, 64, 80, [100, 90]
+    res = []
+    for slots in (1, 2097150):
+        p = pb.PyrPages(n_kv_heads=hkv, head_dim=D, group=64, page_rows=1024, n_pages=2, n_lists=2, max_pages=slots)
+        g = torch.Generator().manual_seed(4)
+        k, v, q = (torch.randn(2, r, h, D, generator=g).to(dtype).to(DEV) for r, h in ((100, hkv), (100, hkv), (T, hq)))
+        p.reserve(_ids(0, 1), 100)
+        p.write(k, v, counts=_ids(*lens))
+        out, lse = p.attn(q, lse=True)
+        assert p.status() == 0 and p.lens.tolist() == lens
+        res.append((out, lse))
+        del p
+    assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1]) and bool(torch.isfinite(res[0][0]).all())
