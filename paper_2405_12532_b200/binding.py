@@ -449,8 +449,9 @@ class PyrCache:
                                      out.data_ptr(), C.c_void_p(_stream_ptr(stream))), "pyr_decode_attn")
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_current_device = torch._C._cuda_getDevice
+# (what torch.cuda asks itself, without the objects around it; a build of torch for the CPU has neither)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _PAGES_DTYPES = {torch.bfloat16: PYR_BF16, torch.float32: PYR_F32}
 
 
