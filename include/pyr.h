@@ -485,7 +485,7 @@ pyr_status_t pyr_pages_read(pyr_pages_t* pages, const int32_t* lists, int32_t n,
  * len_i - (q_len - 1 - t) rows: with q_len = 1 all of them, the row stored last included; with more, the last q_len rows are
  * those of the query tokens themselves (a chunk of a prompt, drafted tokens). A token that sees no row gets zeros.
  * lse (device, may be NULL) is [n, n_q_heads, q_len] fp32, the natural log of the softmax denominator, -inf for such a
- * token. softmax_scale 0 means 1/sqrt(D). Scores, softmax statistics and sums are held in fp32. For bf16, what the matrix
+ * token. softmax_scale (at most 2^127) 0 means 1/sqrt(D). Scores, softmax statistics and sums are held in fp32. For bf16, what the matrix
  * instruction multiplies is f16: query elements, scaled by their row's largest, lose bits below 2^-28 of it and vanish below 2^-36;
  * the weight by which a row's V codes are multiplied is rounded by 2^-11 of itself, one below 2^-18 of the column's largest by up to 2^-29
  * of that, times the largest scale that a group has in 32 neighbouring rows (V's zeros and the denominator take it in fp32).

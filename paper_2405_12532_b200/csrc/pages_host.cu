@@ -295,7 +295,7 @@ pyr_status_t pyr_pages_attn(pyr_pages_t* h, const int32_t* lists, int32_t n, con
   pyr_status_t st = check_call(h, n, false);
   if (st != PYR_OK) return st;
   if (q_len < 1 || n_q_heads < 1 || n_q_heads % h->cfg.n_kv_heads || !default_lists_fit(h, lists, n)) return PYR_ERR_INVALID;
-  if (!(softmax_scale >= 0.0f) || !std::isfinite(softmax_scale)) return PYR_ERR_INVALID;
+  if (!(softmax_scale >= 0.0f) || softmax_scale > 0x1p127f) return PYR_ERR_INVALID;     // (times log2 e it is a number)
   st = check_rows(h, q, q, dtype, qsb, qst, qsh, n, q_len, n_q_heads);
   if (st == PYR_OK) st = check_rows(h, out, out, dtype, osb, ost, osh, n, q_len, n_q_heads);
   if (st != PYR_OK) return st;
