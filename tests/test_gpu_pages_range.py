@@ -235,3 +235,43 @@ def test_what_a_list_could_hold_does_not_refuse_a_call(dtype):
         res.append((out, lse))
         del p
     assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1]) and bool(torch.isfinite(res[0][0]).all())
+
+
+# ------------------------------------------------------------------ long lists
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [1, 3])
+@pytest.mark.parametrize("D,group", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
+def test_means_of_thousands_of_rows(D, group, T, dtype):
+    """Small queries: softmax is almost flat, an output is the mean of thousands of values of about 1, itself about 0.01, and the
+    scores' own errors are far below that. The f16 roundings of the weights (bf16) are of either sign, at most 2^-11, spread
+    evenly: eight standard deviations of their sum; the rest as for a row of many weights. Half an output lost would be 50 times
+    the bound."""
+    lens, hkv, hq = [5000, 4099, 70], 2, 8
+    p = pb.PyrPages(n_kv_heads=hkv, head_dim=D, group=group, page_rows=64, n_pages=200, n_lists=3, max_pages=80)
+    g = torch.Generator().manual_seed(D + group + T)
+    k, v = (torch.randn(3, max(lens), hkv, D, generator=g).to(dtype) for _ in range(2))
+    q = (torch.randn(3, T, hq, D, generator=g) * 2.0 ** -6).to(dtype)
+    p.reserve(_ids(0, 1, 2), _ids(*lens))
+    p.write(k.to(DEV), v.to(DEV), counts=_ids(*lens))
+    out, lse = p.attn(q.to(DEV), lse=True)
+    assert p.status() == 0
+    for i, n in enumerate(lens):
+        parts = [torch.from_numpy(x) for x in _parts(p, i)]
+        for h in range(hq):
+            K, c, s, z0 = (x[:, h // (hq // hkv)] for x in parts)
+            for t in range(T):
+                see = n - (T - 1 - t)
+                x = q[i, t, h].double()
+                z = K[:see] @ x * D ** -0.5
+                w = torch.softmax(z, 0)
+                cs = (c * s)[:see]
+                values = cs + z0[:see]
+                want = w @ values
+                rel = 2 * _score_error(x.numpy(), K.numpy(), D ** -0.5) + 2.0 ** -20 + see * 2.0 ** -26
+                tol = rel * (w @ values.abs() + want.abs()) + 2.0 ** -24 * want.abs()
+                if dtype == BF:
+                    tol = tol + 8 * 2.0 ** -11 / 3 ** 0.5 * torch.sqrt(w.square() @ cs.square()) + 2.0 ** -8 * want.abs()
+                err = (out[i, t, h].double().cpu() - want).abs()
+                assert bool((err <= tol).all()), (i, h, t, float((err / tol).max()))
+                assert abs(float(lse[i, h, t]) - float(torch.logsumexp(z, 0))) <= rel + 2.0 ** -20 * 16
