@@ -673,7 +673,8 @@ struct MmaBody {
         const float m_old = top_score(x), m_new = fmaxf(m_old, mx);
         const float corr = m_new == -INFINITY ? 1.f : ex2((m_old - m_new) * sc2[x]);
         ref[x] = m_new == -INFINITY ? 0.f : m_new;
-        raise[x] = m_new == -INFINITY ? -INFINITY : m_new + kLazy / sc2[x];
+        // (rounded down: where the next number is more than kLazy above, it raises the maximum)
+        raise[x] = m_new == -INFINITY ? -INFINITY : __fadd_rd(m_new, kLazy / sc2[x]);
         l[x] *= corr;
 #pragma unroll
         for (int g = 0; g < G; ++g) zacc[g][x] *= corr;

@@ -192,6 +192,33 @@ def test_columns_with_magnitudes_of_their_own_over_scales_of_many(D, group, orde
     assert told >= 12
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("step", [3.9, 4.1, 5.0, 7.9])
+def test_scores_a_step_of_fp32_apart(step, dtype):
+    """Scores of about 2^26 of which two neighbouring numbers of fp32 are `step` powers of two of weight apart: 32 rows of the
+    lower one, then eight of the upper one. fp32 says no more of the weights than that the upper ones are at least as large; whatever they
+    are, an output lies among the values. (2000 entries: most are one warp's alone, which reads 32 rows, then eight.)"""
+    D, rows, n = 128, 40, 2000
+    p = pb.PyrPages(n_kv_heads=1, head_dim=D, group=32, page_rows=64, n_pages=1, n_lists=1, max_pages=1)
+    g = torch.Generator().manual_seed(5)
+    k = torch.zeros(1, rows, 1, D)
+    k[..., :32] = 1.0                            # 32 of 1 and, in the last rows, 32 of 2^-23: a sum of 32, or of the next number
+    k[:, 32:, :, 32:64] = 2.0 ** -23
+    v = torch.randn(1, rows, 1, D, generator=g)
+    v[..., ::32], v[..., 1::32] = 29.5, -29.5    # every group's scale just below 4
+    p.reserve(_ids(0), rows)
+    p.write(k.to(dtype).to(DEV), v.to(dtype).to(DEV))
+    scale = step * float(np.log(2.0)) * 2.0 ** 18
+    out, lse = p.attn(torch.ones(n, 1, 1, D, dtype=dtype, device=DEV), _ids(*[0] * n), lse=True, softmax_scale=scale)
+    assert p.status() == 0
+    K, c, s, z0 = (torch.from_numpy(x[:, 0]) for x in _parts(p, 0))
+    assert set(K.sum(1).tolist()) == {32.0, 32.0 + 2.0 ** -18}
+    V, got = c * s + z0, out[:, 0, 0].double().cpu()
+    tol = 2.0 ** -8 * V.abs().max(0).values + 2.0 ** -11 * (c * s).max(0).values
+    assert bool((got >= V.min(0).values - tol).all()) and bool((got <= V.max(0).values + tol).all())
+    assert float((lse.double().cpu() / (float(K.sum(1).max()) * scale) - 1).abs().max()) <= 2.0 ** -21
+
+
 def test_tokens_that_see_no_row_get_zeros_whatever_the_values():
     """48 tokens over 40 rows: the first eight, a column group of their own, see nothing, while the scales of V fall from 2^113 to
     2^-22 between two reads of 32 rows (a ratio beyond fp32)."""
