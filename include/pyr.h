@@ -400,8 +400,9 @@ pyr_status_t pyr_glue_argmax(const void* x, int32_t* out, int64_t rows, int32_t 
  * the four dimensions from g * group + 4 * (i * u + t) on.
  * Values, every step in IEEE single precision with rounding to nearest even: zero = min(x) rounded down to bf16, scale =
  * (max(x) - zero) / 15 rounded up to bf16 (0 below 2^-100), code = rint((x - zero) * (1 / scale)), and a code stands for
- * scale * code + zero, which is at most scale / 2 (and a rounding) from x. A group for which max(x) - zero is not finite
- * (an Inf, a NaN, a range beyond single precision) is stored as NaN, so that it shows in what reads it.
+ * scale * code + zero, which is at most scale / 2 (and a rounding) from x; within scale / 2 of single precision's largest number that
+ * can be Inf. A group for which max(x) - zero is not finite (an Inf, a NaN, a range beyond single precision) is stored as NaN,
+ * so that it shows in what reads it.
  *
  * Calls on one handle must be ordered: on one stream, or by events. Two calls, or two replayed graphs, of one handle
  * that can overlap on the GPU race on its tables and on its workspace. Device errors (a list id, count, kept index or
@@ -413,6 +414,8 @@ pyr_status_t pyr_glue_argmax(const void* x, int32_t* out, int64_t rows, int32_t 
  * of 16 rows over a call's entries and KV heads.
  *
  * In every call `lists` (device int32 [n]) names the list of each entry; NULL means lists 0 .. n-1. n = 0 does nothing.
+ * pyr_pages_fork, pyr_pages_compact and, up to 512 rows times KV heads an entry, pyr_pages_write look for a list named twice by
+ * comparing every entry with every other: made for thousands of entries a call, n^2 reads beyond that.
  */
 typedef struct {
   int32_t n_kv_heads;
@@ -481,17 +484,20 @@ pyr_status_t pyr_pages_read(pyr_pages_t* pages, const int32_t* lists, int32_t n,
 
 /*
  * Attention over the lists' rows. q, out (device) are [n, q_len, n_q_heads, head_dim], strides in elements, D contiguous
- * and rows 16-byte aligned, out's rows apart as in pyr_pages_read; n_q_heads a multiple of n_kv_heads. Query token t of entry i sees the first
- * len_i - (q_len - 1 - t) rows: with q_len = 1 all of them, the row stored last included; with more, the last q_len rows are
+ * and rows 16-byte aligned, out's rows apart as in pyr_pages_read; n_q_heads a multiple of n_kv_heads. Query token t of entry i
+ * sees the first len_i - (q_len - 1 - t) rows: with q_len = 1 all of them, the row stored last included; with more, the last q_len rows are
  * those of the query tokens themselves (a chunk of a prompt, drafted tokens). A token that sees no row gets zeros.
  * lse (device, may be NULL) is [n, n_q_heads, q_len] fp32, the natural log of the softmax denominator, -inf for such a
- * token. softmax_scale (at most 2^127) 0 means 1/sqrt(D). Scores, softmax statistics and sums are held in fp32. For bf16, what the matrix
- * instruction multiplies is f16: query elements, scaled by their row's largest, lose bits below 2^-28 of it and vanish below 2^-36;
- * the weight by which a row's V codes are multiplied is rounded by 2^-11 of itself, one below 2^-18 of the column's largest by up to 2^-29
- * of that, times the largest scale that a group has in 32 neighbouring rows (V's zeros and the denominator take it in fp32).
- * Each list is read once per 8 (bf16; 1 to 4 for fp32) query rows of a KV head; bit-reproducible. A list may appear more than once; an entry whose list id
- * is out of range writes nothing. A call whose lists come to more than 2^30 tiles of 16 rows (times KV heads and times eighths of the
- * query rows) for each warp of the machine writes nothing and records PYR_ERR_UNSUPPORTED. bf16 runs on warp-level tensor-core instructions, fp32 on CUDA cores.
+ * token. softmax_scale (at most 2^127) 0 means 1/sqrt(D). Scores, softmax statistics and sums are held in fp32, the sums of
+ * weights times values before they are divided by the weights' (values near the end of fp32's range overflow there).
+ * For bf16, what the matrix instruction multiplies is f16: query elements, scaled by their row's largest, lose bits below 2^-28 of it
+ * and vanish below 2^-36; the weight by which a row's V codes are multiplied is rounded by 2^-11 of itself, one below 2^-18 of the
+ * column's largest by up to 2^-29 of that, times the largest scale that a group has in 32 neighbouring rows (V's zeros and the
+ * denominator take it in fp32).
+ * Each list is read once per 8 (bf16; 1 to 4 for fp32) query rows of a KV head; bit-reproducible. A list may appear more than once;
+ * an entry whose list id is out of range writes nothing. A call whose lists come to more than 2^30 tiles of 16 rows (times KV heads
+ * and times eighths of the query rows) for each warp of the machine writes nothing and records PYR_ERR_UNSUPPORTED.
+ * bf16 runs on warp-level tensor-core instructions, fp32 on CUDA cores.
  */
 pyr_status_t pyr_pages_attn(pyr_pages_t* pages, const int32_t* lists, int32_t n, const void* q, int64_t q_stride_b,
                             int64_t q_stride_t, int64_t q_stride_h, void* out, int64_t o_stride_b, int64_t o_stride_t,
@@ -512,7 +518,8 @@ pyr_status_t pyr_pages_trim(pyr_pages_t* pages, const int32_t* lists, int32_t n,
  * dst_i == src_i compacts in place: idx must ascend strictly, the pages behind the count are given up, and every page in
  * which a row moves must be the list's own. Otherwise dst_i must have pages of its own reserved for count_i rows (what they
  * held is overwritten) and must not be another entry's source; idx may have any order and repeats. A list must not be
- * the destination of two entries. dst_i's length becomes count_i.
+ * the destination of two entries. dst_i's length becomes count_i. Pass one array as src and dst where every list is its own
+ * destination: such an entry of any other call is moved by a single warp for each head.
  */
 pyr_status_t pyr_pages_compact(pyr_pages_t* pages, const int32_t* src, const int32_t* dst, int32_t n, const int32_t* idx,
                                int32_t idx_groups, int64_t idx_stride, const int32_t* counts, int32_t n_rows, void* stream);

@@ -373,19 +373,22 @@ struct CoreBody {
 // is range, so both factors that are not codes are normalised by powers of two: a query row so that its largest element is
 // near f16's (what is then below f16's smallest step is below 2^-35 of that element), and the scales that multiply P, which
 // f16 holds to 2^-11, by a factor per group that follows them (`norm`) and keeps the products near f16's top: many rows of
-// little weight behind one of much add up, and what f16 drops of them is the same for all. (16384 rows of 2^-17.5 of the first one's
-// weight, one of the first 32 with scales 50 times the others': off by up to 0.013 of values of 1.2 with factors near 1.) The factor that a score needs to undo the first, 2^e for
-// a row whose largest element has the exponent e, times 2^9 and the softmax scale, passes fp32 from about e = 122 on:
-// part of it is then multiplied in by itself (`up`), in the stages' branch for edges, which such a segment always takes.
+// little weight behind one of much add up, and what f16 drops of them is the same for all. (16384 rows of 2^-17.5 of the first
+// one's weight, one of the first 32 with scales 50 times the others': off by up to 0.013 of values of 1.2 with factors near 1.)
+// The factor that a score needs to undo the first, 2^e for a row whose largest element has the exponent e, times 2^9 and the
+// softmax scale, passes fp32 from about e = 122 on: part of it is then multiplied in by itself (`up`), in the stages' branch for
+// edges, which such a segment always takes.
 // V's codes have a mean of 7.5, so that o grows with the number of rows while what matters in it grows with its root. The
 // instruction truncates its sums, and an o far above what matters would let that show: every kCentre steps what a group's o
 // have in common is moved to the group's sum of zeros, which is kept apart and rounded. (100 k rows a list, error against 64
 // bits: 1.65e-3 is the output's own rounding, 1.77e-3 with 4 or 8, 1.78e-3 with 16, 1.90e-3 with 64; the rest is P's.)
 //
-// What bounds it: 273 instructions a tile and warp, 88 of them to take codes out of words, half of all on the integer pipe (64 % busy
-// in the main loop) and the rest waiting for one another in 11 warps an SM: 158 registers allow no more (15 warps with 128,
-// some of them spilled, are as fast). Measured with an idle start (64 lists of 1088 rows, 32 heads, 321 MB): 77 us = 4.2 TB/s;
-// 5 us pass before the first tile is there and 7 from the last tile to the end (merging).
+// What bounds it: 277 instructions a tile and warp, 88 of them to take codes out of words, half of all on the integer pipe (52 % busy
+// over a launch) and the rest waiting for one another in 11 warps an SM: 161 registers allow no more (15 warps with 128,
+// some of them spilled, are as fast). Measured with an idle start (64 lists of 1088 rows, 32 heads, 321 MB): 76 us = 4.2 TB/s;
+// by the SMs' clocks about 5 us pass before the first tile is there and 7 from the last tile to the end (merging).
+// A group of V that is zero throughout (heads padded with zeros) has no factor, and every stage looks for one: 64 lists of 1088
+// rows, 32 heads, groups of 32: 94 us, 113 with such a group.
 __device__ __forceinline__ void mma_full(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
                "{%0, %1, %2, %3};"

@@ -379,8 +379,9 @@ __global__ void __launch_bounds__(kRowThreads) write_few_kernel(PagesWriteArgs a
 }
 
 // The values of eight codes: scale * code + zero, the product exact. Codes become numbers two at a time: 0x6400 | n is the f16
-// number 1024 + n, 0x6400 | 16 n is 1024 + 16 n (an integer conversion each kept its pipe, at a quarter of the rate, 58 %
-// busy). 640 k rows of 128 dimensions, K and V, to bf16: 70 us = 6.0 TB/s of 420 MB.
+// number 1024 + n, 0x6400 | 16 n is 1024 + 16 n, which takes no integer conversion. (The conversion pipe is 58 % busy all
+// the same, with those to fp32 and to bf16; DRAM is what bounds it.) 640 k rows of 128 dimensions, K and V, to bf16: 70 us =
+// 6.0 TB/s of 420 MB; a single launch of half of them 38 us = 5.5 TB/s.
 __device__ __forceinline__ void values8(uint32_t codes, uint32_t word, float* x) {
   const float scale = __uint_as_float(word << 16), zero = __uint_as_float(word & 0xFFFF0000u);
 #pragma unroll
