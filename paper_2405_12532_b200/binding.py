@@ -552,7 +552,7 @@ class PyrPages:
         if idx.dim() != 3 or idx.shape[0] != n or idx.dtype is not torch.int32 or idx.get_device() != self._index:
             raise ValueError(f"idx: expected [n, groups, rows] int32 on {self.device}")
         g, rows = idx.shape[1], idx.shape[2]
-        if (rows > 1 and idx.stride(2) != 1) or (g > 1 and idx.stride(1) != rows):
+        if (rows > 1 and idx.stride(2) != 1) or (g > 1 and rows > 0 and idx.stride(1) != rows):
             raise ValueError("idx: its last two dimensions must be contiguous")
         return idx.data_ptr(), g, idx.stride(0) if n > 1 else 0
 
