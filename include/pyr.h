@@ -352,6 +352,8 @@ pyr_status_t pyr_decode_attn_noalloc_status(void* stream, int32_t* host_status);
  *           head_dim] by pos[t] * 10000^(-2i/head_dim): Appendix A.2's "gather" when pos holds the
  *           tokens' original positions (pyr_cache_kept's second pointer), "re-encode" when it counts
  *           from 0. head_dim at most 256.
+ *   rope_table  table[p, :] = the cosines and behind them the sines of (first + p) * base^(-2i/head_dim), i < head_dim / 2, for
+ *           p < n_pos (positions up to 2^31): fp32, taken in double. What pyr_pages_append rotates by.
  *   swiglu  out = silu(gate) * up, n elements.
  *   argmax  out[r] = index of the largest of x[r, 0..n), the lowest index on ties; x [rows, n].
  */
@@ -381,17 +383,18 @@ pyr_status_t pyr_glue_linear_swiglu(const void* x, const void* w_gate, const voi
                                     int32_t k, int32_t dtype, void* stream);
 pyr_status_t pyr_glue_rope(void* x, const int32_t* pos, int64_t tokens, int32_t n_heads, int32_t head_dim,
                            int32_t dtype, void* stream);
+pyr_status_t pyr_glue_rope_table(float* table, int64_t first, int64_t n_pos, int32_t head_dim, double base, void* stream);
 pyr_status_t pyr_glue_swiglu(const void* gate, const void* up, void* out, int64_t n, int32_t dtype, void* stream);
 pyr_status_t pyr_glue_argmax(const void* x, int32_t* out, int64_t rows, int32_t n, int32_t dtype, void* stream);
 
 /*
- * A paged cache held in 4 bits. (No counterpart in the paper, whose cache is one block per layer: this is how a
+ * A paged cache held in 4 or in 8 bits. (No counterpart in the paper, whose cache is one block per layer: this is how a
  * serving engine keeps what the selection leaves.) A POOL of pages, and LISTS of pages that hold rows in order: one list
  * is one layer's cache of one sequence, with a length of its own. Lists share pages: forking one counts its pages once
  * more instead of copying them. All state lies in one device buffer of the caller's, lengths and page tables included,
  * so every call below works from device memory alone and can be captured into a CUDA graph and replayed.
  *
- * Format. A page is [n_kv_heads][page_rows / 16] tiles of 16 rows. A tile is, in this order: the K codes (16 rows of
+ * 4-bit format. A page is [n_kv_heads][page_rows / 16] tiles of 16 rows. A tile is, in this order: the K codes (16 rows of
  * head_dim / 2 bytes), the V codes, and for K and then V one 32-bit word per row and group of `group` dimensions (row
  * major): bf16 scale in the low half, bf16 zero in the high half. tile bytes = 16 * (head_dim + 8 * head_dim / group).
  * Codes lie in the order in which the attention's matrix fragments take them: with u = group / 32 and g the group,
@@ -403,6 +406,19 @@ pyr_status_t pyr_glue_argmax(const void* x, int32_t* out, int64_t rows, int32_t 
  * scale * code + zero, which is at most scale / 2 (and a rounding) from x; within scale / 2 of single precision's largest number that
  * can be Inf. A group for which max(x) - zero is not finite (an Inf, a NaN, a range beyond single precision) is stored as NaN,
  * so that it shows in what reads it.
+ *
+ * 8-bit format (flags PYR_PAGES_8BIT). One scale for a page and head, for K and for V. A page is [n_kv_heads] of: a header of 2 head_dim + 16
+ * bytes, the least and then the largest K code of each dimension (signed bytes), the K scale and the V scale (fp32) and 8 bytes
+ * unused; then page_rows / 16 tiles of 16 rows. A tile is 16 head_dim bytes of K codes, as many of V codes, the two scales once more and 8
+ * bytes unused. A code lies as the byte code + 128. The 16-byte chunk x of K row r (dimensions 16 x ..) lies at r head_dim + 16 (x xor 4 (r & 1))
+ * with head_dim 128, r head_dim + 16 x with 64. Of V, with j = (r & 7) / 2, b = 2 (r & 1) + r / 8, e = head_dim / 8 and w = d mod e, the
+ * code of row r and dimension d lies at 4 head_dim j + 4 e (d / e) + 16 ((w / 4) xor (j mod (e / 4))) + 4 (w mod 4) + b.
+ * Values, every step in IEEE single precision with rounding to nearest even: where rows are stored in a page, its scale becomes s =
+ * max(s_old, amax / 127), amax the largest magnitude among them (amax / 127 below 2^-100 counts as 0) and s_old the scale before if
+ * other rows of the list stay in the page, else 0. Codes of the rows are rint(x * (1 / s)); codes that stay become rint(code * (s_old / s)).
+ * A code stands for s * code: at most s / 2 (and a rounding) from x for a new row, up to another s / 2 away for each time that s grew
+ * since. The header's extrema are those of the codes stored since the page held no other rows (scaled as they are). If amax is not
+ * finite, the page's rows of that head and plane are NaN until it is filled anew; within s / 2 of single precision's largest number a value can be Inf.
  *
  * Calls on one handle must be ordered: on one stream, or by events. Two calls, or two replayed graphs, of one handle
  * that can overlap on the GPU race on its tables and on its workspace. Device errors (a list id, count, kept index or
@@ -417,15 +433,16 @@ pyr_status_t pyr_glue_argmax(const void* x, int32_t* out, int64_t rows, int32_t 
  * pyr_pages_fork, pyr_pages_compact and, up to 512 rows times KV heads an entry, pyr_pages_write look for a list named twice by
  * comparing every entry with every other: made for thousands of entries a call, n^2 reads beyond that.
  */
+#define PYR_PAGES_8BIT 8u
 typedef struct {
   int32_t n_kv_heads;
   int32_t head_dim;    /* 64 or 128                                            */
-  int32_t group;       /* dimensions that share a scale: 32, 64 or 128, at most head_dim */
-  int32_t page_rows;   /* rows of a page: a multiple of 16, at most 1024       */
+  int32_t group;       /* 4 bits: dimensions that share a scale: 32, 64 or 128, at most head_dim; 8 bits: 0 */
+  int32_t page_rows;   /* rows of a page: a multiple of 16, at most 1024 (8 bits: 128) */
   int32_t n_pages;     /* pages of the pool (2^56 bytes at most)               */
   int32_t n_lists;     /* at most 2^19                                         */
   int32_t max_pages;   /* pages that one list can hold                         */
-  uint32_t flags;      /* 0                                                    */
+  uint32_t flags;      /* 0, or PYR_PAGES_8BIT                                 */
 } pyr_pages_config_t;
 
 typedef struct pyr_pages pyr_pages_t;
@@ -464,7 +481,7 @@ pyr_status_t pyr_pages_reserve(pyr_pages_t* pages, const int32_t* lists, int32_t
  * the rows [first_i, first_i + count_i) of its list (first: device int32 [n], each at most the list's length; NULL: the
  * list's end). With idx (device int32 [n, idx_groups, n_rows] with idx_stride elements between entries; idx_groups 1 or
  * n_kv_heads; pyr_cache_kept's first pointer is one) row x of head h is source row idx[i][h's group][x]: the Gather of
- * Algorithm 1 straight into 4-bit pages; without, source row x (an index out of range stores a row of NaN and is reported).
+ * Algorithm 1 straight into pages; without, source row x (an index out of range stores a row of NaN and is reported).
  * The list's length becomes max(length, first_i + count_i).
  * Every page written must be the list's own: reserved, and held by no other list. One row per list is the decode step's
  * append.
@@ -473,6 +490,24 @@ pyr_status_t pyr_pages_write(pyr_pages_t* pages, const int32_t* lists, int32_t n
                              const void* v, int64_t stride_b, int64_t stride_n, int64_t stride_h, int32_t src_rows,
                              int32_t dtype, const int32_t* idx, int32_t idx_groups, int64_t idx_stride, const int32_t* counts,
                              int32_t n_rows, void* stream);
+
+/*
+ * Stores rows as pyr_pages_write does, in an 8-bit cache (PYR_ERR_UNSUPPORTED in 4 bits), with the rotation of positions applied on the
+ * way: keys are turned in fp32 and stored from that, not rounded to dtype in between. pos (device int32 [n, idx_groups, n_rows], pos_stride
+ * elements between entries) is the position of row x of head h's group, the row's place in `rope` (device fp32 [n_pos, head_dim], 16-byte
+ * aligned: head_dim / 2 cosines and as many sines a position, e.g. from pyr_glue_rope_table): (x1, x2) becomes (x1 c - x2 s, x2 c + x1 s) for
+ * the pairs (i, i + head_dim / 2), every product and sum rounded. pos NULL: keys as they are, rope is not looked at. A position
+ * outside [0, n_pos) stores a row of NaN, keys and values, and is reported.
+ * q, q_out (device, may both be NULL; with pos and without idx only) are [n, n_rows, n_q_heads, head_dim] of the same dtype, strided as k: q_out
+ * becomes q turned by the row's position, in fp32 and rounded once (NaN for a position out of range); queries beside rows that are not
+ * stored (behind counts_i, of a refused entry) pass as they are. q_out may be q, with the same strides. n_q_heads at most 65535.
+ */
+pyr_status_t pyr_pages_append(pyr_pages_t* pages, const int32_t* lists, int32_t n, const int32_t* first, const void* k,
+                              const void* v, int64_t stride_b, int64_t stride_n, int64_t stride_h, int32_t src_rows,
+                              int32_t dtype, const int32_t* pos, int64_t pos_stride, const float* rope, int32_t n_pos,
+                              const void* q, void* q_out, int64_t q_stride_b, int64_t q_stride_n, int64_t q_stride_h,
+                              int64_t o_stride_b, int64_t o_stride_n, int64_t o_stride_h, int32_t n_q_heads, const int32_t* idx,
+                              int32_t idx_groups, int64_t idx_stride, const int32_t* counts, int32_t n_rows, void* stream);
 
 /* Reads rows back as the values they stand for: k, v (device) are [n, n_rows, n_kv_heads, head_dim], strided as above, no two rows
  * over one another (each stride passes what the smaller ones span).
@@ -498,11 +533,43 @@ pyr_status_t pyr_pages_read(pyr_pages_t* pages, const int32_t* lists, int32_t n,
  * an entry whose list id is out of range writes nothing. A call whose lists come to more than 2^30 tiles of 16 rows (times KV heads
  * and times eighths of the query rows) for each warp of the machine writes nothing and records PYR_ERR_UNSUPPORTED.
  * bf16 runs on warp-level tensor-core instructions, fp32 on CUDA cores.
+ * In 8 bits both types run on the warp-level instruction, 8 query rows of a KV head at a time, and products are of f16: a query element is
+ * exact in bf16 down to 2^-31 of its row's largest element and held to 2^-39 of that below, for fp32 as two of them to 2^-22 of itself or
+ * 2^-39 of the largest, whichever is more; the weight that multiplies a row's V codes, p times the page's scale, to 2^-11 of itself (fp32: two,
+ * 2^-22) or 2^-35 of the column's largest such weight, whichever is more. Scores and sums are held in fp32, the instruction's own no longer
+ * than 32 rows. A score beyond fp32's range is not a number.
  */
 pyr_status_t pyr_pages_attn(pyr_pages_t* pages, const int32_t* lists, int32_t n, const void* q, int64_t q_stride_b,
                             int64_t q_stride_t, int64_t q_stride_h, void* out, int64_t o_stride_b, int64_t o_stride_t,
                             int64_t o_stride_h, float* lse, int32_t q_len, int32_t n_q_heads, int32_t dtype,
                             float softmax_scale, void* stream);
+
+/*
+ * Which pages of an 8-bit cache a query reads (PYR_ERR_UNSUPPORTED in 4 bits). q as in pyr_pages_attn; slots (device int32
+ * [n, q_len, n_kv_heads, n_slots]) gets, for each token and KV head, the slots in the list's page table of the n_slots pages with the
+ * largest scores, ascending, -1 behind them. Candidates are the pages that hold rows the token sees; where they are no more than
+ * n_slots all are taken. The first keep_first and the last keep_last of them (together at most n_slots) are taken whatever they score; an exact
+ * tie goes to the lower slot. Score: the largest, over the head's query heads, of (s_q * s_K) * sum_d max(qc_d * min_d, qc_d * max_d), min and
+ * max the header's extrema, s_K its K scale, qc = rint(q * (1 / s_q)) with s_q = max|q| / 127 as for rows (products rounded to fp32, the sum
+ * exact): an upper bound of q . K for the page's rows up to the query's rounding. NaN counts as Inf; a page whose id is out of range
+ * comes last and is reported. An entry whose list id is out of range gets -1 throughout. All pages of a list are scored by the CTAs of one
+ * (entry, token, KV head): 4 * max_pages + (n_q_heads / n_kv_heads) * (2 * head_dim + 4) bytes must fit 200 KB.
+ */
+pyr_status_t pyr_pages_select(pyr_pages_t* pages, const int32_t* lists, int32_t n, const void* q, int64_t q_stride_b,
+                              int64_t q_stride_t, int64_t q_stride_h, int32_t q_len, int32_t n_q_heads, int32_t dtype,
+                              int32_t* slots, int32_t n_slots, int32_t keep_first, int32_t keep_last, void* stream);
+
+/*
+ * Attention over chosen pages of an 8-bit cache (PYR_ERR_UNSUPPORTED in 4 bits): pyr_pages_attn for which token t and KV head h of entry i
+ * see only those of their rows that lie in the page slots slots[i, t, h, :] (device int32 [n, q_len, n_kv_heads, n_slots], as pyr_pages_select
+ * writes them or the caller's own). Each page at most once, in any order, -1 only behind them; as many are looked at as pages hold
+ * rows that the token sees. A page behind what the token sees takes no part; so does a slot out of range, which is
+ * reported. Every token reads its pages once per 8 query heads of a KV head. n * q_len at most 2^31 - 4097.
+ */
+pyr_status_t pyr_pages_attn_blocks(pyr_pages_t* pages, const int32_t* lists, int32_t n, const int32_t* slots, int32_t n_slots,
+                                   const void* q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, void* out,
+                                   int64_t o_stride_b, int64_t o_stride_t, int64_t o_stride_h, float* lse, int32_t q_len,
+                                   int32_t n_q_heads, int32_t dtype, float softmax_scale, void* stream);
 
 /* Makes list dst_i a copy of list src_i that shares its pages. dst_i must hold no page and appear nowhere else in the call;
  * src_i may repeat. */
@@ -513,6 +580,7 @@ pyr_status_t pyr_pages_fork(pyr_pages_t* pages, const int32_t* src, const int32_
 pyr_status_t pyr_pages_trim(pyr_pages_t* pages, const int32_t* lists, int32_t n, const int32_t* rows, void* stream);
 
 /*
+ * (4 bits only; rows of pages whose scales differ cannot move as they are: PYR_ERR_UNSUPPORTED in 8 bits.)
  * Moves rows: rows 0 .. count_i - 1 of list dst_i become the rows idx[i][h's group][x] of list src_i, stored bytes as they
  * are (idx, idx_groups, idx_stride, counts, n_rows as in pyr_pages_write; idx NULL: the first count_i rows, a copy).
  * dst_i == src_i compacts in place: idx must ascend strictly, the pages behind the count are given up, and every page in

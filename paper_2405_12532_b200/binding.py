@@ -32,7 +32,7 @@ EXPORTS = [
     "pyr_decode_attn_noalloc", "pyr_decode_attn_noalloc_status",
     "pyr_pages_bytes", "pyr_pages_alloc", "pyr_pages_free", "pyr_pages_reset", "pyr_pages_view", "pyr_pages_status",
     "pyr_pages_reserve", "pyr_pages_write", "pyr_pages_read", "pyr_pages_attn", "pyr_pages_fork", "pyr_pages_trim",
-    "pyr_pages_compact",
+    "pyr_pages_compact", "pyr_pages_append", "pyr_pages_select", "pyr_pages_attn_blocks", "pyr_glue_rope_table",
 ]
 
 
@@ -122,6 +122,11 @@ def lib() -> C.CDLL:
         L.pyr_pages_fork.argtypes = [vp, vp, vp, i32, vp]
         L.pyr_pages_trim.argtypes = [vp, vp, i32, vp, vp]
         L.pyr_pages_compact.argtypes = [vp, vp, vp, i32, vp, i32, i64, vp, i32, vp]
+        L.pyr_pages_append.argtypes = ([vp, vp, i32, vp, vp, vp, i64, i64, i64, i32, i32, vp, i64, vp, i32, vp, vp] + [i64] * 6 +
+                                       [i32, vp, i32, i64, vp, i32, vp])
+        L.pyr_pages_select.argtypes = [vp, vp, i32, vp, i64, i64, i64, i32, i32, i32, vp, i32, i32, i32, vp]
+        L.pyr_pages_attn_blocks.argtypes = [vp, vp, i32, vp, i32, vp, i64, i64, i64, vp, i64, i64, i64, vp, i32, i32, i32, C.c_float, vp]
+        L.pyr_glue_rope_table.argtypes = [vp, i64, i64, i32, C.c_double, vp]
         for name in EXPORTS:
             fn = getattr(L, name)
             if name not in ("pyr_status_string", "pyr_version", "pyr_launch_count", "pyr_recent_len_from_ratio"):
@@ -285,6 +290,15 @@ def glue_rope_(x, pos):
     _check(lib().pyr_glue_rope(x.data_ptr(), pos.data_ptr(), pos.numel(), x.shape[-2], x.shape[-1], _dt(x),
                                C.c_void_p(_stream_ptr(None))), "pyr_glue_rope")
     return x
+
+
+def glue_rope_table(n_pos: int, head_dim: int, base: float = 10000.0, first: int = 0, device="cuda"):
+    """fp32 [n_pos, head_dim]: cosines and sines of the positions first .. first + n_pos - 1 (pyr_glue_rope_table)."""
+    out = torch.empty(n_pos, head_dim, dtype=torch.float32, device=device)
+    with torch.cuda.device(out.device):
+        _check(lib().pyr_glue_rope_table(out.data_ptr(), first, n_pos, head_dim, float(base), C.c_void_p(_stream_ptr(None))),
+               "pyr_glue_rope_table")
+    return out
 
 
 def glue_swiglu(gate, up):
@@ -455,7 +469,17 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 _PAGES_DTYPES = {torch.bfloat16: PYR_BF16, torch.float32: PYR_F32}
 
 
-def make_pages_config(*, n_kv_heads, head_dim, n_pages, n_lists, max_pages, group=64, page_rows=64, flags=0) -> PyrPagesConfig:
+PYR_PAGES_8BIT = 8
+
+
+def make_pages_config(*, n_kv_heads, head_dim, n_pages, n_lists, max_pages, group=None, page_rows=64, flags=0, bits=4) -> PyrPagesConfig:
+    """bits=8: one scale for a page and head, no `group`; bits=4: a scale for each row and `group` (64) dimensions."""
+    if bits not in (4, 8):
+        raise ValueError("bits: 4 or 8")
+    if bits == 8:
+        flags |= PYR_PAGES_8BIT
+    if group is None:
+        group = 0 if bits == 8 else 64
     return PyrPagesConfig(n_kv_heads, head_dim, group, page_rows, n_pages, n_lists, max_pages, flags)
 
 
@@ -466,7 +490,7 @@ def pyr_pages_bytes(cfg: PyrPagesConfig) -> tuple[int, int]:
 
 
 class PyrPages:
-    """A paged 4-bit cache (pyr_pages_*): the handle plus the torch buffer that backs it, emptied on creation. `lists` arguments
+    """A paged cache in 4 or (bits=8) 8 bits (pyr_pages_*): the handle plus the torch buffer that backs it, emptied on creation. `lists` arguments
     are int32 tensors of list ids, `idx` [n, groups, rows] int32 with its last two dimensions contiguous; the views `pool`
     [n_pages, page bytes] uint8, `table`, `lens` and `refs` are the device state itself. A call runs on the current stream of
     the cache's device, or on `stream`; device-side errors are read with status()."""
@@ -546,14 +570,14 @@ class PyrPages:
             raise ValueError(f"k, v: expected {self._heads} heads, and keys and values alike in shape, type and strides")
         return shape, strides, dtype
 
-    def _idx(self, idx, n):
+    def _idx(self, idx, n, what="idx"):
         if idx is None:
             return None, 1, 0
         if idx.dim() != 3 or idx.shape[0] != n or idx.dtype is not torch.int32 or idx.get_device() != self._index:
-            raise ValueError(f"idx: expected [n, groups, rows] int32 on {self.device}")
+            raise ValueError(f"{what}: expected [n, groups, rows] int32 on {self.device}")
         g, rows = idx.shape[1], idx.shape[2]
         if (rows > 1 and idx.stride(2) != 1) or (g > 1 and rows > 0 and idx.stride(1) != rows):
-            raise ValueError("idx: its last two dimensions must be contiguous")
+            raise ValueError(f"{what}: its last two dimensions must be contiguous")
         return idx.data_ptr(), g, idx.stride(0) if n > 1 else 0
 
     # --- state
@@ -585,6 +609,42 @@ class PyrPages:
         self._run("pyr_pages_write", stream, self._ids(lists, n), n, self._ids(first, n, "first"), k.data_ptr(), v.data_ptr(), sb, sn,
                   sh, src, dtype, ip, groups, istride, self._ids(counts, n, "counts"), src if idx is None else idx.shape[2])
 
+    def append(self, k, v, lists=None, first=None, pos=None, rope=None, q=None, q_out=None, idx=None, counts=None, stream=None):
+        """write() into an 8-bit cache with keys turned by the positions pos (int32 [n, groups, rows], groups as in idx, 1 without) in the table
+        rope (fp32 [positions, D], see glue_rope_table). With q [n, rows, Hq, D] also returns the turned queries (in q_out if given)."""
+        if stream is not None:
+            with torch.cuda.device(self._index), torch.cuda.stream(stream):    # what is allocated here is used on that stream
+                return self.append(k, v, lists, first, pos, rope, q, q_out, idx, counts)
+        (n, src, _, _), (sb, sn, sh, _), dtype = self._rows(k, v)
+        ip, groups, istride = self._idx(idx, n)
+        rows = src if idx is None else idx.shape[2]
+        pp, pstride, rp, n_pos = None, 0, None, 0
+        if pos is not None:
+            if pos.dim() != 3 or tuple(pos.shape) != (n, groups, rows):
+                raise ValueError(f"pos: expected int32 [{n}, {groups}, {rows}]")
+            pp, _, pstride = self._idx(pos, n, "pos")
+            if (rope is None or rope.dtype is not torch.float32 or rope.dim() != 2 or rope.shape[1] != self._dim or
+                    rope.get_device() != self._index or not rope.is_contiguous()):
+                raise ValueError(f"rope: expected a contiguous fp32 table [positions, {self._dim}] on {self.device}")
+            rp, n_pos = rope.data_ptr(), rope.shape[0]
+        qp = op = None
+        qs = os = (0, 0, 0)
+        hq = 0
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty_like(q)
+            shape, qs, qdt = self._tensor(q, "q")
+            shape_o, os, odt = self._tensor(q_out, "q_out")
+            if shape[:2] != (n, rows) or qdt != dtype or shape_o != shape or odt != qdt:
+                raise ValueError(f"q, q_out: expected tensors [{n}, {rows}, heads, {self._dim}] of the rows' type")
+            qp, op, hq = q.data_ptr(), q_out.data_ptr(), shape[2]
+        elif q_out is not None:
+            raise ValueError("q_out: only with q")
+        self._run("pyr_pages_append", None, self._ids(lists, n), n, self._ids(first, n, "first"), k.data_ptr(), v.data_ptr(), sb, sn, sh,
+                  src, dtype, pp, pstride, rp, n_pos, qp, op, qs[0], qs[1], qs[2], os[0], os[1], os[2], hq, ip, groups, istride,
+                  self._ids(counts, n, "counts"), rows)
+        return q_out
+
     def read(self, k, v, lists=None, first=None, counts=None, stream=None):
         """Fills k, v [n, rows, Hkv, D] with the lists' rows from row first (0) on; rows a list does not have stay as they are."""
         (n, rows, _, _), (sb, sn, sh, _), dtype = self._rows(k, v)
@@ -606,6 +666,44 @@ class PyrPages:
         stats = torch.empty(n, hq, t, dtype=torch.float32, device=self.device) if lse else None
         self._run("pyr_pages_attn", None, self._ids(lists, n), n, q.data_ptr(), qb, qt, qh, out.data_ptr(), ob, ot, oh,
                   stats.data_ptr() if lse else None, t, hq, dtype, softmax_scale)
+        return (out, stats) if lse else out
+
+    def select(self, q, n_slots: int, lists=None, keep_first: int = 0, keep_last: int = 0, out=None, stream=None):
+        """The page slots that each token and KV head of q [n, q_len, Hq, D] reads, by score: int32 [n, q_len, Hkv, n_slots], ascending, -1
+        behind them; the first keep_first and last keep_last pages always (8-bit caches)."""
+        if stream is not None:
+            with torch.cuda.device(self._index), torch.cuda.stream(stream):
+                return self.select(q, n_slots, lists, keep_first, keep_last, out)
+        (n, t, hq, _), (qb, qt, qh, _), dtype = self._tensor(q, "q")
+        if out is None:
+            out = torch.empty(n, t, self._heads, n_slots, dtype=torch.int32, device=self.device)
+        else:
+            self._slots(out, n, t, n_slots)
+        self._run("pyr_pages_select", None, self._ids(lists, n), n, q.data_ptr(), qb, qt, qh, t, hq, dtype, out.data_ptr(), n_slots, keep_first,
+                  keep_last)
+        return out
+
+    def _slots(self, slots, n, t, n_slots):
+        if (slots.dtype is not torch.int32 or tuple(slots.shape) != (n, t, self._heads, n_slots) or slots.get_device() != self._index or
+                not slots.is_contiguous()):
+            raise ValueError(f"slots: expected contiguous int32 [{n}, {t}, {self._heads}, slots] on {self.device}")
+
+    def attn_blocks(self, q, slots, lists=None, out=None, lse=False, softmax_scale: float = 0.0, stream=None):
+        """attn() over the page slots int32 [n, q_len, Hkv, n_slots] of each token and KV head (8-bit caches)."""
+        if stream is not None:
+            with torch.cuda.device(self._index), torch.cuda.stream(stream):
+                return self.attn_blocks(q, slots, lists, out, lse, softmax_scale)
+        shape, (qb, qt, qh, _), dtype = self._tensor(q, "q")
+        n, t, hq, _ = shape
+        self._slots(slots, n, t, slots.shape[-1])
+        if out is None:
+            out = torch.empty_like(q)
+        shape_o, (ob, ot, oh, _), dtype_o = self._tensor(out, "out")
+        if shape_o != shape or dtype_o != dtype:
+            raise ValueError("out: expected a tensor like q")
+        stats = torch.empty(n, hq, t, dtype=torch.float32, device=self.device) if lse else None
+        self._run("pyr_pages_attn_blocks", None, self._ids(lists, n), n, slots.data_ptr(), slots.shape[-1], q.data_ptr(), qb, qt, qh,
+                  out.data_ptr(), ob, ot, oh, stats.data_ptr() if lse else None, t, hq, dtype, softmax_scale)
         return (out, stats) if lse else out
 
     def fork(self, src, dst, stream=None):

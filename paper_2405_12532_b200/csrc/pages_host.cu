@@ -1,4 +1,4 @@
-// Host side of the paged 4-bit cache (pyr_pages_*): argument checks, carving of the caller's buffer, dispatch. Nothing here
+// Host side of the paged cache (pyr_pages_*): argument checks, carving of the caller's buffer, dispatch. Nothing here
 // reads device memory: lengths and tables live on the device, and what depends on them is checked by the kernels.
 #include <cmath>
 #include <new>
@@ -18,22 +18,31 @@ struct PagesLayout {
   int slices;
 };
 
+int tile_bytes(const pyr_pages_config_t* c) {
+  return c->group ? pyr::pages_tile_bytes(c->head_dim, c->group) : pyr::pages8_tile_bytes(c->head_dim);
+}
+int head_extra(const pyr_pages_config_t* c) { return c->group ? 0 : pyr::pages8_head_extra(c->head_dim); }
+size_t page_bytes(const pyr_pages_config_t* c) {
+  return (size_t)c->n_kv_heads * ((size_t)(c->page_rows / pyr::kPageTile) * tile_bytes(c) + head_extra(c));
+}
+
 pyr_status_t validate(const pyr_pages_config_t* c) {
   if (!c) return PYR_ERR_NULL;
-  if (c->n_kv_heads < 1 || c->n_pages < 1 || c->n_lists < 1 || c->max_pages < 1 || c->page_rows < 1 || c->flags != 0)
+  const bool bytes = c->flags == PYR_PAGES_8BIT;
+  if (c->n_kv_heads < 1 || c->n_pages < 1 || c->n_lists < 1 || c->max_pages < 1 || c->page_rows < 1 || (c->flags != 0 && !bytes) ||
+      (bytes && c->group != 0))
     return PYR_ERR_INVALID;
   if (c->head_dim != 64 && c->head_dim != 128) return PYR_ERR_UNSUPPORTED;
-  if (c->group != 32 && c->group != 64 && c->group != 128) return PYR_ERR_UNSUPPORTED;
+  if (!bytes && c->group != 32 && c->group != 64 && c->group != 128) return PYR_ERR_UNSUPPORTED;
   if (c->group > c->head_dim) return PYR_ERR_INVALID;
-  if (c->page_rows % pyr::kPageTile || c->page_rows > pyr::kMaxPageRows || c->n_lists > pyr::kMaxLists ||
+  if (c->page_rows % pyr::kPageTile || c->page_rows > (bytes ? pyr::kPageRows8 : pyr::kMaxPageRows) || c->n_lists > pyr::kMaxLists ||
       c->n_kv_heads > 65535)
     return PYR_ERR_UNSUPPORTED;
   // a list's length is an int32, and so is every page id that the reserve scan rounds up to whole slices
   if ((int64_t)c->max_pages * c->page_rows > 0x7fffffff - pyr::kMaxPageRows || c->n_pages > 0x7fffffff - pyr::kReserveSlice)
     return PYR_ERR_UNSUPPORTED;
   // the buffer's size in bytes must be a number of 64 bits with room to spare (the table's is: 2^19 lists of 2^27 pages)
-  const uint64_t page_bytes = (uint64_t)c->n_kv_heads * (c->page_rows / pyr::kPageTile) * pyr::pages_tile_bytes(c->head_dim, c->group);
-  if (page_bytes > kMaxPool / (uint64_t)c->n_pages) return PYR_ERR_UNSUPPORTED;
+  if ((uint64_t)page_bytes(c) > kMaxPool / (uint64_t)c->n_pages) return PYR_ERR_UNSUPPORTED;
   return PYR_OK;
 }
 
@@ -53,8 +62,7 @@ void plan(const pyr_pages_config_t* c, PagesLayout* l) {
   l->free_ids = take((size_t)l->slices * pyr::kReserveSlice * 4);
   l->slice_first = take((size_t)(l->slices + 1) * 4);
   l->partial = take((size_t)pyr::kAttnMaxCtas * 2 * pyr::kAttnCols * (c->head_dim + 2) * 4);
-  l->pool = take((size_t)c->n_pages * c->n_kv_heads * (c->page_rows / pyr::kPageTile) *
-                 pyr::pages_tile_bytes(c->head_dim, c->group));
+  l->pool = take((size_t)c->n_pages * page_bytes(c));
   l->total = off;
 }
 
@@ -82,7 +90,8 @@ pyr::PagesView view(const pyr_pages* h) {
   p.status = at<int>(h, h->lay.status);
   p.Hkv = c.n_kv_heads; p.D = c.head_dim; p.group = c.group; p.page_rows = c.page_rows;
   p.tiles_per_page = c.page_rows / pyr::kPageTile;
-  p.tile_bytes = pyr::pages_tile_bytes(c.head_dim, c.group);
+  p.tile_bytes = tile_bytes(&c);
+  p.head_extra = head_extra(&c);
   p.n_pages = c.n_pages; p.n_lists = c.n_lists; p.max_pages = c.max_pages;
   return p;
 }
@@ -134,6 +143,36 @@ bool rows_apart(const pyr_pages* h, int64_t sb, int64_t sn, int64_t sh, int64_t 
     span += (__int128)x.stride * (x.size - 1);
   }
   return true;
+}
+
+// What attention over all rows and over chosen pages ask of their arguments, and those arguments.
+pyr_status_t check_attn(const pyr_pages* h, const int32_t* lists, int32_t n, const void* q, int64_t qsb, int64_t qst, int64_t qsh,
+                        const void* out, int64_t osb, int64_t ost, int64_t osh, int32_t q_len, int32_t n_q_heads, int32_t dtype,
+                        float softmax_scale) {
+  pyr_status_t st = check_call(h, n, false);
+  if (st != PYR_OK) return st;
+  if (q_len < 1 || n_q_heads < 1 || n_q_heads % h->cfg.n_kv_heads || !default_lists_fit(h, lists, n)) return PYR_ERR_INVALID;
+  if (!(softmax_scale >= 0.0f) || softmax_scale > 0x1p127f) return PYR_ERR_INVALID;     // (times log2 e it is a number)
+  st = check_rows(h, q, q, dtype, qsb, qst, qsh, n, q_len, n_q_heads);
+  if (st == PYR_OK) st = check_rows(h, out, out, dtype, osb, ost, osh, n, q_len, n_q_heads);
+  if (st != PYR_OK) return st;
+  const int64_t cols = (int64_t)q_len * (n_q_heads / h->cfg.n_kv_heads);
+  if (cols > (1 << 20)) return PYR_ERR_UNSUPPORTED;
+  if (!rows_apart(h, osb, ost, osh, n, q_len, n_q_heads)) return PYR_ERR_INVALID;
+  return PYR_OK;
+}
+pyr::PagesAttnArgs attn_args(const pyr_pages* h, const int32_t* lists, int32_t n, const void* q, int64_t qsb, int64_t qst, int64_t qsh,
+                             void* out, int64_t osb, int64_t ost, int64_t osh, float* lse, int32_t q_len, int32_t n_q_heads,
+                             int32_t dtype, float softmax_scale) {
+  pyr::PagesAttnArgs a;
+  a.p = view(h);
+  a.lists = lists; a.n = n; a.q = q; a.out = out; a.lse = lse;
+  a.qsb = qsb; a.qst = qst; a.qsh = qsh; a.osb = osb; a.ost = ost; a.osh = osh;
+  a.T = q_len; a.Hq = n_q_heads; a.rep = n_q_heads / h->cfg.n_kv_heads; a.dtype = dtype;
+  a.scale = softmax_scale > 0.0f ? softmax_scale : (float)(1.0 / std::sqrt((double)h->cfg.head_dim));
+  a.partial = at<float>(h, h->lay.partial);
+  a.arrived = at<int32_t>(h, h->lay.arrived);
+  return a;
 }
 
 pyr_status_t check_idx(const pyr_pages* h, const int32_t* idx, int32_t groups, int64_t stride, int32_t n_rows) {
@@ -265,7 +304,57 @@ pyr_status_t pyr_pages_write(pyr_pages_t* h, const int32_t* lists, int32_t n, co
   a.src_rows = src_rows; a.dtype = dtype; a.idx = idx; a.idx_groups = idx ? idx_groups : 1; a.idx_stride = idx_stride;
   a.counts = counts; a.n_rows = n_rows;
   a.plan = at<int32_t>(h, h->lay.plan);
+  if (h->cfg.flags & PYR_PAGES_8BIT) {
+    pyr::PagesAppendArgs b{};
+    b.w = a;
+    b.done = at<int32_t>(h, h->lay.moved);
+    PYR_PAGES(pyr::launch_pages_append8(b, &launches, static_cast<cudaStream_t>(stream)));
+  }
   PYR_PAGES(pyr::launch_pages_write(a, &launches, static_cast<cudaStream_t>(stream)));
+}
+
+pyr_status_t pyr_pages_append(pyr_pages_t* h, const int32_t* lists, int32_t n, const int32_t* first, const void* k,
+                              const void* v, int64_t sb, int64_t sn, int64_t sh, int32_t src_rows, int32_t dtype,
+                              const int32_t* pos, int64_t pos_stride, const float* rope, int32_t n_pos, const void* q, void* q_out,
+                              int64_t qsb, int64_t qsn, int64_t qsh, int64_t osb, int64_t osn, int64_t osh, int32_t n_q_heads,
+                              const int32_t* idx, int32_t idx_groups, int64_t idx_stride, const int32_t* counts, int32_t n_rows,
+                              void* stream) {
+  pyr_status_t st = check_call(h, n, true);
+  if (st == PYR_OK) st = check_rows(h, k, v, dtype, sb, sn, sh, n, src_rows, h->cfg.n_kv_heads);
+  if (st == PYR_OK) st = check_idx(h, idx, idx_groups, idx_stride, n_rows);
+  if (st != PYR_OK) return st;
+  if (n_rows < 0 || src_rows < 0 || (!idx && n_rows > src_rows)) return PYR_ERR_INVALID;
+  if (pos) {
+    if (!rope) return PYR_ERR_NULL;
+    if (n_pos < 1 || pos_stride < 0 || reinterpret_cast<uintptr_t>(rope) % 16) return PYR_ERR_INVALID;
+  }
+  if (q || q_out) {
+    // (queries take the positions of the rows beside them: without an index list)
+    if (!pos || idx || n_q_heads < 1) return PYR_ERR_INVALID;
+    st = check_rows(h, q, q_out, dtype, qsb, qsn, qsh, n, n_rows, n_q_heads);
+    if (st == PYR_OK) st = check_rows(h, q, q_out, dtype, osb, osn, osh, n, n_rows, n_q_heads);
+    if (st != PYR_OK) return st;
+    if (!rows_apart(h, osb, osn, osh, n, n_rows, n_q_heads)) return PYR_ERR_INVALID;
+    if (q == q_out && ((n > 1 && qsb != osb) || (n_rows > 1 && qsn != osn) || (n_q_heads > 1 && qsh != osh))) return PYR_ERR_INVALID;
+  }
+  if (!(h->cfg.flags & PYR_PAGES_8BIT) || n_rows > kMaxRows || !tiles_fit(h, n, n_rows)) return PYR_ERR_UNSUPPORTED;
+  // a launch has a CTA for each page and KV head and for some rows of queries
+  const int64_t rows = (int64_t)n * n_rows, tiles = ((int64_t)n_rows + 2 * pyr::kPageTile - 2) / pyr::kPageTile;
+  if (q && rows > 0 && (n_q_heads > 65535 || n_q_heads > (0x7fffffff - tiles * n * h->cfg.n_kv_heads) / rows)) return PYR_ERR_UNSUPPORTED;
+  PYR_PAGES_READY(h);
+  if (n == 0 || n_rows == 0) return PYR_OK;
+  pyr::PagesAppendArgs a;
+  pyr::PagesWriteArgs& w = a.w;
+  w.p = view(h);
+  w.lists = lists; w.n = n; w.first = first; w.k = k; w.v = v; w.sb = sb; w.sn = sn; w.sh = sh;
+  w.src_rows = src_rows; w.dtype = dtype; w.idx = idx; w.idx_groups = idx ? idx_groups : 1; w.idx_stride = idx_stride;
+  w.counts = counts; w.n_rows = n_rows;
+  w.plan = at<int32_t>(h, h->lay.plan);
+  a.pos = pos; a.pos_stride = pos_stride; a.rope = rope; a.n_pos = n_pos;
+  a.q = q; a.q_out = q_out; a.Hq = n_q_heads;
+  a.qsb = qsb; a.qsn = qsn; a.qsh = qsh; a.osb = osb; a.osn = osn; a.osh = osh;
+  a.done = at<int32_t>(h, h->lay.moved);
+  PYR_PAGES(pyr::launch_pages_append8(a, &launches, static_cast<cudaStream_t>(stream)));
 }
 
 pyr_status_t pyr_pages_read(pyr_pages_t* h, const int32_t* lists, int32_t n, const int32_t* first, void* k, void* v,
@@ -286,33 +375,61 @@ pyr_status_t pyr_pages_read(pyr_pages_t* h, const int32_t* lists, int32_t n, con
   a.src_rows = n_rows; a.dtype = dtype; a.idx = nullptr; a.idx_groups = 1; a.idx_stride = 0;
   a.counts = counts; a.n_rows = n_rows;
   a.plan = nullptr;
+  if (h->cfg.flags & PYR_PAGES_8BIT) PYR_PAGES(pyr::launch_pages_read8(a, &launches, static_cast<cudaStream_t>(stream)));
   PYR_PAGES(pyr::launch_pages_read(a, &launches, static_cast<cudaStream_t>(stream)));
 }
 
 pyr_status_t pyr_pages_attn(pyr_pages_t* h, const int32_t* lists, int32_t n, const void* q, int64_t qsb, int64_t qst,
                             int64_t qsh, void* out, int64_t osb, int64_t ost, int64_t osh, float* lse, int32_t q_len,
                             int32_t n_q_heads, int32_t dtype, float softmax_scale, void* stream) {
+  const pyr_status_t st = check_attn(h, lists, n, q, qsb, qst, qsh, out, osb, ost, osh, q_len, n_q_heads, dtype, softmax_scale);
+  if (st != PYR_OK) return st;
+  PYR_PAGES_READY(h);
+  if (n == 0) return PYR_OK;
+  const pyr::PagesAttnArgs a = attn_args(h, lists, n, q, qsb, qst, qsh, out, osb, ost, osh, lse, q_len, n_q_heads, dtype, softmax_scale);
+  if (h->cfg.flags & PYR_PAGES_8BIT) PYR_PAGES(pyr::launch_pages_attn8(a, &launches, static_cast<cudaStream_t>(stream)));
+  PYR_PAGES(pyr::launch_pages_attn(a, &launches, static_cast<cudaStream_t>(stream)));
+}
+
+pyr_status_t pyr_pages_attn_blocks(pyr_pages_t* h, const int32_t* lists, int32_t n, const int32_t* slots, int32_t n_slots,
+                                   const void* q, int64_t qsb, int64_t qst, int64_t qsh, void* out, int64_t osb, int64_t ost,
+                                   int64_t osh, float* lse, int32_t q_len, int32_t n_q_heads, int32_t dtype, float softmax_scale,
+                                   void* stream) {
+  const pyr_status_t st = check_attn(h, lists, n, q, qsb, qst, qsh, out, osb, ost, osh, q_len, n_q_heads, dtype, softmax_scale);
+  if (st != PYR_OK) return st;
+  if (n_slots < 1) return PYR_ERR_INVALID;
+  if (!slots && n > 0) return PYR_ERR_NULL;
+  if (!(h->cfg.flags & PYR_PAGES_8BIT) || (int64_t)n * q_len > 0x7fffffff - 4096) return PYR_ERR_UNSUPPORTED;
+  PYR_PAGES_READY(h);
+  if (n == 0) return PYR_OK;
+  pyr::PagesAttnArgs a = attn_args(h, lists, n, q, qsb, qst, qsh, out, osb, ost, osh, lse, q_len, n_q_heads, dtype, softmax_scale);
+  a.slots = slots; a.n_slots = n_slots;
+  PYR_PAGES(pyr::launch_pages_attn8(a, &launches, static_cast<cudaStream_t>(stream)));
+}
+
+pyr_status_t pyr_pages_select(pyr_pages_t* h, const int32_t* lists, int32_t n, const void* q, int64_t qsb, int64_t qst,
+                              int64_t qsh, int32_t q_len, int32_t n_q_heads, int32_t dtype, int32_t* slots, int32_t n_slots,
+                              int32_t keep_first, int32_t keep_last, void* stream) {
   pyr_status_t st = check_call(h, n, false);
   if (st != PYR_OK) return st;
   if (q_len < 1 || n_q_heads < 1 || n_q_heads % h->cfg.n_kv_heads || !default_lists_fit(h, lists, n)) return PYR_ERR_INVALID;
-  if (!(softmax_scale >= 0.0f) || softmax_scale > 0x1p127f) return PYR_ERR_INVALID;     // (times log2 e it is a number)
+  if (n_slots < 1 || keep_first < 0 || keep_last < 0 || (int64_t)keep_first + keep_last > n_slots) return PYR_ERR_INVALID;
   st = check_rows(h, q, q, dtype, qsb, qst, qsh, n, q_len, n_q_heads);
-  if (st == PYR_OK) st = check_rows(h, out, out, dtype, osb, ost, osh, n, q_len, n_q_heads);
   if (st != PYR_OK) return st;
-  const int64_t cols = (int64_t)q_len * (n_q_heads / h->cfg.n_kv_heads);
-  if (cols > (1 << 20)) return PYR_ERR_UNSUPPORTED;
-  if (!rows_apart(h, osb, ost, osh, n, q_len, n_q_heads)) return PYR_ERR_INVALID;
+  if (!slots && n > 0) return PYR_ERR_NULL;
+  const int32_t rep = n_q_heads / h->cfg.n_kv_heads;
+  if (!(h->cfg.flags & PYR_PAGES_8BIT) || pyr::pages_select8_shared(h->cfg.max_pages, h->cfg.head_dim, rep) > pyr::kSelect8Shared)
+    return PYR_ERR_UNSUPPORTED;
+  // (a launch has up to 8 CTAs for each entry, token and KV head)
+  if (n > 0 && (int64_t)q_len * h->cfg.n_kv_heads > (0x7fffffff / 8) / n) return PYR_ERR_UNSUPPORTED;
   PYR_PAGES_READY(h);
   if (n == 0) return PYR_OK;
-  pyr::PagesAttnArgs a;
+  pyr::PagesSelectArgs a;
   a.p = view(h);
-  a.lists = lists; a.n = n; a.q = q; a.out = out; a.lse = lse;
-  a.qsb = qsb; a.qst = qst; a.qsh = qsh; a.osb = osb; a.ost = ost; a.osh = osh;
-  a.T = q_len; a.Hq = n_q_heads; a.rep = n_q_heads / h->cfg.n_kv_heads; a.dtype = dtype;
-  a.scale = softmax_scale > 0.0f ? softmax_scale : (float)(1.0 / std::sqrt((double)h->cfg.head_dim));
-  a.partial = at<float>(h, h->lay.partial);
-  a.arrived = at<int32_t>(h, h->lay.arrived);
-  PYR_PAGES(pyr::launch_pages_attn(a, &launches, static_cast<cudaStream_t>(stream)));
+  a.lists = lists; a.n = n; a.q = q; a.qsb = qsb; a.qst = qst; a.qsh = qsh;
+  a.T = q_len; a.Hq = n_q_heads; a.rep = rep; a.dtype = dtype;
+  a.slots = slots; a.n_slots = n_slots; a.keep_first = keep_first; a.keep_last = keep_last;
+  PYR_PAGES(pyr::launch_pages_select8(a, &launches, static_cast<cudaStream_t>(stream)));
 }
 
 pyr_status_t pyr_pages_fork(pyr_pages_t* h, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
@@ -339,7 +456,8 @@ pyr_status_t pyr_pages_compact(pyr_pages_t* h, const int32_t* src, const int32_t
   if (st == PYR_OK) st = check_idx(h, idx, idx_groups, idx_stride, n_rows);
   if (st != PYR_OK) return st;
   if (n_rows < 0) return PYR_ERR_INVALID;
-  if (n_rows > kMaxRows || !tiles_fit(h, n, n_rows)) return PYR_ERR_UNSUPPORTED;
+  // (rows of pages whose scales differ cannot move as they are)
+  if (n_rows > kMaxRows || !tiles_fit(h, n, n_rows) || h->cfg.flags & PYR_PAGES_8BIT) return PYR_ERR_UNSUPPORTED;
   if (n > 0 && (!src || !dst)) return PYR_ERR_NULL;
   PYR_PAGES_READY(h);
   if (n == 0) return PYR_OK;

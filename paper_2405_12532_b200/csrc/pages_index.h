@@ -1,4 +1,4 @@
-// Addresses inside the paged 4-bit cache: where a row, a code and a scale lie, and the checks that keep every access in
+// Addresses inside the paged cache, in 4 and in 8 bits: where a row, a code and a scale lie, and the checks that keep every access in
 // bounds whatever the tables hold. Plain C++ (host and device), so that the arithmetic can be tested without a GPU.
 #pragma once
 #include <stddef.h>
@@ -17,17 +17,19 @@ constexpr int kMaxPageRows = 1024;
 constexpr int kMaxLists = 1 << 19;
 
 struct PagesView {
-  uint8_t* pool;       // [n_pages][Hkv][tiles_per_page][tile_bytes]
+  uint8_t* pool;       // [n_pages][Hkv][head_extra + tiles_per_page * tile_bytes]
   int32_t* table;      // [n_lists][max_pages]
   int32_t* lens;       // [n_lists]
   int32_t* refs;       // [n_pages]
   int* status;
-  int Hkv, D, group, page_rows, tiles_per_page, tile_bytes;
+  int Hkv, D, group, page_rows, tiles_per_page, tile_bytes;      // group 0: 8 bits
+  int head_extra;      // bytes of a (page, head) before its tiles: 0 in 4 bits
   int n_pages, n_lists, max_pages;
 };
 
 PYR_HD int pages_tile_bytes(int D, int group) { return kPageTile * (D + 8 * (D / group)); }
-PYR_HD size_t pages_page_bytes(const PagesView& p) { return (size_t)p.Hkv * p.tiles_per_page * p.tile_bytes; }
+PYR_HD int pages_head_bytes(const PagesView& p) { return p.tiles_per_page * p.tile_bytes + p.head_extra; }
+PYR_HD size_t pages_page_bytes(const PagesView& p) { return (size_t)p.Hkv * pages_head_bytes(p); }
 
 // The list of entry i, or -1 if its id is out of range.
 PYR_HD int pages_list(const PagesView& p, const int32_t* lists, int i) {
@@ -48,7 +50,7 @@ PYR_HD int pages_len(const PagesView& p, int l) {
 }
 // Byte offset in the pool of tile `tile` (of the page) of head h.
 PYR_HD size_t pages_tile(const PagesView& p, int page, int h, int tile) {
-  return (((size_t)page * p.Hkv + h) * p.tiles_per_page + tile) * (size_t)p.tile_bytes;
+  return ((size_t)page * p.Hkv + h) * (size_t)pages_head_bytes(p) + p.head_extra + (size_t)tile * p.tile_bytes;
 }
 
 // Offsets inside a tile: codes of a row, (scale, zero) words.
@@ -75,6 +77,27 @@ PYR_HD int v_slot_half(int D, int group, int slot) {
   const int u = group / 32, i = slot / (D / 32), r = slot % (D / 32);
   return r / u * (group / 4) + i * u + r % u;
 }
+
+// The 8-bit format. A (page, head) begins with the least and the largest code of each dimension (D signed bytes each) and the
+// two scales (K's, V's); its tiles hold the codes as bytes code + 128, K's and then V's, and the scales once more, so that a copy
+// of a tile is all that attention needs of it.
+constexpr int kPageRows8 = 128;          // rows of a page at most: a CTA stores them with a warp a tile
+PYR_HD int pages8_tile_bytes(int D) { return 2 * kPageTile * D + 16; }
+PYR_HD int pages8_head_extra(int D) { return 2 * D + 16; }
+PYR_HD int tile8_scales(int D) { return 2 * kPageTile * D; }
+// Byte of a K code. A lane reads 16 dimensions of a row; rows of 128 bytes have their halves swapped in odd rows, which
+// spreads eight such reads over all banks.
+PYR_HD int tile8_k(int D, int r, int d) { return r * D + 16 * ((d >> 4) ^ (D == 128 ? 4 * (r & 1) : 0)) + (d & 15); }
+// Byte of a V code. A word is four rows of one dimension: those of a lane's two operand registers. Lane j's words lie
+// together, an eighth of the dimensions in a row (16-byte chunks in an order that differs between the lanes, for the banks).
+PYR_HD int tile8_v(int D, int r, int d) {
+  const int j = (r & 7) >> 1, b = 2 * (r & 1) + (r >> 3), e = D / 8, w = d % e;
+  return kPageTile * D + 4 * D * j + 4 * e * (d / e) + 16 * ((w >> 2) ^ (j & (e / 4 - 1))) + 4 * (w & 3) + b;
+}
+
+// Shared memory in which the selection keeps a list's scores and a KV head's queries, and what it may take.
+constexpr int kSelect8Shared = 200 * 1024;
+inline int64_t pages_select8_shared(int64_t max_pages, int D, int64_t rep) { return (max_pages + 3) / 4 * 16 + rep * (2 * D + 4); }
 
 // How the attention's work is dealt out. A unit is one tile of one (entry, KV head, column group); an entry without rows
 // still has one tile per head, so that its zeros get written. Before its tiles each (entry, KV head, column group) has

@@ -1,4 +1,4 @@
-// Page management of the paged 4-bit cache: taking pages (with the copy that a shared, part-filled last page needs),
+// Page management of the paged cache: taking pages (with the copy that a shared, part-filled last page needs),
 // forking, giving up and compacting lists. Tables, lengths and reference counts are device memory, so a call plans on
 // the device, and every id that a table or a caller's list holds is range-checked before it is used.
 #include "pyr_internal.h"
@@ -154,8 +154,19 @@ __device__ __forceinline__ int free_page(const PagesReserveArgs& a, int rank) {
 // Copies the first `rows` rows of the heads [h0, h1) of a page to another page, 16 bytes a thread at a time whatever the head:
 // whole tiles as they lie, of a part-filled tile the rows' codes and (4 bytes at a time) words.
 __device__ __forceinline__ void copy_rows_of_page(const PagesView& p, int from, int to, int h0, int h1, int rows) {
+  const size_t head_bytes = pages_head_bytes(p);
+  if (p.group == 0) {                            // 8 bits: what comes before the tiles, and tiles as they lie
+    const int per16 = (p.head_extra + (rows + kPageTile - 1) / kPageTile * p.tile_bytes) / 16;
+    const uint8_t* s8 = p.pool + pages_tile(p, from, h0, 0) - p.head_extra;
+    uint8_t* d8 = p.pool + pages_tile(p, to, h0, 0) - p.head_extra;
+#pragma unroll 4
+    for (int x = threadIdx.x; x < (h1 - h0) * per16; x += kThreads) {
+      const size_t at = x / per16 * head_bytes + x % per16 * 16;
+      *reinterpret_cast<uint4*>(d8 + at) = *reinterpret_cast<const uint4*>(s8 + at);
+    }
+    return;
+  }
   const int G = p.D / p.group, half = kPageTile * p.D / 2, heads = h1 - h0;
-  const size_t head_bytes = (size_t)p.tiles_per_page * p.tile_bytes;
   const uint8_t* s = p.pool + pages_tile(p, from, h0, 0);
   uint8_t* d = p.pool + pages_tile(p, to, h0, 0);
   const int whole = rows / kPageTile * p.tile_bytes, left = rows % kPageTile;

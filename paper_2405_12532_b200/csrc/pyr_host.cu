@@ -647,6 +647,13 @@ pyr_status_t pyr_glue_rope(void* x, const int32_t* pos, int64_t tokens, int32_t 
   if (head_dim > 256) return PYR_ERR_UNSUPPORTED;
   PYR_GLUE(pyr::launch_glue_rope(x, pos, tokens, n_heads, head_dim, dtype, static_cast<cudaStream_t>(stream)));
 }
+pyr_status_t pyr_glue_rope_table(float* table, int64_t first, int64_t n_pos, int32_t head_dim, double base, void* stream) {
+  if (!table && n_pos > 0) return PYR_ERR_NULL;
+  if (first < 0 || n_pos < 0 || head_dim < 2 || head_dim % 2 || !(base > 0.0) || !(base <= 1e300)) return PYR_ERR_INVALID;
+  if (first + n_pos > (1ll << 31) || first > (1ll << 31) || head_dim > 256) return PYR_ERR_UNSUPPORTED;
+  if (n_pos == 0) return PYR_OK;
+  PYR_GLUE(pyr::launch_glue_rope_table(table, first, n_pos, head_dim, base, static_cast<cudaStream_t>(stream)));
+}
 pyr_status_t pyr_glue_swiglu(const void* gate, const void* up, void* out, int64_t n, int32_t dtype, void* stream) {
   if (!glue_ok(dtype, {gate, up, out})) return dtype == PYR_BF16 || dtype == PYR_F32 ? PYR_ERR_NULL : PYR_ERR_UNSUPPORTED;
   if (n < 0) return PYR_ERR_INVALID;

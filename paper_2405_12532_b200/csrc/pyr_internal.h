@@ -187,7 +187,7 @@ __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontr
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 #endif
 
-// Paged 4-bit cache (csrc/pages_*.cu).
+// Paged cache (csrc/pages_*.cu; what ends in 8: its 8-bit format).
 struct PagesWriteArgs {
   PagesView p;
   const int32_t* lists; int n;
@@ -226,6 +226,25 @@ struct PagesAttnArgs {
   float scale;
   float* partial;                  // [kAttnMaxCtas][2][kAttnCols][D + 2]
   int32_t* arrived;                // [kAttnMaxCtas], zero between calls
+  const int32_t* slots = nullptr;  // [n, T, Hkv, n_slots]: the pages that are read (null: all)
+  int n_slots = 0;
+};
+// What an 8-bit store does besides: rotation and queries.
+struct PagesAppendArgs {
+  PagesWriteArgs w;
+  const int32_t* pos; int64_t pos_stride;      // [n, idx_groups, n_rows] or null: keys as they are
+  const float* rope; int n_pos;                // [n_pos, D]: cosines, sines
+  const void* q; void* q_out;                  // [n, n_rows, Hq, D] or null
+  int64_t qsb, qsn, qsh, osb, osn, osh;
+  int Hq;
+  int32_t* done;                               // [n_lists], zero between calls
+};
+struct PagesSelectArgs {
+  PagesView p;
+  const int32_t* lists; int n;
+  const void* q; int64_t qsb, qst, qsh;
+  int T, Hq, rep, dtype;
+  int32_t* slots; int n_slots, keep_first, keep_last;
 };
 constexpr int kReserveSlice = 4096;
 constexpr int kAttnMaxCtas = 640;
@@ -238,6 +257,11 @@ cudaError_t launch_pages_trim(const PagesView& p, const int32_t* lists, int n, c
                               cudaStream_t s);
 cudaError_t launch_pages_compact(const PagesMoveArgs& a, int* launches, cudaStream_t s);
 cudaError_t launch_pages_attn(const PagesAttnArgs& a, int* launches, cudaStream_t s);
+cudaError_t launch_pages_append8(const PagesAppendArgs& a, int* launches, cudaStream_t s);
+cudaError_t launch_pages_read8(const PagesWriteArgs& a, int* launches, cudaStream_t s);
+cudaError_t launch_pages_attn8(const PagesAttnArgs& a, int* launches, cudaStream_t s);
+cudaError_t launch_pages_select8(const PagesSelectArgs& a, int* launches, cudaStream_t s);
+cudaError_t launch_glue_rope_table(float* table, int64_t first, int64_t n_pos, int D, double base, cudaStream_t s);
 
 int gen_score_qtiles(int Lw);
 cudaError_t launch_gen_score(const GenScoreArgs& a, cudaStream_t s);     // two kernels
