@@ -18,7 +18,6 @@ namespace pyr {
 namespace {
 
 namespace cg = cooperative_groups;
-constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr float kScaleMin = 7.888609052210118e-31f;   // 2^-100
 constexpr uint32_t kForced = 0xFFFFFFFFu;              // the key of a page that is taken whatever its score
 
@@ -33,13 +32,12 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t b = __float_as_uint(x == x ? x + 0.f : INFINITY);
   return b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u);
 }
-__device__ __forceinline__ float at(const float* p) { return *p; }
-__device__ __forceinline__ float at(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 
 // R query heads at a time, D / 16 lanes a page.
-template <class T, int D, int R>
-__global__ void __launch_bounds__(kThreads) select8_kernel(PagesSelectArgs a) {
-  constexpr int LPP = D / 16, PPW = 32 / LPP, W = D / 4, U = R == 8 ? 2 : 4;    // lanes a page, pages a warp and step, words of a row, steps at once
+template <int D, int R, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : (R == 8 ? 640 : 768) / kThreads) select8_kernel(PagesSelectArgs a) {
+  constexpr int kWarps = kThreads / 32;
+  constexpr int LPP = D / 16, PPW = 32 / LPP, W = D / 4, U = 2;    // lanes a page, pages a warp and step, words of a row, steps at once
   extern __shared__ __align__(16) uint32_t shared[];
   __shared__ uint32_t hist[256];
   __shared__ uint32_t warp_sums[kWarps];
@@ -67,11 +65,24 @@ __global__ void __launch_bounds__(kThreads) select8_kernel(PagesSelectArgs a) {
   }
   // ---- the queries in 8 bits, a warp a head
   for (int r = warp; r < a.rep; r += kWarps) {
-    const T* q = static_cast<const T*>(a.q) + (int64_t)e * a.qsb + (int64_t)tok * a.qst + (int64_t)(h * a.rep + r) * a.qsh;
+    const int64_t row = (int64_t)e * a.qsb + (int64_t)tok * a.qst + (int64_t)(h * a.rep + r) * a.qsh;
     constexpr int N = D / 32;                                      // elements a lane: side by side
     float x[N], top = 0.f;
+    if (a.dtype == PYR_F32) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) { x[k] = at(q + N * lane + k); top = max_nan(top, fabsf(x[k])); }
+      for (int k = 0; k < N; k += 2) {
+        const float2 v = *reinterpret_cast<const float2*>(static_cast<const float*>(a.q) + row + N * lane + k);
+        x[k] = v.x; x[k + 1] = v.y;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; k += 2) {
+        const uint32_t v = *reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(a.q) + row + N * lane + k);
+        x[k] = __uint_as_float(v << 16); x[k + 1] = __uint_as_float(v & 0xffff0000u);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) top = max_nan(top, fabsf(x[k]));
     // (magnitudes, Inf and NaN among them, are ordered as their bits are)
     top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu));
     float s = __fdiv_rn(top, 127.f);
@@ -94,45 +105,62 @@ __global__ void __launch_bounds__(kThreads) select8_kernel(PagesSelectArgs a) {
   const int32_t* table = a.p.table + (size_t)l * a.p.max_pages;
   const int head_bytes = pages_head_bytes(a.p);
   const int step = kWarps * PPW * U;                               // pages of a CTA's step
+  // (a step's extrema are on their way while the one before is worked out, and its page ids before that)
+  int ids[U];
+  uint4 mn_next[U], mx_next[U];
+  float sk_next[U];
+  auto fetch_ids = [&](int base) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int x = base + (u * kWarps + warp) * PPW + sub;
+      ids[u] = x < pages ? table[x] : -1;
+    }
+  };
+  auto fetch = [&] {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      mn_next[u] = mx_next[u] = make_uint4(0, 0, 0, 0);
+      sk_next[u] = -1.f;                                           // no page
+      if (ids[u] >= 0 && ids[u] < a.p.n_pages) {
+        const uint8_t* head = a.p.pool + ((size_t)ids[u] * a.p.Hkv + h) * head_bytes;
+        mn_next[u] = reinterpret_cast<const uint4*>(head)[part];
+        mx_next[u] = reinterpret_cast<const uint4*>(head + D)[part];
+        sk_next[u] = *reinterpret_cast<const float*>(head + 2 * D);
+      }
+    }
+  };
+  fetch_ids(rank * step);
+  fetch();
+  fetch_ids((rank + ranks) * step);
   for (int base = rank * step; base < pages; base += ranks * step) {
     uint4 mn[U], mx[U];
     float sk[U], best[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int x = base + (u * kWarps + warp) * PPW + sub;
-      const int page = x < pages ? table[x] : -1;
-      mn[u] = mx[u] = make_uint4(0, 0, 0, 0);
-      sk[u] = -1.f;                                                // no page
-      if (page >= 0 && page < a.p.n_pages) {
-        const uint8_t* head = a.p.pool + ((size_t)page * a.p.Hkv + h) * head_bytes;
-        mn[u] = reinterpret_cast<const uint4*>(head)[part];
-        mx[u] = reinterpret_cast<const uint4*>(head + D)[part];
-        sk[u] = *reinterpret_cast<const float*>(head + 2 * D);
-      }
-      best[u] = -INFINITY;
-    }
+    for (int u = 0; u < U; ++u) { mn[u] = mn_next[u]; mx[u] = mx_next[u]; sk[u] = sk_next[u]; best[u] = -INFINITY; }
+    fetch();
+    fetch_ids(base + 2 * ranks * step);
     for (int r0 = 0; r0 < a.rep; r0 += R) {
-      uint4 qp[R], qn[R];
+      int sums[U][R];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const int head = min(r0 + r, a.rep - 1);
-        qp[r] = reinterpret_cast<const uint4*>(plus + head * W)[part];
-        qn[r] = reinterpret_cast<const uint4*>(plus + (a.rep + head) * W)[part];
+        const uint4 qp = reinterpret_cast<const uint4*>(plus + head * W)[part];
+        const uint4 qn = reinterpret_cast<const uint4*>(plus + (a.rep + head) * W)[part];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          int s = __dp4a((int)mx[u].x, (int)qp.x, 0);
+          s = __dp4a((int)mn[u].x, (int)qn.x, s);
+          s = __dp4a((int)mx[u].y, (int)qp.y, s);
+          s = __dp4a((int)mn[u].y, (int)qn.y, s);
+          s = __dp4a((int)mx[u].z, (int)qp.z, s);
+          s = __dp4a((int)mn[u].z, (int)qn.z, s);
+          s = __dp4a((int)mx[u].w, (int)qp.w, s);
+          sums[u][r] = __dp4a((int)mn[u].w, (int)qn.w, s);
+        }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        int sum[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          int s = __dp4a((int)mx[u].x, (int)qp[r].x, 0);
-          s = __dp4a((int)mn[u].x, (int)qn[r].x, s);
-          s = __dp4a((int)mx[u].y, (int)qp[r].y, s);
-          s = __dp4a((int)mn[u].y, (int)qn[r].y, s);
-          s = __dp4a((int)mx[u].z, (int)qp[r].z, s);
-          s = __dp4a((int)mn[u].z, (int)qn[r].z, s);
-          s = __dp4a((int)mx[u].w, (int)qp[r].w, s);
-          sum[r] = __dp4a((int)mn[u].w, (int)qn[r].w, s);
-        }
+        int* sum = sums[u];
         // sums over the lanes of the page: each step halves the heads that a lane goes on with, as long as there are several
         int first = 0, left = R;
 #pragma unroll
@@ -179,7 +207,7 @@ __global__ void __launch_bounds__(kThreads) select8_kernel(PagesSelectArgs a) {
   // ---- the n_slots-th largest key, from its highest bits down; `need` of those that share the bits found so far are wanted
   uint32_t prefix = 0, need = a.n_slots;
   for (int shift = 24; shift >= 0; shift -= 8) {
-    if (t < 256) hist[t] = 0;
+    for (int x = t; x < 256; x += kThreads) hist[x] = 0;
     __syncthreads();
     const uint32_t mask = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
     for (int x0 = 0; x0 < pages; x0 += kThreads) {
@@ -244,36 +272,45 @@ __global__ void __launch_bounds__(kThreads) select8_kernel(PagesSelectArgs a) {
   }
 }
 
-template <class T, int D, int R>
+template <int D, int R, int kThreads>
 cudaError_t run(const PagesSelectArgs& a, int smem, cudaStream_t s) {
-  const cudaError_t e = allow_shared<select8_kernel<T, D, R>>(kSelect8Shared);
+  const cudaError_t e = allow_shared<select8_kernel<D, R, kThreads>>(kSelect8Shared);
   if (e != cudaSuccess) return e;
   const int sms = device_sm_count();
   if (sms <= 0) return cudaErrorUnknown;
   const int64_t items = (int64_t)a.n * a.T * a.p.Hkv;
   // several CTAs a list where that many find room at once and each has a step or more to do
   int ranks = 1;
-  while (ranks < 8 && items * ranks * 2 <= sms && a.p.max_pages > ranks * 128) ranks *= 2;
+  while (kThreads == 512 && ranks < 8 && items * ranks * 2 <= sms && a.p.max_pages > ranks * 128) ranks *= 2;
   if (items * ranks > 0x7fffffffLL) return cudaErrorInvalidValue;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(items * ranks)); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
   cudaLaunchAttribute at{};
   at.id = cudaLaunchAttributeClusterDimension;
   at.val.clusterDim.x = ranks; at.val.clusterDim.y = at.val.clusterDim.z = 1;
-  cfg.attrs = &at; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, select8_kernel<T, D, R>, a);
+  cfg.attrs = &at; cfg.numAttrs = ranks > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, select8_kernel<D, R, kThreads>, a);
 }
-template <class T, int D>
+// As many threads for a list as there is room for, where its table is long enough to occupy them.
+template <int D, int R>
+cudaError_t by_length(const PagesSelectArgs& a, int smem, cudaStream_t s) {
+  const int sms = device_sm_count();
+  if (sms <= 0) return cudaErrorUnknown;
+  const int64_t items = (int64_t)a.n * a.T * a.p.Hkv;
+  const auto fits = [&](int threads) { return items * threads <= (int64_t)sms * 1024 && a.p.max_pages * 2 >= threads; };
+  return fits(512) ? run<D, R, 512>(a, smem, s) : fits(256) ? run<D, R, 256>(a, smem, s) : fits(128) ? run<D, R, 128>(a, smem, s)
+         : a.p.max_pages > 1024 ? run<D, R, 256>(a, smem, s) : run<D, R, 32>(a, smem, s);
+}
+template <int D>
 cudaError_t by_heads(const PagesSelectArgs& a, int smem, cudaStream_t s) {
-  return a.rep == 1 ? run<T, D, 1>(a, smem, s) : a.rep <= 4 ? run<T, D, 4>(a, smem, s) : run<T, D, 8>(a, smem, s);
+  return a.rep == 1 ? by_length<D, 1>(a, smem, s) : a.rep <= 4 ? by_length<D, 4>(a, smem, s) : by_length<D, 8>(a, smem, s);
 }
 
 }  // namespace
 
 cudaError_t launch_pages_select8(const PagesSelectArgs& a, int* launches, cudaStream_t s) {
   const int smem = (int)pages_select8_shared(a.p.max_pages, a.p.D, a.rep);
-  const cudaError_t e = a.p.D == 128 ? (a.dtype == PYR_F32 ? by_heads<float, 128>(a, smem, s) : by_heads<__nv_bfloat16, 128>(a, smem, s))
-                                     : (a.dtype == PYR_F32 ? by_heads<float, 64>(a, smem, s) : by_heads<__nv_bfloat16, 64>(a, smem, s));
+  const cudaError_t e = a.p.D == 128 ? by_heads<128>(a, smem, s) : by_heads<64>(a, smem, s);
   if (e == cudaSuccess) ++*launches;
   return e;
 }

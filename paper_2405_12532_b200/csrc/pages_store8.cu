@@ -15,14 +15,32 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kOneWarps = 8;                     // of a CTA that stores an entry's one row, a warp a head
 constexpr int kReadThreads = 64;
+constexpr int kSelfEntries = 512;                // up to this many entries each CTA decides for itself, and a call of many rows is one launch
+constexpr int kQueryHeads = 4;                   // heads of a query row that a thread turns
 constexpr float kScaleMin = 7.888609052210118e-31f;   // 2^-100
-constexpr float kRound = 12582912.f;             // 1.5 2^23: added, it rounds to the nearest integer (ties to even) and leaves it in the low bits
+constexpr float kRound = 12583040.f;             // 1.5 2^23 + 128: added, it rounds to the nearest integer (ties to even) and leaves it, plus 128, in the low bits
 
 __device__ __forceinline__ void record(int* status, int code) { atomicCAS(status, 0, code); }
 __device__ __forceinline__ float nan_f() { return __uint_as_float(0x7FC00000u); }
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// The largest magnitude of three, NaN if one is NaN.
+__device__ __forceinline__ float most_of(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float min_of(float a, float b, float c) {
+  float r;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float max_of(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 
@@ -39,6 +57,14 @@ template <int N> struct Some<float, N> {
     for (int k = 0; k < N; ++k) x[k] = v;
   }
   __device__ __forceinline__ float at(int k) const { return x[k]; }
+  // the bits of the largest magnitude so far (Inf and NaN in the order of their bits)
+  __device__ __forceinline__ void most(uint32_t* bits) const {
+    float m = __uint_as_float(*bits);
+#pragma unroll
+    for (int k = 0; k < N; k += 2) m = most_of(m, x[k], x[k + 1]);
+    *bits = __float_as_uint(m);
+  }
+  static __device__ __forceinline__ uint32_t finish(uint32_t bits) { return bits & 0x7fffffffu; }
 };
 template <int N> struct Some<__nv_bfloat16, N> {
   uint32_t w[N / 2];
@@ -52,6 +78,12 @@ template <int N> struct Some<__nv_bfloat16, N> {
     for (int k = 0; k < N / 2; ++k) w[k] = b | b << 16;
   }
   __device__ __forceinline__ float at(int k) const { return __uint_as_float(k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16); }
+  // (two at a time, until finish())
+  __device__ __forceinline__ void most(uint32_t* bits) const {
+    if constexpr (N == 4) *bits = __vimax3_u16x2(*bits, w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu);
+    else *bits = __vmaxu2(*bits, w[0] & 0x7fff7fffu);
+  }
+  static __device__ __forceinline__ uint32_t finish(uint32_t bits) { return max(bits & 0xffff0000u, bits << 16); }
 };
 template <int N> __device__ __forceinline__ void store_some(float* p, const float* x) {
   if constexpr (N == 4) *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
@@ -65,18 +97,27 @@ template <int N> __device__ __forceinline__ void store_some(__nv_bfloat16* p, co
   else *reinterpret_cast<uint32_t*>(p) = two_bf16(x[0], x[1]);
 }
 
+__device__ __forceinline__ void store_eight(float* p, const float* x) { store_some<4>(p, x); store_some<4>(p + 4, x + 4); }
+__device__ __forceinline__ void store_eight(__nv_bfloat16* p, const float* x) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
+}
+
 // N pairs (lo, hi) turned by the angles whose cosines and sines lie at rope[d0 ..] and rope[D / 2 + d0 ..].
-template <int N, int D>
-__device__ __forceinline__ void rotate(float* lo, float* hi, const float* rope, int d0) {
-  Some<float, N> c, s;
-  c.load(rope + d0);
-  s.load(rope + D / 2 + d0);
+template <int N>
+__device__ __forceinline__ void turn(float* lo, float* hi, const Some<float, N>& c, const Some<float, N>& s) {
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     const float a = lo[k], b = hi[k];
     lo[k] = __fsub_rn(__fmul_rn(a, c.x[k]), __fmul_rn(b, s.x[k]));
     hi[k] = __fadd_rn(__fmul_rn(b, c.x[k]), __fmul_rn(a, s.x[k]));
   }
+}
+template <int N, int D>
+__device__ __forceinline__ void rotate(float* lo, float* hi, const float* rope, int d0) {
+  Some<float, N> c, s;
+  c.load(rope + d0);
+  s.load(rope + D / 2 + d0);
+  turn<N>(lo, hi, c, s);
 }
 
 // The scale that rows with the largest magnitude amax bring a (page, head) to, from `before`; what codes that stay and new values are
@@ -92,15 +133,15 @@ __device__ __forceinline__ Scale scale_of(float amax, float before) {
   r.inverse = some ? __fdiv_rn(1.f, r.s) : 0.f;
   return r;
 }
-// A code in the low byte (two's complement), from its number times 1 / step; the sums are monotone in the number.
+// A code's stored byte in the low byte, from its number times 1 / step; the sums are monotone in the number.
 __device__ __forceinline__ float code_sum(float x, float by) { return __fadd_rn(__fmul_rn(x, by), kRound); }
-__device__ __forceinline__ int code_int(float sum) { return (int)(__float_as_uint(sum) - 0x4B400000u); }
+__device__ __forceinline__ int code_int(float sum) { return (int)(__float_as_uint(sum) - 0x4B400080u); }
 // Four stored bytes (code + 128) brought to another scale.
 __device__ __forceinline__ uint32_t recode4(uint32_t w, float factor) {
   uint32_t r = 0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) r |= (__float_as_uint(code_sum((float)((int)(w >> (8 * k) & 255u) - 128), factor)) & 255u) << (8 * k);
-  return r ^ 0x80808080u;
+  return r;
 }
 __device__ __forceinline__ uint32_t bytes4(float a, float b, float c, float d) {      // their low bytes
   return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040), __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
@@ -148,59 +189,74 @@ __device__ __forceinline__ void query_row(const PagesAppendArgs& a, int e, int x
   store_some<W>(out + D / 2 + d0, f[1]);
 }
 
+// Whether entry e is stored, where and how long its list was, decided by a whole CTA.
+struct Entry { int list, start, count, len; bool bad; };
+__device__ __forceinline__ Entry decide(const PagesWriteArgs& a, int e) {
+  Entry d{pages_list(a.p, a.lists, e), 0, a.counts ? a.counts[e] : a.n_rows, 0, false};
+  bool bad = d.list < 0 || d.count < 0 || d.count > a.n_rows;
+  if (!bad) {
+    d.len = pages_len(a.p, d.list);
+    d.start = a.first ? a.first[e] : d.len;
+    bad = d.start < 0 || d.start > d.len || (int64_t)d.start + d.count > (int64_t)a.p.max_pages * a.p.page_rows;
+    if (!bad && d.count > 0)
+      for (int s = d.start / a.p.page_rows + threadIdx.x; s <= (d.start + d.count - 1) / a.p.page_rows; s += blockDim.x) {
+        const int page = pages_page(a.p, d.list, s);
+        bad |= page < 0 || a.p.refs[page] != 1;
+      }
+  }
+  if (a.lists)
+#pragma unroll 4
+    for (int x = threadIdx.x; x < a.n; x += blockDim.x) bad |= x != e && a.lists[x] == d.list;
+  d.bad = __syncthreads_or(bad);
+  return d;
+}
+// Called once by every CTA of an entry, after decide(): the last of `ctas` sets the length, which the others have read by then, and
+// reports what is wrong.
+__device__ __forceinline__ void finish(const PagesWriteArgs& a, int e, const Entry& d, int32_t* all_done, int ctas) {
+  int32_t* done = all_done + e;
+  if (threadIdx.x != 0 || (ctas > 1 && atomicAdd(done, 1) != ctas - 1)) return;
+  if (ctas > 1) *done = 0;
+  a.plan[2 * e] = d.bad ? -1 : d.start;           // for what comes behind
+  if (d.bad) record(a.p.status, PYR_ERR_INVALID);
+  else if (d.start + d.count > d.len) a.p.lens[d.list] = d.start + d.count;
+}
+
 // ------------------------------------------------------------------ one row an entry (a decode step)
-// grid (entries, groups of kOneWarps heads and then groups of query heads). Every CTA of an entry decides for itself; the one that
-// is done last sets the length, which the others have read by then. A warp stores a head: its lower half the key, its upper half
+// grid (entries, groups of kOneWarps heads and then groups of query heads). A warp stores a head: its lower half the key, its upper half
 // the value, a thread D / 32 dimensions from either half of them.
 template <class T, int D>
 __global__ void __launch_bounds__(kOneWarps * 32) append_one_kernel(PagesAppendArgs p, int kv_parts) {
   constexpr int W = D / 32;
   const PagesWriteArgs& a = p.w;
   const int e = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5;
-  const int l = pages_list(a.p, a.lists, e);
-  const int cnt = a.counts ? a.counts[e] : 1;
-  bool bad = l < 0 || cnt < 0 || cnt > 1;
-  int row = 0, len = 0, page = -1;
-  if (!bad) {
-    len = pages_len(a.p, l);
-    row = a.first ? a.first[e] : len;
-    bad = row < 0 || row > len || (int64_t)row + cnt > (int64_t)a.p.max_pages * a.p.page_rows;
-    if (!bad && cnt > 0) {
-      page = pages_page(a.p, l, row / a.p.page_rows);
-      bad = page < 0 || a.p.refs[page] != 1;
+  // (the row is on its way before anything is decided)
+  const bool is_query = (int)blockIdx.y >= kv_parts;
+  const int h = blockIdx.y * kOneWarps + warp, kv = lane >> 4, d0 = W * (lane & 15);
+  float x[2][W];
+  bool good = false;
+  if (!is_query && h < a.p.Hkv) {
+    const int src = source_row(a, e, h, 0), pos = position(p, e, h, 0);
+    good = src >= 0 && pos >= 0;
+    if (good) {
+      const T* from = source<T>(kv ? a.v : a.k, a, e, h) + (int64_t)src * a.sn;
+      Some<T, W> lo, hi;
+      lo.load(from + d0);
+      hi.load(from + D / 2 + d0);
+#pragma unroll
+      for (int k = 0; k < W; ++k) { x[0][k] = lo.at(k); x[1][k] = hi.at(k); }
+      if (p.pos && kv == 0) rotate<W, D>(x[0], x[1], p.rope + (int64_t)pos * D, d0);
     }
   }
-  if (a.lists)
-#pragma unroll 4
-    for (int x = t; x < a.n; x += kOneWarps * 32) bad |= x != e && a.lists[x] == l;
-  bad = __syncthreads_or(bad);                    // (all threads have read the length by now)
-  if (t == 0) {
-    if (bad && blockIdx.y == 0) record(a.p.status, PYR_ERR_INVALID);
-    const bool last = gridDim.y == 1 || atomicAdd(&p.done[e], 1) == (int)gridDim.y - 1;
-    if (last) {
-      if (gridDim.y > 1) p.done[e] = 0;
-      if (!bad && row + cnt > len) a.p.lens[l] = row + cnt;
-    }
-  }
-  if ((int)blockIdx.y >= kv_parts) {
+  const Entry d = decide(a, e);
+  finish(a, e, d, p.done, gridDim.y);
+  if (is_query) {
     const int head = ((int)blockIdx.y - kv_parts) * (2 * kOneWarps) + (t >> 4);
-    if (head < p.Hq) query_row<T, D>(p, e, 0, head, t & 15, !bad && cnt > 0);
+    if (head < p.Hq) query_row<T, D>(p, e, 0, head, t & 15, !d.bad && d.count > 0);
     return;
   }
-  const int h = blockIdx.y * kOneWarps + warp;
-  if (bad || cnt == 0 || h >= a.p.Hkv) return;
-  const int kv = lane >> 4, d0 = W * (lane & 15);
-  const int src = source_row(a, e, h, 0), pos = position(p, e, h, 0);
-  float x[2][W];
-  if (src >= 0 && pos >= 0) {
-    const T* from = source<T>(kv ? a.v : a.k, a, e, h) + (int64_t)src * a.sn;
-    Some<T, W> lo, hi;
-    lo.load(from + d0);
-    hi.load(from + D / 2 + d0);
-#pragma unroll
-    for (int k = 0; k < W; ++k) { x[0][k] = lo.at(k); x[1][k] = hi.at(k); }
-    if (p.pos && kv == 0) rotate<W, D>(x[0], x[1], p.rope + (int64_t)pos * D, d0);
-  } else {
+  if (d.bad || d.count == 0 || h >= a.p.Hkv) return;
+  const int row = d.start, len = d.len, page = pages_page(a.p, d.list, row / a.p.page_rows);
+  if (!good) {
     if (lane == 0) record(a.p.status, PYR_ERR_INVALID);
 #pragma unroll
     for (int k = 0; k < W; ++k) x[0][k] = x[1][k] = nan_f();
@@ -238,12 +294,12 @@ __global__ void __launch_bounds__(kOneWarps * 32) append_one_kernel(PagesAppendA
   __syncwarp();
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    const int d = half * (D / 2) + d0;
+    const int at0 = half * (D / 2) + d0;
     int c[W];
 #pragma unroll
     for (int k = 0; k < W; ++k) c[k] = sc.s == sc.s ? code_int(code_sum(x[half][k], sc.inverse)) : 0;
     if (kv == 0) {
-      uint8_t* at = tile + tile8_k(D, r, d);
+      uint8_t* at = tile + tile8_k(D, r, at0);
       if constexpr (W == 4) *reinterpret_cast<uchar4*>(at) = make_uchar4(c[0] + 128, c[1] + 128, c[2] + 128, c[3] + 128);
       else *reinterpret_cast<uchar2*>(at) = make_uchar2(c[0] + 128, c[1] + 128);
       int8_t* ends = reinterpret_cast<int8_t*>(head);
@@ -251,15 +307,15 @@ __global__ void __launch_bounds__(kOneWarps * 32) append_one_kernel(PagesAppendA
       for (int k = 0; k < W; ++k) {
         int lo = c[k], hi = c[k];
         if (held) {
-          lo = min(lo, code_int(code_sum((float)ends[d + k], sc.factor)));
-          hi = max(hi, code_int(code_sum((float)ends[D + d + k], sc.factor)));
+          lo = min(lo, code_int(code_sum((float)ends[at0 + k], sc.factor)));
+          hi = max(hi, code_int(code_sum((float)ends[D + at0 + k], sc.factor)));
         }
-        ends[d + k] = (int8_t)lo;
-        ends[D + d + k] = (int8_t)hi;
+        ends[at0 + k] = (int8_t)lo;
+        ends[D + at0 + k] = (int8_t)hi;
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < W; ++k) tile[tile8_v(D, r, d + k)] = (uint8_t)(c[k] + 128);
+      for (int k = 0; k < W; ++k) tile[tile8_v(D, r, at0 + k)] = (uint8_t)(c[k] + 128);
     }
   }
   if ((lane & 15) == 0) {
@@ -309,208 +365,345 @@ __global__ void __launch_bounds__(kPlanThreads) append_plan_kernel(PagesWriteArg
   }
 }
 
-// The row of a tile that a thread holds as its p-th (of 8): four after the other are the bytes of a V word, in the order 0, 2, 1, 3.
-__device__ __forceinline__ int tile_row(int half, int p) { return 4 * half + 2 * (p >> 2) + (p & 1) + 8 * (p >> 1 & 1); }
+// A copy of a thread's own from global to shared memory, of as many bytes as a T[W]; what a thread copies only that thread reads.
+template <int kBytes>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "n"(kBytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
-// One CTA per (entry, KV head, page), a warp per tile; heads side by side, whose rows lie side by side. A thread holds D / 32
-// dimensions from either half of eight rows: both members of the rotation's pairs, and whole words of V. `pages` cover n_rows
-// rows wherever in a page they begin. CTAs from `items` on turn queries.
-template <class T, int D>
-__global__ void __launch_bounds__(kPageRows8 * 2) append_pages_kernel(PagesAppendArgs p, int pages, int64_t items) {
+// One CTA per (entry, page, `heads` KV heads one after the other), two warps a tile. A thread holds D / 32 dimensions from either half of
+// four rows: both members of the rotation's pairs, and whole words of V. Rows 2 j, 2 j + 1, 2 j + 8 and 2 j + 9 of the tile (j = 0 .. 3 for
+// the half warps) are bytes 0, 2, 1 and 3 of its words. Rows come through shared memory, with two `stages` those of the next two heads
+// while one is worked on. `pages` cover n_rows rows wherever in a page they begin.
+template <class T, int D, bool kSelf>
+__global__ void __launch_bounds__(kPageRows8 * 4, 1) append_pages_kernel(PagesAppendArgs p, int pages, int heads, int stages) {
   constexpr int W = D / 32;
-  __shared__ float top[2][kPageRows8 / kPageTile];
-  __shared__ int8_t ends[kPageRows8 / kPageTile][2][D];
+  using Part = Some<T, W>;
+  extern __shared__ __align__(16) uint8_t shared[];         // [stages][warps][16 parts: K's 4 rows x 2 halves, V's][lanes]
+  __shared__ uint2 top[kPageRows8 / 8];
+  __shared__ uint32_t ends[kPageRows8 / 8][2][D / 2];       // extrema's bytes as 16-bit halves
   const PagesWriteArgs& a = p.w;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, half = lane >> 4, d0 = W * (lane & 15), pr = a.p.page_rows;
-  wait_for_previous();
-  if (blockIdx.x >= items) {
-    const int64_t unit = ((int64_t)blockIdx.x - items) * (blockDim.x / 16) + (t >> 4);
-    const int64_t at = unit / p.Hq;
-    if (at >= (int64_t)a.n * a.n_rows) return;
-    const int e = (int)(at / a.n_rows), x = (int)(at - (int64_t)e * a.n_rows);
-    query_row<T, D>(p, e, x, (int)(unit - at * p.Hq), t & 15, a.plan[2 * e] >= 0 && x < (a.counts ? a.counts[e] : a.n_rows));
-    return;
+  const int chunks = (a.p.Hkv + heads - 1) / heads, per_entry = pages * chunks;
+  const int e = (int)(blockIdx.x / per_entry), part = (int)(blockIdx.x - (unsigned)e * per_entry);
+  let_next_start();
+  Entry d;
+  if constexpr (kSelf) {
+    d = decide(a, e);
+    finish(a, e, d, p.done, per_entry);
+  } else {
+    wait_for_previous();
+    d = Entry{pages_list(a.p, a.lists, e), a.plan[2 * e], a.counts ? a.counts[e] : a.n_rows, a.plan[2 * e + 1], a.plan[2 * e] < 0};
   }
-  const int h = (int)(blockIdx.x % a.p.Hkv);
-  const int64_t ep = blockIdx.x / a.p.Hkv;
-  const int e = (int)(ep / pages);
-  const int start = a.plan[2 * e], len = a.plan[2 * e + 1];
-  if (start < 0) return;
-  const int cnt = a.counts ? a.counts[e] : a.n_rows, end = start + cnt;
-  const int slot = start / pr + (int)(ep - (int64_t)e * pages);
+  if (d.bad) return;
+  const int h0 = part % chunks * heads, h1 = min(h0 + heads, a.p.Hkv), start = d.start, end = start + d.count;
+  const int slot = start / pr + part / chunks;
   const int64_t page0 = (int64_t)slot * pr;
   if (page0 >= end) return;
-  const int page = pages_page(a.p, pages_list(a.p, a.lists, e), slot);
-  if (page < 0) return;                           // (the plan has seen a valid page here)
-  const int upto = (int)min((int64_t)len, page0 + pr);       // rows of the list that were in this page: up to here
+  const int page = pages_page(a.p, d.list, slot);
+  if (page < 0) return;                           // (a valid page has been seen here)
+  const int upto = (int)min((int64_t)d.len, page0 + pr);     // rows of the list that were in this page: up to here
   const bool held = start > page0 || upto > end;
-  const int row0 = (int)page0 + warp * kPageTile;
+  const int row = (int)page0 + (warp >> 1) * kPageTile + lane, j = 2 * (warp & 1) + half;      // (lanes 0 .. 15: the row that a lane looks up)
 
-  // ---- this thread's rows: sources and positions by the lane of the row, new ones and those that stay as bits
-  int src = -1, pos = -1;
-  bool is_new = false, stays = false;
-  if (lane < kPageTile) {
-    const int row = row0 + lane;
-    is_new = row >= start && row < end;
-    stays = !is_new && row < upto;
-    if (is_new) {
-      src = source_row(a, e, h, row - start);
-      pos = position(p, e, h, row - start);
-      if (src < 0 || pos < 0) { src = -1; record(a.p.status, PYR_ERR_INVALID); }
-    }
-  }
+  // ---- this thread's rows: new ones and those that stay as bits; sources and positions by the lane of the row
+  const bool is_new = lane < kPageTile && row >= start && row < end, stays = lane < kPageTile && !is_new && row < upto;
   const uint32_t news = __ballot_sync(0xffffffffu, is_new), kept = __ballot_sync(0xffffffffu, stays);
-  float k[8][2 * W];
-  Some<T, W> v[8][2];
-  {
-    const T* kp = source<T>(a.k, a, e, h) + d0;
-    const T* vp = source<T>(a.v, a, e, h) + d0;
-#pragma unroll
-    for (int b = 0; b < 8; b += 4) {
-      Some<T, W> raw[4][2];
-      int at[4], ps[4];
+  auto row_of = [&](int q) { return 2 * j + (q & 1) + 8 * (q >> 1); };
+  const bool same = a.idx_groups == 1;            // every head has the same rows
+  // where the rows of head `to_copy` come from, looked up an iteration before they are copied; positions of that one and of the one before
+  int src = -1, pos = 0, pos_copied = 0;
+  auto look_up = [&](int h) {
+    if (!is_new || h >= h1) return;
+    const int64_t group = same ? 0 : (int64_t)h * a.n_rows;
+    src = a.idx ? a.idx[(int64_t)e * a.idx_stride + group + row - start] : row - start;
+    pos = p.pos ? p.pos[(int64_t)e * p.pos_stride + group + row - start] : 0;
+  };
+  Part* const mine = reinterpret_cast<Part*>(shared) + warp * 512 + lane;
+  const int stage_parts = blockDim.x * 16;
+  int to = 0;                                     // the stage of the next copy
+  const T* kp = source<T>(a.k, a, e, h0) + d0;    // of the head that is copied next
+  const T* vp = source<T>(a.v, a, e, h0) + d0;
+  auto copy = [&] {                               // and checks what has been looked up
+    const bool fine = is_new && src >= 0 && src < a.src_rows && (!p.pos || (pos >= 0 && pos < p.n_pos));
+    const uint32_t there = __ballot_sync(0xffffffffu, fine);
+    pos_copied = fine ? pos : -1;
+    Part* dst = mine + to;
+    if (there == 0xffffu) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int r = tile_row(half, b + q);
-        at[q] = __shfl_sync(0xffffffffu, src, r);
-        ps[q] = __shfl_sync(0xffffffffu, pos, r);
-        if (at[q] >= 0) {
-          const int64_t off = (int64_t)at[q] * a.sn;
-          raw[q][0].load(kp + off);
-          raw[q][1].load(kp + off + D / 2);
-          v[b + q][0].load(vp + off);
-          v[b + q][1].load(vp + off + D / 2);
-        } else {                                  // not a new row: nothing; one without a source: NaN
-          const float x = news >> r & 1u ? nan_f() : 0.f;
-          raw[q][0].set(x); raw[q][1].set(x);
-          v[b + q][0].set(x); v[b + q][1].set(x);
+        const int64_t off = (int64_t)__shfl_sync(0xffffffffu, src, row_of(q)) * a.sn;
+        const T *kr = kp + off, *vr = vp + off;
+        copy_async<sizeof(Part)>(dst + 64 * q, kr);
+        copy_async<sizeof(Part)>(dst + 64 * q + 32, kr + D / 2);
+        copy_async<sizeof(Part)>(dst + 64 * q + 256, vr);
+        copy_async<sizeof(Part)>(dst + 64 * q + 288, vr + D / 2);
+      }
+    } else {
+      if (is_new && !fine) record(a.p.status, PYR_ERR_INVALID);
+#pragma unroll 1
+      for (int q = 0; q < 4; ++q) {
+        const int r = row_of(q), at = __shfl_sync(0xffffffffu, src, r);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          Part* to_k = dst + 64 * q + 32 * g;
+          if (there >> r & 1u) {
+            const int64_t off = (int64_t)at * a.sn + g * (D / 2);
+            copy_async<sizeof(Part)>(to_k, kp + off);
+            copy_async<sizeof(Part)>(to_k + 256, vp + off);
+          } else {                                // not a new row: nothing; one without a source: NaN
+            Part none;
+            none.set(news >> r & 1u ? nan_f() : 0.f);
+            *to_k = none;
+            to_k[256] = none;
+          }
         }
       }
+    }
+    kp += a.sh;
+    vp += a.sh;
+    to = stages > 1 ? stage_parts - to : 0;
+  };
+  Some<float, W> rope[4][2];
+  auto fetch_rope = [&] {                         // for the head copied last
+    const bool all = __all_sync(0xffffffffu, lane >= kPageTile || pos_copied >= 0);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) { k[b + q][i] = raw[q][0].at(i); k[b + q][W + i] = raw[q][1].at(i); }
-        if (p.pos && at[q] >= 0) rotate<W, D>(k[b + q], k[b + q] + W, p.rope + (int64_t)ps[q] * D, d0);
+    for (int q = 0; q < 4; ++q) {
+      const int at = __shfl_sync(0xffffffffu, pos_copied, row_of(q));
+      if (all || at >= 0) {
+        rope[q][0].load(p.rope + (int64_t)at * D + d0);
+        rope[q][1].load(p.rope + (int64_t)at * D + D / 2 + d0);
+      } else {
+        rope[q][0].set(1.f);
+        rope[q][1].set(0.f);
       }
     }
+  };
+  look_up(h0);
+  copy();
+  copies_commit();
+  if (p.pos) fetch_rope();
+  if (stages > 1) {
+    if (!same) look_up(h0 + 1);
+    if (h0 + 1 < h1) copy();
+    copies_commit();
   }
-  float mk = 0.f, mv = 0.f;
+  uint8_t* head = head_of(a.p, page, h0);
+  const int head_bytes = pages_head_bytes(a.p), tile_at = a.p.head_extra + (warp >> 1) * a.p.tile_bytes;
+  int from = 0;                                   // the stage that is worked on
+#pragma unroll 1
+  for (int h = h0; h < h1; ++h, head += head_bytes, from = stages > 1 ? stage_parts - from : 0) {
+    const Part* part_of = mine + from;            // K: row q's halves at 64 q, 64 q + 32; V's 256 behind
+    const float2 old = *reinterpret_cast<const float2*>(head + 2 * D);
+    if (!same) look_up(h + stages);
+    if (stages > 1) copies_wait<1>(); else copies_wait<0>();
+    float k[4][2 * W], mk = 0.f;
+    uint32_t mv = 0;
 #pragma unroll
-  for (int q = 0; q < 8; ++q)
+    for (int q = 0; q < 4; ++q) {
+      const Part lo = part_of[64 * q], hi = part_of[64 * q + 32];
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-      mk = max_nan(mk, max_nan(fabsf(k[q][i]), fabsf(k[q][W + i])));
-      mv = max_nan(mv, max_nan(fabsf(v[q][0].at(i)), fabsf(v[q][1].at(i))));
+      for (int i = 0; i < W; ++i) { k[q][i] = lo.at(i); k[q][W + i] = hi.at(i); }
+      if (p.pos) turn<W>(k[q], k[q] + W, rope[q][0], rope[q][1]);      // (nothing and NaN stay what they are)
+#pragma unroll
+      for (int i = 0; i < W; ++i) mk = most_of(mk, k[q][i], k[q][W + i]);
+      part_of[64 * q + 256].most(&mv);
+      part_of[64 * q + 288].most(&mv);
     }
-  // (magnitudes, Inf and NaN among them, are ordered as their bits are)
-  const uint32_t bk = __reduce_max_sync(0xffffffffu, __float_as_uint(mk) & 0x7fffffffu);
-  const uint32_t bv = __reduce_max_sync(0xffffffffu, __float_as_uint(mv) & 0x7fffffffu);
-  if (lane == 0) { top[0][warp] = __uint_as_float(bk); top[1][warp] = __uint_as_float(bv); }
-  uint8_t* head = head_of(a.p, page, h);
-  const float2 old = *reinterpret_cast<const float2*>(head + 2 * D);
-  __syncthreads();                                // (the old scales are read, too)
-  const int warps = a.p.tiles_per_page;
-  uint32_t ak = 0, av = 0;
-  for (int w = 0; w < warps; ++w) { ak = max(ak, __float_as_uint(top[0][w])); av = max(av, __float_as_uint(top[1][w])); }
-  const float before_k = held ? old.x : 0.f, before_v = held ? old.y : 0.f;
-  const Scale sk = scale_of(__uint_as_float(ak), before_k), sv = scale_of(__uint_as_float(av), before_v);
+    if (p.pos && !same && stages > 1 && h + 1 < h1) fetch_rope();
+    // (magnitudes, Inf and NaN among them, are ordered as their bits are)
+    const uint32_t bk = __reduce_max_sync(0xffffffffu, __float_as_uint(mk) & 0x7fffffffu);
+    const uint32_t bv = __reduce_max_sync(0xffffffffu, Some<T, W>::finish(mv));
+    if (lane == 0) top[warp] = make_uint2(bk, bv);
+    __syncthreads();                              // (the old scales are read, too)
+    const int warps = 2 * a.p.tiles_per_page;
+    uint2 all = make_uint2(0, 0);
+    if (lane < warps) all = top[lane];
+    all.x = __reduce_max_sync(0xffffffffu, all.x);
+    all.y = __reduce_max_sync(0xffffffffu, all.y);
+    const float before_k = held ? old.x : 0.f, before_v = held ? old.y : 0.f;
+    // (even lanes K's, odd lanes V's)
+    const Scale mine = scale_of(__uint_as_float(lane & 1 ? all.y : all.x), lane & 1 ? before_v : before_k);
+    const Scale sk{__shfl_sync(0xffffffffu, mine.s, 0), __shfl_sync(0xffffffffu, mine.factor, 0), __shfl_sync(0xffffffffu, mine.inverse, 0)};
+    const Scale sv{__shfl_sync(0xffffffffu, mine.s, 1), __shfl_sync(0xffffffffu, mine.factor, 1), __shfl_sync(0xffffffffu, mine.inverse, 1)};
 
-  // ---- codes
-  uint8_t* tile = head + a.p.head_extra + warp * a.p.tile_bytes;
-  constexpr float kNone = kRound;                 // the sum of code 0
-  const bool fine_k = sk.s == sk.s, fine_v = sv.s == sv.s;
-  float lo[2 * W], hi[2 * W];
+    // ---- codes
+    uint8_t* tile = head + tile_at;
+    float lo[2 * W], hi[2 * W];
 #pragma unroll
-  for (int i = 0; i < 2 * W; ++i) { lo[i] = kRound + 127.f; hi[i] = kRound - 127.f; }
-  if (news || (kept && !(sk.s == before_k))) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const int r = tile_row(half, q);
-      const bool fresh = news >> r & 1u, stay = kept >> r & 1u;
+    for (int i = 0; i < 2 * W; ++i) { lo[i] = kRound + 127.f; hi[i] = kRound - 127.f; }
+    if (news == 0xffffu && sk.s == sk.s && sv.s == sv.s) {
+      // a whole tile of new rows (rows of K two by two: their halves lie the other way round in odd rows, with 128 dimensions)
+      uint8_t* kat = tile + 2 * j * D + d0;
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        uint8_t* at = tile + tile8_k(D, r, g * (D / 2) + d0);
-        float c[W];
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          c[i] = fine_k ? code_sum(k[q][g * W + i], sk.inverse) : kNone;
-          if (fresh) { lo[g * W + i] = fminf(lo[g * W + i], c[i]); hi[g * W + i] = fmaxf(hi[g * W + i], c[i]); }
-        }
-        uint32_t w;
-        if constexpr (W == 4) w = bytes4(c[0], c[1], c[2], c[3]) ^ 0x80808080u;
-        else w = __byte_perm(__float_as_uint(c[0]), __float_as_uint(c[1]), 0x0040) ^ 0x8080u;
-        if constexpr (W == 4) {
-          if (stay) w = recode4(*reinterpret_cast<const uint32_t*>(at), sk.factor);
-          *reinterpret_cast<uint32_t*>(at) = w;
-        } else {
-          if (stay) w = recode4(*reinterpret_cast<const uint16_t*>(at), sk.factor);
-          *reinterpret_cast<uint16_t*>(at) = (uint16_t)w;
-        }
-      }
-    }
-  }
-  if (news || (kept && !(sv.s == before_v))) {
-    const uint32_t mine = half ? 0xF0F0u : 0x0F0Fu;           // this thread's rows
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        uint32_t* at = reinterpret_cast<uint32_t*>(tile + tile8_v(D, tile_row(half, 4 * j), g * (D / 2) + d0));
+        uint32_t* vat = reinterpret_cast<uint32_t*>(tile + tile8_v(D, 2 * j, g * (D / 2) + d0));
         uint32_t w[W];
 #pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float c[W];
+#pragma unroll
+          for (int i = 0; i < W; ++i) c[i] = k[q][g * W + i] = code_sum(k[q][g * W + i], sk.inverse);
+          uint8_t* at = kat + (q & 1) * D + (q >> 1) * (8 * D) + (D / 2) * (D == 128 ? g ^ (q & 1) : g);
+          if constexpr (W == 4) *reinterpret_cast<uint32_t*>(at) = bytes4(c[0], c[1], c[2], c[3]);
+          else *reinterpret_cast<uint16_t*>(at) = (uint16_t)__byte_perm(__float_as_uint(c[0]), __float_as_uint(c[1]), 0x0040);
+        }
+#pragma unroll
         for (int i = 0; i < W; ++i) {
-          float c[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) c[q] = fine_v ? code_sum(v[4 * j + q][g].at(i), sv.inverse) : kNone;
-          w[i] = bytes4(c[0], c[2], c[1], c[3]) ^ 0x80808080u;
+          const int x = g * W + i;
+          lo[x] = min_of(min_of(k[0][x], k[1][x], k[2][x]), k[3][x], k[3][x]);
+          hi[x] = max_of(max_of(k[0][x], k[1][x], k[2][x]), k[3][x], k[3][x]);
         }
-        if (kept & mine) {
-          uint32_t from = 0;                      // bytes of rows that stay
+        const Part v[4] = {part_of[256 + 32 * g], part_of[320 + 32 * g], part_of[384 + 32 * g], part_of[448 + 32 * g]};
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int r = tile_row(half, 4 * j + q), b = 2 * (r & 1) + (r >> 3);
-            if (kept >> r & 1u) from |= 255u << (8 * b);
-          }
-#pragma unroll
-          for (int i = 0; i < W; ++i) w[i] = (w[i] & ~from) | (recode4(at[i], sv.factor) & from);
-        }
-        if constexpr (W == 4) *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
-        else *reinterpret_cast<uint2*>(at) = make_uint2(w[0], w[1]);
+        for (int i = 0; i < W; ++i)
+          w[i] = bytes4(code_sum(v[0].at(i), sv.inverse), code_sum(v[2].at(i), sv.inverse), code_sum(v[1].at(i), sv.inverse),
+                        code_sum(v[3].at(i), sv.inverse));
+        if constexpr (W == 4) *reinterpret_cast<uint4*>(vat) = make_uint4(w[0], w[1], w[2], w[3]);
+        else *reinterpret_cast<uint2*>(vat) = make_uint2(w[0], w[1]);
       }
-  }
-  if (lane == 0 && (news | kept)) *reinterpret_cast<float2*>(tile + tile8_scales(D)) = make_float2(sk.s, sv.s);
+    } else {
+      const bool fine_k = sk.s == sk.s, fine_v = sv.s == sv.s;
+      if (news || (kept && !(sk.s == before_k))) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int r = row_of(q);
+          const bool fresh = news >> r & 1u, stay = kept >> r & 1u;
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            uint8_t* at = tile + tile8_k(D, r, g * (D / 2) + d0);
+            float c[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+              c[i] = fine_k ? code_sum(k[q][g * W + i], sk.inverse) : kRound;
+              if (fresh) { lo[g * W + i] = fminf(lo[g * W + i], c[i]); hi[g * W + i] = fmaxf(hi[g * W + i], c[i]); }
+            }
+            if constexpr (W == 4) {
+              uint32_t w = bytes4(c[0], c[1], c[2], c[3]);
+              if (stay) w = recode4(*reinterpret_cast<const uint32_t*>(at), sk.factor);
+              *reinterpret_cast<uint32_t*>(at) = w;
+            } else {
+              uint32_t w = __byte_perm(__float_as_uint(c[0]), __float_as_uint(c[1]), 0x0040);
+              if (stay) w = recode4(*reinterpret_cast<const uint16_t*>(at), sk.factor);
+              *reinterpret_cast<uint16_t*>(at) = (uint16_t)w;
+            }
+          }
+        }
+      }
+      if (news || (kept && !(sv.s == before_v))) {
+        uint32_t from = 0;                        // bytes of rows that stay
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (kept >> row_of(q) & 1u) from |= 255u << (8 * (2 * (q & 1) + (q >> 1)));
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          uint32_t* at = reinterpret_cast<uint32_t*>(tile + tile8_v(D, 2 * j, g * (D / 2) + d0));
+          const Part v[4] = {part_of[256 + 32 * g], part_of[320 + 32 * g], part_of[384 + 32 * g], part_of[448 + 32 * g]};
+          uint32_t w[W];
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            float c[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) c[q] = fine_v ? code_sum(v[q].at(i), sv.inverse) : kRound;
+            w[i] = bytes4(c[0], c[2], c[1], c[3]);
+          }
+          if (from)
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i] = (w[i] & ~from) | (recode4(at[i], sv.factor) & from);
+          if constexpr (W == 4) *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+          else *reinterpret_cast<uint2*>(at) = make_uint2(w[0], w[1]);
+        }
+      }
+    }
+    if (lane == 0 && (warp & 1) == 0 && (news | kept)) *reinterpret_cast<float2*>(tile + tile8_scales(D)) = make_float2(sk.s, sv.s);
 
-  // ---- extrema of the codes, a dimension a thread
+    // ---- the stage is free: rows of the head that takes it
+    if (h + stages < h1) {
+      copy();
+      if (stages == 1 && p.pos && !same) fetch_rope();
+    }
+    copies_commit();
+
+    // ---- extrema of the codes, two dimensions to a word: of the half warps, of the warps
+    uint32_t lo2[W], hi2[W];
 #pragma unroll
-  for (int i = 0; i < 2 * W; ++i) {
-    lo[i] = fminf(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], 16));
-    hi[i] = fmaxf(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], 16));
-  }
-  if (half == 0)
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
+    for (int i = 0; i < W; ++i) {
+      lo2[i] = __byte_perm(__float_as_uint(lo[2 * i]), __float_as_uint(lo[2 * i + 1]), 0x5410);
+      hi2[i] = __byte_perm(__float_as_uint(hi[2 * i]), __float_as_uint(hi[2 * i + 1]), 0x5410);
+      lo2[i] = __vminu2(lo2[i], __shfl_xor_sync(0xffffffffu, lo2[i], 16));
+      hi2[i] = __vmaxu2(hi2[i], __shfl_xor_sync(0xffffffffu, hi2[i], 16));
+    }
+    if (half == 0)
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        ends[warp][0][g * (D / 2) + d0 + i] = (int8_t)code_int(lo[g * W + i]);
-        ends[warp][1][g * (D / 2) + d0 + i] = (int8_t)code_int(hi[g * W + i]);
+        const int at = (i / (W / 2) * (D / 2) + d0) / 2 + i % (W / 2);
+        ends[warp][0][at] = lo2[i];
+        ends[warp][1][at] = hi2[i];
       }
-  __syncthreads();
-  int8_t* kept_ends = reinterpret_cast<int8_t*>(head);
-  for (int d = t; d < D; d += blockDim.x) {
-    int least = 127, most = -127;
-    for (int w = 0; w < warps; ++w) { least = min(least, (int)ends[w][0][d]); most = max(most, (int)ends[w][1][d]); }
-    if (held) {
-      least = min(least, code_int(code_sum((float)kept_ends[d], sk.factor)));
-      most = max(most, code_int(code_sum((float)kept_ends[D + d], sk.factor)));
+    __syncthreads();
+    int8_t* kept_ends = reinterpret_cast<int8_t*>(head);
+    for (int x = t; x < D / 2; x += blockDim.x) {
+      uint32_t least = 0x00ff00ffu, most = 0;
+      for (int w = 0; w < warps; ++w) { least = __vminu2(least, ends[w][0][x]); most = __vmaxu2(most, ends[w][1][x]); }
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int d = 2 * x + y;
+        int l = (int)(least >> (16 * y) & 255u) - 128, m = (int)(most >> (16 * y) & 255u) - 128;
+        if (held) {
+          l = min(l, code_int(code_sum((float)kept_ends[d], sk.factor)));
+          m = max(m, code_int(code_sum((float)kept_ends[D + d], sk.factor)));
+        }
+        kept_ends[d] = (int8_t)l;
+        kept_ends[D + d] = (int8_t)m;
+      }
     }
-    kept_ends[d] = (int8_t)least;
-    kept_ends[D + d] = (int8_t)most;
+    if (t == 0) *reinterpret_cast<float2*>(head + 2 * D) = make_float2(sk.s, sv.s);
   }
-  if (t == 0) *reinterpret_cast<float2*>(head + 2 * D) = make_float2(sk.s, sv.s);
+}
+
+// Queries beside rows that the kernel before has stored: 16 threads a row and kQueryHeads heads of it.
+template <class T, int D>
+__global__ void __launch_bounds__(256) turn_queries_kernel(PagesAppendArgs p, int64_t units) {
+  constexpr int W = D / 32;
+  const int64_t unit = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  if (unit >= units) return;
+  const PagesWriteArgs& a = p.w;
+  const int groups = (p.Hq + kQueryHeads - 1) / kQueryHeads, d0 = W * (threadIdx.x & 15);
+  const int64_t at = unit / groups;
+  const int h0 = (int)(unit - at * groups) * kQueryHeads;
+  const int e = (int)(at / a.n_rows), x = (int)(at - (int64_t)e * a.n_rows);
+  const int pos = x < (a.counts ? a.counts[e] : a.n_rows) ? position(p, e, 0, x) : -1;
+  const T* q = static_cast<const T*>(p.q) + (int64_t)e * p.qsb + (int64_t)x * p.qsn + d0;
+  T* out = static_cast<T*>(p.q_out) + (int64_t)e * p.osb + (int64_t)x * p.osn + d0;
+  Some<T, W> lo[kQueryHeads], hi[kQueryHeads];
+  Some<float, W> c, s;
+  c.set(nan_f()); s.set(nan_f());
+  if (pos >= 0) { c.load(p.rope + (int64_t)pos * D + d0); s.load(p.rope + (int64_t)pos * D + D / 2 + d0); }
+#pragma unroll
+  for (int i = 0; i < kQueryHeads; ++i)
+    if (h0 + i < p.Hq) {
+      lo[i].load(q + (int64_t)(h0 + i) * p.qsh);
+      hi[i].load(q + (int64_t)(h0 + i) * p.qsh + D / 2);
+    }
+  wait_for_previous();
+  const bool stored = a.plan[2 * e] >= 0 && x < (a.counts ? a.counts[e] : a.n_rows);
+#pragma unroll
+  for (int i = 0; i < kQueryHeads; ++i)
+    if (h0 + i < p.Hq) {
+      float f[2][W];
+#pragma unroll
+      for (int k = 0; k < W; ++k) { f[0][k] = lo[i].at(k); f[1][k] = hi[i].at(k); }
+      if (stored) turn<W>(f[0], f[1], c, s);
+      store_some<W>(out + (int64_t)(h0 + i) * p.osh, f[0]);
+      store_some<W>(out + (int64_t)(h0 + i) * p.osh + D / 2, f[1]);
+    }
 }
 
 // ------------------------------------------------------------------ rows as values
-// One warp per (entry, KV head, tile of its list): a lane takes 16 dimensions of a row of K, four dimensions of four rows of V.
+// One warp per (entry, KV head, tile of its list): a lane takes 8 dimensions of a row of K, four dimensions of four rows of V, so that what
+// a warp stores at once lies together.
 template <class T, int D>
 __global__ void __launch_bounds__(kReadThreads) read8_kernel(PagesWriteArgs a, int blocks, int64_t items) {
   constexpr int P = D / 32, E = D / 8;
@@ -540,23 +733,21 @@ __global__ void __launch_bounds__(kReadThreads) read8_kernel(PagesWriteArgs a, i
   T* k = const_cast<T*>(source<T>(a.k, a, e, h));
   T* v = const_cast<T*>(source<T>(a.v, a, e, h));
   const float2 scale = *reinterpret_cast<const float2*>(tile + tile8_scales(D));
-  uint4 kc[P], vc[P];
+  uint2 kc[2 * P];
+  uint4 vc[P];
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
-    kc[i] = reinterpret_cast<const uint4*>(tile)[i * 32 + lane];
-    vc[i] = reinterpret_cast<const uint4*>(tile + kPageTile * D)[i * 32 + lane];
-  }
+  for (int i = 0; i < 2 * P; ++i) kc[i] = reinterpret_cast<const uint2*>(tile)[i * 32 + lane];
+#pragma unroll
+  for (int i = 0; i < P; ++i) vc[i] = reinterpret_cast<const uint4*>(tile + kPageTile * D)[i * 32 + lane];
   auto value = [](uint32_t w, int b, float s) { return __fmul_rn((float)((int)(w >> (8 * b) & 255u) - 128), s); };
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
-    const int piece = i * 32 + lane, r = piece / (D / 16), x = (piece % (D / 16)) ^ (D == 128 ? 4 * (r & 1) : 0), row = row0 + r;
+  for (int i = 0; i < 2 * P; ++i) {
+    const int piece = i * 32 + lane, r = piece / (D / 8), x = (piece % (D / 8)) ^ (D == 128 ? 8 * (r & 1) : 0), row = row0 + r;
     if (row < first || row >= end) continue;
-    const uint32_t w[4] = {kc[i].x, kc[i].y, kc[i].z, kc[i].w};
+    float f[8];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float f[4] = {value(w[q], 0, scale.x), value(w[q], 1, scale.x), value(w[q], 2, scale.x), value(w[q], 3, scale.x)};
-      store_some<4>(k + (int64_t)(row - first) * a.sn + 16 * x + 4 * q, f);
-    }
+    for (int b = 0; b < 8; ++b) f[b] = value(b < 4 ? kc[i].x : kc[i].y, b & 3, scale.x);
+    store_eight(k + (int64_t)(row - first) * a.sn + 8 * x, f);
   }
 #pragma unroll
   for (int i = 0; i < P; ++i) {
@@ -588,10 +779,22 @@ struct RunOne {
     return cudaGetLastError();
   }
 };
+constexpr int kStageBytes = 200 * 1024;          // shared memory of a CTA's stages at most
 struct RunPages {
-  const PagesAppendArgs& a; int pages; int64_t items; unsigned grid; cudaStream_t s;
+  const PagesAppendArgs& a; int pages, heads; unsigned grid; bool self; cudaStream_t s;
   template <class T, int D> cudaError_t run() {
-    return launch_behind(append_pages_kernel<T, D>, dim3(grid), dim3(2 * a.w.p.page_rows), 0, s, a, pages, items);
+    const int threads = 4 * a.w.p.page_rows, stage = threads * 16 * (int)sizeof(Some<T, D / 32>), stages = heads > 1 && 2 * stage <= kStageBytes ? 2 : 1;
+    cudaError_t e = self ? allow_shared<append_pages_kernel<T, D, true>>(kStageBytes) : allow_shared<append_pages_kernel<T, D, false>>(kStageBytes);
+    if (e != cudaSuccess) return e;
+    if (!self) return launch_behind(append_pages_kernel<T, D, false>, dim3(grid), dim3(threads), stages * stage, s, a, pages, heads, stages);
+    append_pages_kernel<T, D, true><<<grid, threads, stages * stage, s>>>(a, pages, heads, stages);
+    return cudaGetLastError();
+  }
+};
+struct RunQueries {
+  const PagesAppendArgs& a; int64_t units; cudaStream_t s;
+  template <class T, int D> cudaError_t run() {
+    return launch_behind(turn_queries_kernel<T, D>, dim3((unsigned)((units + 15) / 16)), dim3(256), 0, s, a, units);
   }
 };
 struct RunRead {
@@ -629,15 +832,28 @@ cudaError_t launch_pages_append8(const PagesAppendArgs& a, int* launches, cudaSt
   const int words = (w.p.n_lists + 31) / 32, pr = w.p.page_rows;
   const int pages = (int)(((int64_t)w.n_rows + pr - 2) / pr) + 1;
   const int64_t items = (int64_t)w.n * w.p.Hkv * pages;
-  const int64_t queries = a.q ? ((int64_t)w.n * w.n_rows * a.Hq + 2 * pr / 16 - 1) / (2 * pr / 16) : 0;
-  if (items + queries > 0x7fffffffLL) return cudaErrorInvalidValue;
-  e = allow_shared<append_plan_kernel>(2 * (kMaxLists / 32) * 4);
-  if (e != cudaSuccess) return e;
-  append_plan_kernel<<<1, kPlanThreads, 2 * words * sizeof(uint32_t), s>>>(w, words);
-  e = cudaGetLastError();
+  const int64_t units = a.q ? (int64_t)w.n * w.n_rows * ((a.Hq + kQueryHeads - 1) / kQueryHeads) : 0;
+  const int sms = device_sm_count();
+  if (sms <= 0) return cudaErrorUnknown;
+  // several heads a CTA where there are more than the machine holds: what a CTA has to look up first takes microseconds
+  const int most = (int)(items / (4 * sms) < 1 ? 1 : items / (4 * sms) > 8 ? 8 : items / (4 * sms));
+  const int chunks = (w.p.Hkv + most - 1) / most, heads = (w.p.Hkv + chunks - 1) / chunks;
+  const int64_t grid = (int64_t)w.n * pages * ((w.p.Hkv + heads - 1) / heads);
+  if (grid > 0x7fffffffLL || units > 16 * 0x7fffffffLL) return cudaErrorInvalidValue;
+  const bool self = w.n <= kSelfEntries;
+  if (!self) {
+    e = allow_shared<append_plan_kernel>(2 * (kMaxLists / 32) * 4);
+    if (e != cudaSuccess) return e;
+    append_plan_kernel<<<1, kPlanThreads, 2 * words * sizeof(uint32_t), s>>>(w, words);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    ++*launches;
+  }
+  e = by_format(w.p, w.dtype, RunPages{a, pages, heads, (unsigned)grid, self, s});
   if (e != cudaSuccess) return e;
   ++*launches;
-  e = by_format(w.p, w.dtype, RunPages{a, pages, items, (unsigned)(items + queries), s});
+  if (!a.q) return cudaSuccess;
+  e = by_format(w.p, w.dtype, RunQueries{a, units, s});
   if (e == cudaSuccess) ++*launches;
   return e;
 }
