@@ -493,21 +493,35 @@ pyr_status_t pyr_pages_write(pyr_pages_t* pages, const int32_t* lists, int32_t n
 
 /*
  * Stores rows as pyr_pages_write does, in an 8-bit cache (PYR_ERR_UNSUPPORTED in 4 bits), with the rotation of positions applied on the
- * way: keys are turned in fp32 and stored from that, not rounded to dtype in between. pos (device int32 [n, idx_groups, n_rows], pos_stride
- * elements between entries) is the position of row x of head h's group, the row's place in `rope` (device fp32 [n_pos, head_dim], 16-byte
- * aligned: head_dim / 2 cosines and as many sines a position, e.g. from pyr_glue_rope_table): (x1, x2) becomes (x1 c - x2 s, x2 c + x1 s) for
- * the pairs (i, i + head_dim / 2), every product and sum rounded. pos NULL: keys as they are, rope is not looked at. A position
- * outside [0, n_pos) stores a row of NaN, keys and values, and is reported.
- * q, q_out (device, may both be NULL; with pos and without idx only) are [n, n_rows, n_q_heads, head_dim] of the same dtype, strided as k: q_out
- * becomes q turned by the row's position, in fp32 and rounded once (NaN for a position out of range); queries beside rows that are not
- * stored (behind counts_i, of a refused entry) pass as they are. q_out may be q, with the same strides. n_q_heads at most 65535.
+ * way: keys are turned in fp32 and stored from that, not rounded to dtype in between. pos is the position of row x of head h's group, the row's
+ * place in `rope`: (x1, x2) becomes (x1 c - x2 s, x2 c + x1 s) for the pairs (i, i + head_dim / 2), every product and sum rounded. pos NULL:
+ * keys as they are, rope is not looked at. A position outside [0, n_pos) stores a row of NaN, keys and values, and is reported.
+ * q_out becomes q turned by the positions of the rows beside it, in fp32 and rounded once (NaN for a position out of range); queries beside
+ * rows that are not stored (behind counts_i, of a refused entry) pass as they are. With pos and without idx only. q_out may be q,
+ * with the same strides.
  */
-pyr_status_t pyr_pages_append(pyr_pages_t* pages, const int32_t* lists, int32_t n, const int32_t* first, const void* k,
-                              const void* v, int64_t stride_b, int64_t stride_n, int64_t stride_h, int32_t src_rows,
-                              int32_t dtype, const int32_t* pos, int64_t pos_stride, const float* rope, int32_t n_pos,
-                              const void* q, void* q_out, int64_t q_stride_b, int64_t q_stride_n, int64_t q_stride_h,
-                              int64_t o_stride_b, int64_t o_stride_n, int64_t o_stride_h, int32_t n_q_heads, const int32_t* idx,
-                              int32_t idx_groups, int64_t idx_stride, const int32_t* counts, int32_t n_rows, void* stream);
+typedef struct {
+  const int32_t* lists;   /* what pyr_pages_write takes under these names ...                        */
+  const int32_t* first;
+  const void* k;
+  const void* v;
+  int64_t stride_b, stride_n, stride_h;
+  const int32_t* idx;
+  int64_t idx_stride;
+  const int32_t* counts;
+  const int32_t* pos;     /* device int32 [n, idx_groups, n_rows], or NULL                           */
+  int64_t pos_stride;     /* elements between entries of pos                                         */
+  const float* rope;      /* device fp32 [n_pos, head_dim], 16-byte aligned: head_dim / 2 cosines and as many sines a position,
+                             e.g. from pyr_glue_rope_table                                           */
+  const void* q;          /* device [n, n_rows, n_q_heads, head_dim] of the same dtype, strided as k; NULL with q_out: no queries */
+  void* q_out;
+  int64_t q_stride_b, q_stride_n, q_stride_h, o_stride_b, o_stride_n, o_stride_h;
+  int32_t n;              /* ... and these                                                           */
+  int32_t src_rows, dtype, idx_groups, n_rows;
+  int32_t n_pos;
+  int32_t n_q_heads;      /* at most 65535                                                           */
+} pyr_append_t;
+pyr_status_t pyr_pages_append(pyr_pages_t* pages, const pyr_append_t* args, void* stream);
 
 /* Reads rows back as the values they stand for: k, v (device) are [n, n_rows, n_kv_heads, head_dim], strided as above, no two rows
  * over one another (each stride passes what the smaller ones span).
@@ -553,7 +567,7 @@ pyr_status_t pyr_pages_attn(pyr_pages_t* pages, const int32_t* lists, int32_t n,
  * max the header's extrema, s_K its K scale, qc = rint(q * (1 / s_q)) with s_q = max|q| / 127 as for rows (products rounded to fp32, the sum
  * exact): an upper bound of q . K for the page's rows up to the query's rounding. NaN counts as Inf; a page whose id is out of range
  * comes last and is reported. An entry whose list id is out of range gets -1 throughout. All pages of a list are scored by the CTAs of one
- * (entry, token, KV head): 4 * max_pages + (n_q_heads / n_kv_heads) * (2 * head_dim + 4) bytes must fit 200 KB.
+ * (entry, token, KV head): 4 bytes a page of max_pages and 2 * head_dim + 4 a query head of the KV head, in eights, must fit 200 KB.
  */
 pyr_status_t pyr_pages_select(pyr_pages_t* pages, const int32_t* lists, int32_t n, const void* q, int64_t q_stride_b,
                               int64_t q_stride_t, int64_t q_stride_h, int32_t q_len, int32_t n_q_heads, int32_t dtype,

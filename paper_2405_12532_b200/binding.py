@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import math
 import os
+import struct
 
 import torch
 
@@ -122,8 +123,7 @@ def lib() -> C.CDLL:
         L.pyr_pages_fork.argtypes = [vp, vp, vp, i32, vp]
         L.pyr_pages_trim.argtypes = [vp, vp, i32, vp, vp]
         L.pyr_pages_compact.argtypes = [vp, vp, vp, i32, vp, i32, i64, vp, i32, vp]
-        L.pyr_pages_append.argtypes = ([vp, vp, i32, vp, vp, vp, i64, i64, i64, i32, i32, vp, i64, vp, i32, vp, vp] + [i64] * 6 +
-                                       [i32, vp, i32, i64, vp, i32, vp])
+        L.pyr_pages_append.argtypes = [vp, vp, vp]
         L.pyr_pages_select.argtypes = [vp, vp, i32, vp, i64, i64, i64, i32, i32, i32, vp, i32, i32, i32, vp]
         L.pyr_pages_attn_blocks.argtypes = [vp, vp, i32, vp, i32, vp, i64, i64, i64, vp, i64, i64, i64, vp, i32, i32, i32, C.c_float, vp]
         L.pyr_glue_rope_table.argtypes = [vp, i64, i64, i32, C.c_double, vp]
@@ -466,6 +466,7 @@ class PyrCache:
 # (what torch.cuda asks itself, without the objects around it; a build of torch for the CPU has neither)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_INT32 = torch.int32
 _PAGES_DTYPES = {torch.bfloat16: PYR_BF16, torch.float32: PYR_F32}
 
 
@@ -489,6 +490,9 @@ def pyr_pages_bytes(cfg: PyrPagesConfig) -> tuple[int, int]:
     return b.value, a.value
 
 
+_APPEND = struct.Struct("@PPPPqqqPqPPqPPPqqqqqqiiiiiii")     # pyr_append_t
+
+
 class PyrPages:
     """A paged cache in 4 or (bits=8) 8 bits (pyr_pages_*): the handle plus the torch buffer that backs it, emptied on creation. `lists` arguments
     are int32 tensors of list ids, `idx` [n, groups, rows] int32 with its last two dimensions contiguous; the views `pool`
@@ -503,6 +507,8 @@ class PyrPages:
         self.device = self.buf.device
         self._index, self._heads, self._dim = self.device.index, self.cfg.n_kv_heads, self.cfg.head_dim
         self._fn = {name: getattr(lib(), name) for name in EXPORTS if name.startswith("pyr_pages_")}
+        self._args = bytearray(_APPEND.size)
+        self._args_at = C.addressof(C.c_char.from_buffer(self._args))
         off = (-self.buf.data_ptr()) % align
         self.handle = C.c_void_p()
         _check(lib().pyr_pages_alloc(C.byref(self.cfg), C.c_void_p(self.buf.data_ptr() + off), nbytes, C.byref(self.handle)),
@@ -549,7 +555,7 @@ class PyrPages:
         """Pointer to an int32 vector of n entries on the cache's device, None for NULL."""
         if t is None:
             return None
-        if t.dtype is not torch.int32 or t.get_device() != self._index or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        if t.dtype is not _INT32 or t.get_device() != self._index or t.shape != (n,) or not t.is_contiguous():
             raise ValueError(f"{what}: expected {n} contiguous int32 entries on {self.device}")
         return t.data_ptr()
 
@@ -616,33 +622,40 @@ class PyrPages:
             with torch.cuda.device(self._index), torch.cuda.stream(stream):    # what is allocated here is used on that stream
                 return self.append(k, v, lists, first, pos, rope, q, q_out, idx, counts)
         (n, src, _, _), (sb, sn, sh, _), dtype = self._rows(k, v)
-        ip, groups, istride = self._idx(idx, n)
-        rows = src if idx is None else idx.shape[2]
-        pp, pstride, rp, n_pos = None, 0, None, 0
+        ip, groups, istride, rows = 0, 1, 0, src
+        if idx is not None:
+            ip, groups, istride = self._idx(idx, n)
+            rows = idx.shape[2]
+        pp = pstride = rp = n_pos = qp = op = qb = qn = qh = ob = on = oh = hq = 0
         if pos is not None:
-            if pos.dim() != 3 or tuple(pos.shape) != (n, groups, rows):
+            pp, pgroups, pstride = self._idx(pos, n, "pos")
+            if pgroups != groups or pos.shape[2] != rows:
                 raise ValueError(f"pos: expected int32 [{n}, {groups}, {rows}]")
-            pp, _, pstride = self._idx(pos, n, "pos")
-            if (rope is None or rope.dtype is not torch.float32 or rope.dim() != 2 or rope.shape[1] != self._dim or
-                    rope.get_device() != self._index or not rope.is_contiguous()):
+            if rope is None or rope.dtype is not torch.float32 or rope.get_device() != self._index or not rope.is_contiguous():
                 raise ValueError(f"rope: expected a contiguous fp32 table [positions, {self._dim}] on {self.device}")
-            rp, n_pos = rope.data_ptr(), rope.shape[0]
-        qp = op = None
-        qs = os = (0, 0, 0)
-        hq = 0
+            n_pos, dim = rope.shape
+            if dim != self._dim:
+                raise ValueError(f"rope: expected {self._dim} columns")
+            rp = rope.data_ptr()
         if q is not None:
+            shape, (qb, qn, qh, _), dtype_q = self._tensor(q, "q")
+            n_q, rows_q, hq, _ = shape
             if q_out is None:
                 q_out = torch.empty_like(q)
-            shape, qs, qdt = self._tensor(q, "q")
-            shape_o, os, odt = self._tensor(q_out, "q_out")
-            if shape[:2] != (n, rows) or qdt != dtype or shape_o != shape or odt != qdt:
+                ob, on, oh, _ = q_out.stride()
+                shape_o, dtype_o = shape, dtype_q
+            else:
+                shape_o, (ob, on, oh, _), dtype_o = self._tensor(q_out, "q_out")
+            if n_q != n or rows_q != rows or dtype_q != dtype or shape_o != shape or dtype_o != dtype:
                 raise ValueError(f"q, q_out: expected tensors [{n}, {rows}, heads, {self._dim}] of the rows' type")
-            qp, op, hq = q.data_ptr(), q_out.data_ptr(), shape[2]
+            qp, op = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             raise ValueError("q_out: only with q")
-        self._run("pyr_pages_append", None, self._ids(lists, n), n, self._ids(first, n, "first"), k.data_ptr(), v.data_ptr(), sb, sn, sh,
-                  src, dtype, pp, pstride, rp, n_pos, qp, op, qs[0], qs[1], qs[2], os[0], os[1], os[2], hq, ip, groups, istride,
-                  self._ids(counts, n, "counts"), rows)
+        args = self._args                        # (one structure: thirty arguments one by one take ctypes longer than all of the above)
+        _APPEND.pack_into(args, 0, self._ids(lists, n) or 0, self._ids(first, n, "first") or 0, k.data_ptr(), v.data_ptr(), sb, sn, sh, ip or 0,
+                          istride, self._ids(counts, n, "counts") or 0, pp or 0, pstride, rp, qp, op, qb, qn, qh, ob, on, oh, n, src, dtype,
+                          groups, rows, n_pos, hq)
+        self._run("pyr_pages_append", None, self._args_at)
         return q_out
 
     def read(self, k, v, lists=None, first=None, counts=None, stream=None):
@@ -660,9 +673,11 @@ class PyrPages:
         n, t, hq, _ = shape
         if out is None:
             out = torch.empty_like(q)
-        shape_o, (ob, ot, oh, _), dtype_o = self._tensor(out, "out")
-        if shape_o != shape or dtype_o != dtype:
-            raise ValueError("out: expected a tensor like q")
+            ob, ot, oh, _ = out.stride()
+        else:
+            shape_o, (ob, ot, oh, _), dtype_o = self._tensor(out, "out")
+            if shape_o != shape or dtype_o != dtype:
+                raise ValueError("out: expected a tensor like q")
         stats = torch.empty(n, hq, t, dtype=torch.float32, device=self.device) if lse else None
         self._run("pyr_pages_attn", None, self._ids(lists, n), n, q.data_ptr(), qb, qt, qh, out.data_ptr(), ob, ot, oh,
                   stats.data_ptr() if lse else None, t, hq, dtype, softmax_scale)
@@ -698,9 +713,11 @@ class PyrPages:
         self._slots(slots, n, t, slots.shape[-1])
         if out is None:
             out = torch.empty_like(q)
-        shape_o, (ob, ot, oh, _), dtype_o = self._tensor(out, "out")
-        if shape_o != shape or dtype_o != dtype:
-            raise ValueError("out: expected a tensor like q")
+            ob, ot, oh, _ = out.stride()
+        else:
+            shape_o, (ob, ot, oh, _), dtype_o = self._tensor(out, "out")
+            if shape_o != shape or dtype_o != dtype:
+                raise ValueError("out: expected a tensor like q")
         stats = torch.empty(n, hq, t, dtype=torch.float32, device=self.device) if lse else None
         self._run("pyr_pages_attn_blocks", None, self._ids(lists, n), n, slots.data_ptr(), slots.shape[-1], q.data_ptr(), qb, qt, qh,
                   out.data_ptr(), ob, ot, oh, stats.data_ptr() if lse else None, t, hq, dtype, softmax_scale)

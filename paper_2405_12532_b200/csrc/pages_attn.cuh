@@ -103,7 +103,7 @@ __device__ __forceinline__ void entry_list(const PagesAttnArgs& a, int i, int* l
 template <class Body>
 __device__ __forceinline__ int entry_tiles(const PagesAttnArgs& a, int len) {
   if constexpr (Body::kSparse)
-    return min(a.n_slots, max(1, (int)(((int64_t)len + a.p.page_rows - 1) / a.p.page_rows))) * a.p.tiles_per_page;
+    return min(a.n_slots, max(1, pages_for(a.p, len))) * a.p.tiles_per_page;
   else
     return (int)attn_tiles(len);
 }
@@ -573,7 +573,7 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
     // the first CTA holds the beginning (place 1), the others go on with it (place 0)
     const float* src = a.partial + (size_t)c1 * 2 * (kAttnCols * (D + 2));
     const size_t step = 2 * (size_t)(kAttnCols * (D + 2)), second = kAttnCols * (D + 2);
-    constexpr int kFew = 8;
+    constexpr int kFew = Body::kFew;
     if (cn <= kFew) {                            // everything a thread needs in one round of loads
       for (int o = t; o < ncols * (D / 4); o += kThreads) {
         const int x = o / (D / 4), d = o % (D / 4) * 4;

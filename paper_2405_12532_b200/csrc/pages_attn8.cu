@@ -72,7 +72,7 @@ template <class T, int D, bool kChosen>
 struct ByteBody {
   using Type = T;
   static constexpr bool kSparse = kChosen, kTwo = sizeof(T) == 4;
-  static constexpr int kSegment = 4;
+  static constexpr int kSegment = 4, kFew = 16;
   static constexpr int kDim = D, COLS = 8, kWarps = 7, kBlocks = 1, kQueryFloats = 0;
   static constexpr int kTileBytes = 2 * kPageTile * D + 16, kStages = D == 128 ? 3 : 6;
   static constexpr int X = D / 64, KS = 4 * X, NS = kTwo ? 2 : 1, VC = D / 32;   // K chunks a lane and row, steps over D, operands, V chunks

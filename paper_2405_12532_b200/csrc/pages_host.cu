@@ -313,32 +313,33 @@ pyr_status_t pyr_pages_write(pyr_pages_t* h, const int32_t* lists, int32_t n, co
   PYR_PAGES(pyr::launch_pages_write(a, &launches, static_cast<cudaStream_t>(stream)));
 }
 
-pyr_status_t pyr_pages_append(pyr_pages_t* h, const int32_t* lists, int32_t n, const int32_t* first, const void* k,
-                              const void* v, int64_t sb, int64_t sn, int64_t sh, int32_t src_rows, int32_t dtype,
-                              const int32_t* pos, int64_t pos_stride, const float* rope, int32_t n_pos, const void* q, void* q_out,
-                              int64_t qsb, int64_t qsn, int64_t qsh, int64_t osb, int64_t osn, int64_t osh, int32_t n_q_heads,
-                              const int32_t* idx, int32_t idx_groups, int64_t idx_stride, const int32_t* counts, int32_t n_rows,
-                              void* stream) {
+pyr_status_t pyr_pages_append(pyr_pages_t* h, const pyr_append_t* x, void* stream) {
+  if (!h || !x) return PYR_ERR_NULL;
+  const int32_t n = x->n, n_rows = x->n_rows;
   pyr_status_t st = check_call(h, n, true);
-  if (st == PYR_OK) st = check_rows(h, k, v, dtype, sb, sn, sh, n, src_rows, h->cfg.n_kv_heads);
-  if (st == PYR_OK) st = check_idx(h, idx, idx_groups, idx_stride, n_rows);
+  if (st == PYR_OK) st = check_rows(h, x->k, x->v, x->dtype, x->stride_b, x->stride_n, x->stride_h, n, x->src_rows, h->cfg.n_kv_heads);
+  if (st == PYR_OK) st = check_idx(h, x->idx, x->idx_groups, x->idx_stride, n_rows);
   if (st != PYR_OK) return st;
-  if (n_rows < 0 || src_rows < 0 || (!idx && n_rows > src_rows)) return PYR_ERR_INVALID;
-  if (pos) {
-    if (!rope) return PYR_ERR_NULL;
-    if (n_pos < 1 || pos_stride < 0 || reinterpret_cast<uintptr_t>(rope) % 16) return PYR_ERR_INVALID;
+  if (n_rows < 0 || x->src_rows < 0 || (!x->idx && n_rows > x->src_rows)) return PYR_ERR_INVALID;
+  if (x->pos) {
+    if (!x->rope) return PYR_ERR_NULL;
+    if (x->n_pos < 1 || x->pos_stride < 0 || reinterpret_cast<uintptr_t>(x->rope) % 16) return PYR_ERR_INVALID;
   }
-  if (q || q_out) {
+  const void* q = x->q;
+  const int32_t n_q_heads = x->n_q_heads;
+  if (q || x->q_out) {
     // (queries take the positions of the rows beside them: without an index list)
-    if (!pos || idx || n_q_heads < 1) return PYR_ERR_INVALID;
-    st = check_rows(h, q, q_out, dtype, qsb, qsn, qsh, n, n_rows, n_q_heads);
-    if (st == PYR_OK) st = check_rows(h, q, q_out, dtype, osb, osn, osh, n, n_rows, n_q_heads);
+    if (!x->pos || x->idx || n_q_heads < 1) return PYR_ERR_INVALID;
+    st = check_rows(h, q, x->q_out, x->dtype, x->q_stride_b, x->q_stride_n, x->q_stride_h, n, n_rows, n_q_heads);
+    if (st == PYR_OK) st = check_rows(h, q, x->q_out, x->dtype, x->o_stride_b, x->o_stride_n, x->o_stride_h, n, n_rows, n_q_heads);
     if (st != PYR_OK) return st;
-    if (!rows_apart(h, osb, osn, osh, n, n_rows, n_q_heads)) return PYR_ERR_INVALID;
-    if (q == q_out && ((n > 1 && qsb != osb) || (n_rows > 1 && qsn != osn) || (n_q_heads > 1 && qsh != osh))) return PYR_ERR_INVALID;
+    if (!rows_apart(h, x->o_stride_b, x->o_stride_n, x->o_stride_h, n, n_rows, n_q_heads)) return PYR_ERR_INVALID;
+    if (q == x->q_out && ((n > 1 && x->q_stride_b != x->o_stride_b) || (n_rows > 1 && x->q_stride_n != x->o_stride_n) ||
+                          (n_q_heads > 1 && x->q_stride_h != x->o_stride_h)))
+      return PYR_ERR_INVALID;
   }
   if (!(h->cfg.flags & PYR_PAGES_8BIT) || n_rows > kMaxRows || !tiles_fit(h, n, n_rows)) return PYR_ERR_UNSUPPORTED;
-  // a launch has a CTA for each page and KV head and for some rows of queries
+  // a launch has CTAs for pages and KV heads, and another for query rows
   const int64_t rows = (int64_t)n * n_rows, tiles = ((int64_t)n_rows + 2 * pyr::kPageTile - 2) / pyr::kPageTile;
   if (q && rows > 0 && (n_q_heads > 65535 || n_q_heads > (0x7fffffff - tiles * n * h->cfg.n_kv_heads) / rows)) return PYR_ERR_UNSUPPORTED;
   PYR_PAGES_READY(h);
@@ -346,13 +347,13 @@ pyr_status_t pyr_pages_append(pyr_pages_t* h, const int32_t* lists, int32_t n, c
   pyr::PagesAppendArgs a;
   pyr::PagesWriteArgs& w = a.w;
   w.p = view(h);
-  w.lists = lists; w.n = n; w.first = first; w.k = k; w.v = v; w.sb = sb; w.sn = sn; w.sh = sh;
-  w.src_rows = src_rows; w.dtype = dtype; w.idx = idx; w.idx_groups = idx ? idx_groups : 1; w.idx_stride = idx_stride;
-  w.counts = counts; w.n_rows = n_rows;
+  w.lists = x->lists; w.n = n; w.first = x->first; w.k = x->k; w.v = x->v; w.sb = x->stride_b; w.sn = x->stride_n; w.sh = x->stride_h;
+  w.src_rows = x->src_rows; w.dtype = x->dtype; w.idx = x->idx; w.idx_groups = x->idx ? x->idx_groups : 1; w.idx_stride = x->idx_stride;
+  w.counts = x->counts; w.n_rows = n_rows;
   w.plan = at<int32_t>(h, h->lay.plan);
-  a.pos = pos; a.pos_stride = pos_stride; a.rope = rope; a.n_pos = n_pos;
-  a.q = q; a.q_out = q_out; a.Hq = n_q_heads;
-  a.qsb = qsb; a.qsn = qsn; a.qsh = qsh; a.osb = osb; a.osn = osn; a.osh = osh;
+  a.pos = x->pos; a.pos_stride = x->pos_stride; a.rope = x->rope; a.n_pos = x->n_pos;
+  a.q = q; a.q_out = x->q_out; a.Hq = n_q_heads;
+  a.qsb = x->q_stride_b; a.qsn = x->q_stride_n; a.qsh = x->q_stride_h; a.osb = x->o_stride_b; a.osn = x->o_stride_n; a.osh = x->o_stride_h;
   a.done = at<int32_t>(h, h->lay.moved);
   PYR_PAGES(pyr::launch_pages_append8(a, &launches, static_cast<cudaStream_t>(stream)));
 }

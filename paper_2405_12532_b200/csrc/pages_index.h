@@ -48,6 +48,8 @@ PYR_HD int pages_len(const PagesView& p, int l) {
   const int len = p.lens[l];
   return len < 0 ? 0 : (len > most ? (int)most : len);
 }
+// Pages that hold `rows` rows of a list (at most those of a table: the sum stays within 32 bits, whose division takes a tenth of 64's).
+PYR_HD int pages_for(const PagesView& p, int rows) { return (int)(((uint32_t)rows + (uint32_t)p.page_rows - 1u) / (uint32_t)p.page_rows); }
 // Byte offset in the pool of tile `tile` (of the page) of head h.
 PYR_HD size_t pages_tile(const PagesView& p, int page, int h, int tile) {
   return ((size_t)page * p.Hkv + h) * (size_t)pages_head_bytes(p) + p.head_extra + (size_t)tile * p.tile_bytes;
@@ -97,7 +99,7 @@ PYR_HD int tile8_v(int D, int r, int d) {
 
 // Shared memory in which the selection keeps a list's scores and a KV head's queries, and what it may take.
 constexpr int kSelect8Shared = 200 * 1024;
-inline int64_t pages_select8_shared(int64_t max_pages, int D, int64_t rep) { return (max_pages + 3) / 4 * 16 + rep * (2 * D + 4); }
+inline int64_t pages_select8_shared(int64_t max_pages, int D, int64_t rep) { return (max_pages + 3) / 4 * 16 + (rep + 7) / 8 * 8 * (2 * D + 4); }
 
 // How the attention's work is dealt out. A unit is one tile of one (entry, KV head, column group); an entry without rows
 // still has one tile per head, so that its zeros get written. Before its tiles each (entry, KV head, column group) has

@@ -665,15 +665,15 @@ __global__ void __launch_bounds__(kPageRows8 * 4, 1) append_pages_kernel(PagesAp
 
 // Queries beside rows that the kernel before has stored: 16 threads a row and kQueryHeads heads of it.
 template <class T, int D>
-__global__ void __launch_bounds__(256) turn_queries_kernel(PagesAppendArgs p, int64_t units) {
+__global__ void __launch_bounds__(256) turn_queries_kernel(PagesAppendArgs p, uint32_t units) {
   constexpr int W = D / 32;
-  const int64_t unit = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const uint32_t unit = blockIdx.x * 16u + (threadIdx.x >> 4);
   if (unit >= units) return;
   const PagesWriteArgs& a = p.w;
   const int groups = (p.Hq + kQueryHeads - 1) / kQueryHeads, d0 = W * (threadIdx.x & 15);
-  const int64_t at = unit / groups;
+  const uint32_t at = unit / (uint32_t)groups;
   const int h0 = (int)(unit - at * groups) * kQueryHeads;
-  const int e = (int)(at / a.n_rows), x = (int)(at - (int64_t)e * a.n_rows);
+  const int e = (int)(at / (uint32_t)a.n_rows), x = (int)(at - (uint32_t)e * a.n_rows);
   const int pos = x < (a.counts ? a.counts[e] : a.n_rows) ? position(p, e, 0, x) : -1;
   const T* q = static_cast<const T*>(p.q) + (int64_t)e * p.qsb + (int64_t)x * p.qsn + d0;
   T* out = static_cast<T*>(p.q_out) + (int64_t)e * p.osb + (int64_t)x * p.osn + d0;
@@ -705,14 +705,13 @@ __global__ void __launch_bounds__(256) turn_queries_kernel(PagesAppendArgs p, in
 // One warp per (entry, KV head, tile of its list): a lane takes 8 dimensions of a row of K, four dimensions of four rows of V, so that what
 // a warp stores at once lies together.
 template <class T, int D>
-__global__ void __launch_bounds__(kReadThreads) read8_kernel(PagesWriteArgs a, int blocks, int64_t items) {
+__global__ void __launch_bounds__(kReadThreads) read8_kernel(PagesWriteArgs a, int blocks, uint32_t items) {
   constexpr int P = D / 32, E = D / 8;
   const int lane = threadIdx.x & 31;
-  const int64_t item = (int64_t)blockIdx.x * (kReadThreads / 32) + (threadIdx.x >> 5);
+  const uint32_t item = blockIdx.x * (kReadThreads / 32u) + (threadIdx.x >> 5);
   if (item >= items) return;
-  const int blk = (int)(item % blocks);
-  const int h = (int)(item / blocks % a.p.Hkv);
-  const int e = (int)(item / blocks / a.p.Hkv);
+  const uint32_t eh = item / (uint32_t)blocks;
+  const int blk = (int)(item - eh * blocks), e = (int)(eh / (uint32_t)a.p.Hkv), h = (int)(eh - (uint32_t)e * a.p.Hkv);
   const int l = pages_list(a.p, a.lists, e);
   const int first = a.first ? a.first[e] : 0;
   const int cnt = a.counts ? a.counts[e] : a.n_rows;
@@ -792,13 +791,13 @@ struct RunPages {
   }
 };
 struct RunQueries {
-  const PagesAppendArgs& a; int64_t units; cudaStream_t s;
+  const PagesAppendArgs& a; uint32_t units; cudaStream_t s;
   template <class T, int D> cudaError_t run() {
     return launch_behind(turn_queries_kernel<T, D>, dim3((unsigned)((units + 15) / 16)), dim3(256), 0, s, a, units);
   }
 };
 struct RunRead {
-  const PagesWriteArgs& a; int blocks; int64_t items; unsigned grid; cudaStream_t s;
+  const PagesWriteArgs& a; int blocks; uint32_t items; unsigned grid; cudaStream_t s;
   template <class T, int D> cudaError_t run() {
     read8_kernel<T, D><<<grid, kReadThreads, 0, s>>>(a, blocks, items);
     return cudaGetLastError();
@@ -839,7 +838,7 @@ cudaError_t launch_pages_append8(const PagesAppendArgs& a, int* launches, cudaSt
   const int most = (int)(items / (4 * sms) < 1 ? 1 : items / (4 * sms) > 8 ? 8 : items / (4 * sms));
   const int chunks = (w.p.Hkv + most - 1) / most, heads = (w.p.Hkv + chunks - 1) / chunks;
   const int64_t grid = (int64_t)w.n * pages * ((w.p.Hkv + heads - 1) / heads);
-  if (grid > 0x7fffffffLL || units > 16 * 0x7fffffffLL) return cudaErrorInvalidValue;
+  if (grid > 0x7fffffffLL || units > 0x7fffffffLL) return cudaErrorInvalidValue;
   const bool self = w.n <= kSelfEntries;
   if (!self) {
     e = allow_shared<append_plan_kernel>(2 * (kMaxLists / 32) * 4);
@@ -853,7 +852,7 @@ cudaError_t launch_pages_append8(const PagesAppendArgs& a, int* launches, cudaSt
   if (e != cudaSuccess) return e;
   ++*launches;
   if (!a.q) return cudaSuccess;
-  e = by_format(w.p, w.dtype, RunQueries{a, units, s});
+  e = by_format(w.p, w.dtype, RunQueries{a, (uint32_t)units, s});
   if (e == cudaSuccess) ++*launches;
   return e;
 }
@@ -863,7 +862,7 @@ cudaError_t launch_pages_read8(const PagesWriteArgs& a, int* launches, cudaStrea
   const int64_t items = (int64_t)a.n * a.p.Hkv * blocks;
   const int64_t grid = (items + kReadThreads / 32 - 1) / (kReadThreads / 32);
   if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
-  const cudaError_t e = by_format(a.p, a.dtype, RunRead{a, blocks, items, (unsigned)grid, s});
+  const cudaError_t e = by_format(a.p, a.dtype, RunRead{a, blocks, (uint32_t)items, (unsigned)grid, s});
   if (e == cudaSuccess) ++*launches;
   return e;
 }

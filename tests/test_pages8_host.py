@@ -2,6 +2,7 @@
 share (csrc/pages_index.h, compiled for the host)."""
 import ctypes as C
 import os
+import re
 import shutil
 import subprocess
 
@@ -55,10 +56,32 @@ def test_bytes_and_view(D):
         _cfg(bits=5)
 
 
+class Append(C.Structure):
+    _fields_ = ([(x, C.c_void_p) for x in ("lists", "first", "k", "v")] + [(x, C.c_int64) for x in ("stride_b", "stride_n", "stride_h")] +
+                [("idx", C.c_void_p), ("idx_stride", C.c_int64), ("counts", C.c_void_p), ("pos", C.c_void_p), ("pos_stride", C.c_int64),
+                 ("rope", C.c_void_p), ("q", C.c_void_p), ("q_out", C.c_void_p)] +
+                [(x, C.c_int64) for x in ("q_stride_b", "q_stride_n", "q_stride_h", "o_stride_b", "o_stride_n", "o_stride_h")] +
+                [(x, C.c_int32) for x in ("n", "src_rows", "dtype", "idx_groups", "n_rows", "n_pos", "n_q_heads")])
+
+
 def _append(h, n=2, k=P, v=P, sb=5120, sn=512, sh=128, src=10, dtype=pb.PYR_BF16, pos=N, pstride=10, rope=P, n_pos=100, q=N, qo=N, qb=10240,
             qn=1024, qh=128, ob=10240, on=1024, oh=128, hq=8, idx=N, groups=1, istride=0, rows=10):
-    return pb.lib().pyr_pages_append(h, N, n, N, k, v, sb, sn, sh, src, dtype, pos, pstride, rope, n_pos, q, qo, qb, qn, qh, ob, on, oh, hq, idx,
-                                     groups, istride, N, rows, N)
+    x = Append(N, N, k, v, sb, sn, sh, idx, istride, N, pos, pstride, rope, q, qo, qb, qn, qh, ob, on, oh, n, src, dtype, groups, rows, n_pos, hq)
+    return pb.lib().pyr_pages_append(h, C.byref(x), N)
+
+
+def test_the_binding_packs_the_structure_of_the_header():
+    """Field by field: what the binding's packed bytes say, read through the structure."""
+    assert C.sizeof(Append) == (pb._APPEND.size + 7) // 8 * 8
+    values = list(range(1, len(Append._fields_) + 1))
+    x = Append.from_buffer_copy(pb._APPEND.pack(*values) + bytes(C.sizeof(Append) - pb._APPEND.size))
+    assert [getattr(x, f) for f, _ in Append._fields_] == values
+    with open(os.path.join(ROOT, "include", "pyr.h")) as f:
+        text = f.read()
+    body = text[text.index("const int32_t* lists;   /*"):text.index("} pyr_append_t;")]
+    body = re.sub(r"/\*.*?\*/", "", body, flags=re.S)
+    names = re.findall(r"(\w+)\s*[;,]", body)
+    assert names == [f for f, _ in Append._fields_]
 
 
 def test_append_arguments():
@@ -67,6 +90,7 @@ def test_append_arguments():
     Q = C.c_void_p(FAKE + (1 << 20))
     assert _append(h) == ORD and _append(h, pos=P) == ORD and _append(h, pos=P, q=P, qo=Q) == ORD and _append(h, pos=P, q=P, qo=P) == ORD
     assert _append(h, idx=P, groups=4, istride=40, rows=99) == ORD and _append(h, idx=P, pos=P) == ORD and _append(h, n=0, k=N, v=N) == ORD
+    assert pb.lib().pyr_pages_append(h, N, N) == NUL
     assert _append(None) == NUL and _append(h, k=N) == NUL and _append(h, pos=P, rope=N) == NUL
     assert _append(h, pos=P, q=P) == NUL and _append(h, pos=P, qo=P) == NUL
     assert _append(h, dtype=4) == UNS and _append(h4) == UNS and _append(h, idx=P, rows=(1 << 30) + 1) == UNS
@@ -93,8 +117,8 @@ def test_select_and_attn_blocks_arguments():
     assert select(ns=0, first=0, last=0) == INV and select(first=-1) == INV and select(last=2) == INV and select(last=0x7fffffff) == INV
     assert select(t=0) == INV and select(hq=6) == INV and select(n=6) == INV and select(qh=132) == INV
     assert select(n=1, t=1 << 28) == UNS
-    big = _handle(max_pages=51100)
-    assert select(h=big, hq=4) == ORD and select(h=big) == UNS                 # 4 * max_pages + rep * 260 bytes
+    big = _handle(max_pages=50500)                                             # 4 * max_pages + 260 bytes a head, in eights, of 204 800
+    assert select(h=big, hq=4) == ORD and select(h=big, hq=32, qb=4096) == ORD and select(h=big, hq=36, qb=8192) == UNS
     wide = _handle(max_pages=51200)
     assert select(h=wide, hq=4) == UNS
 
@@ -181,13 +205,13 @@ def test_codes_have_the_documented_places(index, D):
 def test_offsets_pass_32_bits(index):
     hb = o8.head_bytes(128, 128)
     assert index.tile_at(128, 40, 128, 600000, 39, 7) == (600000 * 40 + 39) * hb + 272 + 7 * 4112 > 1 << 32
-    assert index.shared8(51000, 128, 1) == 204260 and index.shared8(5, 64, 3) == 32 + 3 * 132
+    assert index.shared8(50500, 128, 1) == 204080 and index.shared8(5, 64, 9) == 32 + 16 * 132
 
 
 def test_binding_refuses_tensors_it_cannot_pass_on():
     """(Tensors of the CPU: nothing gets as far as the library.)"""
     p = object.__new__(pb.PyrPages)
-    p.cfg, p.device, p._index, p._heads, p._dim = _cfg(), torch.device("cpu"), -1, 4, 128
+    p.cfg, p.device, p._index, p._heads, p._dim, p._args = _cfg(), torch.device("cpu"), -1, 4, 128, bytearray(pb._APPEND.size)
     k = torch.zeros(2, 3, 4, 128, dtype=torch.bfloat16)
     pos, rope = torch.zeros(2, 1, 3, dtype=torch.int32), torch.zeros(5, 128)
     for bad in (dict(pos=pos[:, :, :2], rope=rope), dict(pos=pos, rope=rope.double()), dict(pos=pos, rope=rope[:, :64]), dict(pos=pos), dict(pos=pos.long(), rope=rope),
