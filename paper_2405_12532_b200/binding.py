@@ -6,6 +6,7 @@ the library has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import math
 import os
 import struct
@@ -473,6 +474,24 @@ _PAGES_DTYPES = {torch.bfloat16: PYR_BF16, torch.float32: PYR_F32}
 PYR_PAGES_8BIT = 8
 
 
+_CALL_PATH = os.path.join(_HERE, "_pages_call.so")
+_call = None
+
+
+def _calls():
+    """The compiled form of the calls that a decode step makes (csrc/pages_call.cpp), or False where it has not been built."""
+    global _call
+    if _call is None:
+        _call = False
+        if os.path.exists(_CALL_PATH):
+            spec = importlib.util.spec_from_file_location("_pages_call", _CALL_PATH)
+            module = importlib.util.module_from_spec(spec)
+            spec.loader.exec_module(module)
+            module.setup(*[C.cast(getattr(lib(), "pyr_pages_" + name), C.c_void_p).value for name in ("attn", "attn_blocks", "select", "append", "read")])
+            _call = module
+    return _call
+
+
 def make_pages_config(*, n_kv_heads, head_dim, n_pages, n_lists, max_pages, group=None, page_rows=64, flags=0, bits=4) -> PyrPagesConfig:
     """bits=8: one scale for a page and head, no `group`; bits=4: a scale for each row and `group` (64) dimensions."""
     if bits not in (4, 8):
@@ -521,9 +540,13 @@ class PyrPages:
         self.table = self._view(table.value, (c.n_lists, c.max_pages), torch.int32)
         self.lens = self._view(lens.value, (c.n_lists,), torch.int32)
         self.refs = self._view(refs.value, (c.n_pages,), torch.int32)
+        # what the compiled calls take first; they return None for what is not plainly right, which then goes through the checks below
+        calls = self.device.type == "cuda" and _calls()
+        self._call = calls.cache(self.handle.value, self._index, self._heads, self._dim) if calls else None
         self.reset()
 
     def close(self):
+        self._call = None
         if getattr(self, "handle", None):
             lib().pyr_pages_free(self.handle)
             self.handle = C.c_void_p()
@@ -550,6 +573,13 @@ class PyrPages:
                 st = self._fn[name](self.handle, *args, ptr)
         if st:
             _check(st, name)
+
+    def _result(self, r, name):
+        """What a compiled call gives back: a status (0: None), or its tensors."""
+        if type(r) is not int:
+            return r
+        if r:
+            _check(r, name)
 
     def _ids(self, t, n, what="lists"):
         """Pointer to an int32 vector of n entries on the cache's device, None for NULL."""
@@ -618,6 +648,10 @@ class PyrPages:
     def append(self, k, v, lists=None, first=None, pos=None, rope=None, q=None, q_out=None, idx=None, counts=None, stream=None):
         """write() into an 8-bit cache with keys turned by the positions pos (int32 [n, groups, rows], groups as in idx, 1 without) in the table
         rope (fp32 [positions, D], see glue_rope_table). With q [n, rows, Hq, D] also returns the turned queries (in q_out if given)."""
+        if stream is None and self._call is not None:
+            r = _call.append(self._call, k, v, lists, first, pos, rope, q, q_out, idx, counts)
+            if r is not None:
+                return self._result(r, "pyr_pages_append")
         if stream is not None:
             with torch.cuda.device(self._index), torch.cuda.stream(stream):    # what is allocated here is used on that stream
                 return self.append(k, v, lists, first, pos, rope, q, q_out, idx, counts)
@@ -660,12 +694,20 @@ class PyrPages:
 
     def read(self, k, v, lists=None, first=None, counts=None, stream=None):
         """Fills k, v [n, rows, Hkv, D] with the lists' rows from row first (0) on; rows a list does not have stay as they are."""
+        if stream is None and self._call is not None:
+            r = _call.read(self._call, k, v, lists, first, counts)
+            if r is not None:
+                return self._result(r, "pyr_pages_read")
         (n, rows, _, _), (sb, sn, sh, _), dtype = self._rows(k, v)
         self._run("pyr_pages_read", stream, self._ids(lists, n), n, self._ids(first, n, "first"), k.data_ptr(), v.data_ptr(), sb, sn,
                   sh, dtype, self._ids(counts, n, "counts"), rows)
 
     def attn(self, q, lists=None, out=None, lse=False, softmax_scale: float = 0.0, stream=None):
         """Attention of q [n, q_len, Hq, D] over the lists' rows: out like q, and with lse=True also lse [n, Hq, q_len] fp32."""
+        if stream is None and self._call is not None:
+            r = _call.attn(self._call, q, lists, None, out, lse, softmax_scale)
+            if r is not None:
+                return self._result(r, "pyr_pages_attn")
         if stream is not None:
             with torch.cuda.device(self._index), torch.cuda.stream(stream):    # what is allocated here is used on that stream
                 return self.attn(q, lists, out, lse, softmax_scale)
@@ -686,6 +728,10 @@ class PyrPages:
     def select(self, q, n_slots: int, lists=None, keep_first: int = 0, keep_last: int = 0, out=None, stream=None):
         """The page slots that each token and KV head of q [n, q_len, Hq, D] reads, by score: int32 [n, q_len, Hkv, n_slots], ascending, -1
         behind them; the first keep_first and last keep_last pages always (8-bit caches)."""
+        if stream is None and self._call is not None:
+            r = _call.select(self._call, q, n_slots, lists, keep_first, keep_last, out)
+            if r is not None:
+                return self._result(r, "pyr_pages_select")
         if stream is not None:
             with torch.cuda.device(self._index), torch.cuda.stream(stream):
                 return self.select(q, n_slots, lists, keep_first, keep_last, out)
@@ -705,6 +751,10 @@ class PyrPages:
 
     def attn_blocks(self, q, slots, lists=None, out=None, lse=False, softmax_scale: float = 0.0, stream=None):
         """attn() over the page slots int32 [n, q_len, Hkv, n_slots] of each token and KV head (8-bit caches)."""
+        if stream is None and self._call is not None and slots is not None:
+            r = _call.attn(self._call, q, lists, slots, out, lse, softmax_scale)
+            if r is not None:
+                return self._result(r, "pyr_pages_attn_blocks")
         if stream is not None:
             with torch.cuda.device(self._index), torch.cuda.stream(stream):
                 return self.attn_blocks(q, slots, lists, out, lse, softmax_scale)

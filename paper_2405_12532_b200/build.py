@@ -10,6 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpyr.so")
+CALL = os.path.join(HERE, "_pages_call.so")         # the paged cache's calls from Python (csrc/pages_call.cpp)
 SOURCES = ["pyr_host.cu", "prefill_simt.cu", "prefill_tc.cu", "attn_tc.cu", "select_compact.cu", "decode.cu", "decode_noalloc.cu", "gen_reselect.cu", "pages_host.cu", "pages_store.cu", "pages_ops.cu", "pages_attn.cu", "pages_store8.cu", "pages_attn8.cu", "pages_select8.cu", "glue.cu", "gemm_tc.cu", "gemm_skinny.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
@@ -22,10 +23,24 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found")
 
 
+def _call_command() -> list[str] | None:
+    """The compiler's command for CALL; None where torch has no CUDA parts to build against (binding.py does without it)."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    if torch.version.cuda is None:
+        return None
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-o", CALL, os.path.join(CSRC, "pages_call.cpp"), "-I", os.path.join(ROOT, "include"),
+             "-I", sysconfig.get_paths()["include"], f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
+            ["-I" + p for p in cpp_extension.include_paths(device_type="cuda")] + ["-L" + p for p in cpp_extension.library_paths(device_type="cuda")] +
+            ["-lc10", "-lc10_cuda", "-ltorch", "-ltorch_cpu", "-ltorch_python"])
+
+
 def needs_build() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALL):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALL))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "pyr.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -55,6 +70,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     os.makedirs(objdir, exist_ok=True)
     nvcc = _nvcc()
     procs = []
+    call = _call_command()
+    call = call and subprocess.Popen(call, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     for src in SOURCES:
         obj = os.path.join(objdir, src.replace(".cu", ".o"))
         cmd = [nvcc, *NVCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c",
@@ -77,6 +94,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}{r.stderr}")
+    if call:
+        out, _ = call.communicate()
+        if call.returncode != 0:
+            raise RuntimeError(f"g++ failed on pages_call.cpp:\n{out}")
     return LIB
 
 

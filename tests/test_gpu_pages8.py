@@ -497,6 +497,56 @@ def test_attention_splits_long_lists():
     assert p.status() == 0
 
 
+def _sampled(p, want_of, out, lse, q, lists, rep, T, dtype, at, H, pr, slots=None):
+    for i in at:
+        w = want_of(lists[i])
+        K, V = w.values()
+        seen = _dense(w.len, T, H, pr, None if slots is None else slots[i].cpu().numpy())
+        _compare(dtype, _np(out[i]), _np(lse[i]), o8.attention(_np(q[i]).astype(np.float64), K, V, seen, 1 / math.sqrt(q.shape[-1])))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_one_long_list_in_hundreds_of_pieces(dtype):
+    """A list of 60 001 rows: every head's states come from hundreds of ranges, and are merged in three rounds; one and nine query heads."""
+    H, D, pr, n = 8, 128, 128, 60001
+    p, want = _filled(H, D, pr, [n, 3], seed=81, spare=1)
+    for rep in (1, 9):
+        q = _rand(2, 1, H * rep, D, seed=82, dtype=dtype)
+        out, lse = p.attn(q, lse=True)
+        for _ in range(2):
+            again, lse2 = p.attn(q, lse=True)
+            assert torch.equal(out, again) and torch.equal(lse, lse2)              # bit-reproducible
+        _sampled(p, lambda l: want[l], out, lse, q, [0, 1], rep, 1, dtype, (0, 1), H, pr)
+    assert p.status() == 0
+
+
+def test_hundreds_of_ragged_lists():
+    """More work than warps by far, over lists from none to 1200 rows, one that does not exist among them; more entries than a CTA has threads, and
+    more than it has a table for; dense and over chosen pages."""
+    H, D, pr, rep, n = 8, 128, 64, 2, 300
+    lens = [(i * 7919) % 1201 if i % 13 else 0 for i in range(n)]
+    p, want = _filled(H, D, pr, lens, seed=83, spare=2)
+    sample = [0, 1, 13, 57, 100, 255, 256, 257, 299]
+    q = _rand(n, 2, H * rep, D, seed=84, dtype=BF)
+    out, lse = p.attn(q, lse=True)
+    _sampled(p, lambda l: want[l], out, lse, q, list(range(n)), rep, 2, BF, sample, H, pr)
+    slots = p.select(q, 6, keep_first=1, keep_last=1)
+    blocks, blse = p.attn_blocks(q, slots, lse=True)
+    _sampled(p, lambda l: want[l], blocks, blse, q, list(range(n)), rep, 2, BF, sample, H, pr, slots)
+    for i in sample:
+        np.testing.assert_array_equal(slots[i].cpu().numpy(), _slots_of(want[i], _np(q[i]), lens[i], pr, 6, 1, 1))
+    again, blse2 = p.attn_blocks(q, slots, lse=True)
+    assert torch.equal(blocks, again) and torch.equal(blse, blse2) and p.status() == 0
+    lists = [(i * 37) % n for i in range(1100)]
+    lists[500] = n + 5
+    many = _rand(1100, 1, H * rep, D, seed=85, dtype=BF)
+    for count in (900, 1100):
+        out = torch.full((count, 1, H * rep, D), 3.0, dtype=BF, device=DEV)
+        _, lse = p.attn(many[:count], _ids(*lists[:count]), out=out, lse=True)
+        assert p.status() == pb.PYR_ERR_INVALID and (out[500] == 3).all()
+        _sampled(p, lambda l: want[l], out, lse, many, lists, rep, 1, BF, [0, 1, 2, 499, 501, count - 1], H, pr)
+
+
 def test_pages_beyond_32_bits():
     """A pool of 5 GB: rows in its last pages are stored, read, selected and attended where they lie."""
     H, D, pr = 40, 128, 128
@@ -699,3 +749,46 @@ def test_calls_that_a_format_does_not_have():
     p8.append(k[:0], k[:0], _ids())
     p8.append(k[:, :0], k[:, :0], _ids(0))
     assert p8.status() == 0 and p8.lens.tolist() == [0, 0]
+
+
+def test_compiled_calls_and_the_binding_do_the_same():
+    """The same arguments through both: results, errors, outputs that are passed in, empty and odd tensors."""
+    H, D, pr = 2, 128, 16
+    rope = pb.glue_rope_table(300, D)
+    handles = [_filled(H, D, pr, [70, 5, 31], seed=91, spare=30)[0] for _ in range(2)]
+    handles[1]._call = None
+    assert handles[0]._call is not None
+    got = []
+    for p in handles:
+        r = []
+        k, v = _rand(3, 4, H, D, seed=1, dtype=BF), _rand(3, 4, H, D, seed=2, dtype=BF)
+        q = _rand(3, 4, 3 * H, D, seed=3, dtype=BF)
+        pos = (torch.arange(12, dtype=torch.int32, device=DEV) * 7).view(3, 1, 4)
+        idx = torch.tensor([[[3, 1]], [[0, 0]], [[2, 3]]], dtype=torch.int32, device=DEV)
+        r.append(p.append(k, v, _ids(2, 0, 1), pos=pos, rope=rope, q=q, counts=_ids(4, 3, 0)))
+        out = torch.zeros_like(q)
+        assert p.append(k, v, pos=pos, rope=rope, q=q, q_out=out) is out
+        r.append(out)
+        assert p.append(k, v, idx=idx, pos=pos[:, :, :2].contiguous(), rope=rope) is None
+        assert p.append(k[:, :1], v[:, :1], first=_ids(3, 3, 3)) is None
+        ko, vo = torch.zeros(3, 20, H, D, device=DEV), torch.zeros(3, 20, H, D, device=DEV)
+        assert p.read(ko, vo, _ids(1, 0, 2), first=_ids(0, 60, 10), counts=_ids(20, 19, 1)) is None
+        r += [ko, vo, *p.attn(q, lse=True), p.attn(q[:2], _ids(2, 1), out=out[:2], softmax_scale=1)]
+        s = p.select(q, 3, _ids(0, 1, 2), keep_first=1)
+        assert p.select(q, 3, out=s) is s
+        r += [s, *p.attn_blocks(q, s, lse=True), p.attn_blocks(q[:, :1], s[:, :1].contiguous()), p.attn(q[:0], _ids())]
+        for call in (lambda: p.attn(q, _ids(0)), lambda: p.attn(q.half()), lambda: p.attn(q, out=out.float()), lambda: p.select(q, 3, out=s[:1]),
+                     lambda: p.attn_blocks(q, s.long()), lambda: p.append(k, v, pos=pos), lambda: p.append(k, v.float()), lambda: p.read(ko, vo[:, :3])):
+            with pytest.raises(ValueError):
+                call()
+        for call in (lambda: p.attn(q[:, :, :3]), lambda: p.attn(q, softmax_scale=-1.0), lambda: p.select(q, 2, keep_first=1, keep_last=2), lambda: p.select(q, 0),
+                     lambda: p.append(k.repeat(2, 1, 1, 1), v.repeat(2, 1, 1, 1)), lambda: p.read(ko[:, :1].expand(-1, 20, -1, -1), vo[:, :1].expand(-1, 20, -1, -1))):
+            with pytest.raises(pb.PyrError):
+                call()
+        assert p.status() == 0
+        got.append(r + [p.lens.clone()])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    p = handles[0]
+    p.close()
+    with pytest.raises(pb.PyrError):
+        p.attn(_rand(3, 1, H, D, seed=1, dtype=BF))

@@ -212,6 +212,7 @@ def test_binding_refuses_tensors_it_cannot_pass_on():
     """(Tensors of the CPU: nothing gets as far as the library.)"""
     p = object.__new__(pb.PyrPages)
     p.cfg, p.device, p._index, p._heads, p._dim, p._args = _cfg(), torch.device("cpu"), -1, 4, 128, bytearray(pb._APPEND.size)
+    p._call = None
     k = torch.zeros(2, 3, 4, 128, dtype=torch.bfloat16)
     pos, rope = torch.zeros(2, 1, 3, dtype=torch.int32), torch.zeros(5, 128)
     for bad in (dict(pos=pos[:, :, :2], rope=rope), dict(pos=pos, rope=rope.double()), dict(pos=pos, rope=rope[:, :64]), dict(pos=pos), dict(pos=pos.long(), rope=rope),
@@ -226,3 +227,25 @@ def test_binding_refuses_tensors_it_cannot_pass_on():
             p.attn_blocks(q, bad)
     with pytest.raises(ValueError):
         p.select(q, 4, out=slots)
+
+
+def test_compiled_calls_leave_what_is_not_plainly_right_to_the_binding():
+    """(Tensors of the CPU are none of theirs.) They load, and return None."""
+    calls = pb._calls()
+    if not calls:
+        assert torch.version.cuda is None
+        return
+    before = pb.launch_count()
+    c = calls.cache(FAKE, 0, 4, 128)
+    k, q = torch.zeros(2, 3, 4, 128), torch.zeros(2, 1, 8, 128)
+    ids, slots = torch.zeros(2, dtype=torch.int32), torch.zeros(2, 1, 4, 3, dtype=torch.int32)
+    assert calls.attn(c, q, ids, None, None, True, 0.0) is None and calls.attn(c, q, None, slots, None, False, 0.0) is None
+    assert calls.attn(c, q, None, None, None, False, "x") is None and calls.attn(c, 5, None, None, None, False, 0.0) is None
+    assert calls.select(c, q, 4, None, 0, 1, None) is None and calls.select(c, q, 0, None, 0, 0, None) is None and calls.select(c, q, 1 << 70, None, 0, 0, None) is None
+    assert calls.append(c, k, k, ids, None, None, None, None, None, None, None) is None and calls.read(c, k, k, None, None, None) is None
+    for bad in (lambda: calls.attn(c, q), lambda: calls.read(c), lambda: calls.setup(1), lambda: calls.cache(1)):
+        with pytest.raises(TypeError):
+            bad()
+    with pytest.raises(ValueError):
+        calls.read(5, k, k, None, None, None)
+    assert pb.launch_count() == before
