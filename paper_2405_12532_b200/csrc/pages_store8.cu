@@ -44,6 +44,21 @@ __device__ __forceinline__ float max_of(float a, float b, float c) {
   return r;
 }
 
+// Two numbers at once, each rounded as alone. A sum is a product with `one` = 1 (or -1), which the kernel gets as an argument: packed
+// products and sums are otherwise contracted when they are assembled (measured: rounded once), and so are products with a constant 1.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmul.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b, float one) {        // a + one b
+  float2 r;
+  asm("{\n.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 w, {%6, %6};\nfma.rn.f32x2 z, y, w, x;\nmov.b64 {%0, %1}, z;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(one));
+  return r;
+}
+
 // N elements of a row (2 or 4) as they are loaded, and as numbers.
 template <class T, int N> struct Some;
 template <int N> struct Some<float, N> {
@@ -57,6 +72,7 @@ template <int N> struct Some<float, N> {
     for (int k = 0; k < N; ++k) x[k] = v;
   }
   __device__ __forceinline__ float at(int k) const { return x[k]; }
+  __device__ __forceinline__ float2 two(int k) const { return make_float2(x[2 * k], x[2 * k + 1]); }
   // the bits of the largest magnitude so far (Inf and NaN in the order of their bits)
   __device__ __forceinline__ void most(uint32_t* bits) const {
     float m = __uint_as_float(*bits);
@@ -78,6 +94,7 @@ template <int N> struct Some<__nv_bfloat16, N> {
     for (int k = 0; k < N / 2; ++k) w[k] = b | b << 16;
   }
   __device__ __forceinline__ float at(int k) const { return __uint_as_float(k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16); }
+  __device__ __forceinline__ float2 two(int k) const { return make_float2(at(2 * k), at(2 * k + 1)); }
   // (two at a time, until finish())
   __device__ __forceinline__ void most(uint32_t* bits) const {
     if constexpr (N == 4) *bits = __vimax3_u16x2(*bits, w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu);
@@ -129,13 +146,19 @@ __device__ __forceinline__ Scale scale_of(float amax, float before) {
   if (want < kScaleMin) want = 0.f;
   r.s = amax <= 3.402823466e38f && before == before ? fmaxf(before, want) : nan_f();
   const bool some = r.s > 0.f;                   // (not so for NaN: every code 0)
-  r.factor = some ? __fdiv_rn(before, r.s) : 0.f;
+  r.factor = some && before > 0.f ? __fdiv_rn(before, r.s) : 0.f;
   r.inverse = some ? __fdiv_rn(1.f, r.s) : 0.f;
   return r;
 }
 // A code's stored byte in the low byte, from its number times 1 / step; the sums are monotone in the number.
 __device__ __forceinline__ float code_sum(float x, float by) { return __fadd_rn(__fmul_rn(x, by), kRound); }
+__device__ __forceinline__ float2 code_sums(float2 x, float by, float one) {
+  return add2(make_float2(kRound, kRound), mul2(x, make_float2(by, by)), one);
+}
 __device__ __forceinline__ int code_int(float sum) { return (int)(__float_as_uint(sum) - 0x4B400080u); }
+// Two codes' stored bytes as 16-bit halves, from their sums; four bytes from two of those.
+__device__ __forceinline__ uint32_t halves2(float2 c) { return __byte_perm(__float_as_uint(c.x), __float_as_uint(c.y), 0x5410); }
+__device__ __forceinline__ uint32_t bytes_of(uint32_t lo, uint32_t hi) { return __byte_perm(lo, hi, 0x6420); }
 // Four stored bytes (code + 128) brought to another scale.
 __device__ __forceinline__ uint32_t recode4(uint32_t w, float factor) {
   uint32_t r = 0;
@@ -378,12 +401,12 @@ template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatil
 // the half warps) are bytes 0, 2, 1 and 3 of its words. Rows come through shared memory, with two `stages` those of the next two heads
 // while one is worked on. `pages` cover n_rows rows wherever in a page they begin.
 template <class T, int D, bool kSelf>
-__global__ void __launch_bounds__(kPageRows8 * 4, 1) append_pages_kernel(PagesAppendArgs p, int pages, int heads, int stages) {
+__global__ void __launch_bounds__(kPageRows8 * 4, 1) append_pages_kernel(PagesAppendArgs p, int pages, int heads, int stages, float one) {
   constexpr int W = D / 32;
   using Part = Some<T, W>;
   extern __shared__ __align__(16) uint8_t shared[];         // [stages][warps][16 parts: K's 4 rows x 2 halves, V's][lanes]
-  __shared__ uint2 top[kPageRows8 / 8];
-  __shared__ uint32_t ends[kPageRows8 / 8][2][D / 2];       // extrema's bytes as 16-bit halves
+  __shared__ uint2 top[kPageRows8 / 8];                     // of warps: largest magnitudes
+  __shared__ __align__(16) uint32_t ends[kPageRows8 / 4][2][D / 2];     // of half warps: extrema of their codes, bytes as 16-bit halves
   const PagesWriteArgs& a = p.w;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, half = lane >> 4, d0 = W * (lane & 15), pr = a.p.page_rows;
   const int chunks = (a.p.Hkv + heads - 1) / heads, per_entry = pages * chunks;
@@ -493,22 +516,35 @@ __global__ void __launch_bounds__(kPageRows8 * 4, 1) append_pages_kernel(PagesAp
   uint8_t* head = head_of(a.p, page, h0);
   const int head_bytes = pages_head_bytes(a.p), tile_at = a.p.head_extra + (warp >> 1) * a.p.tile_bytes;
   int from = 0;                                   // the stage that is worked on
+  const int warps = 2 * a.p.tiles_per_page;
+  float2 old = make_float2(0.f, 0.f);             // scales of rows that stay
+  if (held) old = *reinterpret_cast<const float2*>(head + 2 * D);
 #pragma unroll 1
   for (int h = h0; h < h1; ++h, head += head_bytes, from = stages > 1 ? stage_parts - from : 0) {
     const Part* part_of = mine + from;            // K: row q's halves at 64 q, 64 q + 32; V's 256 behind
-    const float2 old = *reinterpret_cast<const float2*>(head + 2 * D);
+    const float before_k = old.x, before_v = old.y;
+    if (held && h + 1 < h1) old = *reinterpret_cast<const float2*>(head + head_bytes + 2 * D);
     if (!same) look_up(h + stages);
     if (stages > 1) copies_wait<1>(); else copies_wait<0>();
-    float k[4][2 * W], mk = 0.f;
+    float2 k[4][W];                               // two dimensions each: those of the first half, those of the second
+    float mk = 0.f;
     uint32_t mv = 0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const Part lo = part_of[64 * q], hi = part_of[64 * q + 32];
 #pragma unroll
-      for (int i = 0; i < W; ++i) { k[q][i] = lo.at(i); k[q][W + i] = hi.at(i); }
-      if (p.pos) turn<W>(k[q], k[q] + W, rope[q][0], rope[q][1]);      // (nothing and NaN stay what they are)
-#pragma unroll
-      for (int i = 0; i < W; ++i) mk = most_of(mk, k[q][i], k[q][W + i]);
+      for (int i = 0; i < W / 2; ++i) {
+        float2 x = lo.two(i), y = hi.two(i);
+        if (p.pos) {                              // (nothing and NaN stay what they are)
+          const float2 c = rope[q][0].two(i), s = rope[q][1].two(i), x0 = x;
+          x = add2(mul2(x, c), mul2(y, s), -one);
+          y = add2(mul2(y, c), mul2(x0, s), one);
+        }
+        k[q][i] = x;
+        k[q][W / 2 + i] = y;
+        mk = most_of(mk, x.x, x.y);
+        mk = most_of(mk, y.x, y.y);
+      }
       part_of[64 * q + 256].most(&mv);
       part_of[64 * q + 288].most(&mv);
     }
@@ -518,12 +554,10 @@ __global__ void __launch_bounds__(kPageRows8 * 4, 1) append_pages_kernel(PagesAp
     const uint32_t bv = __reduce_max_sync(0xffffffffu, Some<T, W>::finish(mv));
     if (lane == 0) top[warp] = make_uint2(bk, bv);
     __syncthreads();                              // (the old scales are read, too)
-    const int warps = 2 * a.p.tiles_per_page;
     uint2 all = make_uint2(0, 0);
     if (lane < warps) all = top[lane];
     all.x = __reduce_max_sync(0xffffffffu, all.x);
     all.y = __reduce_max_sync(0xffffffffu, all.y);
-    const float before_k = held ? old.x : 0.f, before_v = held ? old.y : 0.f;
     // (even lanes K's, odd lanes V's)
     const Scale mine = scale_of(__uint_as_float(lane & 1 ? all.y : all.x), lane & 1 ? before_v : before_k);
     const Scale sk{__shfl_sync(0xffffffffu, mine.s, 0), __shfl_sync(0xffffffffu, mine.factor, 0), __shfl_sync(0xffffffffu, mine.inverse, 0)};
@@ -531,36 +565,43 @@ __global__ void __launch_bounds__(kPageRows8 * 4, 1) append_pages_kernel(PagesAp
 
     // ---- codes
     uint8_t* tile = head + tile_at;
-    float lo[2 * W], hi[2 * W];
+    uint32_t lo2[W], hi2[W];                      // extrema of the codes' bytes, two dimensions to a word
 #pragma unroll
-    for (int i = 0; i < 2 * W; ++i) { lo[i] = kRound + 127.f; hi[i] = kRound - 127.f; }
+    for (int i = 0; i < W; ++i) { lo2[i] = 0x00ff00ffu; hi2[i] = 0; }
     if (news == 0xffffu && sk.s == sk.s && sv.s == sv.s) {
       // a whole tile of new rows (rows of K two by two: their halves lie the other way round in odd rows, with 128 dimensions)
       uint8_t* kat = tile + 2 * j * D + d0;
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+          uint32_t c[2][W / 2];
+#pragma unroll
+          for (int i = 0; i < W / 2; ++i) {
+            const int x = g * (W / 2) + i;
+            c[0][i] = halves2(code_sums(k[q][x], sk.inverse, one));
+            c[1][i] = halves2(code_sums(k[q + 1][x], sk.inverse, one));
+            lo2[x] = __vimin3_u16x2(lo2[x], c[0][i], c[1][i]);
+            hi2[x] = __vimax3_u16x2(hi2[x], c[0][i], c[1][i]);
+          }
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            uint8_t* at = kat + y * D + (q >> 1) * (8 * D) + (D / 2) * (D == 128 ? g ^ y : g);
+            if constexpr (W == 4) *reinterpret_cast<uint32_t*>(at) = bytes_of(c[y][0], c[y][1]);
+            else *reinterpret_cast<uint16_t*>(at) = (uint16_t)bytes_of(c[y][0], 0u);
+          }
+        }
         uint32_t* vat = reinterpret_cast<uint32_t*>(tile + tile8_v(D, 2 * j, g * (D / 2) + d0));
         uint32_t w[W];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float c[W];
-#pragma unroll
-          for (int i = 0; i < W; ++i) c[i] = k[q][g * W + i] = code_sum(k[q][g * W + i], sk.inverse);
-          uint8_t* at = kat + (q & 1) * D + (q >> 1) * (8 * D) + (D / 2) * (D == 128 ? g ^ (q & 1) : g);
-          if constexpr (W == 4) *reinterpret_cast<uint32_t*>(at) = bytes4(c[0], c[1], c[2], c[3]);
-          else *reinterpret_cast<uint16_t*>(at) = (uint16_t)__byte_perm(__float_as_uint(c[0]), __float_as_uint(c[1]), 0x0040);
-        }
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          const int x = g * W + i;
-          lo[x] = min_of(min_of(k[0][x], k[1][x], k[2][x]), k[3][x], k[3][x]);
-          hi[x] = max_of(max_of(k[0][x], k[1][x], k[2][x]), k[3][x], k[3][x]);
-        }
         const Part v[4] = {part_of[256 + 32 * g], part_of[320 + 32 * g], part_of[384 + 32 * g], part_of[448 + 32 * g]};
 #pragma unroll
-        for (int i = 0; i < W; ++i)
-          w[i] = bytes4(code_sum(v[0].at(i), sv.inverse), code_sum(v[2].at(i), sv.inverse), code_sum(v[1].at(i), sv.inverse),
-                        code_sum(v[3].at(i), sv.inverse));
+        for (int i = 0; i < W / 2; ++i) {
+          float2 c[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) c[q] = code_sums(v[q].two(i), sv.inverse, one);
+          w[2 * i] = bytes4(c[0].x, c[2].x, c[1].x, c[3].x);
+          w[2 * i + 1] = bytes4(c[0].y, c[2].y, c[1].y, c[3].y);
+        }
         if constexpr (W == 4) *reinterpret_cast<uint4*>(vat) = make_uint4(w[0], w[1], w[2], w[3]);
         else *reinterpret_cast<uint2*>(vat) = make_uint2(w[0], w[1]);
       }
@@ -574,18 +615,19 @@ __global__ void __launch_bounds__(kPageRows8 * 4, 1) append_pages_kernel(PagesAp
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             uint8_t* at = tile + tile8_k(D, r, g * (D / 2) + d0);
-            float c[W];
+            uint32_t c[W / 2];
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
-              c[i] = fine_k ? code_sum(k[q][g * W + i], sk.inverse) : kRound;
-              if (fresh) { lo[g * W + i] = fminf(lo[g * W + i], c[i]); hi[g * W + i] = fmaxf(hi[g * W + i], c[i]); }
+            for (int i = 0; i < W / 2; ++i) {
+              const int x = g * (W / 2) + i;
+              c[i] = fine_k ? halves2(code_sums(k[q][x], sk.inverse, one)) : 0x00800080u;
+              if (fresh) { lo2[x] = __vminu2(lo2[x], c[i]); hi2[x] = __vmaxu2(hi2[x], c[i]); }
             }
             if constexpr (W == 4) {
-              uint32_t w = bytes4(c[0], c[1], c[2], c[3]);
+              uint32_t w = bytes_of(c[0], c[1]);
               if (stay) w = recode4(*reinterpret_cast<const uint32_t*>(at), sk.factor);
               *reinterpret_cast<uint32_t*>(at) = w;
             } else {
-              uint32_t w = __byte_perm(__float_as_uint(c[0]), __float_as_uint(c[1]), 0x0040);
+              uint32_t w = bytes_of(c[0], 0u);
               if (stay) w = recode4(*reinterpret_cast<const uint16_t*>(at), sk.factor);
               *reinterpret_cast<uint16_t*>(at) = (uint16_t)w;
             }
@@ -626,38 +668,36 @@ __global__ void __launch_bounds__(kPageRows8 * 4, 1) append_pages_kernel(PagesAp
     }
     copies_commit();
 
-    // ---- extrema of the codes, two dimensions to a word: of the half warps, of the warps
-    uint32_t lo2[W], hi2[W];
+    // ---- extrema of the half warps' codes
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-      lo2[i] = __byte_perm(__float_as_uint(lo[2 * i]), __float_as_uint(lo[2 * i + 1]), 0x5410);
-      hi2[i] = __byte_perm(__float_as_uint(hi[2 * i]), __float_as_uint(hi[2 * i + 1]), 0x5410);
-      lo2[i] = __vminu2(lo2[i], __shfl_xor_sync(0xffffffffu, lo2[i], 16));
-      hi2[i] = __vmaxu2(hi2[i], __shfl_xor_sync(0xffffffffu, hi2[i], 16));
+    for (int g = 0; g < 2; ++g) {
+      const int x = g * (W / 2);
+      uint32_t* at = &ends[2 * warp + half][0][(g * (D / 2) + d0) / 2];
+      if constexpr (W == 4) {
+        *reinterpret_cast<uint2*>(at) = make_uint2(lo2[x], lo2[x + 1]);
+        *reinterpret_cast<uint2*>(at + D / 2) = make_uint2(hi2[x], hi2[x + 1]);
+      } else {
+        at[0] = lo2[x];
+        at[D / 2] = hi2[x];
+      }
     }
-    if (half == 0)
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const int at = (i / (W / 2) * (D / 2) + d0) / 2 + i % (W / 2);
-        ends[warp][0][at] = lo2[i];
-        ends[warp][1][at] = hi2[i];
-      }
     __syncthreads();
-    int8_t* kept_ends = reinterpret_cast<int8_t*>(head);
-    for (int x = t; x < D / 2; x += blockDim.x) {
-      uint32_t least = 0x00ff00ffu, most = 0;
-      for (int w = 0; w < warps; ++w) { least = __vminu2(least, ends[w][0][x]); most = __vmaxu2(most, ends[w][1][x]); }
+    for (int x = t; x < D; x += blockDim.x) {     // two dimensions' least codes, then their largest
+      const bool largest = x >= D / 2;
+      const uint32_t flip = largest ? 0x00ff00ffu : 0u;
+      const uint32_t* at = &ends[0][0][x];
+      uint32_t least = 0x00ff00ffu;
+      for (int w = 0; w < 2 * warps; w += 2) least = __vimin3_u16x2(least, at[w * D] ^ flip, at[w * D + D] ^ flip);
+      least ^= flip;
+      int c[2] = {(int)(least & 255u) - 128, (int)(least >> 16 & 255u) - 128};
+      char2* kept_ends = reinterpret_cast<char2*>(head) + x;
+      if (held) {
+        const char2 was = *kept_ends;
+        const int o[2] = {code_int(code_sum((float)was.x, sk.factor)), code_int(code_sum((float)was.y, sk.factor))};
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const int d = 2 * x + y;
-        int l = (int)(least >> (16 * y) & 255u) - 128, m = (int)(most >> (16 * y) & 255u) - 128;
-        if (held) {
-          l = min(l, code_int(code_sum((float)kept_ends[d], sk.factor)));
-          m = max(m, code_int(code_sum((float)kept_ends[D + d], sk.factor)));
-        }
-        kept_ends[d] = (int8_t)l;
-        kept_ends[D + d] = (int8_t)m;
+        for (int y = 0; y < 2; ++y) c[y] = largest ? max(c[y], o[y]) : min(c[y], o[y]);
       }
+      *kept_ends = make_char2((signed char)c[0], (signed char)c[1]);
     }
     if (t == 0) *reinterpret_cast<float2*>(head + 2 * D) = make_float2(sk.s, sv.s);
   }
@@ -785,8 +825,8 @@ struct RunPages {
     const int threads = 4 * a.w.p.page_rows, stage = threads * 16 * (int)sizeof(Some<T, D / 32>), stages = heads > 1 && 2 * stage <= kStageBytes ? 2 : 1;
     cudaError_t e = self ? allow_shared<append_pages_kernel<T, D, true>>(kStageBytes) : allow_shared<append_pages_kernel<T, D, false>>(kStageBytes);
     if (e != cudaSuccess) return e;
-    if (!self) return launch_behind(append_pages_kernel<T, D, false>, dim3(grid), dim3(threads), stages * stage, s, a, pages, heads, stages);
-    append_pages_kernel<T, D, true><<<grid, threads, stages * stage, s>>>(a, pages, heads, stages);
+    if (!self) return launch_behind(append_pages_kernel<T, D, false>, dim3(grid), dim3(threads), stages * stage, s, a, pages, heads, stages, 1.f);
+    append_pages_kernel<T, D, true><<<grid, threads, stages * stage, s>>>(a, pages, heads, stages, 1.f);
     return cudaGetLastError();
   }
 };
