@@ -526,8 +526,6 @@ class PyrPages:
         self.device = self.buf.device
         self._index, self._heads, self._dim = self.device.index, self.cfg.n_kv_heads, self.cfg.head_dim
         self._fn = {name: getattr(lib(), name) for name in EXPORTS if name.startswith("pyr_pages_")}
-        self._args = bytearray(_APPEND.size)
-        self._args_at = C.addressof(C.c_char.from_buffer(self._args))
         off = (-self.buf.data_ptr()) % align
         self.handle = C.c_void_p()
         _check(lib().pyr_pages_alloc(C.byref(self.cfg), C.c_void_p(self.buf.data_ptr() + off), nbytes, C.byref(self.handle)),
@@ -685,11 +683,11 @@ class PyrPages:
             qp, op = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             raise ValueError("q_out: only with q")
-        args = self._args                        # (one structure: thirty arguments one by one take ctypes longer than all of the above)
-        _APPEND.pack_into(args, 0, self._ids(lists, n) or 0, self._ids(first, n, "first") or 0, k.data_ptr(), v.data_ptr(), sb, sn, sh, ip or 0,
+        # (one structure: thirty arguments one by one take ctypes longer than all of the above)
+        args = _APPEND.pack(self._ids(lists, n) or 0, self._ids(first, n, "first") or 0, k.data_ptr(), v.data_ptr(), sb, sn, sh, ip or 0,
                           istride, self._ids(counts, n, "counts") or 0, pp or 0, pstride, rp, qp, op, qb, qn, qh, ob, on, oh, n, src, dtype,
                           groups, rows, n_pos, hq)
-        self._run("pyr_pages_append", None, self._args_at)
+        self._run("pyr_pages_append", None, args)
         return q_out
 
     def read(self, k, v, lists=None, first=None, counts=None, stream=None):

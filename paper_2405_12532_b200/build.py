@@ -38,9 +38,9 @@ def _call_command() -> list[str] | None:
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(CALL):
+    if not os.path.exists(LIB) or (not os.path.exists(CALL) and _call_command()):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(CALL))
+    t = min(os.path.getmtime(f) for f in (LIB, CALL) if os.path.exists(f))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "pyr.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 

@@ -129,7 +129,8 @@ PyObject* attn(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     }
     const at::Tensor* out = result_of(args[4], *q.t, &mine);
     if (!out || !rows_of(*out, *c, &o) || out->sizes() != q.t->sizes() || o.dtype != q.dtype) Py_RETURN_NONE;
-    const bool stats = PyObject_IsTrue(args[5]) == 1;
+    const int stats = PyObject_IsTrue(args[5]);
+    if (stats < 0) { PyErr_Clear(); Py_RETURN_NONE; }
     if (stats) lse = at::empty({q.n, q.heads, q.rows}, q.t->options().dtype(at::kFloat));
     float* const l = stats ? static_cast<float*>(lse.data_ptr()) : nullptr;
     const pyr_status_t st =

@@ -792,3 +792,58 @@ def test_compiled_calls_and_the_binding_do_the_same():
     p.close()
     with pytest.raises(pb.PyrError):
         p.attn(_rand(3, 1, H, D, seed=1, dtype=BF))
+
+
+@pytest.mark.parametrize("rows", [1, 19])
+def test_more_entries_than_decide_for_themselves(rows):
+    """640 ragged lists in one call, twice (the second in pages that hold rows already), queries beside them; a list twice and one that does not
+    exist among them."""
+    H, D, pr, hq, n, n_lists = 3, 64, 16, 5, 640, 700
+    p = _pages(H, D, pr, 3 * n_lists, n_lists, 3)
+    rope = pb.glue_rope_table(400, D)
+    lists = [(i * 31) % n_lists for i in range(n)]
+    lists[600] = lists[7]
+    lists[77] = n_lists
+    bad = {7, 600, 77}
+    counts = [(i * 5) % (rows + 1) if i % 9 else rows for i in range(n)]
+    p.reserve(torch.arange(n_lists, dtype=torch.int32, device=DEV), 40)
+    assert p.status() == 0
+    sample = [0, 1, 6, 76, 78, 333, 511, 512, 513, 599, 601, 639]
+    want = {i: o8.List8(H, D, pr, 48) for i in sample}
+    lens = [0] * n_lists
+    for step in range(2):
+        k, v = _rand(n, rows, H, D, seed=5 * step, dtype=BF, scale=1 + 3 * step), _rand(n, rows, H, D, seed=5 * step + 1, dtype=BF, scale=3 - 2 * step)
+        q = _rand(n, rows, hq, D, seed=5 * step + 2, dtype=BF)
+        pos = (torch.arange(n * rows, dtype=torch.int32, device=DEV) % 399 + step).view(n, 1, rows)
+        out = p.append(k, v, _ids(*lists), pos=pos, rope=rope, q=q, counts=_ids(*counts))
+        assert p.status() == pb.PYR_ERR_INVALID
+        turned = torch.from_numpy(o8.rotate(_np(q), _np(rope)[pos.cpu().numpy()[:, 0]][:, :, None])).to(BF).float().numpy()
+        for i in range(n):
+            c = 0 if i in bad else counts[i]
+            turned[i, c:] = _np(q[i, c:])
+            if i not in bad:
+                lens[lists[i]] += c
+        np.testing.assert_array_equal(_np(out), turned)
+        assert p.lens.tolist() == lens
+        for i, w in want.items():
+            c = counts[i]
+            if c:
+                w.store(w.len, o8.rotate(_np(k[i, :c]), _np(rope)[pos[i, 0, :c].cpu().numpy()][:, None]), _np(v[i, :c]))
+                _check(p, lists[i], w)
+
+
+def test_calls_under_inference_mode_and_beside_gradients():
+    """A call asks for no gradient, whatever its tensors say, and gives the same in every mode."""
+    H, D, pr = 2, 128, 16
+    p, _ = _filled(H, D, pr, [100, 3], seed=95)
+    q = _rand(2, 2, 4 * H, D, seed=96, dtype=BF)
+    slots = p.select(q, 2)
+    want = [*p.attn(q, lse=True), *p.attn_blocks(q, slots, lse=True), slots]
+    leaf = q.clone().requires_grad_()
+    got = [*p.attn(leaf, lse=True), *p.attn_blocks(leaf, p.select(leaf, 2), lse=True), p.select(leaf, 2)]
+    assert not any(t.requires_grad for t in got) and all(torch.equal(a, b) for a, b in zip(got, want))
+    with torch.inference_mode():
+        got = [*p.attn(q, lse=1), *p.attn_blocks(q, p.select(q, 2), lse=True), p.select(q, 2)]
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    with pytest.raises(RuntimeError):
+        p.attn(q, lse=torch.zeros(2))                          # neither true nor false
