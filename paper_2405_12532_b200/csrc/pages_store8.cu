@@ -15,7 +15,7 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kOneWarps = 8;                     // of a CTA that stores an entry's one row, a warp a head
 constexpr int kReadThreads = 64;
-constexpr int kSelfEntries = 512;                // up to this many entries each CTA decides for itself, and a call of many rows is one launch
+constexpr int kSelfEntries = 256;                // up to this many entries each CTA may decide for itself, and a call of many rows is one launch
 constexpr int kQueryHeads = 4;                   // heads of a query row that a thread turns
 constexpr float kScaleMin = 7.888609052210118e-31f;   // 2^-100
 constexpr float kRound = 12583040.f;             // 1.5 2^23 + 128: added, it rounds to the nearest integer (ties to even) and leaves it, plus 128, in the low bits
@@ -348,7 +348,8 @@ __global__ void __launch_bounds__(kOneWarps * 32) append_one_kernel(PagesAppendA
 }
 
 // ------------------------------------------------------------------ many rows
-// Decides every entry before any row moves: plan[2 i] = first row (-1: refused), plan[2 i + 1] = the length before. A warp per entry.
+// Decides every entry before any row moves: plan[2 i] = first row (-1: refused), plan[2 i + 1] = the length before. A warp per entry;
+// every CTA goes through all of the call's lists for those that are named twice.
 __global__ void __launch_bounds__(kPlanThreads) append_plan_kernel(PagesWriteArgs a, int words) {
   extern __shared__ uint32_t seen[];              // two bits per list: met, met twice
   let_next_start();
@@ -361,7 +362,7 @@ __global__ void __launch_bounds__(kPlanThreads) append_plan_kernel(PagesWriteArg
     if (l >= 0 && (atomicOr(&seen[l >> 5], 1u << (l & 31)) >> (l & 31) & 1u)) atomicOr(&twice[l >> 5], 1u << (l & 31));
   }
   __syncthreads();
-  for (int i = t >> 5; i < a.n; i += kPlanThreads / 32) {
+  for (int i = blockIdx.x * (kPlanThreads / 32) + (t >> 5); i < a.n; i += gridDim.x * (kPlanThreads / 32)) {
     const int l = pages_list(a.p, a.lists, i);
     const int cnt = a.counts ? a.counts[i] : a.n_rows;
     bool ok = l >= 0 && cnt >= 0 && cnt <= a.n_rows && !(twice[l >> 5] >> (l & 31) & 1u);
@@ -879,11 +880,16 @@ cudaError_t launch_pages_append8(const PagesAppendArgs& a, int* launches, cudaSt
   const int chunks = (w.p.Hkv + most - 1) / most, heads = (w.p.Hkv + chunks - 1) / chunks;
   const int64_t grid = (int64_t)w.n * pages * ((w.p.Hkv + heads - 1) / heads);
   if (grid > 0x7fffffffLL || units > 0x7fffffffLL) return cudaErrorInvalidValue;
-  const bool self = w.n <= kSelfEntries;
+  // Where the CTAs fit twice into the machine at most (512 threads an SM, by registers) each decides for itself; where there are more a launch
+  // in front decides for all, since looking up takes each of them 2 us: 4 lists of 512 rows, 160 CTAs, 23.3 us (with the launch 24.8);
+  // 32 lists of 512 rows of 8 heads, 1088 CTAs of 128 threads, 28.2 (29.9); 8 lists of 2005 rows, 1320 of 256 threads, 132 (119); 1024 lists of 4
+  // rows, 2048 of 128 threads, 55 (48).
+  const bool self = w.n <= kSelfEntries && grid * 4 * pr <= (int64_t)2 * 512 * sms;
   if (!self) {
     e = allow_shared<append_plan_kernel>(2 * (kMaxLists / 32) * 4);
     if (e != cudaSuccess) return e;
-    append_plan_kernel<<<1, kPlanThreads, 2 * words * sizeof(uint32_t), s>>>(w, words);
+    const int each = (w.n + kPlanThreads / 32 - 1) / (kPlanThreads / 32);
+    append_plan_kernel<<<each < sms ? each : sms, kPlanThreads, 2 * words * sizeof(uint32_t), s>>>(w, words);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     ++*launches;
