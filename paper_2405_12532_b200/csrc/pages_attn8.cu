@@ -68,13 +68,18 @@ template <> __device__ __forceinline__ void load16<__nv_bfloat16>(const __nv_bfl
 // a row lies 2^4 above it. So f16 holds a weight to 2^-11 of itself (fp32: 2^-22) from 2^-24 of the largest on, and smaller ones to
 // 2^-35 of that. The denominator takes p in fp32, relative to a maximum of its own.
 // The instruction truncates its sums: each stage's products are summed by it from zero and added to the sums in fp32.
-template <class T, int D, bool kChosen>
+// Warps and stages of the ring: 7 and 3 of two tiles fill shared memory (5 and 4: attention over 64 lists 121 us, 16 grouped ones 44, 32 x 2 chosen
+// sets 66; 7 and 2: 106, 40 and 58; 10 and 2: 101, 38.5 and 56; 7 and 3: 101, 38 and 53.5). Where a warp has a stage or two in all (kShort) more warps
+// are what counts: 64 chosen pages of one list 14.0 us with 10 and 2, 16.7 with 7 and 3.
+// kSegment: 64 lists, 16 grouped ones, 32 x 2 chosen sets: 121, 38.7 and 55.8 us with 1, 101, 38.0 and 53.5 with 4, 101, 37.7 and 55.3 with 8.
+// kFew (CTAs whose states a thread merges for itself): 64 chosen pages of one list 17.8 us with 4, 16.7 with 16.
+template <class T, int D, bool kChosen, bool kShort>
 struct ByteBody {
   using Type = T;
   static constexpr bool kSparse = kChosen, kTwo = sizeof(T) == 4;
   static constexpr int kSegment = 4, kFew = 16;
-  static constexpr int kDim = D, COLS = 8, kWarps = 7, kBlocks = 1, kQueryFloats = 0;
-  static constexpr int kTileBytes = 2 * kPageTile * D + 16, kStages = D == 128 ? 3 : 6;
+  static constexpr int kDim = D, COLS = 8, kWarps = kShort ? 10 : 7, kBlocks = 1, kQueryFloats = 0;
+  static constexpr int kTileBytes = 2 * kPageTile * D + 16, kStages = (kShort ? 2 : 3) * (128 / D);
   static constexpr int X = D / 64, KS = 4 * X, NS = kTwo ? 2 : 1, VC = D / 32;   // K chunks a lane and row, steps over D, operands, V chunks
   static constexpr float kLazy = 4.f, kFar = 64.f;
   uint32_t qf[NS][KS][2];
@@ -302,16 +307,22 @@ struct ByteBody {
   }
 };
 
-template <bool kChosen>
+template <bool kChosen, bool kShort>
 cudaError_t by_type(const PagesAttnArgs& a, cudaStream_t s) {
-  if (a.p.D == 128) return a.dtype == PYR_F32 ? run_attn<ByteBody<float, 128, kChosen>>(a, s) : run_attn<ByteBody<__nv_bfloat16, 128, kChosen>>(a, s);
-  return a.dtype == PYR_F32 ? run_attn<ByteBody<float, 64, kChosen>>(a, s) : run_attn<ByteBody<__nv_bfloat16, 64, kChosen>>(a, s);
+  if (a.p.D == 128)
+    return a.dtype == PYR_F32 ? run_attn<ByteBody<float, 128, kChosen, kShort>>(a, s) : run_attn<ByteBody<__nv_bfloat16, 128, kChosen, kShort>>(a, s);
+  return a.dtype == PYR_F32 ? run_attn<ByteBody<float, 64, kChosen, kShort>>(a, s) : run_attn<ByteBody<__nv_bfloat16, 64, kChosen, kShort>>(a, s);
+}
+// (a list's length is not known here, how many pages are chosen of it is: at most four tiles a warp of ten)
+bool is_short(const PagesAttnArgs& a) {
+  const int64_t heads = (int64_t)a.n * a.T * a.p.Hkv * ((a.rep + 7) / 8), tiles = (int64_t)(a.n_slots < a.p.max_pages ? a.n_slots : a.p.max_pages) * a.p.tiles_per_page;
+  return heads <= 40LL * device_sm_count() / tiles;
 }
 
 }  // namespace
 
 cudaError_t launch_pages_attn8(const PagesAttnArgs& a, int* launches, cudaStream_t s) {
-  const cudaError_t e = a.slots ? by_type<true>(a, s) : by_type<false>(a, s);
+  const cudaError_t e = !a.slots ? by_type<false, false>(a, s) : is_short(a) ? by_type<true, true>(a, s) : by_type<true, false>(a, s);
   if (e == cudaSuccess) ++*launches;
   return e;
 }

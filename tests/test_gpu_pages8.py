@@ -847,3 +847,21 @@ def test_calls_under_inference_mode_and_beside_gradients():
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     with pytest.raises(RuntimeError):
         p.attn(q, lse=torch.zeros(2))                          # neither true nor false
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_chosen_pages_of_many_lists(D, dtype):
+    """More work than a stage or two a warp, of every type: lists from none to 300 rows, two tokens each."""
+    H, pr, rep, n, n_slots = 8, 16, 3, 70, 9
+    lens = [(i * 53) % 301 if i % 11 else 0 for i in range(n)]
+    p, want = _filled(H, D, pr, lens, seed=97, spare=2, dtype=dtype)
+    q = _rand(n, 2, H * rep, D, seed=98, dtype=dtype)
+    slots = p.select(q, n_slots, keep_last=1)
+    out, lse = p.attn_blocks(q, slots, lse=True)
+    sample = [0, 1, 2, 11, 33, 34, 69]
+    _sampled(p, lambda l: want[l], out, lse, q, list(range(n)), rep, 2, dtype, sample, H, pr, slots)
+    for i in sample:
+        np.testing.assert_array_equal(slots[i].cpu().numpy(), _slots_of(want[i], _np(q[i]), lens[i], pr, n_slots, 0, 1))
+    again, lse2 = p.attn_blocks(q, slots, lse=True)
+    assert torch.equal(out, again) and torch.equal(lse, lse2) and p.status() == 0
