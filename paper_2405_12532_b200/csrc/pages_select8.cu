@@ -5,7 +5,7 @@
 // the query's rounding. The sums are whole numbers below 2^21, exact in any order; what follows is two products rounded to fp32, so
 // equal inputs give the same pages everywhere. With qc split by its sign a term is one of two products, and the sums are those of
 // two matrix products, of max with the codes above 0 and of min with those below: on m16n8k16 with 16 pages as rows and 8 query
-// heads as columns. (Whole numbers up to 127 are f16 numbers, their products and sums exact in fp32. Byte-wise dot products on the
+// heads as columns; with one query head a KV head as dot products of bytes. (Whole numbers up to 127 are f16 numbers, their products and sums exact in fp32. Byte-wise dot products on the
 // integer side took 30 us for two tokens of 32 lists of up to 512 pages, 8 heads; the warp-level instruction because the
 // operands are bytes in registers.)
 //
@@ -55,6 +55,138 @@ __device__ __forceinline__ void codes_of(uint32_t w, uint32_t* even, uint32_t* o
   *odd = as_u32(__hadd2(as_half2(__byte_perm(w, 0x64646464u, 0x4341)), off));
 }
 
+// A query row (at element `row` of q) in 8 bits by a warp: a lane's D / 32 codes, side by side; its scale (NaN if an element is not finite).
+template <int D>
+__device__ __forceinline__ float codes_of_query(const PagesSelectArgs& a, int64_t row, int* code) {
+  constexpr int N = D / 32;
+  const int lane = threadIdx.x & 31;
+  float x[N], top = 0.f;
+  if (a.dtype == PYR_F32) {
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+      const float2 v = *reinterpret_cast<const float2*>(static_cast<const float*>(a.q) + row + N * lane + k);
+      x[k] = v.x; x[k + 1] = v.y;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+      const uint32_t v = *reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(a.q) + row + N * lane + k);
+      x[k] = __uint_as_float(v << 16); x[k + 1] = __uint_as_float(v & 0xffff0000u);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) top = max_nan(top, fabsf(x[k]));
+  // (magnitudes, Inf and NaN among them, are ordered as their bits are)
+  top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu));
+  float s = __fdiv_rn(top, 127.f);
+  if (s < kScaleMin) s = 0.f;
+  const bool fine = top <= 3.402823466e38f;
+  const float inverse = fine && s > 0.f ? __fdiv_rn(1.f, s) : 0.f;
+#pragma unroll
+  for (int k = 0; k < N; ++k) code[k] = fine ? __float2int_rn(__fmul_rn(x[k], inverse)) : 0;
+  return fine ? s : __uint_as_float(0x7FC00000u);
+}
+
+// The n_slots pages (of npages, more than that) with the largest keys, in order, by a whole CTA.
+template <int kThreads>
+struct Choice {
+  alignas(16) uint32_t hist[256];
+  uint32_t warp_sums[kThreads / 32], both[2][kThreads / 32];
+  uint32_t bin, before, count;
+};
+template <int kThreads>
+__device__ __forceinline__ void choose_pages(const uint32_t* keys, int npages, int n_slots, int32_t* out, Choice<kThreads>& sh) {
+  constexpr int kWarps = kThreads / 32;
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  // Keys that are not forced share their high bits: the 8 bits from the first that differs on are looked at first, and so on until a
+  // group is taken whole (or its keys are equal: the first of them are).
+  uint32_t ones = 0xFFFFFFFFu, any = 0, forced = 0;
+  for (int x0 = 0; x0 < npages; x0 += kThreads) {
+    const uint32_t key = x0 + t < npages ? keys[x0 + t] : kForced;
+    if (key == kForced) forced += x0 + t < npages;
+    else { ones &= key; any |= key; }
+  }
+  ones = __reduce_and_sync(0xffffffffu, ones);
+  any = __reduce_or_sync(0xffffffffu, any);
+  forced = __reduce_add_sync(0xffffffffu, forced);
+  if (lane == 0) { sh.both[0][warp] = ones; sh.both[1][warp] = any; sh.warp_sums[warp] = forced; }
+  __syncthreads();
+  forced = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) { ones &= sh.both[0][w]; any |= sh.both[1][w]; forced += sh.warp_sums[w]; }
+  // keys with these bits above `shift`, `need` of which are wanted (all with larger ones are)
+  uint32_t need = n_slots - forced, prefix = any, threshold = any;
+  int shift = 32 - __clz(ones ^ any);          // bits that differ (0: all keys are the same)
+  prefix = shift < 32 ? prefix >> shift << shift : 0u;
+  bool whole = need == 0;                      // every key that is left is taken, or none
+  if (whole) threshold = kForced;
+  while (!whole && shift > 0) {
+    const int low = max(shift - 8, 0);
+    const uint32_t mask = shift < 32 ? 0xFFFFFFFFu << shift : 0u;
+    for (int x = t; x < 256; x += kThreads) sh.hist[x] = 0;
+    __syncthreads();
+    for (int x = t; x < npages; x += kThreads) {
+      const uint32_t key = keys[x];
+      if (key != kForced && (key & mask) == prefix) atomicAdd(&sh.hist[key >> low & 255u & ((1u << (shift - low)) - 1u)], 1u);
+    }
+    __syncthreads();
+    if (warp == 0) {                           // lane i: bins 255 - 8 i and the seven below it, the largest first
+      const uint4 lo = reinterpret_cast<const uint4*>(sh.hist)[62 - 2 * lane], hi = reinterpret_cast<const uint4*>(sh.hist)[63 - 2 * lane];
+      const uint32_t c[8] = {hi.w, hi.z, hi.y, hi.x, lo.w, lo.z, lo.y, lo.x};
+      uint32_t mine8 = 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) mine8 += c[k];
+      uint32_t incl = mine8;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+      }
+      uint32_t before = incl - mine8;
+      if (before < need && need <= incl) {
+        bool found = false;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (!found && before + c[k] >= need) { sh.bin = 255 - 8 * lane - k; sh.before = before; sh.count = c[k]; found = true; }
+          if (!found) before += c[k];
+        }
+      }
+    }
+    __syncthreads();
+    prefix |= sh.bin << low;
+    need -= sh.before;
+    whole = sh.count == need;
+    shift = low;
+    threshold = prefix;
+  }
+  // ---- pages above it, and those equal to it in what has been looked at: all of them, or the first `need`, in order
+  const uint32_t mask = shift < 32 ? 0xFFFFFFFFu << shift : 0u;
+  uint32_t done = 0, equal = 0;
+  if (whole && need > 0) need = 0xFFFFu << 16;
+  __syncthreads();
+  for (int x0 = 0; x0 < npages; x0 += kThreads) {
+    const int x = x0 + t;
+    const uint32_t key = x < npages ? keys[x] : 0u, bits = key == kForced ? key : key & mask;
+    const bool above = x < npages && (key == kForced || bits > threshold), same = x < npages && key != kForced && bits == threshold;
+    const uint32_t ba = __ballot_sync(0xffffffffu, above), bs = __ballot_sync(0xffffffffu, same);
+    if (lane == 0) sh.warp_sums[warp] = __popc(ba) | __popc(bs) << 16;
+    __syncthreads();
+    uint32_t before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const uint32_t n = sh.warp_sums[w];
+      before += w < warp ? n : 0;
+      total += n;
+    }
+    const uint32_t lower = (1u << lane) - 1u;
+    const uint32_t a0 = done + (before & 0xFFFFu) + __popc(ba & lower), e0 = equal + (before >> 16) + __popc(bs & lower);
+    if (above || (same && e0 < need)) out[a0 + min(e0, need)] = x;
+    done += total & 0xFFFFu;
+    equal += total >> 16;
+    __syncthreads();
+  }
+}
+
 // The extrema of two pages that a lane feeds to the instruction, and their scales (-1: no page).
 template <int X> struct Extrema { uint4 least[2][X], most[2][X]; float scale[2]; };
 
@@ -64,9 +196,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 640 / kThreads
   constexpr int kWarps = kThreads / 32;
   constexpr int X = D / 64, KS = D / 16;         // 16-byte pieces of a row of extrema a lane, steps over D
   extern __shared__ __align__(16) uint32_t shared[];
-  __shared__ __align__(16) uint32_t hist[256];
-  __shared__ uint32_t warp_sums[kWarps], both[2][kWarps];
-  __shared__ uint32_t sh_bin, sh_before, sh_count;
+  __shared__ Choice<kThreads> sh;
   __shared__ int pages_of[kTokens];              // that hold rows the token sees
   const int key_stride = (a.p.max_pages + 3) / 4 * 4, tok_groups = (a.T + tokens - 1) / tokens, groups = (a.rep + 7) / 8;
   uint32_t* keys = shared;                                         // [tokens][max_pages]
@@ -138,31 +268,11 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 640 / kThreads
     uint16_t half[N] = {};
     if (c < a.rep) {
       const int64_t row = (int64_t)e * a.qsb + (int64_t)(tok0 + tok) * a.qst + (int64_t)(h * a.rep + c) * a.qsh;
-      float x[N], top = 0.f;
-      if (a.dtype == PYR_F32) {
+      int code[N];
+      const float s = codes_of_query<D>(a, row, code);
 #pragma unroll
-        for (int k = 0; k < N; k += 2) {
-          const float2 v = *reinterpret_cast<const float2*>(static_cast<const float*>(a.q) + row + N * lane + k);
-          x[k] = v.x; x[k + 1] = v.y;
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < N; k += 2) {
-          const uint32_t v = *reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(a.q) + row + N * lane + k);
-          x[k] = __uint_as_float(v << 16); x[k + 1] = __uint_as_float(v & 0xffff0000u);
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < N; ++k) top = max_nan(top, fabsf(x[k]));
-      // (magnitudes, Inf and NaN among them, are ordered as their bits are)
-      top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu));
-      float s = __fdiv_rn(top, 127.f);
-      if (s < kScaleMin) s = 0.f;
-      const bool fine = top <= 3.402823466e38f;
-      const float inverse = fine && s > 0.f ? __fdiv_rn(1.f, s) : 0.f;
-#pragma unroll
-      for (int k = 0; k < N; ++k) half[k] = __half_as_ushort(__int2half_rn(fine ? __float2int_rn(__fmul_rn(x[k], inverse)) : 0));
-      if (lane == 0) sq[r] = fine ? s : __uint_as_float(0x7FC00000u);
+      for (int k = 0; k < N; ++k) half[k] = __half_as_ushort(__int2half_rn(code[k]));
+      if (lane == 0) sq[r] = s;
     }
     uint16_t* dst = reinterpret_cast<uint16_t*>(codes + at);       // dimensions 0 and 2 of a word, 1 and 3
     if constexpr (N == 4) {
@@ -263,103 +373,127 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 640 / kThreads
       for (int x = t; x < a.n_slots; x += kThreads) out[x] = x < npages ? x : -1;
       continue;
     }
-    // ---- the n_slots-th largest key. Those that are not forced share their high bits: the 8 bits from the first that differs on are
-    // looked at first, and so on until a group is taken whole (or its keys are equal: the first of them are).
-    uint32_t ones = 0xFFFFFFFFu, any = 0, forced = 0;
-    for (int x0 = 0; x0 < npages; x0 += kThreads) {
-      const uint32_t key = x0 + t < npages ? keys[x0 + t] : kForced;
-      if (key == kForced) forced += x0 + t < npages;
-      else { ones &= key; any |= key; }
-    }
-    ones = __reduce_and_sync(0xffffffffu, ones);
-    any = __reduce_or_sync(0xffffffffu, any);
-    forced = __reduce_add_sync(0xffffffffu, forced);
-    if (lane == 0) { both[0][warp] = ones; both[1][warp] = any; warp_sums[warp] = forced; }
-    __syncthreads();
-    forced = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) { ones &= both[0][w]; any |= both[1][w]; forced += warp_sums[w]; }
-    // keys with these bits above `shift`, `need` of which are wanted (all with larger ones are)
-    uint32_t need = a.n_slots - forced, prefix = any, threshold = any;
-    int shift = 32 - __clz(ones ^ any);          // bits that differ (0: all keys are the same)
-    prefix = shift < 32 ? prefix >> shift << shift : 0u;
-    bool whole = need == 0;                      // every key that is left is taken, or none
-    if (whole) threshold = kForced;
-    while (!whole && shift > 0) {
-      const int low = max(shift - 8, 0);
-      const uint32_t mask = shift < 32 ? 0xFFFFFFFFu << shift : 0u;
-      for (int x = t; x < 256; x += kThreads) hist[x] = 0;
-      __syncthreads();
-      for (int x = t; x < npages; x += kThreads) {
-        const uint32_t key = keys[x];
-        if (key != kForced && (key & mask) == prefix) atomicAdd(&hist[key >> low & 255u & ((1u << (shift - low)) - 1u)], 1u);
-      }
-      __syncthreads();
-      if (warp == 0) {                           // lane i: bins 255 - 8 i and the seven below it, the largest first
-        const uint4 lo = reinterpret_cast<const uint4*>(hist)[62 - 2 * lane], hi = reinterpret_cast<const uint4*>(hist)[63 - 2 * lane];
-        const uint32_t c[8] = {hi.w, hi.z, hi.y, hi.x, lo.w, lo.z, lo.y, lo.x};
-        uint32_t mine8 = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) mine8 += c[k];
-        uint32_t incl = mine8;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t y = __shfl_up_sync(0xffffffffu, incl, o);
-          if (lane >= o) incl += y;
-        }
-        uint32_t before = incl - mine8;
-        if (before < need && need <= incl) {
-          bool found = false;
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            if (!found && before + c[k] >= need) { sh_bin = 255 - 8 * lane - k; sh_before = before; sh_count = c[k]; found = true; }
-            if (!found) before += c[k];
-          }
-        }
-      }
-      __syncthreads();
-      prefix |= sh_bin << low;
-      need -= sh_before;
-      whole = sh_count == need;
-      shift = low;
-      threshold = prefix;
-    }
-    // ---- pages above it, and those equal to it in what has been looked at: all of them, or the first `need`, in order
-    const uint32_t mask = shift < 32 ? 0xFFFFFFFFu << shift : 0u;
-    uint32_t done = 0, equal = 0;
-    if (whole && need > 0) need = 0xFFFFu << 16;
-    __syncthreads();
-    for (int x0 = 0; x0 < npages; x0 += kThreads) {
-      const int x = x0 + t;
-      const uint32_t key = x < npages ? keys[x] : 0u, bits = key == kForced ? key : key & mask;
-      const bool above = x < npages && (key == kForced || bits > threshold), same = x < npages && key != kForced && bits == threshold;
-      const uint32_t ba = __ballot_sync(0xffffffffu, above), bs = __ballot_sync(0xffffffffu, same);
-      if (lane == 0) warp_sums[warp] = __popc(ba) | __popc(bs) << 16;
-      __syncthreads();
-      uint32_t before = 0, total = 0;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const uint32_t n = warp_sums[w];
-        before += w < warp ? n : 0;
-        total += n;
-      }
-      const uint32_t lower = (1u << lane) - 1u;
-      const uint32_t a0 = done + (before & 0xFFFFu) + __popc(ba & lower), e0 = equal + (before >> 16) + __popc(bs & lower);
-      if (above || (same && e0 < need)) out[a0 + min(e0, need)] = x;
-      done += total & 0xFFFFu;
-      equal += total >> 16;
-      __syncthreads();
-    }
+    choose_pages<kThreads>(keys, npages, a.n_slots, out, sh);
   }
 }
 
-template <int D, int kGroups, int kThreads>
-cudaError_t run(const PagesSelectArgs& a, int tokens, int smem, cudaStream_t s) {
-  const cudaError_t e = allow_shared<select8_kernel<D, kGroups, kThreads>>(kSelect8Shared);
-  if (e != cudaSuccess) return e;
+// One query head a KV head: words of four bytes multiplied on the integer side, D / 16 lanes a page, a CTA (or a cluster) a token. The matrix
+// instruction takes eight heads whether they are there or not (64 lists of 32 heads, 69 pages, 12.7 us, by it 18.5; one list of 502 pages of 8 heads 7.2,
+// 8.4; four tokens of 64 lists of 8 heads, 63 pages, 11.4, 20.9. With two to four heads this form, four at a time, took 19 for 15 us on 32 lists of
+// 250 pages and 12 for 8 on one list of 32 heads, 12 for 14 on 64 short lists).
+template <int D, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 768 / kThreads) select8_bytes_kernel(PagesSelectArgs a) {
+  constexpr int kWarps = kThreads / 32;
+  constexpr int LPP = D / 16, PPW = 32 / LPP, W = D / 4, U = 2;    // lanes a page, pages a warp and step, words of a row, steps at once
+  extern __shared__ __align__(16) uint32_t shared[];
+  __shared__ Choice<kThreads> sh;
+  uint32_t* keys = shared;                                         // [max_pages] rounded up to 4
+  __shared__ __align__(16) uint32_t plus[2 * W];                   // the query's codes above 0, then those below
+  __shared__ float sq;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = cluster.block_rank(), ranks = cluster.num_blocks();
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const uint32_t item = blockIdx.x / (uint32_t)ranks, et = item / (uint32_t)a.p.Hkv;
+  const int h = (int)(item - et * a.p.Hkv), e = (int)(et / (uint32_t)a.T), tok = (int)(et - (uint32_t)e * a.T);
+  int32_t* out = a.slots + (int64_t)item * a.n_slots;
+  const int l = pages_list(a.p, a.lists, e);
+  const int len = l < 0 ? 0 : max(0, pages_len(a.p, l) - (a.T - 1 - tok));
+  const int pages = pages_for(a.p, len);
+  if (pages <= a.n_slots) {                                        // (the whole cluster)
+    if (rank == 0) {
+      if (l < 0 && t == 0) record(a.p.status, PYR_ERR_INVALID);
+      for (int x = t; x < a.n_slots; x += kThreads) out[x] = x < pages ? x : -1;
+    }
+    return;
+  }
+  // ---- the query in 8 bits
+  if (warp == 0) {
+    constexpr int N = D / 32;
+    int c[N];
+    const float s = codes_of_query<D>(a, (int64_t)e * a.qsb + (int64_t)tok * a.qst + (int64_t)h * a.qsh, c);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      reinterpret_cast<int8_t*>(plus)[N * lane + k] = (int8_t)max(c[k], 0);
+      reinterpret_cast<int8_t*>(plus + W)[N * lane + k] = (int8_t)min(c[k], 0);
+    }
+    if (lane == 0) sq = s;
+  }
+  uint32_t* keys0 = ranks > 1 ? cluster.map_shared_rank(keys, 0) : keys;
+  if (ranks > 1) cluster.sync(); else __syncthreads();
+
+  // ---- scores
+  const int sub = lane / LPP, part = lane % LPP;
+  const int32_t* table = a.p.table + (size_t)l * a.p.max_pages;
+  const int head_bytes = pages_head_bytes(a.p);
+  const int step = kWarps * PPW * U;                               // pages of a CTA's step
+  // (a step's extrema are on their way while the one before is worked out, and its page ids before that)
+  int ids[U];
+  uint4 mn_next[U], mx_next[U];
+  float sk_next[U];
+  auto fetch_ids = [&](int base) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int x = base + (u * kWarps + warp) * PPW + sub;
+      ids[u] = x < pages ? table[x] : -1;
+    }
+  };
+  auto fetch = [&] {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      mn_next[u] = mx_next[u] = make_uint4(0, 0, 0, 0);
+      sk_next[u] = -1.f;                                           // no page
+      if (ids[u] >= 0 && ids[u] < a.p.n_pages) {
+        const uint8_t* head = a.p.pool + ((size_t)ids[u] * a.p.Hkv + h) * head_bytes;
+        mn_next[u] = reinterpret_cast<const uint4*>(head)[part];
+        mx_next[u] = reinterpret_cast<const uint4*>(head + D)[part];
+        sk_next[u] = *reinterpret_cast<const float*>(head + 2 * D);
+      }
+    }
+  };
+  fetch_ids(rank * step);
+  fetch();
+  fetch_ids((rank + ranks) * step);
+  for (int base = rank * step; base < pages; base += ranks * step) {
+    uint4 mn[U], mx[U];
+    float sk[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) { mn[u] = mn_next[u]; mx[u] = mx_next[u]; sk[u] = sk_next[u]; }
+    fetch();
+    fetch_ids(base + 2 * ranks * step);
+    const uint4 qp = reinterpret_cast<const uint4*>(plus)[part], qn = reinterpret_cast<const uint4*>(plus + W)[part];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int x = base + (u * kWarps + warp) * PPW + sub;
+      int sum = __dp4a((int)mx[u].x, (int)qp.x, 0);
+      sum = __dp4a((int)mn[u].x, (int)qn.x, sum);
+      sum = __dp4a((int)mx[u].y, (int)qp.y, sum);
+      sum = __dp4a((int)mn[u].y, (int)qn.y, sum);
+      sum = __dp4a((int)mx[u].z, (int)qp.z, sum);
+      sum = __dp4a((int)mn[u].z, (int)qn.z, sum);
+      sum = __dp4a((int)mx[u].w, (int)qp.w, sum);
+      sum = __dp4a((int)mn[u].w, (int)qn.w, sum);
+#pragma unroll
+      for (int o = LPP / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if (part == 0 && x < pages) {
+        const bool none = sk[u] == -1.f;
+        if (none) record(a.p.status, PYR_ERR_INVALID);
+        keys0[x] = x < a.keep_first || x >= pages - a.keep_last ? kForced : none ? 0u : key_of(__fmul_rn(__fmul_rn(sq, sk[u]), (float)sum));
+      }
+    }
+  }
+  if (ranks > 1) {
+    cluster.sync();
+    if (rank != 0) return;
+  } else {
+    __syncthreads();
+  }
+  choose_pages<kThreads>(keys, pages, a.n_slots, out, sh);
+}
+
+// A call's kernel with up to kThreads threads a CTA, of which `items` work on different lists, heads or tokens.
+template <int kThreads, class... Args>
+cudaError_t run(void (*kernel)(Args...), const PagesSelectArgs& a, int64_t items, int smem, cudaStream_t s, Args... args) {
   const int sms = device_sm_count();
-  if (sms <= 0) return cudaErrorUnknown;
-  const int64_t items = (int64_t)a.n * ((a.T + tokens - 1) / tokens) * a.p.Hkv;
   // several CTAs a list where that many find room at once and each has a step or more to do (one list of 502 pages, 8 heads: 8.6 us, with one 10.1)
   int ranks = 1;
   while (kThreads == 512 && ranks < 8 && items * ranks * 2 <= sms && a.p.max_pages > ranks * (kThreads / 2)) ranks *= 2;
@@ -370,18 +504,34 @@ cudaError_t run(const PagesSelectArgs& a, int tokens, int smem, cudaStream_t s) 
   at.id = cudaLaunchAttributeClusterDimension;
   at.val.clusterDim.x = ranks; at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cfg.attrs = &at; cfg.numAttrs = ranks > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, select8_kernel<D, kGroups, kThreads>, a, tokens);
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
-// As many threads for a list as there is room for, where its table is long enough to occupy them (one list of 502 pages, 32 of up to 512, 64 x 32 heads of
-// up to 69: 8.6, 24.1 and 18.5 us, with 128 throughout 19.4, 33.5 and 21.5).
+template <int D, int kGroups, int kThreads>
+cudaError_t run_mma(const PagesSelectArgs& a, int64_t items, int tokens, int smem, cudaStream_t s) {
+  const cudaError_t e = allow_shared<select8_kernel<D, kGroups, kThreads>>(kSelect8Shared);
+  return e != cudaSuccess ? e : run<kThreads, PagesSelectArgs, int>(select8_kernel<D, kGroups, kThreads>, a, items, smem, s, a, tokens);
+}
+template <int D, int kThreads>
+cudaError_t run_bytes(const PagesSelectArgs& a, int64_t items, int smem, cudaStream_t s) {
+  const cudaError_t e = allow_shared<select8_bytes_kernel<D, kThreads>>(kSelect8Shared);
+  return e != cudaSuccess ? e : run<kThreads, PagesSelectArgs>(select8_bytes_kernel<D, kThreads>, a, items, smem, s, a);
+}
+// As many threads for a list as there is room for, where its table is long enough to occupy them (one list of 502 pages and 32 of up to
+// 512, 8 heads: 8.6 and 24.1 us, with 128 throughout 19.4 and 33.5).
 template <int D, int kGroups>
-cudaError_t by_length(const PagesSelectArgs& a, int tokens, int smem, cudaStream_t s) {
-  const int sms = device_sm_count();
-  if (sms <= 0) return cudaErrorUnknown;
+cudaError_t by_length(const PagesSelectArgs& a, int sms, int tokens, int smem, cudaStream_t s) {
   const int64_t items = (int64_t)a.n * ((a.T + tokens - 1) / tokens) * a.p.Hkv;
   const auto fits = [&](int threads) { return items * threads <= (int64_t)sms * 640 && a.p.max_pages * 2 >= threads; };
-  return fits(512) ? run<D, kGroups, 512>(a, tokens, smem, s) : fits(256) ? run<D, kGroups, 256>(a, tokens, smem, s) : fits(128) ? run<D, kGroups, 128>(a, tokens, smem, s)
-         : fits(64) ? run<D, kGroups, 64>(a, tokens, smem, s) : a.p.max_pages > 512 ? run<D, kGroups, 128>(a, tokens, smem, s) : run<D, kGroups, 32>(a, tokens, smem, s);
+  return fits(512) ? run_mma<D, kGroups, 512>(a, items, tokens, smem, s) : fits(256) ? run_mma<D, kGroups, 256>(a, items, tokens, smem, s)
+         : fits(128) ? run_mma<D, kGroups, 128>(a, items, tokens, smem, s) : fits(64) ? run_mma<D, kGroups, 64>(a, items, tokens, smem, s)
+         : a.p.max_pages > 512 ? run_mma<D, kGroups, 128>(a, items, tokens, smem, s) : run_mma<D, kGroups, 32>(a, items, tokens, smem, s);
+}
+template <int D>
+cudaError_t by_length_bytes(const PagesSelectArgs& a, int sms, int smem, cudaStream_t s) {
+  const int64_t items = (int64_t)a.n * a.T * a.p.Hkv;
+  const auto fits = [&](int threads) { return items * threads <= (int64_t)sms * 1024 && a.p.max_pages * 2 >= threads; };
+  return fits(512) ? run_bytes<D, 512>(a, items, smem, s) : fits(256) ? run_bytes<D, 256>(a, items, smem, s)
+         : fits(128) ? run_bytes<D, 128>(a, items, smem, s) : a.p.max_pages > 1024 ? run_bytes<D, 256>(a, items, smem, s) : run_bytes<D, 32>(a, items, smem, s);
 }
 
 }  // namespace
@@ -392,12 +542,17 @@ cudaError_t launch_pages_select8(const PagesSelectArgs& a, int* launches, cudaSt
   const int sms = device_sm_count();
   if (sms <= 0) return cudaErrorUnknown;
   const int64_t one = pages_select8_shared(a.p.max_pages, a.p.D, a.rep);
+  if (a.rep == 1) {
+    const cudaError_t e = a.p.D == 128 ? by_length_bytes<128>(a, sms, (int)one, s) : by_length_bytes<64>(a, sms, (int)one, s);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+  }
   int tokens = 1;
   while (tokens < kTokens && tokens < a.T && (tokens + 1) * one <= kSelect8Shared && (int64_t)a.n * a.p.Hkv >= sms) ++tokens;
   const int smem = (int)(tokens * one);
   const bool one_group = tokens == 1 && a.rep <= 8;
-  const cudaError_t e = a.p.D == 128 ? (one_group ? by_length<128, 1>(a, tokens, smem, s) : by_length<128, 4>(a, tokens, smem, s))
-                                     : (one_group ? by_length<64, 1>(a, tokens, smem, s) : by_length<64, 4>(a, tokens, smem, s));
+  const cudaError_t e = a.p.D == 128 ? (one_group ? by_length<128, 1>(a, sms, tokens, smem, s) : by_length<128, 4>(a, sms, tokens, smem, s))
+                                     : (one_group ? by_length<64, 1>(a, sms, tokens, smem, s) : by_length<64, 4>(a, sms, tokens, smem, s));
   if (e == cudaSuccess) ++*launches;
   return e;
 }
