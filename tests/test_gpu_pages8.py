@@ -865,3 +865,42 @@ def test_chosen_pages_of_many_lists(D, dtype):
         np.testing.assert_array_equal(slots[i].cpu().numpy(), _slots_of(want[i], _np(q[i]), lens[i], pr, n_slots, 0, 1))
     again, lse2 = p.attn_blocks(q, slots, lse=True)
     assert torch.equal(out, again) and torch.equal(lse, lse2) and p.status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D,n", [(64, 9000), (128, 9000), (64, 20000)])
+def test_selection_with_one_query_head_a_kv_head(D, n, dtype):
+    """Few and many entries over long lists: clusters of CTAs, one CTA, one warp a list; two tokens, which see different rows."""
+    H, pr = 3, 16
+    p, want = _filled(H, D, pr, [n, 700], seed=43, dtype=dtype)
+    for count in (1, 20, 150, 600):
+        lists = [1 if i % 5 == 4 else 0 for i in range(count)]
+        q = _rand(count, 2, H, D, seed=count, dtype=dtype)
+        slots = p.select(q, 40, _ids(*lists), keep_first=1, keep_last=3).cpu().numpy()
+        for i in sorted({0, min(4, count - 1), count - 1}):
+            l = lists[i]
+            np.testing.assert_array_equal(slots[i], _slots_of(want[l], _np(q[i]), want[l].len, pr, 40, 1, 3))
+    assert p.status() == 0
+
+
+def test_ties_and_nan_with_one_query_head():
+    H, D, pr = 1, 128, 16
+    p = _pages(H, D, pr, 80, 2, 40)
+    p.reserve(_ids(0, 1), 40 * 16)
+    k = torch.ones(1, 16, 1, D, device=DEV).repeat(1, 40, 1, 1)
+    k[0, 5 * 16:6 * 16], k[0, 9 * 16] = 2.0, 2.0
+    p.write(k, k, _ids(0))
+    q = torch.ones(1, 1, 1, D, dtype=BF, device=DEV)
+    assert p.select(q, 6, _ids(0)).tolist() == [[[[0, 1, 2, 3, 5, 9]]]]
+    assert p.select(-q, 3, _ids(0)).tolist() == [[[[0, 1, 2]]]]
+    assert p.select(q * 0, 3, _ids(0), keep_first=1).tolist() == [[[[0, 1, 2]]]]
+    k[0, 7 * 16 + 3, 0, 0], k[0, 30 * 16, 0, 1] = math.nan, math.inf
+    p.write(k, k, _ids(1))
+    assert p.select(q, 3, _ids(1), keep_last=1).tolist() == [[[[7, 30, 39]]]]
+    q[0, 0, 0, 0] = math.nan
+    assert p.select(q, 3, _ids(1)).tolist() == [[[[0, 1, 2]]]] and p.status() == 0
+    p.table[1, 3] = 1 << 20                                              # a page out of range comes last
+    q[0, 0, 0, 0] = 1
+    assert p.select(q, 39, _ids(1)).tolist() == [[[[x for x in range(40) if x != 3]]]]
+    assert p.status() == pb.PYR_ERR_INVALID
+    assert p.select(q, 3, _ids(7)).tolist() == [[[[-1, -1, -1]]]] and p.status() == pb.PYR_ERR_INVALID
