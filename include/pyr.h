@@ -551,7 +551,7 @@ pyr_status_t pyr_pages_read(pyr_pages_t* pages, const int32_t* lists, int32_t n,
  * exact in bf16 down to 2^-31 of its row's largest element and held to 2^-39 of that below, for fp32 as two of them to 2^-22 of itself or
  * 2^-39 of the largest, whichever is more; the weight that multiplies a row's V codes, p times the page's scale, to 2^-11 of itself (fp32: two,
  * 2^-22) or 2^-35 of the column's largest such weight, whichever is more. Scores and sums are held in fp32, the instruction's own no longer
- * than 32 rows. A score beyond fp32's range is not a number.
+ * than 32 rows. A score beyond fp32's range is not a number (a row of K whose codes are all 0 scores 0 whatever the factors).
  */
 pyr_status_t pyr_pages_attn(pyr_pages_t* pages, const int32_t* lists, int32_t n, const void* q, int64_t q_stride_b,
                             int64_t q_stride_t, int64_t q_stride_h, void* out, int64_t o_stride_b, int64_t o_stride_t,

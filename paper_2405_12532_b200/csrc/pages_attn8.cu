@@ -36,6 +36,11 @@ __device__ __forceinline__ float power_of_two(int k) {
 }
 // The exponent of |x| (-127 for 0 and subnormals, 128 for Inf and NaN).
 __device__ __forceinline__ int exponent_of(float x) { return (int)(__float_as_uint(x) >> 23 & 255u) - 127; }
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 // lo and hi as a pair of f16, and what is left of them as another (of which f16 holds 11 bits more)
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return as_u32(__floats2half2_rn(lo, hi)); }
 __device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t packed) {
@@ -84,9 +89,10 @@ struct ByteBody {
   static constexpr float kLazy = 4.f, kFar = 64.f;
   uint32_t qf[NS][KS][2];
   float acc[2 * VC][4], l[2];
-  float qpow[2], ref[2], top[2], raise[2];       // a query's power of two; references of V's weights and of the denominator; kLazy, or -Inf: nothing seen
+  float pow1[2], pow2[2];                        // a query's power of two times the softmax scale's, in two factors that are both at most or at least 1
+  float ref[2], top[2], raise[2];                // references of V's weights and of the denominator; kLazy, or -Inf: nothing seen
   int ref_e[2], limit[2], limit_min;
-  float scale;
+  float scale;                                   // the softmax scale without its power of two, times log2 e
 
   __device__ __forceinline__ void begin(const PagesAttnArgs& a, const Place& c, int cols_total, float*, int lane) {
     const int i = lane >> 2, j = lane & 3, col0 = c.cg * COLS;
@@ -124,14 +130,19 @@ struct ByteBody {
           qf[NS - 1][4 * x + t][1] = pack_rest(v[1], v[3], qf[0][4 * x + t][1]);
         }
       }
+    // (2^64: the exponent of a scale that is subnormal)
+    const float wide = a.scale < 0x1p-60f ? a.scale * 0x1p64f : a.scale;
+    const int scale_e = exponent_of(wide);
+    scale = wide * power_of_two(-scale_e) * kLog2e;
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      qpow[y] = power_of_two(__shfl_sync(0xffffffffu, ex, (2 * j + y) * 4) - 14);
+      const int e = __shfl_sync(0xffffffffu, ex, (2 * j + y) * 4) - 14 + scale_e - (a.scale < 0x1p-60f ? 64 : 0), e1 = min(max(e, -126), 127);
+      pow1[y] = power_of_two(e1);
+      pow2[y] = power_of_two(max(e - e1, -127));
       raise[y] = -INFINITY; ref[y] = top[y] = l[y] = 0.f; ref_e[y] = 0;
       limit[y] = kSparse ? c.len : c.len - (a.T - 1 - (col0 + 2 * j + y) / a.rep);
     }
     limit_min = kSparse ? c.len : c.len - (a.T - 1 - col0 / a.rep);
-    scale = a.scale * kLog2e;
 #pragma unroll
     for (int x = 0; x < 2 * VC; ++x) acc[x][0] = acc[x][1] = acc[x][2] = acc[x][3] = 0.f;
   }
@@ -163,8 +174,10 @@ struct ByteBody {
       }
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        // (the factors that may be far apart first; the product is rounded in one place, so that it is the same wherever it is used)
-        const float f = __fmul_rn(__fmul_rn(qpow[y], sc.x), scale);
+        // (rounded once, by the first product; the powers of two after it lie on one side of 1, so that what is between leaves fp32 only where
+        // all of it does. Beyond the largest number a code of 0 still gives 0. The score is rounded in one place, so that it is the
+        // same wherever it is used)
+        const float f = min_nan(__fmul_rn(__fmul_rn(__fmul_rn(sc.x, scale), pow1[y]), pow2[y]), 3.402823466e38f);
 #pragma unroll
         for (int r = 0; r < 2; ++r) s[b][2 * r + y] = __fmul_rn(kTwo ? c[0][2 * r + y] + c[NS - 1][2 * r + y] : c[0][2 * r + y], f);
       }
