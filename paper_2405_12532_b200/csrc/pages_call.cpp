@@ -6,6 +6,7 @@
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "pyr.h"
@@ -91,16 +92,13 @@ PyObject* given_or(PyObject* x, at::Tensor&& mine) {
 // None: the caller's own path; a number: a status that is not 0.
 PyObject* status_of(pyr_status_t st) { return PyLong_FromLong(st); }
 
-// C++ exceptions (out of memory) become Python's.
+// C++ exceptions become those that torch makes of them (out of memory: torch.OutOfMemoryError).
 template <class F>
 PyObject* guarded(F f) {
-  try {
-    at::AutoDispatchBelowADInplaceOrView below;
-    return f();
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-    return nullptr;
-  }
+  HANDLE_TH_ERRORS
+  at::AutoDispatchBelowADInplaceOrView below;
+  return f();
+  END_HANDLE_TH_ERRORS
 }
 #define PYR_ARGS(count) if (n_args != count) { PyErr_SetString(PyExc_TypeError, "wrong number of arguments"); return nullptr; } \
                         Cache* const c = cache_of(args[0]); if (!c) return nullptr
