@@ -100,6 +100,16 @@ PyObject* guarded(F f) {
   return f();
   END_HANDLE_TH_ERRORS
 }
+// The library's call without the interpreter's lock, as through ctypes: a launch can wait for room in the queue, and what it waits for for a
+// host function that wants the lock.
+template <class F>
+pyr_status_t unlocked(F f) {
+  pyr_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f();
+  Py_END_ALLOW_THREADS
+  return st;
+}
 #define PYR_ARGS(count) if (n_args != count) { PyErr_SetString(PyExc_TypeError, "wrong number of arguments"); return nullptr; } \
                         Cache* const c = cache_of(args[0]); if (!c) return nullptr
 
@@ -131,12 +141,13 @@ PyObject* attn(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     if (stats < 0) { PyErr_Clear(); Py_RETURN_NONE; }
     if (stats) lse = at::empty({q.n, q.heads, q.rows}, q.t->options().dtype(at::kFloat));
     float* const l = stats ? static_cast<float*>(lse.data_ptr()) : nullptr;
-    const pyr_status_t st =
-        args[3] == Py_None
-            ? g_calls.attn(c->handle, lists, (int32_t)q.n, q.at, q.sb, q.sn, q.sh, o.at, o.sb, o.sn, o.sh, l, (int32_t)q.rows, (int32_t)q.heads,
-                           q.dtype, (float)scale, stream)
-            : g_calls.attn_blocks(c->handle, lists, (int32_t)q.n, slots, (int32_t)n_slots, q.at, q.sb, q.sn, q.sh, o.at, o.sb, o.sn, o.sh, l,
-                                  (int32_t)q.rows, (int32_t)q.heads, q.dtype, (float)scale, stream);
+    const bool all = args[3] == Py_None;
+    const pyr_status_t st = unlocked([&] {
+      return all ? g_calls.attn(c->handle, lists, (int32_t)q.n, q.at, q.sb, q.sn, q.sh, o.at, o.sb, o.sn, o.sh, l, (int32_t)q.rows, (int32_t)q.heads,
+                                q.dtype, (float)scale, stream)
+                 : g_calls.attn_blocks(c->handle, lists, (int32_t)q.n, slots, (int32_t)n_slots, q.at, q.sb, q.sn, q.sh, o.at, o.sb, o.sn, o.sh, l,
+                                       (int32_t)q.rows, (int32_t)q.heads, q.dtype, (float)scale, stream);
+    });
     if (st != PYR_OK) return status_of(st);
     PyObject* first = given_or(args[4], std::move(mine));
     if (!stats || !first) return first;
@@ -171,8 +182,11 @@ PyObject* select(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
           out->size(3) != n_slots || !out->is_cuda() || out->get_device() != c->device || !out->is_contiguous())
         Py_RETURN_NONE;
     }
-    const pyr_status_t st = g_calls.select(c->handle, lists, (int32_t)q.n, q.at, q.sb, q.sn, q.sh, (int32_t)q.rows, (int32_t)q.heads, q.dtype,
-                                           static_cast<int32_t*>(out->data_ptr()), (int32_t)n_slots, (int32_t)first, (int32_t)last, stream);
+    int32_t* const slots = static_cast<int32_t*>(out->data_ptr());
+    const pyr_status_t st = unlocked([&] {
+      return g_calls.select(c->handle, lists, (int32_t)q.n, q.at, q.sb, q.sn, q.sh, (int32_t)q.rows, (int32_t)q.heads, q.dtype, slots,
+                            (int32_t)n_slots, (int32_t)first, (int32_t)last, stream);
+    });
     return st != PYR_OK ? status_of(st) : given_or(args[6], std::move(mine));
   });
 }
@@ -218,7 +232,7 @@ PyObject* append(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     x.k = k.at; x.v = v.at;
     x.stride_b = k.sb; x.stride_n = k.sn; x.stride_h = k.sh;
     x.n = (int32_t)k.n; x.src_rows = (int32_t)k.rows; x.dtype = k.dtype; x.idx_groups = (int32_t)groups; x.n_rows = (int32_t)rows;
-    const pyr_status_t st = g_calls.append(c->handle, &x, stream);
+    const pyr_status_t st = unlocked([&] { return g_calls.append(c->handle, &x, stream); });
     return st != PYR_OK || args[7] == Py_None ? status_of(st) : given_or(args[8], std::move(mine));
   });
 }
@@ -233,7 +247,9 @@ PyObject* read(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     if (!pair_of(args[1], args[2], *c, &k, &v) || !ids_of(args[3], k.n, *c, &lists) || !ids_of(args[4], k.n, *c, &first) ||
         !ids_of(args[5], k.n, *c, &counts) || !stream_of(*c, &stream))
       Py_RETURN_NONE;
-    return status_of(g_calls.read(c->handle, lists, (int32_t)k.n, first, k.at, v.at, k.sb, k.sn, k.sh, k.dtype, counts, (int32_t)k.rows, stream));
+    return status_of(unlocked([&] {
+      return g_calls.read(c->handle, lists, (int32_t)k.n, first, k.at, v.at, k.sb, k.sn, k.sh, k.dtype, counts, (int32_t)k.rows, stream);
+    }));
   });
 }
 
