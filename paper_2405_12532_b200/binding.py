@@ -10,6 +10,7 @@ import importlib.util
 import math
 import os
 import struct
+import warnings
 
 import torch
 
@@ -479,16 +480,21 @@ _call = None
 
 
 def _calls():
-    """The compiled form of the calls that a decode step makes (csrc/pages_call.cpp), or False where it has not been built."""
+    """The compiled form of the calls that a decode step makes (csrc/pages_call.cpp), or False where it has not been built or does not load."""
     global _call
     if _call is None:
-        _call = False
+        module = False
         if os.path.exists(_CALL_PATH):
             spec = importlib.util.spec_from_file_location("_pages_call", _CALL_PATH)
-            module = importlib.util.module_from_spec(spec)
-            spec.loader.exec_module(module)
+            try:
+                module = importlib.util.module_from_spec(spec)
+                spec.loader.exec_module(module)
+            except ImportError as e:             # built for another torch or Python
+                warnings.warn(f"{_CALL_PATH} does not load and is done without: {e}", RuntimeWarning, stacklevel=3)
+                module = False
+        if module:
             module.setup(*[C.cast(getattr(lib(), "pyr_pages_" + name), C.c_void_p).value for name in ("attn", "attn_blocks", "select", "append", "read")])
-            _call = module
+        _call = module
     return _call
 
 
