@@ -505,7 +505,7 @@ def make_pages_config(*, n_kv_heads, head_dim, n_pages, n_lists, max_pages, grou
     if bits == 8:
         flags |= PYR_PAGES_8BIT
     if group is None:
-        group = 0 if bits == 8 else 64
+        group = 0 if flags & PYR_PAGES_8BIT else 64
     return PyrPagesConfig(n_kv_heads, head_dim, group, page_rows, n_pages, n_lists, max_pages, flags)
 
 
