@@ -71,3 +71,23 @@ def test_query_rows_over_the_whole_range_of_bf16(D, dtype, softmax_scale):
                 lerr = abs(float(lse[i, h, t]) - want_lse)
                 assert lerr <= ds + 2.0 ** -20 * (1 + abs(want_lse)), (EXPONENTS[i], t, h, lerr)
     assert told > n * T * hq * 3 // 4
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_rows_whose_codes_a_query_does_not_meet_score_zero(dtype):
+    """A query of 2^126 in one dimension, keys of 2^60 in another: every factor of a score leaves fp32, every score is 0."""
+    D, rows = 128, 40
+    p = pb.PyrPages(bits=8, n_kv_heads=1, head_dim=D, page_rows=64, n_pages=1, n_lists=1, max_pages=1)
+    k, q = torch.zeros(1, rows, 1, D, device=DEV), torch.zeros(1, 1, 1, D, dtype=dtype, device=DEV)
+    k[..., 3], q[..., 90] = 2.0 ** 60, 2.0 ** 126
+    v = torch.randn(1, rows, 1, D, generator=torch.Generator().manual_seed(1)).to(DEV)
+    p.reserve(torch.zeros(1, dtype=torch.int32, device=DEV), rows)
+    p.write(k, v)
+    out, lse = p.attn(q, lse=True)
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+    p.read(ko, vo)
+    assert p.status() == 0 and abs(float(lse) - np.log(rows)) <= 2.0 ** -20
+    want = vo.double().mean(1)
+    # all weights are alike and f16 numbers: the sums' 2^-20 of the mean magnitude and the output's rounding
+    tol = 2.0 ** -20 * vo.double().abs().mean(1) + (2.0 ** -8 if dtype == BF else 2.0 ** -22) * want.abs() + 2.0 ** -11 * vo.double().abs().mean(1) * (dtype == BF)
+    assert bool(((out[:, 0].double() - want).abs() <= tol).all())
