@@ -18,7 +18,7 @@ template <int D, int GROUP, int kCols>
 struct CoreBody {
   using Type = float;
   static constexpr bool kSparse = false;
-  static constexpr int kSegment = kAttnSegmentUnits, kFew = 8;
+  static constexpr int kSegment = kAttnSegmentUnits, kFew = 8, kAtOnce = 2, kRounds = 1;
   static constexpr int kDim = D, COLS = kCols, kWarps = 7, kBlocks = 1, kQueryFloats = COLS * D + 4;   // queries and their scores' factors lie in shared memory
   static constexpr int kStages = 3, kTileBytes = kPageTile * (D + 8 * (D / GROUP));
   static constexpr int G = D / GROUP, U = GROUP / 32, X = D / 32;   // X: words of K / halves of V in a lane's chunk
@@ -265,7 +265,7 @@ struct MmaBody {
   using Type = __nv_bfloat16;
   static constexpr int G = D / GROUP, U = GROUP / 32, X = D / 32;
   static constexpr bool kSparse = false;
-  static constexpr int kSegment = kAttnSegmentUnits, kFew = 8;
+  static constexpr int kSegment = kAttnSegmentUnits, kFew = 8, kAtOnce = 2, kRounds = 1;
   static constexpr int kDim = D, COLS = 8, kWarps = 11, kBlocks = 1, kQueryFloats = 0;
   static constexpr int kTileBytes = kPageTile * (D + 8 * G), kStages = kTileBytes > 2304 ? 2 : 3;
   static constexpr float kLazy = 4.f;            // the maximum is raised once a score is 2^4 above it

@@ -33,6 +33,9 @@ constexpr int kStageTiles = 2;           // a stage of a warp's ring: one copy o
 constexpr int kStageRows = kStageTiles * kPageTile;
 // Body::kSegment: what beginning and ending a (entry, head, column group) costs a warp, in tiles: its queries, a first step that sets the
 // maximum and the scales' factors, its sums (4 bits, 64 ragged lists of 32 heads: 102 us with 2, 96 with 3, 92 with 4, 90 with 6 and 8).
+// Body::kFew, kAtOnce, kRounds: merges across CTAs. Up to kFew states a thread merges for itself, kAtOnce of them loaded at once; of more, the loops
+// over 32 states are unrolled kRounds times. Sums go state by state whatever these are. The code runs once, so its size counts (4 bits, 2 lists
+// of 100 k rows, 64/8 heads: 60.2 us with 2 and 1, 60.7 with 4 and 4; the 8-bit form of that 82.3 with 4 and 4, 83.1 with 2 and 1).
 // A warp's share is at least this much: next to nothing, since small calls are bound by a warp's own latency, 2 us a step
 // (with 2 instead of 4 and 8: 385 rows of 32 heads 20.5, 22.5 and 24.6 us, the small fp32 model 21, 26 and 32 us).
 constexpr int kMinUnits = 2;
@@ -573,9 +576,9 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
     // the first CTA holds the beginning (place 1), the others go on with it (place 0)
     const float* src = a.partial + (size_t)c1 * 2 * (kAttnCols * (D + 2));
     const size_t step = 2 * (size_t)(kAttnCols * (D + 2)), second = kAttnCols * (D + 2);
-    constexpr int kFew = Body::kFew;
-    if (cn <= kFew) {                            // a thread for itself, in few instructions (all loads in one round: 17.3 us for one list's 64 chosen pages,
-                                                 // as below 16.7: this code runs once, and fetching it takes as long as the loads)
+    constexpr int kFew = Body::kFew, kAtOnce = Body::kAtOnce;
+    if (cn <= kFew) {                            // a thread for itself, in few instructions (one list's 64 chosen pages, 7 warps a CTA: all loads in one
+                                                 // round 17.3 us, as below 16.7: fetching the code takes as long as the loads)
       for (int o = t; o < ncols * (D / 4); o += kThreads) {
         const int x = o / (D / 4), d = o % (D / 4) * 4;
         const float* st = src + x * (D + 2);
@@ -590,10 +593,10 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
         }
         const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll 1
-        for (int k0 = 0; k0 < cn; k0 += 4) {
-          float2 ml[4], u[4], v[4];
+        for (int k0 = 0; k0 < cn; k0 += kAtOnce) {
+          float2 ml[kAtOnce], u[kAtOnce], v[kAtOnce];
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+          for (int k = 0; k < kAtOnce; ++k)
             if (k0 + k < cn) {
               const float* at = st + (k0 + k) * step + (k0 + k == 0 ? second : 0);
               ml[k] = __ldcg(reinterpret_cast<const float2*>(at + D));
@@ -601,7 +604,7 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
               v[k] = __ldcg(reinterpret_cast<const float2*>(at + d + 2));
             }
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+          for (int k = 0; k < kAtOnce; ++k)
             if (k0 + k < cn) {
               const float w = ex2(ml[k].x - ref);
               num[0] = fmaf(w, u[k].x, num[0]); num[1] = fmaf(w, u[k].y, num[1]);
@@ -619,11 +622,13 @@ __global__ void __launch_bounds__((Body::kWarps + 1) * 32, Body::kBlocks) attn_k
     __syncthreads();
     for (int x = warp; x < ncols; x += kWarps + 1) {
       float M = -INFINITY;
+#pragma unroll (Body::kRounds)
       for (int k = lane; k < cn; k += 32) M = fmaxf(M, __ldcg(src + k * step + (k == 0 ? second : 0) + x * (D + 2) + D));
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
       const float ref = M == -INFINITY ? 0.f : M;
       float den = 0.f;
+#pragma unroll (Body::kRounds)
       for (int k = lane; k < cn; k += 32) {
         const float* st = src + k * step + (k == 0 ? second : 0) + x * (D + 2) + D;
         const float w = ex2(__ldcg(st) - ref);

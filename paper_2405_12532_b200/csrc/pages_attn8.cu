@@ -82,7 +82,7 @@ template <class T, int D, bool kChosen, bool kShort>
 struct ByteBody {
   using Type = T;
   static constexpr bool kSparse = kChosen, kTwo = sizeof(T) == 4;
-  static constexpr int kSegment = 4, kFew = 16;
+  static constexpr int kSegment = 4, kFew = 16, kAtOnce = 4, kRounds = 4;
   static constexpr int kDim = D, COLS = 8, kWarps = kShort ? 10 : 7, kBlocks = 1, kQueryFloats = 0;
   static constexpr int kTileBytes = 2 * kPageTile * D + 16, kStages = (kShort ? 2 : 3) * (128 / D);
   static constexpr int X = D / 64, KS = 4 * X, NS = kTwo ? 2 : 1, VC = D / 32;   // K chunks a lane and row, steps over D, operands, V chunks
