@@ -431,7 +431,9 @@ pyr_status_t pyr_glue_argmax(const void* x, int32_t* out, int64_t rows, int32_t 
  *
  * In every call `lists` (device int32 [n]) names the list of each entry; NULL means lists 0 .. n-1. n = 0 does nothing.
  * pyr_pages_fork, pyr_pages_compact and, up to 512 rows times KV heads an entry, pyr_pages_write look for a list named twice by
- * comparing every entry with every other: made for thousands of entries a call, n^2 reads beyond that.
+ * comparing every entry with every other: made for thousands of entries a call, n^2 reads beyond that. In 8 bits pyr_pages_write and
+ * pyr_pages_append do so where n_rows is 1 (once for every 8 KV heads and every 16 query heads of an entry) and for up to 256 entries; not with
+ * lists NULL.
  */
 #define PYR_PAGES_8BIT 8u
 typedef struct {

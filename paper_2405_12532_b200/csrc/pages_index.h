@@ -83,7 +83,7 @@ PYR_HD int v_slot_half(int D, int group, int slot) {
 // The 8-bit format. A (page, head) begins with the least and the largest code of each dimension (D signed bytes each) and the
 // two scales (K's, V's); its tiles hold the codes as bytes code + 128, K's and then V's, and the scales once more, so that a copy
 // of a tile is all that attention needs of it.
-constexpr int kPageRows8 = 128;          // rows of a page at most: a CTA stores them with a warp a tile
+constexpr int kPageRows8 = 128;          // rows of a page at most: a CTA stores them with two warps a tile
 PYR_HD int pages8_tile_bytes(int D) { return 2 * kPageTile * D + 16; }
 PYR_HD int pages8_head_extra(int D) { return 2 * D + 16; }
 PYR_HD int tile8_scales(int D) { return 2 * kPageTile * D; }

@@ -517,7 +517,8 @@ cudaError_t run_bytes(const PagesSelectArgs& a, int64_t items, int smem, cudaStr
   return e != cudaSuccess ? e : run<kThreads, PagesSelectArgs>(select8_bytes_kernel<D, kThreads>, a, items, smem, s, a);
 }
 // As many threads for a list as there is room for, where its table is long enough to occupy them (one list of 502 pages and 32 of up to
-// 512, 8 heads: 8.6 and 24.1 us, with 128 throughout 19.4 and 33.5).
+// 512, 8 heads: 8.6 and 24.1 us, with 128 throughout 19.4 and 33.5). The table's width decides, since lengths lie on the device: short lists in wide
+// tables get as many.
 template <int D, int kGroups>
 cudaError_t by_length(const PagesSelectArgs& a, int sms, int tokens, int smem, cudaStream_t s) {
   const int64_t items = (int64_t)a.n * ((a.T + tokens - 1) / tokens) * a.p.Hkv;

@@ -247,6 +247,8 @@ __device__ __forceinline__ void finish(const PagesWriteArgs& a, int e, const Ent
 // ------------------------------------------------------------------ one row an entry (a decode step)
 // Bound by its launch and a chain of loads (list, length, page, header): 64 lists of 32 heads with queries 6.8 us in a graph (50.8 by the kernel
 // for many rows, which goes through whole pages).
+// Every CTA compares its entry's list with all others: n^2 reads for n entries, which count from a thousand on (8 KV and 64 query heads, lists
+// named and not: 64 entries 4.7 and 4.5 us, 1024 22.4 and 19.9, 4096 116 and 79, 16 384 925 and 371).
 // grid (entries, groups of kOneWarps heads and then groups of query heads). A warp stores a head: its lower half the key, its upper half
 // the value, a thread D / 32 dimensions from either half of them.
 template <class T, int D>
@@ -825,7 +827,9 @@ struct RunOne {
     return cudaGetLastError();
   }
 };
-constexpr int kStageBytes = 200 * 1024;          // shared memory of a CTA's stages at most
+// Shared memory of a CTA's stages at most: two, but one in fp32 with 128 dimensions and more than 96 rows a page (8 x 2005 rows of 40 heads: 179 us with
+// pages of 128 rows, 170 with two stages and pages of 64, floor 125; bf16, which has two with both, 138 and 116).
+constexpr int kStageBytes = 200 * 1024;
 struct RunPages {
   const PagesAppendArgs& a; int pages, heads; unsigned grid; bool self; cudaStream_t s;
   template <class T, int D> cudaError_t run() {
