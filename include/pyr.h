@@ -548,7 +548,8 @@ pyr_status_t pyr_pages_read(pyr_pages_t* pages, const int32_t* lists, int32_t n,
  * Each list is read once per 8 (bf16; 1 to 4 for fp32) query rows of a KV head; bit-reproducible. A list may appear more than once;
  * an entry whose list id is out of range writes nothing. A call whose lists come to more than 2^30 tiles of 16 rows (times KV heads
  * and times eighths of the query rows) for each warp of the machine writes nothing and records PYR_ERR_UNSUPPORTED.
- * bf16 runs on warp-level tensor-core instructions, fp32 on CUDA cores.
+ * bf16 runs on warp-level tensor-core instructions, fp32 on CUDA cores. In 4 bits q . K and its terms are held in fp32 before softmax_scale
+ * is applied: with a scale near 2^-126 or 2^60 they can leave it, or lose bits there, though the score does not.
  * In 8 bits both types run on the warp-level instruction, 8 query rows of a KV head at a time, and products are of f16: a query element is
  * exact in bf16 down to 2^-31 of its row's largest element and held to 2^-39 of that below, for fp32 as two of them to 2^-22 of itself or
  * 2^-39 of the largest, whichever is more; the weight that multiplies a row's V codes, p times the page's scale, to 2^-11 of itself (fp32: two,
